@@ -312,6 +312,81 @@ abs_status abs_average_bf16(void *params_dev, int M, int64_t n, void *scratch_de
  */
 abs_status abs_average_bf16_static(void *params_dev, int M, int64_t n, void *hip_stream);
 
+/* Types of the values in device memory that the operators below take. */
+enum { ABS_TYPE_F32 = 0, ABS_TYPE_BF16 = 1, ABS_TYPE_F16 = 2 };
+
+/*
+ * Orthogonalisation of `batch` matrices by Newton-Schulz products: the factor U V^T of G = U S V^T, approximately.
+ *   X = G / (||G||_F + eps);   in each of `steps` steps:   A = X X^T,  X <- a X + (b A + c A A) X
+ * (with A = X^T X on the right where rows > cols: the same X).  A zero matrix gives zeros, one with an infinity or NaN gives NaN
+ * and leaves the others alone.
+ *   g_dev, o_dev : device, [batch][rows][cols]; ldg, ldo: values from row to row (>= cols), stride_g, stride_o: from matrix to
+ *                  matrix.  Any alignment of the type; rows that start on 16 bytes and hold a multiple of 8 values are faster.
+ *                  o_dev may be g_dev (same type and strides); it must not overlap it otherwise.
+ *   steps        : 1 .. 32.
+ *   coef         : host, 3 * steps floats a, b, c, step by step, or NULL: (3.4445, -4.7750, 2.0315) in all, which takes singular
+ *                  values from 0.01 on to about 0.7 .. 1.2 in five steps.  Coefficients that let a singular value of at most 1 grow
+ *                  beyond 256 are refused.
+ *   prec         : ABS_PREC_BF16: products of 16-bit operands (fp16 with powers of two that keep them in range; X itself is held
+ *                  in 32 bits): relative error of the result 0.5 to 2.1e-3, less than a bf16 result's own rounding adds.
+ *                  ABS_PREC_F32: as exact as fp32 products, at three times the operations.
+ * Asynchronous on the stream; sums are in a fixed order (the same bits every time).  workspace: device, 256-byte aligned,
+ * abs_orthogonalize_workspace_bytes, used until the call's work has run.  A matrix of 2^30 values or more: ABS_EUNSUPPORTED.
+ */
+abs_status abs_orthogonalize_workspace_bytes(int batch, int rows, int cols, int prec, size_t *bytes /*host*/);
+abs_status abs_orthogonalize(const void *g_dev, int g_type, int64_t ldg, int64_t stride_g, void *o_dev, int o_type, int64_t ldo,
+                             int64_t stride_o, int batch, int rows, int cols, int steps, const float *coef /*host*/, float eps,
+                             int prec, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * One step with orthogonalised momentum on `batch` weight matrices (a worker's, or all workers' side by side):
+ *   v <- momentum v + g;   u = nesterov ? g + momentum v : v;   x <- (1 - lr weight_decay) x - lr scale orth(u)
+ * orth as above.  scale: 0.2 sqrt(max(rows, cols)) gives an update the size of AdamW's.
+ *   x_dev, g_dev : device, [batch][rows][cols] without gaps, of types x_type and g_type;   v_dev : the same, fp32.
+ * None of them overlaps another.  Workspace: abs_orthogonalize_workspace_bytes.  Asynchronous on the stream.
+ */
+abs_status abs_muon_step(void *x_dev, int x_type, const void *g_dev, int g_type, float *v_dev, int batch, int rows, int cols,
+                         float lr, float momentum, int nesterov, float weight_decay, float scale, int steps,
+                         const float *coef /*host*/, float eps, int prec, void *workspace, size_t workspace_bytes,
+                         void *hip_stream);
+
+/*
+ * Layer norm over the last dimension, M replicas with gains and biases of their own (fp32 arithmetic, one rounding at the end):
+ *   mu = mean_d x,  r = 1 / sqrt(mean_d (x - mu)^2 + eps),  y = (x - mu) r gamma + beta
+ */
+typedef struct {
+  int M, b, T, D;             /* replicas, samples of each, rows of a sample (tokens), values of a row; all >= 1 */
+  int type;                   /* ABS_TYPE_* of x, y, dy and dx */
+  int param_type;             /* ABS_TYPE_* of gamma and beta [M x D]: ABS_TYPE_F32 or `type` */
+  int64_t ldx, stride_x;      /* x: values from row to row (>= D) and from replica to replica */
+  int64_t ldy, stride_y;      /* y, or dy */
+  int64_t lddx, stride_dx;    /* dx (backward) */
+} abs_layer_norm_shape;
+
+/*   beta_dev may be NULL (no bias); mean_dev, rstd_dev : device, float [M x b x T], each may be NULL.  y_dev may be x_dev with the
+ *   same strides.  0 <= eps.  Asynchronous on the stream. */
+abs_status abs_layer_norm(const abs_layer_norm_shape *shape /*host*/, const void *x_dev, const void *gamma_dev, const void *beta_dev,
+                          float eps, void *y_dev, float *mean_dev, float *rstd_dev, void *hip_stream);
+
+/*
+ * Its gradients, from the backprop signals dy of the per-sample losses (as elsewhere here, not divided by the batch size), and
+ * the batch tests' statistics of the gradient of gamma and beta, which has no factored form:
+ *   xh = (x - mu) r,  h = dy gamma,  dx = r (h - mean_d h - xh mean_d(h xh))
+ *   g_i = (sum_t dy xh, sum_t dy) over the T rows of sample i;  (dgamma, dbeta) = gbar = (1 / b) sum_i g_i
+ *   n_i = ||g_i||^2,  q_i = <g_i, gbar>    (without beta: of the gamma part alone)
+ * n_i and q_i add to those of other layers (abs_layer_stats): S1 = sum_i n_i, S2 = ||gbar||^2, S3 = sum_i q_i^2, S4 = sum_i q_i.
+ *   mean_dev, rstd_dev : device, float [M x b x T], of the forward pass.
+ *   dx_dev : overlaps neither x nor dy.   dgamma_dev, dbeta_dev : device, float [M x D]; dbeta_dev NULL: the layer has no bias.
+ *   n_dev, q_dev : device, float [M x b], either may be NULL.
+ * Asynchronous on the stream; sums in a fixed order.  workspace: device, 256-byte aligned, of the size the other call tells for
+ * the same shape and the same outputs asked for, used until the call's work has run.
+ */
+abs_status abs_layer_norm_backward_workspace_bytes(const abs_layer_norm_shape *shape /*host*/, int want_n, int want_q, size_t *bytes /*host*/);
+abs_status abs_layer_norm_backward(const abs_layer_norm_shape *shape /*host*/, const void *dy_dev, const void *x_dev,
+                                   const void *gamma_dev, const float *mean_dev, const float *rstd_dev, void *dx_dev,
+                                   float *dgamma_dev, float *dbeta_dev, float *n_dev, float *q_dev, void *workspace,
+                                   size_t workspace_bytes, void *hip_stream);
+
 /*
  * Per-kernel timing (measurement aid; not part of the method).  While enabled, every kernel
  * launch of abs_local_step / abs_average_replicas is bracketed by two HIP events on the

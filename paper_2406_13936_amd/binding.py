@@ -29,6 +29,8 @@ EXPORTS = [
     "abs_local_step_accumulated", "abs_profile_pause", "abs_local_step_graphed", "abs_graph_count",
     "abs_get_counters", "abs_get_opt_state", "abs_average_bf16_static",
     "abs_set_fused_update", "abs_set_gram_ip_max_batch",
+    "abs_orthogonalize", "abs_orthogonalize_workspace_bytes", "abs_muon_step",
+    "abs_layer_norm", "abs_layer_norm_backward", "abs_layer_norm_backward_workspace_bytes",
 ]
 
 
@@ -57,6 +59,12 @@ class TestResult(C.Structure):
 class ProfileEntry(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("calls", C.c_longlong), ("total_ms", C.c_double),
                 ("flops", C.c_double), ("bytes", C.c_double)]
+
+
+class LayerNormShape(C.Structure):
+    _fields_ = [("M", C.c_int), ("b", C.c_int), ("T", C.c_int), ("D", C.c_int), ("type", C.c_int),
+                ("param_type", C.c_int), ("ldx", C.c_int64), ("stride_x", C.c_int64), ("ldy", C.c_int64),
+                ("stride_y", C.c_int64), ("lddx", C.c_int64), ("stride_dx", C.c_int64)]
 
 
 def load_library(reload: bool = False):
@@ -116,6 +124,17 @@ def load_library(reload: bool = False):
     lib.abs_profile_enable.argtypes = [C.c_void_p, C.c_int]
     lib.abs_profile_pause.argtypes = [C.c_void_p, C.c_int]
     lib.abs_profile_read.argtypes = [C.c_void_p, C.c_int, C.POINTER(ProfileEntry), C.POINTER(C.c_int)]
+    lib.abs_orthogonalize_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+    lib.abs_orthogonalize.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_int64,
+                                      C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_float, C.c_int, C.c_void_p,
+                                      C.c_size_t, C.c_void_p]
+    lib.abs_muon_step.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_float,
+                                  C.c_float, C.c_int, C.c_float, C.c_float, C.c_int, C.c_void_p, C.c_float, C.c_int,
+                                  C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.abs_layer_norm.argtypes = [C.POINTER(LayerNormShape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p,
+                                   C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.abs_layer_norm_backward_workspace_bytes.argtypes = [C.POINTER(LayerNormShape), C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+    lib.abs_layer_norm_backward.argtypes = [C.POINTER(LayerNormShape)] + [C.c_void_p] * 11 + [C.c_size_t, C.c_void_p]
     _lib = lib
     return lib
 
@@ -424,3 +443,208 @@ def average_bf16_static(params):
     lib = load_library()
     M, n = int(params.shape[0]), int(params[0].numel())
     _check(lib.abs_average_bf16_static(params.data_ptr(), M, n, _stream_ptr()))
+
+
+# -- operators beside the replicas' step -------------------------------------------------------------------------------
+
+def _type_of(t, what: str) -> int:
+    import torch
+    kinds = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    if t.dtype not in kinds:
+        raise AbsError(f"{what} must be float32, bfloat16 or float16, not {t.dtype}")
+    if not t.is_cuda:
+        raise AbsError(f"{what} must be in device memory")
+    return kinds[t.dtype]
+
+
+def _rows(t, lead: int, what: str):
+    """(stride of the first dimension, stride of a row) of a tensor whose dimensions between `lead` and the last are one run
+    of equally spaced rows."""
+    if t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise AbsError(f"{what}: values of a row must be consecutive")
+    ld, n = None, 1
+    for d in range(t.dim() - 2, lead - 1, -1):
+        if t.shape[d] == 1:
+            continue
+        if ld is None:
+            ld = t.stride(d)
+        elif t.stride(d) != ld * n:
+            raise AbsError(f"{what}: rows must be equally spaced")
+        n *= t.shape[d]
+    return (t.stride(0) if lead and t.shape[0] > 1 else 0), (t.shape[-1] if ld is None else ld)
+
+
+def _same_device(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise AbsError(f"tensors on different devices: {first.device} and {t.device}")
+
+
+class _Workspace:
+    """256-byte aligned device memory of one call (from torch's allocator, on the current stream)."""
+
+    def __init__(self, nbytes: int, device):
+        import torch
+        self._mem = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+        self.ptr, self.nbytes = (self._mem.data_ptr() + 255) // 256 * 256, nbytes
+
+
+def _coefficients(coefficients, steps: int):
+    if coefficients is None:
+        return None
+    flat = np.ascontiguousarray(coefficients, dtype=np.float32).reshape(-1)
+    if flat.size == 3:
+        flat = np.tile(flat, int(steps))
+    if flat.size != 3 * int(steps):
+        raise AbsError("coefficients: (a, b, c), or one such triple per step")
+    return flat
+
+
+def _matrices(t, what: str):
+    """(batch, rows, cols, stride from matrix to matrix, stride from row to row) of [..., rows, cols]."""
+    if t.dim() < 2:
+        raise AbsError(f"{what} must have at least two dimensions")
+    rows, cols = int(t.shape[-2]), int(t.shape[-1])
+    if t.stride(-1) != 1 and cols != 1:
+        raise AbsError(f"{what}: values of a row must be consecutive")
+    batch, stride = 1, None
+    for d in range(t.dim() - 3, -1, -1):
+        if t.shape[d] == 1:
+            continue
+        if stride is None:
+            stride = t.stride(d)
+        elif t.stride(d) != stride * batch:
+            raise AbsError(f"{what}: matrices must be equally spaced")
+        batch *= t.shape[d]
+    return int(batch), rows, cols, int(stride or 0), int(t.stride(-2)) if rows > 1 else cols
+
+
+def orthogonalize(g, steps: int = 5, coefficients=None, eps: float = 1e-7, prec: Optional[int] = None, out=None):
+    """Newton-Schulz orthogonalisation of [..., rows, cols] device matrices (abs_orthogonalize); `out` defaults to a new
+    tensor of g's type and may be g itself.  prec: PREC_BF16 (16-bit products) or PREC_F32; by default as exact as the
+    result's type."""
+    import torch
+    lib = load_library()
+    gt = _type_of(g, "g")
+    if out is None:
+        out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
+    ot = _type_of(out, "out")
+    _same_device(g, out)
+    if out.shape != g.shape:
+        raise AbsError("out must have g's shape")
+    batch, rows, cols, sg, ldg = _matrices(g, "g")
+    _, _, _, so, ldo = _matrices(out, "out")
+    prec = (PREC_F32 if ot == 0 else PREC_BF16) if prec is None else int(prec)
+    coef = _coefficients(coefficients, steps)
+    nbytes = C.c_size_t(0)
+    with torch.cuda.device(g.device):
+        _check(lib.abs_orthogonalize_workspace_bytes(batch, rows, cols, prec, C.byref(nbytes)))
+        ws = _Workspace(nbytes.value, g.device)
+        _check(lib.abs_orthogonalize(g.data_ptr(), gt, ldg, sg, out.data_ptr(), ot, ldo, so, batch, rows, cols, int(steps),
+                                     None if coef is None else coef.ctypes.data, float(eps), prec, ws.ptr, ws.nbytes,
+                                     _stream_ptr()))
+    return out
+
+
+def muon_step(x, g, v, lr: float, momentum: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
+              scale: Optional[float] = None, steps: int = 5, coefficients=None, eps: float = 1e-7, prec: Optional[int] = None):
+    """One step with orthogonalised momentum on [..., rows, cols] device matrices, in place on x and on the fp32 momentum v
+    (abs_muon_step).  scale defaults to 0.2 sqrt(max(rows, cols)); prec by default as exact as x's type."""
+    import torch
+    lib = load_library()
+    xt, gt = _type_of(x, "x"), _type_of(g, "g")
+    if _type_of(v, "v") != 0:
+        raise AbsError("v must be float32")
+    _same_device(x, g, v)
+    if x.shape != g.shape or x.shape != v.shape:
+        raise AbsError("x, g and v must have the same shape")
+    if not (x.is_contiguous() and g.is_contiguous() and v.is_contiguous()):
+        raise AbsError("x, g and v must be contiguous")
+    batch, rows, cols, _, _ = _matrices(x, "x")
+    prec = (PREC_F32 if xt == 0 else PREC_BF16) if prec is None else int(prec)
+    coef = _coefficients(coefficients, steps)
+    if scale is None:
+        scale = 0.2 * max(rows, cols) ** 0.5
+    nbytes = C.c_size_t(0)
+    with torch.cuda.device(x.device):
+        _check(lib.abs_orthogonalize_workspace_bytes(batch, rows, cols, prec, C.byref(nbytes)))
+        ws = _Workspace(nbytes.value, x.device)
+        _check(lib.abs_muon_step(x.data_ptr(), xt, g.data_ptr(), gt, v.data_ptr(), batch, rows, cols, float(lr), float(momentum),
+                                 int(bool(nesterov)), float(weight_decay), float(scale), int(steps),
+                                 None if coef is None else coef.ctypes.data, float(eps), prec, ws.ptr, ws.nbytes, _stream_ptr()))
+
+
+def _norm_params(x, p, what: str) -> int:
+    t = _type_of(p, what)
+    _same_device(x, p)
+    if tuple(p.shape) != (x.shape[0], x.shape[-1]) or not p.is_contiguous():
+        raise AbsError(f"{what} must be a contiguous [M, D] tensor")
+    return t
+
+
+def _norm_shape(x, param_type: int) -> LayerNormShape:
+    if x.dim() < 3:
+        raise AbsError("x must be [M, b, ..., D]")
+    M, b, D = int(x.shape[0]), int(x.shape[1]), int(x.shape[-1])
+    T = 1
+    for n in x.shape[2:-1]:
+        T *= int(n)
+    sx, ldx = _rows(x, 1, "x")
+    return LayerNormShape(M, b, T, D, _type_of(x, "x"), param_type, ldx, sx, D, b * T * D, D, b * T * D)
+
+
+def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None):
+    """Layer norm of [M, b, ..., D] over the last dimension with weights and biases [M, D] (fp32 or x's type), one set per
+    replica.  Returns (y, mean, rstd), the latter two fp32 [M, b, ...]; `out` may be x itself."""
+    import torch
+    lib = load_library()
+    _type_of(x, "x")
+    pt = _norm_params(x, weight, "weight")
+    if bias is not None and _norm_params(x, bias, "bias") != pt:
+        raise AbsError("weight and bias must have the same type")
+    shape = _norm_shape(x, pt)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    _same_device(x, y)
+    if y.shape != x.shape or y.dtype != x.dtype:
+        raise AbsError("out must have x's shape and type")
+    shape.stride_y, shape.ldy = _rows(y, 1, "out")
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    with torch.cuda.device(x.device):
+        _check(lib.abs_layer_norm(C.byref(shape), x.data_ptr(), weight.data_ptr(), bias.data_ptr() if bias is not None else None,
+                                  float(eps), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _stream_ptr()))
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy, x, weight, mean, rstd, has_bias: bool = True, want_norms: bool = False, want_inner: bool = False):
+    """Gradients of layer_norm from the signals dy [M, b, ..., D] of the per-sample losses, and the batch tests' statistics of
+    the gradient of weight and bias.  Returns (dx, dweight, dbias, n, q): batch gradients fp32 [M, D] (means over the b
+    samples; dbias None without a bias), n_i = ||g_i||^2 and q_i = <g_i, gbar> fp32 [M, b], None unless asked for."""
+    import torch
+    lib = load_library()
+    _type_of(x, "x")
+    shape = _norm_shape(x, _norm_params(x, weight, "weight"))
+    _type_of(dy, "dy")
+    _same_device(x, dy, mean, rstd)
+    if dy.shape != x.shape or dy.dtype != x.dtype:
+        raise AbsError("dy must have x's shape and type")
+    for t, what in ((mean, "mean"), (rstd, "rstd")):
+        if t.dtype != torch.float32 or t.shape != x.shape[:-1] or not t.is_contiguous():
+            raise AbsError(f"{what} must be a contiguous float32 tensor [M, b, ...]")
+    shape.stride_y, shape.ldy = _rows(dy, 1, "dy")
+    dev, M, b, D = x.device, shape.M, shape.b, shape.D
+    dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    dw = torch.empty((M, D), dtype=torch.float32, device=dev)
+    db = torch.empty((M, D), dtype=torch.float32, device=dev) if has_bias else None
+    n = torch.empty((M, b), dtype=torch.float32, device=dev) if want_norms else None
+    q = torch.empty((M, b), dtype=torch.float32, device=dev) if want_inner else None
+    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    nbytes = C.c_size_t(0)
+    with torch.cuda.device(dev):
+        _check(lib.abs_layer_norm_backward_workspace_bytes(C.byref(shape), int(bool(want_norms)), int(bool(want_inner)),
+                                                           C.byref(nbytes)))
+        ws = _Workspace(nbytes.value, dev)
+        _check(lib.abs_layer_norm_backward(C.byref(shape), dy.data_ptr(), x.data_ptr(), weight.data_ptr(), mean.data_ptr(),
+                                           rstd.data_ptr(), dx.data_ptr(), dw.data_ptr(), ptr(db), ptr(n), ptr(q), ws.ptr,
+                                           ws.nbytes, _stream_ptr()))
+    return dx, dw, db, n, q

@@ -14,6 +14,7 @@
 
 #include "../../include/abs.h"
 #include "abs_internal.h"
+#include "api_status.h"
 
 using namespace absk;
 
@@ -1872,4 +1873,6 @@ abs_status abs_average_bf16(void *params_dev, int M, int64_t n, void *scratch_de
 
 }  // extern "C"
 
+abs_status absk::set_error(abs_status st, const std::string &msg) { return fail(st, msg); }
+abs_status absk::exception_status() noexcept { return on_exception(); }
 void absk::set_chain_polls(abs_ctx *c, int polls) { c->chain_polls = polls; }

@@ -1,0 +1,618 @@
+// Layer norm, its gradients, and the statistics that the batch tests take of them.
+//
+//   mu = mean_d x,  r = 1 / sqrt(mean_d (x - mu)^2 + eps),  xh = (x - mu) r,  y = xh gamma + beta
+//   h = dy gamma,  dx = r (h - mean_d h - xh mean_d(h xh))
+//   sample i (T rows):  g_i = (sum_t dy xh, sum_t dy),   gbar = mean_i g_i,   n_i = ||g_i||^2,   q_i = <g_i, gbar>
+//
+// All of it is bound by memory: forward reads x and writes y, backward reads x and dy and writes dx.  A row lives in the
+// registers of a group of G lanes (16, 64 or 256, V vectors of 8 values to a lane), so it is read once; gains, biases and
+// the sums for gbar stay in the registers of the lanes that own their columns, over all rows of a block.  A block leaves
+// one partial of (sum dy xh, sum dy), and a second launch adds the partials in order: no atomics, the same bits every time.
+// The gradient of a gain is no outer product, so n_i has no factored form: samples of several rows are summed in
+// registers by the block that has all of their rows, or from the partials where a sample is spread over blocks.
+#include <algorithm>
+#include <cstring>
+#include "device_utils.h"
+#include "ops.h"
+#include "typed_mem.h"
+
+namespace absk {
+namespace {
+
+// ---- groups of lanes -----------------------------------------------------------------------------------------------
+
+// Sum over the 16 lanes of a DPP row, over a wavefront: every lane has it.
+template <int G> __device__ __forceinline__ float lanes_sum(float v) {
+  static_assert(G == 16 || G == 64, "a row or a wavefront");
+  v += dpp<0xB1>(v);                              // quad_perm [1,0,3,2]
+  v += dpp<0x4E>(v);                              // quad_perm [2,3,0,1]
+  v += dpp<0x141>(v);                             // row_half_mirror
+  v += dpp<0x140>(v);                             // row_mirror
+  if (G == 64) {
+    v += __shfl_xor(v, 16, 64);
+    v += __shfl_xor(v, 32, 64);
+  }
+  return v;
+}
+
+// Sums of N values over the group.  G = 256: through LDS, one barrier a call (`turn` picks one of two buffers, so that the
+// next call's values do not meet this one's readers); every thread of the block takes part.
+template <int G, int N>
+__device__ __forceinline__ void group_sums(float (&v)[N], float (*sm)[N * 4], int turn) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = lanes_sum<(G < 64 ? G : 64)>(v[i]);
+  if (G <= 64) return;
+  float *s = sm[turn & 1];
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i * 4 + wave] = v[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float4 f = *reinterpret_cast<const float4 *>(s + i * 4);
+    v[i] = (f.x + f.y) + (f.z + f.w);
+  }
+}
+
+// Columns of lane l in a row: VEC: vectors of eight, (v G + l) 8 + e; else single values, (8 v + e) G + l (rows that do not start
+// on 16 bytes or end inside a vector).
+template <int G, bool VEC> __device__ __forceinline__ int col_of(int v, int e, int l) { return VEC ? (v * G + l) * 8 + e : (v * 8 + e) * G + l; }
+
+// What a lane holds of a row as it comes from memory
+template <int TYPE, int V> struct Raw { uint4 q[V * (TYPE == TYPE_F32 ? 2 : 1)]; };
+
+template <int TYPE, int G, int V, bool VEC>
+__device__ __forceinline__ void load_raw(Raw<TYPE, V> &r, const void *p, long long at, int D, int l) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    if constexpr (TYPE == TYPE_F32) {
+      const float *f = static_cast<const float *>(p) + at;
+      if constexpr (VEC) {
+        const int c = col_of<G, true>(v, 0, l);
+        const bool in = c < D;
+        r.q[2 * v] = in ? *reinterpret_cast<const uint4 *>(f + c) : make_uint4(0, 0, 0, 0);
+        r.q[2 * v + 1] = in ? *reinterpret_cast<const uint4 *>(f + c + 4) : make_uint4(0, 0, 0, 0);
+      } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int c = col_of<G, false>(v, e, l);
+          w[e] = c < D ? __float_as_uint(f[c]) : 0u;
+        }
+        r.q[2 * v] = make_uint4(w[0], w[1], w[2], w[3]);
+        r.q[2 * v + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+      }
+    } else {
+      const uint16_t *h = static_cast<const uint16_t *>(p) + at;
+      if constexpr (VEC) {
+        const int c = col_of<G, true>(v, 0, l);
+        r.q[v] = c < D ? *reinterpret_cast<const uint4 *>(h + c) : make_uint4(0, 0, 0, 0);
+      } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int c = col_of<G, false>(v, e, l);
+          w[e] = c < D ? h[c] : 0u;
+        }
+        r.q[v] = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4] | (w[5] << 16), w[6] | (w[7] << 16));
+      }
+    }
+  }
+}
+template <int TYPE, int V> __device__ __forceinline__ void raw_vals(const Raw<TYPE, V> &r, int v, float (&f)[8]) {
+  if constexpr (TYPE == TYPE_F32) {
+    const uint4 a = r.q[2 * v], b = r.q[2 * v + 1];
+    f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
+    f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
+  } else {
+    unpack8(r.q[v], TYPE, f);
+  }
+}
+template <int TYPE, int G, bool VEC>
+__device__ __forceinline__ void store_vals(void *p, long long at, int D, int l, int v, const float (&f)[8]) {
+  if constexpr (VEC) {
+    const int c = col_of<G, true>(v, 0, l);
+    if (c < D) store8(p, TYPE, at + c, f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = col_of<G, false>(v, e, l);
+      if (c < D) store_from_f32(p, TYPE, at + c, f[e]);
+    }
+  }
+}
+template <int G, int V, bool VEC>
+__device__ __forceinline__ void load_param(float (&f)[V][8], const void *p, int type, long long at, int D, int l, float none) {
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = col_of<G, VEC>(v, e, l);
+      f[v][e] = p && c < D ? load_as_f32(p, type, at + c) : none;
+    }
+}
+
+// ---- forward -------------------------------------------------------------------------------------------------------
+
+// nb blocks per replica; a group takes every (nb 256 / G)-th row
+template <int TYPE, int G, int V, bool VEC>
+__global__ void __launch_bounds__(256) ln_forward_kernel(const LayerNormP p, const int nb) {
+  constexpr int GP = 256 / G;
+  __shared__ __attribute__((aligned(16))) float sm[2][4];
+  const int m = blockIdx.x / nb, j = blockIdx.x - m * nb, gid = threadIdx.x / G, l = threadIdx.x % G;
+  const long long rows = (long long)p.b * p.T;
+  const int D = p.D;
+  const float n = (float)D;                       // (divided by, not multiplied with its inverse: rows of one value have variance 0)
+  float ga[V][8], be[V][8];
+  load_param<G, V, VEC>(ga, p.gamma, p.ptype, (long long)m * D, D, l, 0.0f);
+  load_param<G, V, VEC>(be, p.beta, p.ptype, (long long)m * D, D, l, 0.0f);
+  int turn = 0;
+  for (long long r = (long long)j * GP + gid; r < rows; r += (long long)nb * GP) {
+    Raw<TYPE, V> raw;
+    load_raw<TYPE, G, V, VEC>(raw, p.x, m * p.sx + r * p.ldx, D, l);
+    float x[V][8], s[1] = {0.0f};
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      raw_vals<TYPE, V>(raw, v, x[v]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[0] += x[v][e];        // (zeros beyond the row)
+    }
+    group_sums<G, 1>(s, sm, turn++);
+    const float mean = s[0] / n;
+    s[0] = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float d = col_of<G, VEC>(v, e, l) < D ? x[v][e] - mean : 0.0f;
+        x[v][e] = d;
+        s[0] = fmaf(d, d, s[0]);
+      }
+    group_sums<G, 1>(s, sm, turn++);
+    const float rstd = 1.0f / sqrtf(s[0] / n + p.eps);
+    if (l == 0) {
+      if (p.mean) p.mean[m * rows + r] = mean;
+      if (p.rstd) p.rstd[m * rows + r] = rstd;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[v][e] = fmaf(x[v][e] * rstd, ga[v][e], be[v][e]);
+      store_vals<TYPE, G, VEC>(p.y, m * p.sy + r * p.ldy, D, l, v, x[v]);
+    }
+  }
+}
+
+// Rows longer than the registers of a block hold: three passes over the row, the later two out of the caches
+__global__ void __launch_bounds__(256) ln_forward_long_kernel(const LayerNormP p) {
+  __shared__ __attribute__((aligned(16))) float sm[2][4];
+  const long long rows = (long long)p.b * p.T, m = blockIdx.x / rows, r = blockIdx.x - m * rows;
+  const long long xa = m * p.sx + r * p.ldx, ya = m * p.sy + r * p.ldy, pa = m * p.D;
+  const float n = (float)p.D;
+  float s[1] = {0.0f};
+  for (int c = threadIdx.x; c < p.D; c += 256) s[0] += load_as_f32(p.x, p.type, xa + c);
+  group_sums<256, 1>(s, sm, 0);
+  const float mean = s[0] / n;
+  s[0] = 0.0f;
+  for (int c = threadIdx.x; c < p.D; c += 256) {
+    const float d = load_as_f32(p.x, p.type, xa + c) - mean;
+    s[0] = fmaf(d, d, s[0]);
+  }
+  group_sums<256, 1>(s, sm, 1);
+  const float rstd = 1.0f / sqrtf(s[0] / n + p.eps);
+  if (threadIdx.x == 0) {
+    if (p.mean) p.mean[m * rows + r] = mean;
+    if (p.rstd) p.rstd[m * rows + r] = rstd;
+  }
+  for (int c = threadIdx.x; c < p.D; c += 256) {
+    const float xh = (load_as_f32(p.x, p.type, xa + c) - mean) * rstd;
+    store_from_f32(p.y, p.type, ya + c, fmaf(xh, load_as_f32(p.gamma, p.ptype, pa + c), p.beta ? load_as_f32(p.beta, p.ptype, pa + c) : 0.0f));
+  }
+}
+
+// ---- backward ------------------------------------------------------------------------------------------------------
+
+enum { STAT_NONE = 0, STAT_ROW = 1, STAT_SAMPLE = 2 };   // n_i: not here; of samples that are one row; of samples of several
+
+// How the rows of a replica are dealt to its nb blocks: `per` whole samples each (chunks == 1; without statistics every row is a
+// sample), or a sample's rows in `chunks` blocks of `per` rows.
+struct LnSplit {
+  int samples, T, nb, chunks, per;
+  int tiles;             // column tiles of a row longer than a block's registers
+  float *part;           // [M nb][2][D] partial sums of dy xh and dy
+  float *npart;          // [tiles][M samples] partial n (tiles > 1 or chunks > 1)
+  const float *sums;     // [M rows][2] mean_d h, mean_d(h xh) of long rows
+};
+
+template <int TYPE, int G, int V, bool VEC, int R, int STAT, bool LONG>
+__global__ void __launch_bounds__(256) ln_backward_kernel(const LayerNormP p, const LnSplit w) {
+  constexpr int GP = 256 / G;
+  constexpr int NS = STAT == STAT_NONE ? 2 : 3;
+  static_assert(!LONG || G == 256, "a tile of a long row is a block's");
+  __shared__ __attribute__((aligned(16))) float sm[2][R * NS * 4];
+  __shared__ float comb[GP > 1 ? GP * G * V * 8 : 1];
+  const int bid = LONG ? blockIdx.x / w.tiles : blockIdx.x, tile = LONG ? blockIdx.x - bid * w.tiles : 0;
+  const int m = bid / w.nb, j = bid - m * w.nb, gid = threadIdx.x / G, l = threadIdx.x % G;
+  const int c0 = tile * G * V * 8, D = min(p.D - c0, G * V * 8);      // this block's columns
+  const long long rows = (long long)p.b * p.T;
+  const float inv = 1.0f / (float)p.D;
+  // the group's rows: count of them, the q-th at row(q); samples end where t == T - 1
+  long long first, count, hop;
+  const int T = w.T;
+  if (w.chunks > 1) {
+    const int i = j / w.chunks, ch = j - i * w.chunks;
+    const long long r0 = (long long)i * T + (long long)ch * w.per, r1 = min(r0 + w.per, (long long)(i + 1) * T);
+    first = r0 + gid;
+    count = first < r1 ? (r1 - first + GP - 1) / GP : 0;
+    hop = GP;
+  } else {
+    const long long i0 = (long long)j * w.per + gid, i1 = min((long long)(j + 1) * w.per, (long long)w.samples);
+    first = i0 * T;
+    count = i0 < i1 ? (i1 - i0 + GP - 1) / GP * T : 0;
+    hop = 0;                                      // rows of a sample, then the sample GP further on
+  }
+  float ga[V][8], tw[V][8], tb[V][8], gw[STAT == STAT_SAMPLE ? V : 1][8], gb[STAT == STAT_SAMPLE ? V : 1][8];
+  load_param<G, V, VEC>(ga, p.gamma, p.ptype, (long long)m * p.D + c0, D, l, 0.0f);
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      tw[v][e] = tb[v][e] = 0.0f;
+      if (STAT == STAT_SAMPLE) gw[v][e] = gb[v][e] = 0.0f;
+    }
+  const bool bias = p.dbeta != nullptr;
+  int turn = 0, t = 0;
+  long long row = first;
+  for (long long q = 0; q < count; q += R, ++turn) {
+    Raw<TYPE, V> rx[R], ry[R];
+    float mean[R], rstd[R], s[R * NS];
+    long long at[R];
+    bool ends[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const bool in = q + k < count;
+      at[k] = in ? row : -1;
+      ends[k] = false;
+      if (in) {
+        load_raw<TYPE, G, V, VEC>(rx[k], p.x, m * p.sx + row * p.ldx + c0, D, l);
+        load_raw<TYPE, G, V, VEC>(ry[k], p.dy, m * p.sy + row * p.ldy + c0, D, l);
+        mean[k] = p.mean[m * rows + row];
+        rstd[k] = p.rstd[m * rows + row];
+        ends[k] = t == T - 1;
+        if (hop) row += hop;
+        else if (ends[k]) { t = 0; row += (long long)(GP - 1) * T + 1; }
+        else { ++t; ++row; }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      float s1 = 0.0f, s2 = 0.0f, sn = 0.0f;
+      if (at[k] >= 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          float x[8], dy[8];
+          raw_vals<TYPE, V>(rx[k], v, x);
+          raw_vals<TYPE, V>(ry[k], v, dy);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            // (beyond the row dy is zero; x - mean is not, so nothing but products with dy may use it)
+            const float xh = (x[e] - mean[k]) * rstd[k], h = dy[e] * ga[v][e], dw = dy[e] * xh;
+            s1 += h;
+            s2 = fmaf(h, xh, s2);
+            if (STAT == STAT_SAMPLE) { gw[v][e] += dw; gb[v][e] += dy[e]; }
+            else { tw[v][e] += dw; tb[v][e] += dy[e]; }
+            if (STAT == STAT_ROW) {
+              sn = fmaf(dw, dw, sn);
+              if (bias) sn = fmaf(dy[e], dy[e], sn);
+            }
+          }
+        }
+        if (STAT == STAT_SAMPLE && ends[k]) {
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              sn = fmaf(gw[v][e], gw[v][e], sn);
+              if (bias) sn = fmaf(gb[v][e], gb[v][e], sn);
+              tw[v][e] += gw[v][e]; tb[v][e] += gb[v][e];
+              gw[v][e] = gb[v][e] = 0.0f;
+            }
+        }
+      }
+      s[k * NS] = s1;
+      s[k * NS + 1] = s2;
+      if (NS == 3) s[k * NS + 2] = sn;
+    }
+    if (!LONG || NS == 3) group_sums<G, R * NS>(s, sm, turn);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      if (at[k] < 0) continue;
+      float a = s[k * NS] * inv, c = s[k * NS + 1] * inv;
+      if (LONG) { a = w.sums[(m * rows + at[k]) * 2]; c = w.sums[(m * rows + at[k]) * 2 + 1]; }
+      if (STAT != STAT_NONE && ends[k] && l == 0) {
+        const long long i = (long long)m * p.b + at[k] / T;
+        if (LONG) w.npart[(long long)tile * p.M * p.b + i] = s[k * NS + 2];
+        else p.n[i] = s[k * NS + 2];
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float x[8], dy[8], d[8];
+        raw_vals<TYPE, V>(rx[k], v, x);
+        raw_vals<TYPE, V>(ry[k], v, dy);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float xh = (x[e] - mean[k]) * rstd[k];
+          d[e] = rstd[k] * (fmaf(dy[e], ga[v][e], -a) - xh * c);
+        }
+        store_vals<TYPE, G, VEC>(p.dx, m * p.sdx + at[k] * p.lddx + c0, D, l, v, d);
+      }
+    }
+  }
+  // the block's partial: groups added in order through LDS
+  float *out = w.part + ((long long)m * w.nb + j) * 2 * p.D + c0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (GP == 1) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int c = col_of<G, VEC>(v, e, l);
+          if (c < D) out[(long long)h * p.D + c] = h ? tb[v][e] : tw[v][e];
+        }
+    } else {
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) comb[gid * G * V * 8 + col_of<G, VEC>(v, e, l)] = h ? tb[v][e] : tw[v][e];
+      __syncthreads();
+      for (int c = threadIdx.x; c < D; c += 256) {
+        float a = 0.0f;
+#pragma unroll
+        for (int g = 0; g < GP; ++g) a += comb[g * G * V * 8 + c];
+        out[(long long)h * p.D + c] = a;
+      }
+    }
+  }
+}
+
+// mean_d h and mean_d(h xh) of long rows
+__global__ void __launch_bounds__(256) ln_row_sums_kernel(const LayerNormP p, float *sums) {
+  __shared__ __attribute__((aligned(16))) float sm[2][8];
+  const long long rows = (long long)p.b * p.T, m = blockIdx.x / rows, r = blockIdx.x - m * rows;
+  const float mean = p.mean[m * rows + r], rstd = p.rstd[m * rows + r], inv = 1.0f / (float)p.D;
+  float s[2] = {0.0f, 0.0f};
+  for (int c = threadIdx.x; c < p.D; c += 256) {
+    const float h = load_as_f32(p.dy, p.type, m * p.sy + r * p.ldy + c) * load_as_f32(p.gamma, p.ptype, m * p.D + c);
+    s[0] += h;
+    s[1] = fmaf(h, (load_as_f32(p.x, p.type, m * p.sx + r * p.ldx + c) - mean) * rstd, s[1]);
+  }
+  group_sums<256, 2>(s, sm, 0);
+  if (threadIdx.x == 0) { sums[blockIdx.x * 2LL] = s[0] * inv; sums[blockIdx.x * 2LL + 1] = s[1] * inv; }
+}
+
+// Sample spread over blocks: g_i = sum of its chunks' partials, left in the first of them; n_i's share of 256 columns.
+__global__ void __launch_bounds__(256) ln_sample_kernel(const LayerNormP p, const LnSplit w, const int tiles) {
+  __shared__ double sm[4];
+  const int i = blockIdx.x / tiles, tile = blockIdx.x - i * tiles, c = tile * 256 + threadIdx.x;      // i = m b + sample
+  float *part = w.part + (long long)i * w.chunks * 2 * p.D;
+  float g = 0.0f;
+  if (c < 2 * p.D) {
+    for (int k = 0; k < w.chunks; ++k) g += part[(long long)k * 2 * p.D + c];
+    part[c] = g;
+  }
+  const double n = block_sum<4>(c < (p.dbeta ? 2 : 1) * p.D ? (double)g * g : 0.0, sm);
+  if (threadIdx.x == 0 && w.npart) w.npart[(long long)tile * p.M * p.b + i] = (float)n;
+}
+
+// gbar = (1 / b) sum of the partials j step, j < count, in order; further blocks add n_i's shares.
+__global__ void __launch_bounds__(256) ln_finish_kernel(const LayerNormP p, const LnSplit w, const int count, const int step, const int colblocks, const int nshares) {
+  __shared__ float sm[4][64];
+  const int nfin = colblocks * p.M;
+  if ((int)blockIdx.x >= nfin) {
+    const long long i = (blockIdx.x - nfin) * 256LL + threadIdx.x, n = (long long)p.M * p.b;
+    if (i >= n) return;
+    float a = 0.0f;
+    for (int k = 0; k < nshares; ++k) a += w.npart[k * n + i];
+    p.n[i] = a;
+    return;
+  }
+  const int m = blockIdx.x / colblocks, c = (blockIdx.x - m * colblocks) * 64 + (threadIdx.x & 63), q = threadIdx.x >> 6;
+  const int per = (count + 3) / 4, j1 = min(count, (q + 1) * per);
+  const float *part = w.part + (long long)m * w.nb * 2 * p.D + c;
+  float a = 0.0f;
+  if (c < 2 * p.D)
+    for (int j = q * per; j < j1; ++j) a += part[(long long)j * step * 2 * p.D];
+  sm[q][threadIdx.x & 63] = a;
+  __syncthreads();
+  if (q == 0 && c < 2 * p.D) {
+    const int k = threadIdx.x & 63;
+    const float g = ((sm[0][k] + sm[1][k]) + (sm[2][k] + sm[3][k])) * (1.0f / (float)p.b);
+    if (c < p.D) p.dgamma[(long long)m * p.D + c] = g;
+    else if (p.dbeta) p.dbeta[(long long)m * p.D + c - p.D] = g;
+  }
+}
+
+// q_i from the sums that ln_sample_kernel left
+__global__ void __launch_bounds__(256) ln_inner_partials_kernel(const LayerNormP p, const LnSplit w) {
+  __shared__ double sm[4];
+  const int i = blockIdx.x, m = i / p.b;
+  const float *g = w.part + (long long)i * w.chunks * 2 * p.D;
+  double a = 0.0;
+  for (int c = threadIdx.x; c < p.D; c += 256) {
+    a += (double)g[c] * p.dgamma[(long long)m * p.D + c];
+    if (p.dbeta) a += (double)g[p.D + c] * p.dbeta[(long long)m * p.D + c];
+  }
+  a = block_sum<4>(a, sm);
+  if (threadIdx.x == 0) p.q[i] = (float)a;
+}
+
+// q_i from a second look at the rows: sum_t sum_d dy (xh gbar_gamma + gbar_beta).  A group of G lanes per sample.
+template <int G> __global__ void __launch_bounds__(256) ln_inner_rows_kernel(const LayerNormP p) {
+  constexpr int GP = 256 / G;
+  const long long i = (long long)blockIdx.x * GP + threadIdx.x / G, rows = (long long)p.b * p.T;
+  if (i >= (long long)p.M * p.b) return;
+  const int l = threadIdx.x % G;
+  const long long m = i / p.b, r0 = (i - m * p.b) * p.T;
+  float a = 0.0f;
+  for (int t = 0; t < p.T; ++t) {
+    const long long r = r0 + t, xa = m * p.sx + r * p.ldx, ya = m * p.sy + r * p.ldy;
+    const float mean = p.mean[m * rows + r], rstd = p.rstd[m * rows + r];
+    for (int c = l; c < p.D; c += G) {
+      const float xh = (load_as_f32(p.x, p.type, xa + c) - mean) * rstd;
+      a = fmaf(load_as_f32(p.dy, p.type, ya + c), fmaf(xh, p.dgamma[m * p.D + c], p.dbeta ? p.dbeta[m * p.D + c] : 0.0f), a);
+    }
+  }
+  a = lanes_sum<G>(a);
+  if (l == 0) p.q[i] = a;
+}
+
+// ---- choices -------------------------------------------------------------------------------------------------------
+
+constexpr int LN_MAX_D = 8192;           // longest row that a block's registers hold
+constexpr int LN_BLOCKS = 1024;          // blocks of 256 threads that fill the chip
+
+// lanes and vectors to a row: 16 x 1, 64 x 1, 256 x 1, 2, 4
+int ln_shape(int D) { return D <= 128 ? 0 : D <= 512 ? 1 : D <= 2048 ? 2 : D <= 4096 ? 3 : 4; }
+int ln_groups(int D) { return D <= 128 ? 16 : D <= 512 ? 4 : 1; }       // to a block
+
+LnSplit ln_split(const LayerNormP &p, bool want) {
+  LnSplit w;
+  std::memset(&w, 0, sizeof(w));
+  const long long rows = (long long)p.b * p.T;
+  w.tiles = p.D > LN_MAX_D ? (p.D + 2047) / 2048 : 1;
+  const long long most = std::max(1, LN_BLOCKS / std::min(LN_BLOCKS, p.M * w.tiles));
+  const long long few = 16LL * ln_groups(p.D);                          // rows that pay for a partial
+  w.samples = want ? p.b : (int)rows; w.T = want ? p.T : 1; w.chunks = 1;
+  if (want && w.T >= 2 * few && p.b * 2LL <= most) {                    // few long samples: several blocks to each
+    w.chunks = (int)std::max(1LL, std::min((w.T + few - 1) / few, most / p.b));
+    w.per = (w.T + w.chunks - 1) / w.chunks;
+    w.chunks = (w.T + w.per - 1) / w.per;
+    if (w.chunks > 1) { w.nb = w.samples * w.chunks; return w; }
+  }
+  const long long nb = std::max(1LL, std::min(most, (rows + few - 1) / few));
+  w.per = (int)((w.samples + nb - 1) / nb);
+  w.nb = (w.samples + w.per - 1) / w.per;
+  return w;
+}
+int ln_sample_tiles(const LayerNormP &p) { return (2 * p.D + 255) / 256; }
+
+struct LnPieces { size_t part, npart, sums, total; };
+LnPieces ln_pieces(const LayerNormP &p, const LnSplit &w, bool want_n) {
+  LnPieces q;
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t r = o; o = (o + bytes + 255) / 256 * 256; return r; };
+  q.part = take((size_t)p.M * w.nb * 2 * p.D * 4);
+  q.npart = take(want_n ? (size_t)p.M * p.b * 4 * (w.chunks > 1 ? ln_sample_tiles(p) : w.tiles > 1 ? w.tiles : 0) : 0);
+  q.sums = take(w.tiles > 1 ? (size_t)p.M * p.b * p.T * 8 : 0);
+  q.total = o;
+  return q;
+}
+
+template <int TYPE, int G, int V, bool VEC, int R, bool LONG>
+hipError_t backward_stat(const LayerNormP &p, const LnSplit &w, bool want_n, hipStream_t s) {
+  const long long blocks = (long long)p.M * w.nb * w.tiles;
+  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks), block(256);
+  if (!want_n || w.chunks > 1) hipLaunchKernelGGL((ln_backward_kernel<TYPE, G, V, VEC, R, STAT_NONE, LONG>), grid, block, 0, s, p, w);
+  else if (w.T == 1) hipLaunchKernelGGL((ln_backward_kernel<TYPE, G, V, VEC, R, STAT_ROW, LONG>), grid, block, 0, s, p, w);
+  else hipLaunchKernelGGL((ln_backward_kernel<TYPE, G, V, VEC, R, STAT_SAMPLE, LONG>), grid, block, 0, s, p, w);
+  return hipGetLastError();
+}
+template <int TYPE, bool VEC>
+hipError_t backward_shape(const LayerNormP &p, const LnSplit &w, bool want_n, hipStream_t s) {
+  if (w.tiles > 1) return backward_stat<TYPE, 256, 1, VEC, 4, true>(p, w, want_n, s);
+  switch (ln_shape(p.D)) {
+    case 0: return backward_stat<TYPE, 16, 1, VEC, 4, false>(p, w, want_n, s);
+    case 1: return backward_stat<TYPE, 64, 1, VEC, 4, false>(p, w, want_n, s);
+    case 2: return backward_stat<TYPE, 256, 1, VEC, 4, false>(p, w, want_n, s);
+    case 3: return backward_stat<TYPE, 256, 2, VEC, 2, false>(p, w, want_n, s);
+    default: return backward_stat<TYPE, 256, 4, VEC, 1, false>(p, w, want_n, s);
+  }
+}
+
+template <int TYPE, int G, int V, bool VEC> hipError_t forward_cfg(const LayerNormP &p, hipStream_t s) {
+  const long long rows = (long long)p.b * p.T, gp = 256 / G;
+  const long long nb = std::max(1LL, std::min((rows + gp - 1) / gp, (2LL * LN_BLOCKS + p.M - 1) / p.M));
+  hipLaunchKernelGGL((ln_forward_kernel<TYPE, G, V, VEC>), dim3((unsigned)(nb * p.M)), dim3(256), 0, s, p, (int)nb);
+  return hipGetLastError();
+}
+template <int TYPE, bool VEC> hipError_t forward_shape(const LayerNormP &p, hipStream_t s) {
+  switch (ln_shape(p.D)) {
+    case 0: return forward_cfg<TYPE, 16, 1, VEC>(p, s);
+    case 1: return forward_cfg<TYPE, 64, 1, VEC>(p, s);
+    case 2: return forward_cfg<TYPE, 256, 1, VEC>(p, s);
+    case 3: return forward_cfg<TYPE, 256, 2, VEC>(p, s);
+    default: return forward_cfg<TYPE, 256, 4, VEC>(p, s);
+  }
+}
+
+}  // namespace
+
+size_t layer_norm_backward_bytes(const LayerNormP &p, bool want_n, bool want_q) {
+  return ln_pieces(p, ln_split(p, want_n || want_q), want_n).total;
+}
+
+hipError_t launch_layer_norm(const LayerNormP &p, hipStream_t s) {
+  const long long rows = (long long)p.b * p.T;
+  if (rows == 0) return hipSuccess;
+  if (rows * p.M > 0x7fffffff) return hipErrorInvalidValue;
+  if (p.D > LN_MAX_D) {
+    hipLaunchKernelGGL(ln_forward_long_kernel, dim3((unsigned)(rows * p.M)), dim3(256), 0, s, p);
+    return hipGetLastError();
+  }
+  const bool vec = rows_of_vectors(p.x, p.type, p.sx, p.ldx, p.D) && rows_of_vectors(p.y, p.type, p.sy, p.ldy, p.D);
+  switch (p.type) {
+    case TYPE_F32: return vec ? forward_shape<TYPE_F32, true>(p, s) : forward_shape<TYPE_F32, false>(p, s);
+    case TYPE_BF16: return vec ? forward_shape<TYPE_BF16, true>(p, s) : forward_shape<TYPE_BF16, false>(p, s);
+    default: return vec ? forward_shape<TYPE_F16, true>(p, s) : forward_shape<TYPE_F16, false>(p, s);
+  }
+}
+
+hipError_t launch_layer_norm_backward(const LayerNormP &p, void *workspace, hipStream_t s) {
+  const long long rows = (long long)p.b * p.T;
+  if (rows * p.M > 0x7fffffff) return hipErrorInvalidValue;
+  const bool want_n = p.n != nullptr, want = want_n || p.q;
+  LnSplit w = ln_split(p, want);
+  const LnPieces at = ln_pieces(p, w, want_n);
+  unsigned char *ws = static_cast<unsigned char *>(workspace);
+  w.part = reinterpret_cast<float *>(ws + at.part);
+  w.npart = want_n ? reinterpret_cast<float *>(ws + at.npart) : nullptr;
+  if (w.tiles > 1) {
+    float *sums = reinterpret_cast<float *>(ws + at.sums);
+    hipLaunchKernelGGL(ln_row_sums_kernel, dim3((unsigned)(rows * p.M)), dim3(256), 0, s, p, sums);
+    w.sums = sums;
+  }
+  const bool vec = rows_of_vectors(p.x, p.type, p.sx, p.ldx, p.D) && rows_of_vectors(p.dy, p.type, p.sy, p.ldy, p.D) &&
+                   rows_of_vectors(p.dx, p.type, p.sdx, p.lddx, p.D);
+  hipError_t e;
+  switch (p.type) {
+    case TYPE_F32: e = vec ? backward_shape<TYPE_F32, true>(p, w, want_n, s) : backward_shape<TYPE_F32, false>(p, w, want_n, s); break;
+    case TYPE_BF16: e = vec ? backward_shape<TYPE_BF16, true>(p, w, want_n, s) : backward_shape<TYPE_BF16, false>(p, w, want_n, s); break;
+    default: e = vec ? backward_shape<TYPE_F16, true>(p, w, want_n, s) : backward_shape<TYPE_F16, false>(p, w, want_n, s); break;
+  }
+  if (e != hipSuccess) return e;
+  int nshares = 0;
+  if (w.chunks > 1) {
+    nshares = ln_sample_tiles(p);
+    hipLaunchKernelGGL(ln_sample_kernel, dim3((unsigned)((long long)p.M * p.b * nshares)), dim3(256), 0, s, p, w, nshares);
+    if (!want_n) nshares = 0;
+  } else if (w.tiles > 1 && want_n) {
+    nshares = w.tiles;
+  }
+  const int colblocks = (2 * p.D + 63) / 64;
+  const int count = w.chunks > 1 ? w.samples : w.nb;
+  const long long nblocks = nshares ? ((long long)p.M * p.b + 255) / 256 : 0;
+  hipLaunchKernelGGL(ln_finish_kernel, dim3((unsigned)(colblocks * p.M + nblocks)), dim3(256), 0, s, p, w, count, w.chunks, colblocks, nshares);
+  if (p.q) {
+    if (w.chunks > 1) hipLaunchKernelGGL(ln_inner_partials_kernel, dim3((unsigned)((long long)p.M * p.b)), dim3(256), 0, s, p, w);
+    else if (p.D <= 128) hipLaunchKernelGGL(ln_inner_rows_kernel<16>, dim3((unsigned)(((long long)p.M * p.b + 15) / 16)), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(ln_inner_rows_kernel<64>, dim3((unsigned)(((long long)p.M * p.b + 3) / 4)), dim3(256), 0, s, p);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace absk

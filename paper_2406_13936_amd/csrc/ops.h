@@ -1,0 +1,63 @@
+// Internal declarations of the operators that stand beside the replicas' step: the orthogonalised update (orthogonalize.hip)
+// and layer norm (layer_norm.hip).  Host launchers only; kernels stay private to their file.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+#include "abs_internal.h"
+
+namespace absk {
+
+enum { TYPE_F32 = 0, TYPE_BF16 = 1, TYPE_F16 = 2 };
+inline int type_bytes(int t) { return t == TYPE_F32 ? 4 : 2; }
+
+// ---- orthogonalisation ---------------------------------------------------------------------------------------------
+
+constexpr int ORTH_MAX_STEPS = 32;
+constexpr int ORTH_PARTS = 256;          // most partial sums of a matrix's norm
+
+struct OrthPlan {
+  int batch, rows, cols, steps, split;   // split: operands as sums of two fp16 values (fp32-class products)
+  int wide;                              // rows <= cols: the products A = X X^T, else A = X^T X
+  int rp, cp, mp;                        // rows, columns and the smaller side rounded up to 8
+  int nparts;                            // partial sums of a matrix's norm
+  float a[ORTH_MAX_STEPS], b[ORTH_MAX_STEPS], c[ORTH_MAX_STEPS];
+  int ex[ORTH_MAX_STEPS + 1], ea[ORTH_MAX_STEPS], eb[ORTH_MAX_STEPS];   // powers of two that X, A and B are stored with
+  size_t o_part, o_x[2], o_xl[2], o_a, o_al, o_b, o_bl, total;          // pieces of the workspace
+};
+
+// What is orthogonalised: G, or with a momentum buffer (fp32) v <- momentum v + G and u = nesterov ? G + momentum v : v.
+struct OrthIn {
+  const void *g; int type; long long sg; int ldg;
+  float *v; long long sv; float momentum; int nesterov;      // v: rows of cols values
+};
+// Where the result goes: O, or with `update` the step  x <- (1 - lr wd) x - lr scale O  on x (and its bf16 copy).
+struct OrthOut {
+  void *o; int type; long long so; int ldo;
+  int update; float lr, scale, wd;
+  const float *scal;                     // optional (device): lr is read from scal[0], for launches that are replayed
+  bf16_t *shadow; long long sshadow;     // rows of ldo values
+};
+
+// nullptr, or why these coefficients (3 per step; null: the quintic's) cannot be taken
+const char *orth_plan(int batch, int rows, int cols, int split, int steps, const float *coef, OrthPlan &pl);
+hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, void *workspace, hipStream_t s);
+
+// ---- layer norm ----------------------------------------------------------------------------------------------------
+
+// M replicas with gains and biases of their own [M x D]; each has b samples of T rows of D values.
+struct LayerNormP {
+  int M, b, T, D, type, ptype;
+  long long ldx, sx, ldy, sy, lddx, sdx;   // x; y or dy; dx: values from row to row and from replica to replica
+  const void *x, *gamma, *beta;            // beta may be null
+  float eps;
+  void *y; float *mean, *rstd;             // forward: outputs (mean and rstd may be null); backward: inputs
+  const void *dy;
+  void *dx; float *dgamma, *dbeta;         // dbeta, n, q may be null
+  float *n, *q;
+};
+size_t layer_norm_backward_bytes(const LayerNormP &p, bool want_n, bool want_q);
+hipError_t launch_layer_norm(const LayerNormP &p, hipStream_t s);
+hipError_t launch_layer_norm_backward(const LayerNormP &p, void *workspace, hipStream_t s);
+
+}  // namespace absk

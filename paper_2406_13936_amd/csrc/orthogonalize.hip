@@ -1,0 +1,536 @@
+// Orthogonalisation of matrices by Newton-Schulz products, and the update that is taken with the result.
+//
+//   X_0 = G / (||G||_F + eps),    A = X X^T,   B = b A + c A^2,   X <- a X + B X      (rows <= cols)
+//                                 A = X^T X,                      X <- a X + X B      (rows >  cols)
+//
+// X keeps its singular vectors and its singular values s go through p(s) = a s + b s^3 + c s^5 in every step; after five
+// steps of the usual quintic they lie around 1.  The smaller side m is the side of A and B.
+//
+// Numbers.  X is held as the sum of two fp16 values (22 bits and a sign, as exact as fp32 in these sums); the products take
+// the first of them (16-bit mode) or, with `split`, all of (hi + lo)(hi + lo) but lo lo, which is what fp32 products give.
+// fp16 and not bf16, because every entry of X, A and B is bounded by a spectral norm that the host knows beforehand
+// (s <= 1 before the first step and max |p| on that interval after it): each is stored times a power of two that puts
+// this bound just under fp16's largest value, so three more bits of mantissa come free.  Relative error of the result
+// for 64 x 64 to 1536 x 1536 matrices of full rank, rank 64 and of a spectrum falling over five decades: 0.5 to 2.1e-3
+// (bf16 operands 5e-3 to 1.5e-2), with `split` the same as fp32 products (1.2e-6 to 1.2e-5).  Why X cannot be rounded to 16 bits: a step
+// multiplies a singular value near 0 by a = 3.4, five of them by 485, and with it the rounding noise that lies along
+// those directions (rank 64 in 256 x 512: 1.8e-2 with fp16, 0.15 with bf16).  B X makes no such noise from a rounded X,
+// since B's range is that of X.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <mutex>
+#include "device_utils.h"
+#include "mfma_tile.h"
+#include "ops.h"
+#include "typed_mem.h"
+
+namespace absk {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+namespace {
+
+// eight values as fp16 and what that leaves
+__device__ __forceinline__ void split8(const float (&v)[8], uint4 &hi, uint4 &lo) {
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint16_t h0 = f16_bits(v[2 * e]), h1 = f16_bits(v[2 * e + 1]);
+    h[e] = (uint32_t)h0 | ((uint32_t)h1 << 16);
+    l[e] = (uint32_t)f16_bits(v[2 * e] - f16_val(h0)) | ((uint32_t)f16_bits(v[2 * e + 1] - f16_val(h1)) << 16);
+  }
+  hi = make_uint4(h[0], h[1], h[2], h[3]);
+  lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// ---- norm and first X ----------------------------------------------------------------------------------------------
+
+struct OrthPrepP {
+  OrthIn in;
+  int rows, cols, rp, cp, nparts, vec, ex;   // vec: all rows start on 16 bytes, cols is a multiple of 8
+  double *part; uint16_t *xh, *xl;
+  float eps;
+};
+
+// Sum of squares of a matrix in fp64 (entries of any size fp32 has), one partial per block; with a momentum buffer this is
+// where it advances.  One pass over G (and v): bound by memory.
+__global__ void __launch_bounds__(256) orth_norm_kernel(const OrthPrepP p) {
+  __shared__ double sm[4];
+  const int z = blockIdx.y;
+  const long long g0 = z * p.in.sg, v0 = z * p.in.sv;
+  const float mu = p.in.momentum;
+  double sum = 0.0;
+  if (p.vec) {
+    const int cc = p.cols >> 3, n = p.rows * cc;
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+      const int r = i / cc, c = (i - r * cc) * 8;
+      float g[8];
+      load8(p.in.g, p.in.type, g0 + (long long)r * p.in.ldg + c, g);
+      if (p.in.v) {
+        float v[8];
+        const long long at = v0 + (long long)r * p.cols + c;
+        load8(p.in.v, TYPE_F32, at, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[e] = fmaf(mu, v[e], g[e]);
+          g[e] = p.in.nesterov ? fmaf(mu, v[e], g[e]) : v[e];
+        }
+        store8(p.in.v, TYPE_F32, at, v);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fma((double)g[e], (double)g[e], sum);
+    }
+  } else {
+    const long long n = (long long)p.rows * p.cols;
+    for (long long i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+      const int r = (int)(i / p.cols), c = (int)(i - (long long)r * p.cols);
+      float g = load_as_f32(p.in.g, p.in.type, g0 + (long long)r * p.in.ldg + c);
+      if (p.in.v) {
+        const float v = fmaf(mu, p.in.v[v0 + i], g);
+        p.in.v[v0 + i] = v;
+        g = p.in.nesterov ? fmaf(mu, v, g) : v;
+      }
+      sum = fma((double)g, (double)g, sum);
+    }
+  }
+  const double t = block_sum<4>(sum, sm);
+  if (threadIdx.x == 0) p.part[(long long)z * p.nparts + blockIdx.x] = t;
+}
+
+// X_0 2^ex as two fp16 values, zeros in the rows and columns that round the sides up to 8
+__global__ void __launch_bounds__(256) orth_prep_kernel(const OrthPrepP p) {
+  __shared__ double sm[4];
+  __shared__ double scale;
+  const int z = blockIdx.y;
+  const double t = block_sum<4>((int)threadIdx.x < p.nparts ? p.part[(long long)z * p.nparts + threadIdx.x] : 0.0, sm);
+  if (threadIdx.x == 0) scale = ldexp(1.0 / (sqrt(t) + (double)p.eps), p.ex);
+  __syncthreads();
+  const double sc = scale;
+  const long long g0 = z * p.in.sg, v0 = z * p.in.sv, x0 = (long long)z * p.rp * p.cp;
+  const float mu = p.in.momentum;
+  const int cc = p.cp >> 3, n = p.rp * cc;
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+    const int r = i / cc, c = (i - r * cc) * 8;
+    float u[8];
+    if (p.vec && r < p.rows) {                     // (cols is a multiple of 8: the chunk lies inside)
+      load8(p.in.g, p.in.type, g0 + (long long)r * p.in.ldg + c, u);
+      if (p.in.v) {
+        float v[8];
+        load8(p.in.v, TYPE_F32, v0 + (long long)r * p.cols + c, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = p.in.nesterov ? fmaf(mu, v[e], u[e]) : v[e];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        u[e] = 0.0f;
+        if (r < p.rows && c + e < p.cols) {
+          u[e] = load_as_f32(p.in.g, p.in.type, g0 + (long long)r * p.in.ldg + c + e);
+          if (p.in.v) {
+            const float v = p.in.v[v0 + (long long)r * p.cols + c + e];
+            u[e] = p.in.nesterov ? fmaf(mu, v, u[e]) : v;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = (float)((double)u[e] * sc);
+    uint4 h, l;
+    split8(u, h, l);
+    const long long at = x0 + (long long)r * p.cp + c;
+    *reinterpret_cast<uint4 *>(p.xh + at) = h;
+    *reinterpret_cast<uint4 *>(p.xl + at) = l;
+  }
+}
+
+// ---- the products --------------------------------------------------------------------------------------------------
+
+// C[z][m][n] = alpha E[z][m][n] + beta sum_k A[z][m][k] B[z][n][k]   as one or two fp16 values, or the result of the last step
+struct OrthGemmP {
+  const uint16_t *A, *Al, *B, *Bl;       // (Al, Bl: with split)
+  long long sA, sB; int lda, ldb, Md, Nd, Kd, batch;
+  const uint16_t *E, *El; long long sE; int lde;
+  uint16_t *C, *Cl; long long sC; int ldc;
+  float alpha, beta;
+  int sym;                               // C is symmetric: tiles below the diagonal are written from those above it
+  OrthOut out; int rows, cols, vec;      // the last step (C null)
+};
+
+// Tiles BM x BN x BK with WM x WN wavefronts, NS stages of direct global -> LDS loads; operands k-contiguous or row-contiguous as
+// in gemm_bf16.hip.  SPLIT: the reduction runs three times over k, with (hi, lo), (lo, hi) and (hi, hi) as operands.
+template <int BM, int BN, int BK, int WM, int WN, int NS, bool AT, bool BT, bool SPLIT>
+__global__ void __launch_bounds__(WM * WN * 64) orth_gemm_kernel(const OrthGemmP p, const int tilesM, const int tilesN, const int nblk, const int chunk) {
+  constexpr int NW = WM * WN;
+  constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 32, NI = TN / 32;
+  constexpr int STAGE = (BM + BN) * BK, NPART = BK / 16;
+  typedef Operand<BM, BK, AT, NW> OpA;
+  typedef Operand<BN, BK, BT, NW> OpB;
+  constexpr int NL = OpA::NI + OpB::NI;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+  bf16_t *smem = reinterpret_cast<bf16_t *>(smem_raw);
+
+  const int lb = (blockIdx.x & 7) * chunk + (blockIdx.x >> 3);      // an XCD works on a contiguous range of tiles
+  if ((int)(blockIdx.x >> 3) >= chunk || lb >= nblk) return;
+  int z, tm, tn;
+  if (p.sym) {                                    // tiles (tm, tn >= tm) row by row
+    const int T = tilesN, per = T * (T + 1) / 2;
+    z = lb / per;
+    const int t = lb - z * per;
+    tm = (int)((2 * T + 1 - sqrtf((float)((2 * T + 1) * (2 * T + 1) - 8 * t))) * 0.5f);
+    tm = max(0, min(tm, T - 1));
+    while (tm > 0 && t < tm * T - tm * (tm - 1) / 2) --tm;          // (first tile of row tm: sum of T - r over r < tm)
+    while (t >= (tm + 1) * T - (tm + 1) * tm / 2) ++tm;
+    tn = tm + t - (tm * T - tm * (tm - 1) / 2);
+  } else {
+    const int per = tilesM * tilesN;
+    z = lb / per;
+    const int t = lb - z * per;
+    tm = t / tilesN; tn = t - tm * tilesN;
+  }
+  const int m0 = tm * BM, n0 = tn * BN;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+
+  const int abytes = (int)((long long)(AT ? p.Kd : p.Md) * p.lda * 2), bbytes = (int)((long long)(BT ? p.Kd : p.Nd) * p.ldb * 2);
+  auto rsrc = [](const uint16_t *q, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(q), 0, bytes, 0x00020000); };
+  const __amdgpu_buffer_rsrc_t rah = rsrc(p.A + z * p.sA, abytes), rbh = rsrc(p.B + z * p.sB, bbytes);
+  const __amdgpu_buffer_rsrc_t ral = rsrc(SPLIT ? p.Al + z * p.sA : p.A, abytes), rbl = rsrc(SPLIT ? p.Bl + z * p.sB : p.B, bbytes);
+
+  f32x16 acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  const int KT1 = (p.Kd + BK - 1) / BK, KT = SPLIT ? 3 * KT1 : KT1;
+  OpA oa;
+  OpB ob;
+  oa.init(wave, lane, m0, p.Md, p.lda);
+  ob.init(wave, lane, n0, p.Nd, p.ldb);
+  auto issue = [&](int kt, int buf, int part) {
+    bf16_t *sa = smem + buf * STAGE, *sb = sa + BM * BK;
+    const int seg = SPLIT ? (kt >= KT1) + (kt >= 2 * KT1) : 2;
+    const int k = SPLIT ? kt - seg * KT1 : kt;
+    const bool full = (k + 1) * BK <= p.Kd;
+#pragma unroll
+    for (int l = 0; l < NL; ++l) {
+      if (l % NPART != part) continue;
+      if (l < OpA::NI) oa.load(l, SPLIT && seg == 1 ? ral : rah, sa, wave, k, p.Kd, p.lda, full);
+      else ob.load(l - OpA::NI, SPLIT && seg == 0 ? rbl : rbh, sb, wave, k, p.Kd, p.ldb, full);
+    }
+  };
+  Frag<BM, BK, AT> fa[MI];
+  Frag<BN, BK, BT> fb[NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) fa[i].init(wm * TM + i * 32, lane);
+#pragma unroll
+  for (int j = 0; j < NI; ++j) fb[j].init(wn * TN + j * 32, lane);
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s)
+    if (s < KT) {
+#pragma unroll
+      for (int q = 0; q < NPART; ++q) issue(s, s, q);
+    }
+  for (int kt = 0; kt < KT; ++kt) {
+    if (kt + NS - 1 <= KT) wait_vmcnt<(NS - 2) * NL>(); else wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();                 // all waves' loads of kt visible; everyone is done with kt-1
+    const bool more = kt + NS - 1 < KT;
+    const bf16_t *S = smem + (kt % NS) * STAGE;
+    bf16x8 af[2][MI], bfr[2][NI];
+    auto read = [&](int to, int kk) {             // (transpose reads first: the compiler does not count them)
+      if (BT && !AT) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) bfr[to][j] = fb[j].read(S + BM * BK, kk);
+      }
+#pragma unroll
+      for (int i = 0; i < MI; ++i) af[to][i] = fa[i].read(S, kk);
+      if (!(BT && !AT)) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) bfr[to][j] = fb[j].read(S + BM * BK, kk);
+      }
+    };
+    read(0, 0);
+#pragma unroll
+    for (int kk = 0; kk < NPART; ++kk) {
+      const int cur = kk & 1, nxt = cur ^ 1;
+      if (kk + 1 < NPART) read(nxt, kk + 1);
+      if (more) issue(kt + NS - 1, (kt + NS - 1) % NS, kk);
+      if (AT || BT) {
+        constexpr int RD = (AT ? 2 : 1) * MI + (BT ? 2 : 1) * NI;
+        if (kk + 1 < NPART) wait_frags<RD>(af[cur], bfr[cur]); else wait_frags<0>(af[cur], bfr[cur]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)              // operands swapped: a lane owns one row m of C and groups of four columns
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, bfr[cur][j]), __builtin_bit_cast(f16x8, af[cur][i]), acc[i][j], 0, 0, 0);
+      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  __syncthreads();                                // the stages are dead
+
+  // ---- epilogue: 32 rows x TN columns of a wave at a time through its own fp32 slice of LDS, so that global accesses are whole
+  // 16-byte vectors; the mirror image of a symmetric tile is read from the slice by columns
+  constexpr int SLD = TN + 4, CPR = TN / 8, SIT = 32 * CPR / 64;
+  float *stg = reinterpret_cast<float *>(smem_raw) + wave * (32 * SLD);
+  const int lrow = lane & 31, lq = lane >> 5;
+  const bool mirror = p.sym && tm != tn;
+  float lr = p.out.lr;
+  if (!p.C && p.out.scal) lr = p.out.scal[0];
+  const float decay = 1.0f - lr * p.out.wd, gain = lr * p.out.scale;
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<float4 *>(stg + lrow * SLD + j * 32 + c * 8 + lq * 4) =
+            make_float4(acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int it = 0; it < SIT; ++it) {
+      const int q = it * 64 + lane, r = q / CPR, cc = (q % CPR) * 8;
+      const int m = m0 + wm * TM + i * 32 + r, n = n0 + wn * TN + cc;
+      if (m >= p.Md || n >= p.Nd) continue;       // (Nd is a multiple of 8)
+      float v[8];
+      {
+        const float4 x = *reinterpret_cast<const float4 *>(stg + r * SLD + cc), y = *reinterpret_cast<const float4 *>(stg + r * SLD + cc + 4);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= p.beta;
+      if (p.E) {
+        const long long at = z * p.sE + (long long)m * p.lde + n;
+        float h[8], l[8];
+        load8(p.E, TYPE_F16, at, h);
+        if (p.El) {
+          load8(p.El, TYPE_F16, at, l);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) h[e] += l[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(p.alpha, h[e], v[e]);
+      }
+      if (p.C) {
+        const long long at = z * p.sC + (long long)m * p.ldc + n;
+        uint4 h, l;
+        split8(v, h, l);
+        *reinterpret_cast<uint4 *>(p.C + at) = h;
+        if (p.Cl) *reinterpret_cast<uint4 *>(p.Cl + at) = l;
+        if (mirror) {
+          *reinterpret_cast<float4 *>(stg + r * SLD + cc) = make_float4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<float4 *>(stg + r * SLD + cc + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        }
+        continue;
+      }
+      if (m >= p.rows) continue;
+      const long long at = z * p.out.so + (long long)m * p.out.ldo + n, sat = z * p.out.sshadow + (long long)m * p.out.ldo + n;
+      if (p.vec) {                                // (cols is a multiple of 8)
+        if (p.out.update) {
+          float x[8];
+          load8(p.out.o, p.out.type, at, x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(decay, x[e], -gain * v[e]);
+        }
+        store8(p.out.o, p.out.type, at, v);
+        if (p.out.shadow) store8(p.out.shadow, TYPE_BF16, sat, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (n + e >= p.cols) continue;
+          const float x = p.out.update ? fmaf(decay, load_as_f32(p.out.o, p.out.type, at + e), -gain * v[e]) : v[e];
+          store_from_f32(p.out.o, p.out.type, at + e, x);
+          if (p.out.shadow) p.out.shadow[sat + e] = f2bf(x);
+        }
+      }
+    }
+    if (mirror) {
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int it = 0; it < TN * 4 / 64; ++it) {
+        const int q = it * 64 + lane, c = q >> 2, r0 = (q & 3) * 8;
+        const int m = m0 + wm * TM + i * 32 + r0, n = n0 + wn * TN + c;       // C[n][m ..]
+        if (m >= p.Md || n >= p.Nd) continue;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = stg[(r0 + e) * SLD + c];
+        uint4 h, l;
+        split8(v, h, l);
+        const long long at = z * p.sC + (long long)n * p.ldc + m;
+        *reinterpret_cast<uint4 *>(p.C + at) = h;
+        if (p.Cl) *reinterpret_cast<uint4 *>(p.Cl + at) = l;
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <int BM, int BN, int BK, int WM, int WN, int NS, bool AT, bool BT, bool SPLIT>
+hipError_t launch_cfg(const OrthGemmP &p, hipStream_t s) {
+  constexpr size_t tiles = (size_t)NS * (BM + BN) * BK * 2, epi = (size_t)WM * WN * 32 * (BN / WN + 4) * 4;
+  constexpr size_t lds = tiles > epi ? tiles : epi;
+  static_assert(lds <= 160 * 1024, "LDS budget");
+  auto kern = orth_gemm_kernel<BM, BN, BK, WM, WN, NS, AT, BT, SPLIT>;
+  const int tm = (p.Md + BM - 1) / BM, tn = (p.Nd + BN - 1) / BN;
+  if (p.sym && (BM != BN || p.Md != p.Nd)) return hipErrorInvalidValue;
+  const long long nblk = (p.sym ? (long long)tn * (tn + 1) / 2 : (long long)tm * tn) * p.batch;
+  if (nblk > 0x3fffffff) return hipErrorInvalidValue;
+  if (lds > 64 * 1024) {
+    static std::once_flag once;
+    static hipError_t err = hipSuccess;
+    std::call_once(once, [&] { err = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); });
+    if (err != hipSuccess) return err;
+  }
+  const int chunk = (int)((nblk + 7) / 8);
+  hipLaunchKernelGGL(kern, dim3(chunk * 8), dim3(WM * WN * 64), lds, s, p, tm, tn, (int)nblk, chunk);
+  return hipGetLastError();
+}
+
+template <bool AT, bool BT>
+hipError_t launch_product(const OrthGemmP &p, hipStream_t s) {
+  // operand checks the kernel relies on: 16-byte aligned rows of whole chunks, operands below 2 GiB per matrix
+  if (((p.lda | p.ldb | p.Md | p.Nd | p.Kd) & 7) || ((p.sA | p.sB) & 7)) return hipErrorInvalidValue;
+  if ((long long)(AT ? p.Kd : p.Md) * p.lda * 2 >= (1LL << 31) || (long long)(BT ? p.Kd : p.Nd) * p.ldb * 2 >= (1LL << 31)) return hipErrorInvalidValue;
+  return p.Al ? launch_cfg<128, 128, 64, 2, 2, 2, AT, BT, true>(p, s) : launch_cfg<128, 128, 64, 2, 2, 2, AT, BT, false>(p, s);
+}
+
+// Few rows average little of what 16-bit operands round away (relative error up to 1.6e-2 for 2 x 2, 4.4e-3 for 8 x 8, 3.2e-3 for 17 x 33)
+constexpr int SPLIT_ALWAYS = 64;
+
+// power of two that leaves a bound just under fp16's largest value
+int exponent_for(double bound) { return 15 - (int)std::ceil(std::log2(bound)); }
+
+}  // namespace
+
+const char *orth_plan(int batch, int rows, int cols, int split, int steps, const float *coef, OrthPlan &pl) {
+  std::memset(&pl, 0, sizeof(pl));
+  pl.batch = batch; pl.rows = rows; pl.cols = cols; pl.steps = steps;
+  pl.wide = rows <= cols;
+  auto up8 = [](int v) { return (v + 7) / 8 * 8; };
+  pl.rp = up8(rows); pl.cp = up8(cols); pl.mp = std::min(pl.rp, pl.cp);
+  pl.split = split || pl.mp <= SPLIT_ALWAYS;
+  // Bounds of the singular values: 1 at first, then max |p| over [0, bound], with 2^-6 more for what rounding adds.
+  double s = 1.0;
+  pl.ex[0] = exponent_for(s);
+  for (int k = 0; k < steps; ++k) {
+    const double a = coef ? coef[3 * k] : 3.4445, b = coef ? coef[3 * k + 1] : -4.7750, c = coef ? coef[3 * k + 2] : 2.0315;
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return "coefficients must be finite";
+    pl.a[k] = (float)a; pl.b[k] = (float)b; pl.c[k] = (float)c;
+    // extrema of p on [0, s]: the ends and where a + 3 b t + 5 c t^2 = 0, t = sigma^2; of b t + c t^2: the end and -b / 2c
+    const double S = s * s;
+    auto poly = [&](double t) { return std::fabs(std::sqrt(t) * (a + t * (b + t * c))); };
+    double top = poly(S);
+    if (c != 0.0) {
+      const double d = 9.0 * b * b - 20.0 * a * c;
+      if (d >= 0.0)
+        for (double q : {(-3.0 * b + std::sqrt(d)) / (10.0 * c), (-3.0 * b - std::sqrt(d)) / (10.0 * c)})
+          if (q > 0.0 && q < S) top = std::max(top, poly(q));
+    } else if (b != 0.0) {
+      const double q = -a / (3.0 * b);
+      if (q > 0.0 && q < S) top = std::max(top, poly(q));
+    }
+    double inner = std::fabs(b * S + c * S * S);
+    if (c != 0.0) {
+      const double q = -b / (2.0 * c);
+      if (q > 0.0 && q < S) inner = std::max(inner, std::fabs(q * (b + q * c)));
+    }
+    s = top * (1.0 + 1.0 / 64);
+    if (s > 256.0 || s < 1.0 / 256 || inner > 4096.0) return "the coefficients let singular values grow beyond 256 or vanish";
+    pl.ea[k] = exponent_for(S * (1.0 + 1.0 / 32));
+    pl.eb[k] = exponent_for(std::max(inner, 1.0 / 256) * (1.0 + 1.0 / 32));
+    pl.ex[k + 1] = exponent_for(s);
+  }
+  // about 16 chunks of 8 values to a thread of the norm's pass, as long as a matrix has them
+  pl.nparts = (int)std::min<long long>(ORTH_PARTS, ((long long)rows * cols + 256 * 128 - 1) / (256 * 128));
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t r = o; o = (o + bytes + 255) / 256 * 256; return r; };
+  const size_t xb = (size_t)batch * pl.rp * pl.cp * 2, ab = (size_t)batch * pl.mp * pl.mp * 2;
+  pl.o_part = take((size_t)batch * pl.nparts * 8);
+  for (int i = 0; i < 2; ++i) pl.o_x[i] = take(xb);
+  pl.o_xl[0] = take(xb);
+  pl.o_xl[1] = pl.split ? take(xb) : pl.o_xl[0];     // (16-bit mode: no product reads it, each entry is replaced where it was read)
+  pl.o_a = take(ab); pl.o_b = take(ab);
+  pl.o_al = pl.split ? take(ab) : 0; pl.o_bl = pl.split ? take(ab) : 0;
+  pl.total = o;
+  return nullptr;
+}
+
+hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, void *workspace, hipStream_t s) {
+  unsigned char *ws = static_cast<unsigned char *>(workspace);
+  auto at = [&](size_t off) { return reinterpret_cast<uint16_t *>(ws + off); };
+  const long long sx = (long long)pl.rp * pl.cp, sa = (long long)pl.mp * pl.mp;
+  OrthPrepP q;
+  std::memset(&q, 0, sizeof(q));
+  q.in = in; q.rows = pl.rows; q.cols = pl.cols; q.rp = pl.rp; q.cp = pl.cp; q.nparts = pl.nparts; q.ex = pl.ex[0]; q.eps = eps;
+  q.vec = rows_of_vectors(in.g, in.type, in.sg, in.ldg, pl.cols) && (!in.v || rows_of_vectors(in.v, TYPE_F32, in.sv, pl.cols, pl.cols));
+  q.part = reinterpret_cast<double *>(ws + pl.o_part); q.xh = at(pl.o_x[0]); q.xl = at(pl.o_xl[0]);
+  for (int z0 = 0; z0 < pl.batch; z0 += 32768) {  // (grids have 65535 places along y)
+    OrthPrepP b = q;
+    const int nz = std::min(32768, pl.batch - z0);
+    b.in.g = static_cast<const unsigned char *>(in.g) + z0 * in.sg * type_bytes(in.type);
+    if (in.v) b.in.v = in.v + z0 * in.sv;
+    b.part += (long long)z0 * pl.nparts; b.xh += z0 * sx; b.xl += z0 * sx;
+    hipLaunchKernelGGL(orth_norm_kernel, dim3(pl.nparts, nz), dim3(256), 0, s, b);
+    hipLaunchKernelGGL(orth_prep_kernel, dim3((pl.rp * (pl.cp / 8) + 1023) / 1024, nz), dim3(256), 0, s, b);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  for (int k = 0; k < pl.steps; ++k) {
+    const uint16_t *x = at(pl.o_x[k & 1]), *xl = at(pl.o_xl[k & 1]);
+    OrthGemmP p;
+    hipError_t e;
+    // A 2^ea
+    std::memset(&p, 0, sizeof(p));
+    p.batch = pl.batch; p.sym = 1;
+    p.A = p.B = x; p.sA = p.sB = sx; p.lda = p.ldb = pl.cp; p.Md = p.Nd = pl.mp; p.Kd = pl.wide ? pl.cp : pl.rp;
+    if (pl.split) p.Al = p.Bl = xl;
+    p.C = at(pl.o_a); p.Cl = pl.split ? at(pl.o_al) : nullptr; p.sC = sa; p.ldc = pl.mp;
+    p.beta = std::ldexp(1.0f, pl.ea[k] - 2 * pl.ex[k]);
+    e = pl.wide ? launch_product<false, false>(p, s) : launch_product<true, true>(p, s);
+    if (e != hipSuccess) return e;
+    // B 2^eb = (b A + c A A) 2^eb
+    std::memset(&p, 0, sizeof(p));
+    p.batch = pl.batch; p.sym = 1;
+    p.A = p.B = p.E = at(pl.o_a); p.sA = p.sB = p.sE = sa; p.lda = p.ldb = p.lde = pl.mp; p.Md = p.Nd = p.Kd = pl.mp;
+    if (pl.split) p.Al = p.Bl = p.El = at(pl.o_al);
+    p.C = at(pl.o_b); p.Cl = pl.split ? at(pl.o_bl) : nullptr; p.sC = sa; p.ldc = pl.mp;
+    p.alpha = std::ldexp(pl.b[k], pl.eb[k] - pl.ea[k]); p.beta = std::ldexp(pl.c[k], pl.eb[k] - 2 * pl.ea[k]);
+    e = launch_product<false, false>(p, s);
+    if (e != hipSuccess) return e;
+    // X' = a X + B X, or a X + X B
+    std::memset(&p, 0, sizeof(p));
+    p.batch = pl.batch;
+    const bool last = k + 1 == pl.steps;
+    const int et = last ? 0 : pl.ex[k + 1];
+    p.Md = pl.rp; p.Nd = pl.cp; p.Kd = pl.mp;
+    p.E = x; p.El = xl; p.sE = sx; p.lde = pl.cp;
+    p.alpha = std::ldexp(pl.a[k], et - pl.ex[k]); p.beta = std::ldexp(1.0f, et - pl.eb[k] - pl.ex[k]);
+    if (last) {
+      p.out = out; p.rows = pl.rows; p.cols = pl.cols;
+      p.vec = rows_of_vectors(out.o, out.type, out.so, out.ldo, pl.cols) &&
+              (!out.shadow || rows_of_vectors(out.shadow, TYPE_BF16, out.sshadow, out.ldo, pl.cols));
+    } else {
+      p.C = at(pl.o_x[~k & 1]); p.Cl = at(pl.o_xl[~k & 1]); p.sC = sx; p.ldc = pl.cp;
+    }
+    if (pl.wide) {
+      p.A = at(pl.o_b); p.sA = sa; p.lda = pl.mp; p.B = x; p.sB = sx; p.ldb = pl.cp;
+      if (pl.split) { p.Al = at(pl.o_bl); p.Bl = xl; }
+      e = launch_product<false, true>(p, s);
+    } else {
+      p.A = x; p.sA = sx; p.lda = pl.cp; p.B = at(pl.o_b); p.sB = sa; p.ldb = pl.mp;
+      if (pl.split) { p.Al = xl; p.Bl = at(pl.o_bl); }
+      e = launch_product<false, false>(p, s);
+    }
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace absk
