@@ -54,7 +54,10 @@ typedef enum {
 
 enum { ABS_ACT_NONE = 0, ABS_ACT_RELU = 1, ABS_ACT_GELU = 2 };   /* GELU: exact erf form */
 enum { ABS_OPT_SGD = 0, ABS_OPT_SHB = 1, ABS_OPT_ADAMW = 2,   /* Adam = AdamW with weight_decay 0 */
-       ABS_OPT_ADAGRAD = 3 };                                   /* v <- v + g^2 ; x <- x - lr g / (sqrt v + eps) */
+       ABS_OPT_ADAGRAD = 3,                                     /* v <- v + g^2 ; x <- x - lr g / (sqrt v + eps) */
+       ABS_OPT_MUON = 4 };  /* weights of all layers but the last: v <- momentum v + g ; u = g + momentum v ;
+                               x <- (1 - lr weight_decay) x - lr 0.2 sqrt(max(in, out)) orth(u)  (abs_orthogonalize, 5 steps);
+                               the last layer and the biases: AdamW with the same lr and weight_decay.  Needs a hidden layer. */
 enum { ABS_PREC_F32 = 0,    /* fp32 operands and accumulation */
        ABS_PREC_BF16 = 1 }; /* bf16 operands, fp32 accumulation, fp32 master weights */
 enum { ABS_STATS_NORM = 1,  /* sum_i ||g_i||^2 and ||gbar||^2 (norm test) */
@@ -222,7 +225,8 @@ abs_status abs_average_replicas(abs_ctx *ctx);
  * gradient after every step (Alg. 2 with H = 1) may prefer on = 0.  A layer whose weight gradient splits its
  * reduction over the batch (few output tiles, long batches) takes its step in the launch that adds the slices;
  * abs_local_step_accumulated, which keeps the gradient in memory between micro-batches, always updates separately,
- * as does a net with a layer width that is no multiple of 4.  on != 0 with ABS_PREC_F32: ABS_EUNSUPPORTED.
+ * as does a net with a layer width that is no multiple of 4.  on != 0 with ABS_PREC_F32 or ABS_OPT_MUON (whose step needs the
+ * whole gradient of a matrix): ABS_EUNSUPPORTED.
  */
 abs_status abs_set_fused_update(abs_ctx *ctx, int on);
 
@@ -253,7 +257,8 @@ abs_status abs_get_params(abs_ctx *ctx, int m, float *out_host);
 abs_status abs_set_params(abs_ctx *ctx, int m, const float *in_host);
 abs_status abs_get_grad(abs_ctx *ctx, int m, float *out_host);    /* last local batch gradient */
 /* Optimizer state of worker m (local to a worker, never averaged: "synchronizing only the models", Sec. 6):
- * which = 0: heavy-ball buffer v / AdamW second moment / AdaGrad accumulator; which = 1: AdamW first moment. */
+ * which = 0: heavy-ball buffer v / AdamW second moment / AdaGrad accumulator; which = 1: AdamW first moment.  ABS_OPT_MUON: which = 0
+ * is the momentum of the weights that it orthogonalises and AdamW's second moment elsewhere, which = 1 AdamW's first (0 for the former). */
 abs_status abs_get_opt_state(abs_ctx *ctx, int m, int which, float *out_host);
 /* Per-sample ||g_i||^2 (and <g_i,gbar> if gathered; else q_host may be NULL) of worker m
  * for the most recent step: host, b floats each (b^m after a ragged step; see
@@ -328,7 +333,8 @@ enum { ABS_TYPE_F32 = 0, ABS_TYPE_BF16 = 1, ABS_TYPE_F16 = 2 };
  *                  values from 0.01 on to about 0.7 .. 1.2 in five steps.  Coefficients that let a singular value of at most 1 grow
  *                  beyond 256 are refused.
  *   prec         : ABS_PREC_BF16: products of 16-bit operands (fp16 with powers of two that keep them in range; X itself is held
- *                  in 32 bits): relative error of the result 0.5 to 2.1e-3, less than a bf16 result's own rounding adds.
+ *                  in 32 bits): relative error of the result 0.5 to 1.6e-3, no more than a bf16 result's own rounding adds.
+ *                  (Up to 128 rows or columns the products are those of ABS_PREC_F32 all the same.)
  *                  ABS_PREC_F32: as exact as fp32 products, at three times the operations.
  * Asynchronous on the stream; sums are in a fixed order (the same bits every time).  workspace: device, 256-byte aligned,
  * abs_orthogonalize_workspace_bytes, used until the call's work has run.  A matrix of 2^30 values or more: ABS_EUNSUPPORTED.

@@ -521,8 +521,8 @@ def _matrices(t, what: str):
 
 def orthogonalize(g, steps: int = 5, coefficients=None, eps: float = 1e-7, prec: Optional[int] = None, out=None):
     """Newton-Schulz orthogonalisation of [..., rows, cols] device matrices (abs_orthogonalize); `out` defaults to a new
-    tensor of g's type and may be g itself.  prec: PREC_BF16 (16-bit products) or PREC_F32; by default as exact as the
-    result's type."""
+    tensor of g's type and may be g itself.  prec: PREC_BF16 (16-bit products) or PREC_F32; by default what the result's
+    type can tell apart, PREC_BF16 for bfloat16 only."""
     import torch
     lib = load_library()
     gt = _type_of(g, "g")
@@ -534,7 +534,7 @@ def orthogonalize(g, steps: int = 5, coefficients=None, eps: float = 1e-7, prec:
         raise AbsError("out must have g's shape")
     batch, rows, cols, sg, ldg = _matrices(g, "g")
     _, _, _, so, ldo = _matrices(out, "out")
-    prec = (PREC_F32 if ot == 0 else PREC_BF16) if prec is None else int(prec)
+    prec = (PREC_BF16 if ot == 1 else PREC_F32) if prec is None else int(prec)
     coef = _coefficients(coefficients, steps)
     nbytes = C.c_size_t(0)
     with torch.cuda.device(g.device):

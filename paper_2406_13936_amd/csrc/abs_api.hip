@@ -15,6 +15,7 @@
 #include "../../include/abs.h"
 #include "abs_internal.h"
 #include "api_status.h"
+#include "ops.h"
 
 using namespace absk;
 
@@ -50,7 +51,7 @@ struct Plan {
   size_t o_xm = 0, o_xs = 0, o_grad = 0, o_gradbf = 0, o_v = 0, o_m = 0, o_Xbf = 0;
   size_t o_A[MAXL] = {0}, o_Dact[MAXL] = {0}, o_Dl[MAXL + 1] = {0};
   size_t o_Z = 0, o_U = 0, o_gram = 0, o_an[MAXL] = {0}, o_dn[MAXL + 1] = {0}, o_loss = 0, o_nout = 0, o_qout = 0;
-  size_t o_qpart[MAXL] = {0}, o_partials = 0, o_stats = 0, o_cw = 0, o_colpart = 0, o_rows = 0, o_sqwave = 0, o_idx = 0, o_scal = 0, o_mean = 0;
+  size_t o_qpart[MAXL] = {0}, o_partials = 0, o_stats = 0, o_cw = 0, o_colpart = 0, o_rows = 0, o_sqwave = 0, o_idx = 0, o_scal = 0, o_mean = 0, o_orth = 0;
   size_t o_kpart_l[MAXL + 1] = {0};    // per layer: partial products of a split weight-gradient reduction
   size_t kpart_floats_l[MAXL + 1] = {0};
   int softmax_chunks = 0;              // fp32 without hidden layers: chunks to a replica that the scratch of softmax_step.hip holds (0: not taken)
@@ -74,14 +75,33 @@ abs_status check_cfg(const abs_config *c) {
   if (c->M < 1) return fail(ABS_EINVAL, "M < 1");
   if (c->b_cap < 2) return fail(ABS_EINVAL, "b_cap < 2");
   if (c->act < ABS_ACT_NONE || c->act > ABS_ACT_GELU) return fail(ABS_EINVAL, "unknown activation");
-  if (c->opt < ABS_OPT_SGD || c->opt > ABS_OPT_ADAGRAD) return fail(ABS_EINVAL, "unknown optimizer");
+  if (c->opt < ABS_OPT_SGD || c->opt > ABS_OPT_MUON) return fail(ABS_EINVAL, "unknown optimizer");
   if (c->prec != ABS_PREC_F32 && c->prec != ABS_PREC_BF16) return fail(ABS_EINVAL, "unknown precision");
   if (!(c->stats_mask & ABS_STATS_NORM)) return fail(ABS_EINVAL, "stats_mask needs ABS_STATS_NORM");
   if (c->prec == ABS_PREC_BF16)
     for (int l = 0; l < c->n_layers; ++l)
       if (c->dims[l] % 8) return fail(ABS_EUNSUPPORTED, "bf16 mode needs dims[0..L-1] to be multiples of 8");
   if ((long long)c->M * c->b_cap > (1LL << 30)) return fail(ABS_EUNSUPPORTED, "M * b_cap too large");
+  if (c->opt == ABS_OPT_MUON) {
+    if (c->n_layers < 2) return fail(ABS_EINVAL, "ABS_OPT_MUON needs a hidden layer");
+    for (int l = 1; l < c->n_layers; ++l)
+      if (((long long)c->dims[l] + 7) * ((long long)c->dims[l - 1] + 7) >= (1LL << 30))
+        return fail(ABS_EUNSUPPORTED, "ABS_OPT_MUON: a weight matrix must hold fewer than 2^30 values");
+  }
   return ABS_OK;
+}
+
+// v is kept by every optimizer but SGD; the first moment by AdamW, and by Muon for what it leaves to AdamW
+bool has_first_moment(int opt) { return opt == ABS_OPT_ADAMW || opt == ABS_OPT_MUON; }
+
+// ABS_OPT_MUON: the orthogonalisation of hidden layer l's updates, all replicas in one batch; 16-bit products for gradients that
+// 16-bit products made
+constexpr int MUON_STEPS = 5;
+constexpr float MUON_EPS = 1e-7f;
+OrthPlan muon_plan(const Plan &pl, int l) {
+  OrthPlan op;
+  (void)orth_plan(pl.M, pl.dims[l], pl.dims[l - 1], !pl.bf16, MUON_STEPS, nullptr, op);
+  return op;
 }
 
 void make_plan(const abs_config *c, long long N, Plan &pl) {
@@ -117,7 +137,7 @@ void make_plan(const abs_config *c, long long N, Plan &pl) {
   pl.o_grad = take(MP * 4);
   if (pl.bf16 && pl.want_ip) pl.o_gradbf = take(MP * 2);
   if (c->opt != ABS_OPT_SGD) pl.o_v = take(MP * 4);
-  if (c->opt == ABS_OPT_ADAMW) pl.o_m = take(MP * 4);
+  if (has_first_moment(c->opt)) pl.o_m = take(MP * 4);
   if (pl.bf16) pl.o_Xbf = take((size_t)N * pl.dims[0] * 2);
   const size_t MB = (size_t)pl.M * pl.cap;
   for (int l = 0; l < pl.L; ++l) pl.o_A[l] = take(MB * pl.ld[l] * pl.esz);
@@ -192,6 +212,11 @@ void make_plan(const abs_config *c, long long N, Plan &pl) {
     pl.chain_words = small_chain_words(pl.L, pl.dims.data());
     pl.chain_max = (int)std::min<long long>((long long)pl.M * ((pl.cap + 31) / 32), SmallChain::MAX_CHAINS);
     pl.o_chain = take((size_t)pl.chain_max * pl.chain_words * sizeof(int));
+  }
+  if (c->opt == ABS_OPT_MUON) {                               // one hidden layer after the other
+    size_t most = 0;
+    for (int l = 1; l < pl.L; ++l) most = std::max(most, muon_plan(pl, l).total);
+    pl.o_orth = take(most);
   }
   pl.o_mean = take((size_t)pl.Ppad * sizeof(float));          // the mean between the two passes of a large average
   pl.total = off;
@@ -352,13 +377,13 @@ WgradPlan plan_wgrad(const Plan &pl, int b, int fused, const int *b_host) {
 
 // Event-timed launch classes (abs_profile_*): one entry per kernel symbol of interest.
 enum {
-  T_GATHER = 0, T_SOFTMAX, T_ROWNORM, T_COLSUM, T_STATS, T_UPDATE, T_AVERAGE, T_ROWDOT, T_GRAM,
+  T_GATHER = 0, T_SOFTMAX, T_ROWNORM, T_COLSUM, T_STATS, T_UPDATE, T_AVERAGE, T_ROWDOT, T_GRAM, T_MUON,
   T_GEMM0,                       // + epi * 6 + tile shape (bf16) ; fp32 family uses shape 1
   T_GEMM_KINDS = 5 * 6, T_LAYERS = 17,   // GEMM classes are resolved per layer (0: a launch that several layers share)
   T_COUNT = T_GEMM0 + T_GEMM_KINDS * T_LAYERS
 };
 static const char *const kTagNames[T_GEMM0 + T_GEMM_KINDS] = {
-  "gather_rows", "softmax_ce", "row_sqnorm", "col_sum", "stats", "update", "average", "rowdot", "gram_ip",
+  "gather_rows", "softmax_ce", "row_sqnorm", "col_sum", "stats", "update", "average", "rowdot", "gram_ip", "muon",
   "gemm_fwd_128x64", "gemm_fwd_128x128", "gemm_fwd_256x256", "gemm_fwd_64x256", "gemm_fwd_64x128", "gemm_fwd_32x32",
   "gemm_logits_128x64", "gemm_logits_128x128", "gemm_logits_256x256", "gemm_logits_64x256", "gemm_logits_64x128", "gemm_logits_32x32",
   "gemm_bwd_128x64", "gemm_bwd_128x128", "gemm_bwd_256x256", "gemm_bwd_64x256", "gemm_bwd_64x128", "gemm_bwd_32x64",
@@ -664,7 +689,7 @@ abs_status abs_init_replicas(const abs_config *cfg, const float *x0_host, const 
     if ((e = launch_fill_zero(c->at<void>(pl.o_gradbf), MP * 2, c->stream)) != hipSuccess) return bail(hipGetErrorString(e));
   if (cfg->opt != ABS_OPT_SGD)
     if ((e = launch_fill_zero(c->at<void>(pl.o_v), MP * 4, c->stream)) != hipSuccess) return bail(hipGetErrorString(e));
-  if (cfg->opt == ABS_OPT_ADAMW)
+  if (has_first_moment(cfg->opt))
     if ((e = launch_fill_zero(c->at<void>(pl.o_m), MP * 4, c->stream)) != hipSuccess) return bail(hipGetErrorString(e));
   if ((e = hipStreamSynchronize(c->stream)) != hipSuccess) return bail(hipGetErrorString(e));
   std::vector<float> in(pl.Ppad, 0.0f);
@@ -982,11 +1007,12 @@ static abs_status local_step_impl(abs_ctx *c, const int32_t *idx_dev, int ldi, i
   auto f32_plan = [&](int l) { return gemm_f32_wgrad_plan(pl.dims[l], pl.dims[l - 1], b, M, pl.kpart_floats_l[l]); };
   // fp32 mode: the optimizer step where the gradient is finished, one launch of the step less (logistic regression: 2.6 of
   // 22 us), if no layer's reduction is split
-  bool f32_step = !pl.bf16 && ph.wgrad && ph.update && ph.s2 && !ph.acc_grad;
+  const bool muon = c->cfg.opt == ABS_OPT_MUON;     // (its update needs the whole gradient of a matrix)
+  bool f32_step = !muon && !pl.bf16 && ph.wgrad && ph.update && ph.s2 && !ph.acc_grad;
   for (int l = 1; l <= L && f32_step; ++l) f32_step = f32_plan(l).ksplit <= 1;
   // bf16 mode: few output tiles and a long reduction (small layers, or any layer while b is the long side) are cut into
   // slices so that the launch fills the chip; the slices are added in order afterwards (plan_wgrad).
-  const bool want_fused = c->fused_update && pl.bf16 && ph.wgrad && ph.update && ph.s2 && !ph.acc_grad;
+  const bool want_fused = !muon && c->fused_update && pl.bf16 && ph.wgrad && ph.update && ph.s2 && !ph.acc_grad;
   const WgradPlan wplan = pl.bf16 && ph.wgrad ? plan_wgrad(pl, b, want_fused, b_host) : WgradPlan{};
   // The optimizer step moves into the weight-gradient epilogue when the caller asked for it and this call both
   // finishes the gradient and updates, no reduction is split and the per-wavefront sums of squares fit their scratch.
@@ -1248,15 +1274,37 @@ static abs_status local_step_impl(abs_ctx *c, const int32_t *idx_dev, int ldi, i
   std::memset(&up, 0, sizeof(up));
   up.x = xm; up.g = grad;
   up.v = c->cfg.opt != ABS_OPT_SGD ? c->at<float>(pl.o_v) : nullptr;
-  up.m = c->cfg.opt == ABS_OPT_ADAMW ? c->at<float>(pl.o_m) : nullptr;
+  up.m = has_first_moment(c->cfg.opt) ? c->at<float>(pl.o_m) : nullptr;
   up.shadow = pl.bf16 ? c->at<bf16_t>(pl.o_xs) : nullptr;
   up.n = (long long)M * pl.Ppad;
   up.opt = c->cfg.opt; up.lr = lr; up.momentum = c->cfg.momentum;
   up.beta1 = c->cfg.beta1; up.beta2 = c->cfg.beta2; up.eps = c->cfg.eps; up.wd = c->cfg.weight_decay;
   up.c1 = ph.c1; up.c2 = ph.c2; up.scal = ph.scal;
   if (s2_in_update) up.sq_wave = c->at<float>(pl.o_sqwave);
-  { ProfScope ps_(c, T_UPDATE, 0.0, 1.0 * M * pl.P * (c->cfg.opt == ABS_OPT_SGD ? 12 : c->cfg.opt == ABS_OPT_ADAMW ? 28 : 20) + (pl.bf16 ? 2.0 * M * pl.P : 0.0));
-  HIPCHK(c, launch_update(up, s)); }
+  { ProfScope ps_(c, T_UPDATE, 0.0, muon ? 4.0 * M * pl.P : 1.0 * M * pl.P * (c->cfg.opt == ABS_OPT_SGD ? 12 : c->cfg.opt == ABS_OPT_ADAMW ? 28 : 20) + (pl.bf16 ? 2.0 * M * pl.P : 0.0));
+  if (muon) {
+    MuonRestP mr;                        // biases and the last layer take AdamW's step
+    std::memset(&mr, 0, sizeof(mr));
+    mr.u = up; mr.Ppad = pl.Ppad;
+    for (int l = 1; l < L; ++l) { mr.lo[mr.n] = pl.offW[l]; mr.hi[mr.n++] = rup(pl.offW[l] + (long long)pl.dims[l] * pl.dims[l - 1], 64); }
+    HIPCHK(c, launch_muon_rest(mr, s));
+  } else {
+    HIPCHK(c, launch_update(up, s));
+  } }
+  if (muon)
+    for (int l = 1; l < L; ++l) {
+      const OrthPlan op = muon_plan(pl, l);
+      const OrthIn in = {grad + pl.offW[l], TYPE_F32, pl.Ppad, pl.dims[l - 1], c->at<float>(pl.o_v) + pl.offW[l], pl.Ppad, c->cfg.momentum, 1};
+      OrthOut out;
+      std::memset(&out, 0, sizeof(out));
+      out.o = xm + pl.offW[l]; out.type = TYPE_F32; out.so = pl.Ppad; out.ldo = pl.dims[l - 1];
+      out.update = 1; out.lr = lr; out.wd = c->cfg.weight_decay; out.scal = ph.scal;
+      out.scale = 0.2f * std::sqrt((float)std::max(pl.dims[l], pl.dims[l - 1]));
+      if (pl.bf16) { out.shadow = c->at<bf16_t>(pl.o_xs) + pl.offW[l]; out.sshadow = pl.Ppad; }
+      const double m = std::min(op.rows, op.cols), n = std::max(op.rows, op.cols);
+      ProfScope ps_(c, T_MUON, M * MUON_STEPS * (3.0 * m * m * n + m * m * m), M * m * n * (20.0 + (pl.bf16 ? 2 : 0)));
+      HIPCHK(c, launch_orthogonalize(op, in, out, MUON_EPS, c->at<void>(pl.o_orth), s));
+    }
   if (s2_in_update) {
     sp.sq_wave = up.sq_wave; sp.n_sq_wave = pl.Ppad / 256;
     ProfScope ps_(c, T_STATS, 0.0, sp_bytes + 4.0 * M * (pl.Ppad / 256));
@@ -1299,7 +1347,7 @@ static abs_status materialize_grad(abs_ctx *c) {
 // One more optimizer step is about to be taken: advance the counter and return Adam's bias corrections.
 static void next_update(abs_ctx *c, StepPhase &ph) {
   c->t += 1;
-  if (c->cfg.opt == ABS_OPT_ADAMW) {
+  if (has_first_moment(c->cfg.opt)) {
     ph.c1 = (float)(1.0 / (1.0 - std::pow((double)c->cfg.beta1, (double)c->t)));
     ph.c2 = (float)(1.0 / (1.0 - std::pow((double)c->cfg.beta2, (double)c->t)));
   }
@@ -1577,6 +1625,7 @@ abs_status abs_average_replicas(abs_ctx *c) try {
 abs_status abs_set_fused_update(abs_ctx *c, int on) try {
   if (!c) return fail(ABS_EINVAL, "ctx is NULL");
   if (on && !c->pl.bf16) return cfail(c, ABS_EUNSUPPORTED, "the fused update needs ABS_PREC_BF16");
+  if (on && c->cfg.opt == ABS_OPT_MUON) return cfail(c, ABS_EUNSUPPORTED, "ABS_OPT_MUON needs the whole gradient of a matrix: there is no fused update");
   if (c->fused_update != (on != 0)) drop_graphs(c);      // captured steps recorded the other form
   c->fused_update = on != 0;
   return ABS_OK;
@@ -1601,7 +1650,7 @@ abs_status abs_get_counters(const abs_ctx *c, long long *rounds, long long *loca
 abs_status abs_get_opt_state(abs_ctx *c, int m, int which, float *out_host) try {
   if (!c || !out_host) return fail(ABS_EINVAL, "NULL argument");
   if (m < 0 || m >= c->pl.M) return cfail(c, ABS_EINVAL, "replica index out of range");
-  const bool has_v = c->cfg.opt != ABS_OPT_SGD, has_m = c->cfg.opt == ABS_OPT_ADAMW;
+  const bool has_v = c->cfg.opt != ABS_OPT_SGD, has_m = has_first_moment(c->cfg.opt);
   if (!((which == 0 && has_v) || (which == 1 && has_m)))
     return cfail(c, ABS_EINVAL, "this optimizer keeps no such state vector");
   std::vector<float> in(c->pl.Ppad);

@@ -11,7 +11,7 @@ namespace absk {
 typedef uint16_t bf16_t;   // raw bfloat16 bits in memory
 
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2 };
-enum { OPT_SGD = 0, OPT_SHB = 1, OPT_ADAMW = 2, OPT_ADAGRAD = 3 };
+enum { OPT_SGD = 0, OPT_SHB = 1, OPT_ADAMW = 2, OPT_ADAGRAD = 3, OPT_MUON = 4 };
 
 // Epilogues of the grouped GEMM  C[g][m][n] = sum_k A[g][m][k] * B[g][n][k].
 enum {
@@ -346,6 +346,15 @@ struct UpdateP {
                             //   that a captured launch can be replayed with new values
 };
 hipError_t launch_update(const UpdateP &p, hipStream_t s);
+// OPT_MUON: the AdamW step of the parameters outside [lo, hi) of each replica (multiples of 64), whose weights take their step
+// elsewhere; sq_wave covers all.
+struct MuonRestP {
+  enum { MAXN = 15 };
+  UpdateP u;
+  long long Ppad, lo[MAXN], hi[MAXN];
+  int n;
+};
+hipError_t launch_muon_rest(const MuonRestP &p, hipStream_t s);
 hipError_t launch_average_f32(float *x, bf16_t *shadow, float *mean, int groups, long long Ppad, hipStream_t s);
 hipError_t launch_average_bf16(bf16_t *x, bf16_t *mean, int groups, long long n, hipStream_t s);
 // cross-worker statistics: out[0] = sum_m ||g^m||^2, out[1] = ||mean_m g^m||^2;

@@ -407,6 +407,35 @@ __global__ void __launch_bounds__(256) update_kernel(const UpdateP pin) {
   }
 }
 
+// The part of an OPT_MUON step that is AdamW's: biases and the last layer.  The other weights are only read, for ||gbar||^2
+// (a wavefront's 256 values may hold both).
+__global__ void __launch_bounds__(256) muon_rest_kernel(const MuonRestP q) {
+  UpdateP p = q.u;
+  if (p.scal) { p.lr = p.scal[0]; p.c1 = p.scal[1]; p.c2 = p.scal[2]; }
+  const OptHyper h = {p.lr, p.momentum, p.beta1, p.beta2, p.eps, p.wd, p.c1, p.c2};
+  const long long i = blockIdx.x * 256LL + threadIdx.x;
+  if (i * 4 >= p.n) return;                        // (n is a multiple of 256: wavefronts are whole)
+  const long long at = i * 4 % q.Ppad;
+  bool mine = true;
+  for (int k = 0; k < q.n; ++k) mine = mine && !(at >= q.lo[k] && at < q.hi[k]);
+  if (!p.sq_wave && !mine) return;
+  const float4 g = ld_stream(reinterpret_cast<const float4 *>(p.g) + i);
+  if (p.sq_wave) {
+    const float t = wave_sum(fmaf(g.x, g.x, fmaf(g.y, g.y, fmaf(g.z, g.z, g.w * g.w))));
+    if ((threadIdx.x & 63) == 0) p.sq_wave[i >> 6] = t;
+  }
+  if (!mine) return;
+  const float4 x = reinterpret_cast<const float4 *>(p.x)[i], v = reinterpret_cast<const float4 *>(p.v)[i], m = reinterpret_cast<const float4 *>(p.m)[i];
+  float xs[4] = {x.x, x.y, x.z, x.w}, vs[4] = {v.x, v.y, v.z, v.w}, ms[4] = {m.x, m.y, m.z, m.w};
+  const float gs[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) opt_step_elem<OPT_ADAMW>(xs[k], gs[k], vs[k], ms[k], h);
+  reinterpret_cast<float4 *>(p.v)[i] = make_float4(vs[0], vs[1], vs[2], vs[3]);
+  reinterpret_cast<float4 *>(p.m)[i] = make_float4(ms[0], ms[1], ms[2], ms[3]);
+  reinterpret_cast<float4 *>(p.x)[i] = make_float4(xs[0], xs[1], xs[2], xs[3]);
+  if (p.shadow) reinterpret_cast<uint2 *>(p.shadow)[i] = make_uint2(pack2bf(xs[0], xs[1]), pack2bf(xs[2], xs[3]));
+}
+
 // ---- replica average ------------------------------------------------------------------------
 // Thread owns 4 consecutive parameters: reads them from all replicas (in replica order), divides
 // once, writes the mean back to every replica (and the bf16 shadow if there is one).
@@ -867,6 +896,12 @@ hipError_t launch_update(const UpdateP &p, hipStream_t s) {
   else if (p.opt == OPT_ADAGRAD) ABS_UPD(OPT_ADAGRAD);
   else ABS_UPD(OPT_ADAMW);
 #undef ABS_UPD
+  return hipGetLastError();
+}
+
+hipError_t launch_muon_rest(const MuonRestP &p, hipStream_t s) {
+  if ((p.u.n & 255) || p.n > MuonRestP::MAXN || !p.u.v || !p.u.m) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(muon_rest_kernel, dim3((unsigned)(p.u.n / 1024 + (p.u.n % 1024 ? 1 : 0))), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -23,7 +23,7 @@ struct OrthPlan {
   int nparts;                            // partial sums of a matrix's norm
   float a[ORTH_MAX_STEPS], b[ORTH_MAX_STEPS], c[ORTH_MAX_STEPS];
   int ex[ORTH_MAX_STEPS + 1], ea[ORTH_MAX_STEPS], eb[ORTH_MAX_STEPS];   // powers of two that X, A and B are stored with
-  size_t o_part, o_x[2], o_xl[2], o_a, o_al, o_b, o_bl, total;          // pieces of the workspace
+  size_t o_part, o_x[2], o_xl[2], o_a, o_al, o_b, o_bl, o_diag, total;          // pieces of the workspace
 };
 
 // What is orthogonalised: G, or with a momentum buffer (fp32) v <- momentum v + G and u = nesterov ? G + momentum v : v.

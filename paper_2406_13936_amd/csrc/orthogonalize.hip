@@ -10,9 +10,10 @@
 // the first of them (16-bit mode) or, with `split`, all of (hi + lo)(hi + lo) but lo lo, which is what fp32 products give.
 // fp16 and not bf16, because every entry of X, A and B is bounded by a spectral norm that the host knows beforehand
 // (s <= 1 before the first step and max |p| on that interval after it): each is stored times a power of two that puts
-// this bound just under fp16's largest value, so three more bits of mantissa come free.  Relative error of the result
-// for 64 x 64 to 1536 x 1536 matrices of full rank, rank 64 and of a spectrum falling over five decades: 0.5 to 2.1e-3
-// (bf16 operands 5e-3 to 1.5e-2), with `split` the same as fp32 products (1.2e-6 to 1.2e-5).  Why X cannot be rounded to 16 bits: a step
+// this bound just under fp16's largest value, so three more bits of mantissa come free.  B's diagonal, where its largest
+// entries lie (near -2.7 once A is near 1), stays in fp32 and is applied where X' is finished.  Relative error of the result
+// for 64 x 64 to 1536 x 1536 matrices of full rank, rank 64 and of a spectrum falling over five decades: 0.5 to 1.6e-3 (with the
+// diagonal rounded too 0.5 to 2.1e-3, bf16 operands 5e-3 to 1.5e-2), with `split` the same as fp32 products (1.2e-6 to 1.2e-5).  Why X cannot be rounded to 16 bits: a step
 // multiplies a singular value near 0 by a = 3.4, five of them by 485, and with it the rounding noise that lies along
 // those directions (rank 64 in 256 x 512: 1.8e-2 with fp16, 0.15 with bf16).  B X makes no such noise from a rounded X,
 // since B's range is that of X.
@@ -154,11 +155,15 @@ struct OrthGemmP {
   uint16_t *C, *Cl; long long sC; int ldc;
   float alpha, beta;
   int sym;                               // C is symmetric: tiles below the diagonal are written from those above it
+  float *diag; int diag_of;              // [z][mp] fp32 diagonal: DIAG_OUT: C's, which is stored as zeros there; DIAG_ROWS, DIAG_COLS:
+                                         //   beta diag[m] (or [n]) times E's first part is added
   OrthOut out; int rows, cols, vec;      // the last step (C null)
 };
 
 // Tiles BM x BN x BK with WM x WN wavefronts, NS stages of direct global -> LDS loads; operands k-contiguous or row-contiguous as
 // in gemm_bf16.hip.  SPLIT: the reduction runs three times over k, with (hi, lo), (lo, hi) and (hi, hi) as operands.
+enum { DIAG_NONE = 0, DIAG_OUT, DIAG_ROWS, DIAG_COLS };
+
 template <int BM, int BN, int BK, int WM, int WN, int NS, bool AT, bool BT, bool SPLIT>
 __global__ void __launch_bounds__(WM * WN * 64) orth_gemm_kernel(const OrthGemmP p, const int tilesM, const int tilesN, const int nblk, const int chunk) {
   constexpr int NW = WM * WN;
@@ -304,12 +309,22 @@ __global__ void __launch_bounds__(WM * WN * 64) orth_gemm_kernel(const OrthGemmP
         const float4 x = *reinterpret_cast<const float4 *>(stg + r * SLD + cc), y = *reinterpret_cast<const float4 *>(stg + r * SLD + cc + 4);
         v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= p.beta;
       if (p.E) {
         const long long at = z * p.sE + (long long)m * p.lde + n;
         float h[8], l[8];
         load8(p.E, TYPE_F16, at, h);
+        if (p.diag_of == DIAG_ROWS) {
+          const float d = p.diag[(long long)z * p.Md + m];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(d, h[e], v[e]);
+        } else if (p.diag_of == DIAG_COLS) {
+          float d[8];
+          load8(p.diag, TYPE_F32, (long long)z * p.Nd + n, d);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(d[e], h[e], v[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= p.beta;
         if (p.El) {
           load8(p.El, TYPE_F16, at, l);
 #pragma unroll
@@ -317,6 +332,14 @@ __global__ void __launch_bounds__(WM * WN * 64) orth_gemm_kernel(const OrthGemmP
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = fmaf(p.alpha, h[e], v[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= p.beta;
+      }
+      if (p.diag_of == DIAG_OUT) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (n + e == m) { p.diag[(long long)z * p.Md + m] = v[e]; v[e] = 0.0f; }
       }
       if (p.C) {
         const long long at = z * p.sC + (long long)m * p.ldc + n;
@@ -402,7 +425,7 @@ hipError_t launch_product(const OrthGemmP &p, hipStream_t s) {
 }
 
 // Few rows average little of what 16-bit operands round away (relative error up to 1.6e-2 for 2 x 2, 4.4e-3 for 8 x 8, 3.2e-3 for 17 x 33)
-constexpr int SPLIT_ALWAYS = 64;
+constexpr int SPLIT_ALWAYS = 128;
 
 // power of two that leaves a bound just under fp16's largest value
 int exponent_for(double bound) { return 15 - (int)std::ceil(std::log2(bound)); }
@@ -457,6 +480,7 @@ const char *orth_plan(int batch, int rows, int cols, int split, int steps, const
   pl.o_xl[0] = take(xb);
   pl.o_xl[1] = pl.split ? take(xb) : pl.o_xl[0];     // (16-bit mode: no product reads it, each entry is replaced where it was read)
   pl.o_a = take(ab); pl.o_b = take(ab);
+  pl.o_diag = pl.split ? 0 : take((size_t)batch * pl.mp * 4);
   pl.o_al = pl.split ? take(ab) : 0; pl.o_bl = pl.split ? take(ab) : 0;
   pl.total = o;
   return nullptr;
@@ -502,6 +526,8 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
     if (pl.split) p.Al = p.Bl = p.El = at(pl.o_al);
     p.C = at(pl.o_b); p.Cl = pl.split ? at(pl.o_bl) : nullptr; p.sC = sa; p.ldc = pl.mp;
     p.alpha = std::ldexp(pl.b[k], pl.eb[k] - pl.ea[k]); p.beta = std::ldexp(pl.c[k], pl.eb[k] - 2 * pl.ea[k]);
+    float *diag = reinterpret_cast<float *>(ws + pl.o_diag);
+    if (!pl.split) { p.diag = diag; p.diag_of = DIAG_OUT; }
     e = launch_product<false, false>(p, s);
     if (e != hipSuccess) return e;
     // X' = a X + B X, or a X + X B
@@ -511,6 +537,7 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
     const int et = last ? 0 : pl.ex[k + 1];
     p.Md = pl.rp; p.Nd = pl.cp; p.Kd = pl.mp;
     p.E = x; p.El = xl; p.sE = sx; p.lde = pl.cp;
+    if (!pl.split) { p.diag = diag; p.diag_of = pl.wide ? DIAG_ROWS : DIAG_COLS; }
     p.alpha = std::ldexp(pl.a[k], et - pl.ex[k]); p.beta = std::ldexp(1.0f, et - pl.eb[k] - pl.ex[k]);
     if (last) {
       p.out = out; p.rows = pl.rows; p.cols = pl.cols;
