@@ -7,6 +7,7 @@ device memory alive.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -446,47 +447,104 @@ def average_bf16_static(params):
 
 
 # -- operators beside the replicas' step -------------------------------------------------------------------------------
+#
+# Single-token calls run for a few microseconds on the GPU, so the host's part is kept short: checks go by shapes, strides and
+# types and their outcome is kept by these, the device is only switched where it has to be, and the stream is asked for as a
+# plain handle.
+
+_torch = None
+_TYPES = {}
+
+
+def _lib_and_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+        _torch = torch
+    return _lib or load_library(), _torch
+
 
 def _type_of(t, what: str) -> int:
-    import torch
-    kinds = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    if t.dtype not in kinds:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise AbsError(f"{what} must be float32, bfloat16 or float16, not {t.dtype}")
     if not t.is_cuda:
         raise AbsError(f"{what} must be in device memory")
-    return kinds[t.dtype]
+    return kind
 
 
-def _rows(t, lead: int, what: str):
-    """(stride of the first dimension, stride of a row) of a tensor whose dimensions between `lead` and the last are one run
-    of equally spaced rows."""
-    if t.stride(-1) != 1 and t.shape[-1] != 1:
+def _same_device(first, *others) -> int:
+    dev = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise AbsError(f"tensors on different devices: {first.device} and {t.device}")
+    return dev
+
+
+def _call(dev: int, fn, *args):
+    """fn(*args, stream) on the current stream of device `dev`."""
+    if dev == _torch.cuda.current_device():
+        _check(fn(*args, _torch._C._cuda_getCurrentRawStream(dev)))
+    else:
+        with _torch.cuda.device(dev):
+            _check(fn(*args, _torch._C._cuda_getCurrentRawStream(dev)))
+
+
+def _workspace(nbytes: int, device):
+    """(tensor, address on 256 bytes) of device memory for one call, from torch's allocator on the current stream."""
+    t = _torch.empty(nbytes + 256, dtype=_torch.uint8, device=device)
+    return t, (t.data_ptr() + 255) // 256 * 256
+
+
+def _like(t):
+    """A new contiguous tensor of t's shape, type and device."""
+    return _torch.empty_like(t) if t.is_contiguous() else _torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+@functools.lru_cache(maxsize=512)
+def _rows(shape, stride, what: str):
+    """(stride of the first dimension, stride of a row) of a tensor whose dimensions between the first and the last are one
+    run of equally spaced rows."""
+    if stride[-1] != 1 and shape[-1] != 1:
         raise AbsError(f"{what}: values of a row must be consecutive")
     ld, n = None, 1
-    for d in range(t.dim() - 2, lead - 1, -1):
-        if t.shape[d] == 1:
+    for size, step in zip(shape[-2:0:-1], stride[-2:0:-1]):
+        if size == 1:
             continue
         if ld is None:
-            ld = t.stride(d)
-        elif t.stride(d) != ld * n:
+            ld = step
+        elif step != ld * n:
             raise AbsError(f"{what}: rows must be equally spaced")
-        n *= t.shape[d]
-    return (t.stride(0) if lead and t.shape[0] > 1 else 0), (t.shape[-1] if ld is None else ld)
+        n *= size
+    return (stride[0] if shape[0] > 1 else 0), (shape[-1] if ld is None else ld)
 
 
-def _same_device(first, *others):
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise AbsError(f"tensors on different devices: {first.device} and {t.device}")
+@functools.lru_cache(maxsize=512)
+def _matrices(shape, stride, what: str):
+    """(batch, rows, cols, stride from matrix to matrix, stride from row to row) of [..., rows, cols]."""
+    if len(shape) < 2:
+        raise AbsError(f"{what} must have at least two dimensions")
+    rows, cols = shape[-2], shape[-1]
+    if stride[-1] != 1 and cols != 1:
+        raise AbsError(f"{what}: values of a row must be consecutive")
+    batch, step = 1, None
+    for n, st in zip(shape[-3::-1], stride[-3::-1]):
+        if n == 1:
+            continue
+        if step is None:
+            step = st
+        elif st != step * batch:
+            raise AbsError(f"{what}: matrices must be equally spaced")
+        batch *= n
+    return batch, rows, cols, (step or 0), (stride[-2] if rows > 1 else cols)
 
 
-class _Workspace:
-    """256-byte aligned device memory of one call (from torch's allocator, on the current stream)."""
-
-    def __init__(self, nbytes: int, device):
-        import torch
-        self._mem = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
-        self.ptr, self.nbytes = (self._mem.data_ptr() + 255) // 256 * 256, nbytes
+@functools.lru_cache(maxsize=512)
+def _orth_bytes(batch: int, rows: int, cols: int, prec: int) -> int:
+    n = C.c_size_t(0)
+    _check(_lib.abs_orthogonalize_workspace_bytes(batch, rows, cols, prec, C.byref(n)))
+    return n.value
 
 
 def _coefficients(coefficients, steps: int):
@@ -500,119 +558,92 @@ def _coefficients(coefficients, steps: int):
     return flat
 
 
-def _matrices(t, what: str):
-    """(batch, rows, cols, stride from matrix to matrix, stride from row to row) of [..., rows, cols]."""
-    if t.dim() < 2:
-        raise AbsError(f"{what} must have at least two dimensions")
-    rows, cols = int(t.shape[-2]), int(t.shape[-1])
-    if t.stride(-1) != 1 and cols != 1:
-        raise AbsError(f"{what}: values of a row must be consecutive")
-    batch, stride = 1, None
-    for d in range(t.dim() - 3, -1, -1):
-        if t.shape[d] == 1:
-            continue
-        if stride is None:
-            stride = t.stride(d)
-        elif t.stride(d) != stride * batch:
-            raise AbsError(f"{what}: matrices must be equally spaced")
-        batch *= t.shape[d]
-    return int(batch), rows, cols, int(stride or 0), int(t.stride(-2)) if rows > 1 else cols
-
-
 def orthogonalize(g, steps: int = 5, coefficients=None, eps: float = 1e-7, prec: Optional[int] = None, out=None):
     """Newton-Schulz orthogonalisation of [..., rows, cols] device matrices (abs_orthogonalize); `out` defaults to a new
     tensor of g's type and may be g itself.  prec: PREC_BF16 (16-bit products) or PREC_F32; by default what the result's
     type can tell apart, PREC_BF16 for bfloat16 only."""
-    import torch
-    lib = load_library()
+    lib, _ = _lib_and_torch()
     gt = _type_of(g, "g")
     if out is None:
-        out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
-    ot = _type_of(out, "out")
-    _same_device(g, out)
-    if out.shape != g.shape:
-        raise AbsError("out must have g's shape")
-    batch, rows, cols, sg, ldg = _matrices(g, "g")
-    _, _, _, so, ldo = _matrices(out, "out")
+        out, ot = _like(g), gt
+    else:
+        ot = _type_of(out, "out")
+        if out.shape != g.shape:
+            raise AbsError("out must have g's shape")
+    dev = _same_device(g, out)
+    batch, rows, cols, sg, ldg = _matrices(g.shape, g.stride(), "g")
+    _, _, _, so, ldo = _matrices(out.shape, out.stride(), "out")
     prec = (PREC_BF16 if ot == 1 else PREC_F32) if prec is None else int(prec)
     coef = _coefficients(coefficients, steps)
-    nbytes = C.c_size_t(0)
-    with torch.cuda.device(g.device):
-        _check(lib.abs_orthogonalize_workspace_bytes(batch, rows, cols, prec, C.byref(nbytes)))
-        ws = _Workspace(nbytes.value, g.device)
-        _check(lib.abs_orthogonalize(g.data_ptr(), gt, ldg, sg, out.data_ptr(), ot, ldo, so, batch, rows, cols, int(steps),
-                                     None if coef is None else coef.ctypes.data, float(eps), prec, ws.ptr, ws.nbytes,
-                                     _stream_ptr()))
+    nbytes = _orth_bytes(batch, rows, cols, prec)
+    keep, ws = _workspace(nbytes, g.device)
+    _call(dev, lib.abs_orthogonalize, g.data_ptr(), gt, ldg, sg, out.data_ptr(), ot, ldo, so, batch, rows, cols, int(steps),
+          None if coef is None else coef.ctypes.data, eps, prec, ws, nbytes)
     return out
 
 
 def muon_step(x, g, v, lr: float, momentum: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
               scale: Optional[float] = None, steps: int = 5, coefficients=None, eps: float = 1e-7, prec: Optional[int] = None):
     """One step with orthogonalised momentum on [..., rows, cols] device matrices, in place on x and on the fp32 momentum v
-    (abs_muon_step).  scale defaults to 0.2 sqrt(max(rows, cols)); prec by default as exact as x's type."""
-    import torch
-    lib = load_library()
+    (abs_muon_step).  scale defaults to 0.2 sqrt(max(rows, cols)); prec to PREC_F32 where x is float32."""
+    lib, _ = _lib_and_torch()
     xt, gt = _type_of(x, "x"), _type_of(g, "g")
     if _type_of(v, "v") != 0:
         raise AbsError("v must be float32")
-    _same_device(x, g, v)
+    dev = _same_device(x, g, v)
     if x.shape != g.shape or x.shape != v.shape:
         raise AbsError("x, g and v must have the same shape")
     if not (x.is_contiguous() and g.is_contiguous() and v.is_contiguous()):
         raise AbsError("x, g and v must be contiguous")
-    batch, rows, cols, _, _ = _matrices(x, "x")
+    batch, rows, cols, _, _ = _matrices(x.shape, x.stride(), "x")
     prec = (PREC_F32 if xt == 0 else PREC_BF16) if prec is None else int(prec)
     coef = _coefficients(coefficients, steps)
     if scale is None:
         scale = 0.2 * max(rows, cols) ** 0.5
-    nbytes = C.c_size_t(0)
-    with torch.cuda.device(x.device):
-        _check(lib.abs_orthogonalize_workspace_bytes(batch, rows, cols, prec, C.byref(nbytes)))
-        ws = _Workspace(nbytes.value, x.device)
-        _check(lib.abs_muon_step(x.data_ptr(), xt, g.data_ptr(), gt, v.data_ptr(), batch, rows, cols, float(lr), float(momentum),
-                                 int(bool(nesterov)), float(weight_decay), float(scale), int(steps),
-                                 None if coef is None else coef.ctypes.data, float(eps), prec, ws.ptr, ws.nbytes, _stream_ptr()))
+    nbytes = _orth_bytes(batch, rows, cols, prec)
+    keep, ws = _workspace(nbytes, x.device)
+    _call(dev, lib.abs_muon_step, x.data_ptr(), xt, g.data_ptr(), gt, v.data_ptr(), batch, rows, cols, lr, momentum,
+          1 if nesterov else 0, weight_decay, scale, int(steps), None if coef is None else coef.ctypes.data, eps, prec, ws, nbytes)
+
+
+@functools.lru_cache(maxsize=512)
+def _norm_shape(shape, stride, kind: int, param_kind: int, other_shape, other_stride, other: str):
+    """(struct for x and the tensor y or dy beside it, reference to it, workspace bytes by outputs asked for)"""
+    if len(shape) < 3:
+        raise AbsError("x must be [M, b, ..., D]")
+    M, b, D = shape[0], shape[1], shape[-1]
+    T = 1
+    for n in shape[2:-1]:
+        T *= n
+    sx, ldx = _rows(shape, stride, "x")
+    sy, ldy = _rows(other_shape, other_stride, other)
+    s = LayerNormShape(M, b, T, D, kind, param_kind, ldx, sx, ldy, sy, D, b * T * D)
+    return s, C.byref(s), {}
 
 
 def _norm_params(x, p, what: str) -> int:
-    t = _type_of(p, what)
-    _same_device(x, p)
-    if tuple(p.shape) != (x.shape[0], x.shape[-1]) or not p.is_contiguous():
+    if p.shape[0] != x.shape[0] or p.shape[-1] != x.shape[-1] or p.dim() != 2 or not p.is_contiguous():
         raise AbsError(f"{what} must be a contiguous [M, D] tensor")
-    return t
-
-
-def _norm_shape(x, param_type: int) -> LayerNormShape:
-    if x.dim() < 3:
-        raise AbsError("x must be [M, b, ..., D]")
-    M, b, D = int(x.shape[0]), int(x.shape[1]), int(x.shape[-1])
-    T = 1
-    for n in x.shape[2:-1]:
-        T *= int(n)
-    sx, ldx = _rows(x, 1, "x")
-    return LayerNormShape(M, b, T, D, _type_of(x, "x"), param_type, ldx, sx, D, b * T * D, D, b * T * D)
+    return _type_of(p, what)
 
 
 def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None):
     """Layer norm of [M, b, ..., D] over the last dimension with weights and biases [M, D] (fp32 or x's type), one set per
     replica.  Returns (y, mean, rstd), the latter two fp32 [M, b, ...]; `out` may be x itself."""
-    import torch
-    lib = load_library()
-    _type_of(x, "x")
+    lib, torch = _lib_and_torch()
+    kind = _type_of(x, "x")
     pt = _norm_params(x, weight, "weight")
     if bias is not None and _norm_params(x, bias, "bias") != pt:
         raise AbsError("weight and bias must have the same type")
-    shape = _norm_shape(x, pt)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    _same_device(x, y)
+    y = _like(x) if out is None else out
     if y.shape != x.shape or y.dtype != x.dtype:
         raise AbsError("out must have x's shape and type")
-    shape.stride_y, shape.ldy = _rows(y, 1, "out")
+    dev = _same_device(x, weight, bias, y)
+    _, shape, _ = _norm_shape(x.shape, x.stride(), kind, pt, y.shape, y.stride(), "out")
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    with torch.cuda.device(x.device):
-        _check(lib.abs_layer_norm(C.byref(shape), x.data_ptr(), weight.data_ptr(), bias.data_ptr() if bias is not None else None,
-                                  float(eps), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _stream_ptr()))
+    rstd = torch.empty_like(mean)
+    _call(dev, lib.abs_layer_norm, shape, x.data_ptr(), weight.data_ptr(), bias.data_ptr() if bias is not None else None, eps,
+          y.data_ptr(), mean.data_ptr(), rstd.data_ptr())
     return y, mean, rstd
 
 
@@ -620,31 +651,30 @@ def layer_norm_backward(dy, x, weight, mean, rstd, has_bias: bool = True, want_n
     """Gradients of layer_norm from the signals dy [M, b, ..., D] of the per-sample losses, and the batch tests' statistics of
     the gradient of weight and bias.  Returns (dx, dweight, dbias, n, q): batch gradients fp32 [M, D] (means over the b
     samples; dbias None without a bias), n_i = ||g_i||^2 and q_i = <g_i, gbar> fp32 [M, b], None unless asked for."""
-    import torch
-    lib = load_library()
-    _type_of(x, "x")
-    shape = _norm_shape(x, _norm_params(x, weight, "weight"))
-    _type_of(dy, "dy")
-    _same_device(x, dy, mean, rstd)
+    lib, torch = _lib_and_torch()
+    kind = _type_of(x, "x")
+    pt = _norm_params(x, weight, "weight")
     if dy.shape != x.shape or dy.dtype != x.dtype:
         raise AbsError("dy must have x's shape and type")
+    lead = x.shape[:-1]
     for t, what in ((mean, "mean"), (rstd, "rstd")):
-        if t.dtype != torch.float32 or t.shape != x.shape[:-1] or not t.is_contiguous():
+        if t.dtype != torch.float32 or t.shape != lead or not t.is_contiguous():
             raise AbsError(f"{what} must be a contiguous float32 tensor [M, b, ...]")
-    shape.stride_y, shape.ldy = _rows(dy, 1, "dy")
-    dev, M, b, D = x.device, shape.M, shape.b, shape.D
-    dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    dw = torch.empty((M, D), dtype=torch.float32, device=dev)
-    db = torch.empty((M, D), dtype=torch.float32, device=dev) if has_bias else None
-    n = torch.empty((M, b), dtype=torch.float32, device=dev) if want_norms else None
-    q = torch.empty((M, b), dtype=torch.float32, device=dev) if want_inner else None
-    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-    nbytes = C.c_size_t(0)
-    with torch.cuda.device(dev):
-        _check(lib.abs_layer_norm_backward_workspace_bytes(C.byref(shape), int(bool(want_norms)), int(bool(want_inner)),
-                                                           C.byref(nbytes)))
-        ws = _Workspace(nbytes.value, dev)
-        _check(lib.abs_layer_norm_backward(C.byref(shape), dy.data_ptr(), x.data_ptr(), weight.data_ptr(), mean.data_ptr(),
-                                           rstd.data_ptr(), dx.data_ptr(), dw.data_ptr(), ptr(db), ptr(n), ptr(q), ws.ptr,
-                                           ws.nbytes, _stream_ptr()))
+    dev = _same_device(x, dy, weight, mean, rstd)
+    s, shape, sizes = _norm_shape(x.shape, x.stride(), kind, pt, dy.shape, dy.stride(), "dy")
+    wants = (bool(want_norms), bool(want_inner))
+    nbytes = sizes.get(wants)
+    if nbytes is None:
+        n = C.c_size_t(0)
+        _check(lib.abs_layer_norm_backward_workspace_bytes(shape, int(wants[0]), int(wants[1]), C.byref(n)))
+        nbytes = sizes[wants] = n.value
+    dx = _like(x)
+    dw = torch.empty((s.M, s.D), dtype=torch.float32, device=x.device)
+    db = torch.empty_like(dw) if has_bias else None
+    n = torch.empty((s.M, s.b), dtype=torch.float32, device=x.device) if want_norms else None
+    q = (torch.empty((s.M, s.b), dtype=torch.float32, device=x.device) if n is None else torch.empty_like(n)) if want_inner else None
+    keep, ws = _workspace(nbytes, x.device)
+    _call(dev, lib.abs_layer_norm_backward, shape, dy.data_ptr(), x.data_ptr(), weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+          dx.data_ptr(), dw.data_ptr(), db.data_ptr() if has_bias else None, n.data_ptr() if want_norms else None,
+          q.data_ptr() if want_inner else None, ws, nbytes)
     return dx, dw, db, n, q
