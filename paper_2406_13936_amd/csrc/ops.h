@@ -16,6 +16,10 @@ inline int type_bytes(int t) { return t == TYPE_F32 ? 4 : 2; }
 constexpr int ORTH_MAX_STEPS = 32;
 constexpr int ORTH_PARTS = 256;          // most partial sums of a matrix's norm
 
+// Factors of one step between the powers of two that the operands are stored with: A = gram X X^T, B = poly_a A + poly_aa A A,
+// X' = apply_x X + apply_bx B X
+struct OrthScale { float gram, poly_a, poly_aa, apply_x, apply_bx; };
+
 struct OrthPlan {
   int batch, rows, cols, steps, split;   // split: operands as sums of two fp16 values (fp32-class products)
   int wide;                              // rows <= cols: the products A = X X^T, else A = X^T X
@@ -24,6 +28,7 @@ struct OrthPlan {
   float a[ORTH_MAX_STEPS], b[ORTH_MAX_STEPS], c[ORTH_MAX_STEPS];
   int ex[ORTH_MAX_STEPS + 1], ea[ORTH_MAX_STEPS], eb[ORTH_MAX_STEPS];   // powers of two that X, A and B are stored with
   size_t o_part, o_x[2], o_xl[2], o_a, o_al, o_b, o_bl, o_diag, total;          // pieces of the workspace
+  OrthScale scale(int k) const;
 };
 
 // What is orthogonalised: G, or with a momentum buffer (fp32) v <- momentum v + G and u = nesterov ? G + momentum v : v.
@@ -42,6 +47,10 @@ struct OrthOut {
 // nullptr, or why these coefficients (3 per step; null: the quintic's) cannot be taken
 const char *orth_plan(int batch, int rows, int cols, int split, int steps, const float *coef, OrthPlan &pl);
 hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, void *workspace, hipStream_t s);
+
+// orthogonalize_small.hip: a work-group's LDS holds the matrix
+bool orth_small_fits(int rows, int cols);
+hipError_t launch_orth_small(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, hipStream_t s);
 
 // ---- layer norm ----------------------------------------------------------------------------------------------------
 

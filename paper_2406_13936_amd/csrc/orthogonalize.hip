@@ -24,26 +24,12 @@
 #include "device_utils.h"
 #include "mfma_tile.h"
 #include "ops.h"
+#include "orth_parts.h"
 #include "typed_mem.h"
 
 namespace absk {
 
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
 namespace {
-
-// eight values as fp16 and what that leaves
-__device__ __forceinline__ void split8(const float (&v)[8], uint4 &hi, uint4 &lo) {
-  uint32_t h[4], l[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint16_t h0 = f16_bits(v[2 * e]), h1 = f16_bits(v[2 * e + 1]);
-    h[e] = (uint32_t)h0 | ((uint32_t)h1 << 16);
-    l[e] = (uint32_t)f16_bits(v[2 * e] - f16_val(h0)) | ((uint32_t)f16_bits(v[2 * e + 1] - f16_val(h1)) << 16);
-  }
-  hi = make_uint4(h[0], h[1], h[2], h[3]);
-  lo = make_uint4(l[0], l[1], l[2], l[3]);
-}
 
 // ---- norm and first X ----------------------------------------------------------------------------------------------
 
@@ -58,42 +44,14 @@ struct OrthPrepP {
 // where it advances.  One pass over G (and v): bound by memory.
 __global__ void __launch_bounds__(256) orth_norm_kernel(const OrthPrepP p) {
   __shared__ double sm[4];
-  const int z = blockIdx.y;
-  const long long g0 = z * p.in.sg, v0 = z * p.in.sv;
-  const float mu = p.in.momentum;
+  const int z = blockIdx.y, cc = (p.cols + 7) >> 3, n = p.rows * cc;
   double sum = 0.0;
-  if (p.vec) {
-    const int cc = p.cols >> 3, n = p.rows * cc;
-    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
-      const int r = i / cc, c = (i - r * cc) * 8;
-      float g[8];
-      load8(p.in.g, p.in.type, g0 + (long long)r * p.in.ldg + c, g);
-      if (p.in.v) {
-        float v[8];
-        const long long at = v0 + (long long)r * p.cols + c;
-        load8(p.in.v, TYPE_F32, at, v);
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+    const int r = i / cc, c = (i - r * cc) * 8;
+    float u[8];
+    load_u8<true>(p.in, p.rows, p.cols, p.vec, z, r, c, u);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[e] = fmaf(mu, v[e], g[e]);
-          g[e] = p.in.nesterov ? fmaf(mu, v[e], g[e]) : v[e];
-        }
-        store8(p.in.v, TYPE_F32, at, v);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fma((double)g[e], (double)g[e], sum);
-    }
-  } else {
-    const long long n = (long long)p.rows * p.cols;
-    for (long long i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
-      const int r = (int)(i / p.cols), c = (int)(i - (long long)r * p.cols);
-      float g = load_as_f32(p.in.g, p.in.type, g0 + (long long)r * p.in.ldg + c);
-      if (p.in.v) {
-        const float v = fmaf(mu, p.in.v[v0 + i], g);
-        p.in.v[v0 + i] = v;
-        g = p.in.nesterov ? fmaf(mu, v, g) : v;
-      }
-      sum = fma((double)g, (double)g, sum);
-    }
+    for (int e = 0; e < 8; ++e) sum = fma((double)u[e], (double)u[e], sum);
   }
   const double t = block_sum<4>(sum, sm);
   if (threadIdx.x == 0) p.part[(long long)z * p.nparts + blockIdx.x] = t;
@@ -108,33 +66,12 @@ __global__ void __launch_bounds__(256) orth_prep_kernel(const OrthPrepP p) {
   if (threadIdx.x == 0) scale = ldexp(1.0 / (sqrt(t) + (double)p.eps), p.ex);
   __syncthreads();
   const double sc = scale;
-  const long long g0 = z * p.in.sg, v0 = z * p.in.sv, x0 = (long long)z * p.rp * p.cp;
-  const float mu = p.in.momentum;
+  const long long x0 = (long long)z * p.rp * p.cp;
   const int cc = p.cp >> 3, n = p.rp * cc;
   for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
     const int r = i / cc, c = (i - r * cc) * 8;
     float u[8];
-    if (p.vec && r < p.rows) {                     // (cols is a multiple of 8: the chunk lies inside)
-      load8(p.in.g, p.in.type, g0 + (long long)r * p.in.ldg + c, u);
-      if (p.in.v) {
-        float v[8];
-        load8(p.in.v, TYPE_F32, v0 + (long long)r * p.cols + c, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = p.in.nesterov ? fmaf(mu, v[e], u[e]) : v[e];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        u[e] = 0.0f;
-        if (r < p.rows && c + e < p.cols) {
-          u[e] = load_as_f32(p.in.g, p.in.type, g0 + (long long)r * p.in.ldg + c + e);
-          if (p.in.v) {
-            const float v = p.in.v[v0 + (long long)r * p.cols + c + e];
-            u[e] = p.in.nesterov ? fmaf(mu, v, u[e]) : v;
-          }
-        }
-      }
-    }
+    load_u8<false>(p.in, p.rows, p.cols, p.vec, z, r, c, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) u[e] = (float)((double)u[e] * sc);
     uint4 h, l;
@@ -432,6 +369,12 @@ int exponent_for(double bound) { return 15 - (int)std::ceil(std::log2(bound)); }
 
 }  // namespace
 
+OrthScale OrthPlan::scale(int k) const {
+  const int to = k + 1 == steps ? 0 : ex[k + 1];           // (the result itself is not scaled)
+  return {std::ldexp(1.0f, ea[k] - 2 * ex[k]), std::ldexp(b[k], eb[k] - ea[k]), std::ldexp(c[k], eb[k] - 2 * ea[k]),
+          std::ldexp(a[k], to - ex[k]), std::ldexp(1.0f, to - eb[k] - ex[k])};
+}
+
 const char *orth_plan(int batch, int rows, int cols, int split, int steps, const float *coef, OrthPlan &pl) {
   std::memset(&pl, 0, sizeof(pl));
   pl.batch = batch; pl.rows = rows; pl.cols = cols; pl.steps = steps;
@@ -470,6 +413,7 @@ const char *orth_plan(int batch, int rows, int cols, int split, int steps, const
     pl.eb[k] = exponent_for(std::max(inner, 1.0 / 256) * (1.0 + 1.0 / 32));
     pl.ex[k + 1] = exponent_for(s);
   }
+  if (orth_small_fits(rows, cols)) { pl.total = 256; return nullptr; }     // (all of it is in LDS)
   // about 16 chunks of 8 values to a thread of the norm's pass, as long as a matrix has them
   pl.nparts = (int)std::min<long long>(ORTH_PARTS, ((long long)rows * cols + 256 * 128 - 1) / (256 * 128));
   size_t o = 0;
@@ -487,6 +431,7 @@ const char *orth_plan(int batch, int rows, int cols, int split, int steps, const
 }
 
 hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, void *workspace, hipStream_t s) {
+  if (orth_small_fits(pl.rows, pl.cols)) return launch_orth_small(pl, in, out, eps, s);
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   auto at = [&](size_t off) { return reinterpret_cast<uint16_t *>(ws + off); };
   const long long sx = (long long)pl.rp * pl.cp, sa = (long long)pl.mp * pl.mp;
@@ -516,7 +461,7 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
     p.A = p.B = x; p.sA = p.sB = sx; p.lda = p.ldb = pl.cp; p.Md = p.Nd = pl.mp; p.Kd = pl.wide ? pl.cp : pl.rp;
     if (pl.split) p.Al = p.Bl = xl;
     p.C = at(pl.o_a); p.Cl = pl.split ? at(pl.o_al) : nullptr; p.sC = sa; p.ldc = pl.mp;
-    p.beta = std::ldexp(1.0f, pl.ea[k] - 2 * pl.ex[k]);
+    p.beta = pl.scale(k).gram;
     e = pl.wide ? launch_product<false, false>(p, s) : launch_product<true, true>(p, s);
     if (e != hipSuccess) return e;
     // B 2^eb = (b A + c A A) 2^eb
@@ -525,7 +470,7 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
     p.A = p.B = p.E = at(pl.o_a); p.sA = p.sB = p.sE = sa; p.lda = p.ldb = p.lde = pl.mp; p.Md = p.Nd = p.Kd = pl.mp;
     if (pl.split) p.Al = p.Bl = p.El = at(pl.o_al);
     p.C = at(pl.o_b); p.Cl = pl.split ? at(pl.o_bl) : nullptr; p.sC = sa; p.ldc = pl.mp;
-    p.alpha = std::ldexp(pl.b[k], pl.eb[k] - pl.ea[k]); p.beta = std::ldexp(pl.c[k], pl.eb[k] - 2 * pl.ea[k]);
+    p.alpha = pl.scale(k).poly_a; p.beta = pl.scale(k).poly_aa;
     float *diag = reinterpret_cast<float *>(ws + pl.o_diag);
     if (!pl.split) { p.diag = diag; p.diag_of = DIAG_OUT; }
     e = launch_product<false, false>(p, s);
@@ -534,11 +479,10 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
     std::memset(&p, 0, sizeof(p));
     p.batch = pl.batch;
     const bool last = k + 1 == pl.steps;
-    const int et = last ? 0 : pl.ex[k + 1];
     p.Md = pl.rp; p.Nd = pl.cp; p.Kd = pl.mp;
     p.E = x; p.El = xl; p.sE = sx; p.lde = pl.cp;
     if (!pl.split) { p.diag = diag; p.diag_of = pl.wide ? DIAG_ROWS : DIAG_COLS; }
-    p.alpha = std::ldexp(pl.a[k], et - pl.ex[k]); p.beta = std::ldexp(1.0f, et - pl.eb[k] - pl.ex[k]);
+    p.alpha = pl.scale(k).apply_x; p.beta = pl.scale(k).apply_bx;
     if (last) {
       p.out = out; p.rows = pl.rows; p.cols = pl.cols;
       p.vec = rows_of_vectors(out.o, out.type, out.so, out.ldo, pl.cols) &&

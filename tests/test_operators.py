@@ -45,8 +45,8 @@ def _orth(lib, **k):
     (dict(g=None), EINVAL), (dict(o=None), EINVAL), (dict(gt=3), EINVAL), (dict(ot=-1), EINVAL), (dict(batch=0), EINVAL),
     (dict(rows=0), EINVAL), (dict(cols=-1), EINVAL), (dict(steps=0), EINVAL), (dict(steps=33), EINVAL), (dict(eps=0.0), EINVAL),
     (dict(eps=float("nan")), EINVAL), (dict(eps=float("inf")), EINVAL), (dict(prec=2), EINVAL), (dict(ws=None), EINVAL),
-    (dict(ws=WS + 8), EINVAL), (dict(nbytes=1024), ENOMEM), (dict(ldg=15), EINVAL), (dict(so=100), EINVAL), (dict(sg=-256), EINVAL),
-    (dict(g=FAKE + 2), EINVAL), (dict(o=FAKE + 64), EINVAL), (dict(o=FAKE, ot=1), EINVAL), (dict(g=WS + 256), EINVAL),
+    (dict(ws=WS + 8), EINVAL), (dict(nbytes=128), ENOMEM), (dict(rows=200, cols=200, ldg=200, ldo=200, sg=40000, so=40000, nbytes=1 << 18), ENOMEM), (dict(ldg=15), EINVAL), (dict(so=100), EINVAL), (dict(sg=-256), EINVAL),
+    (dict(g=FAKE + 2), EINVAL), (dict(o=FAKE + 64), EINVAL), (dict(o=FAKE, ot=1), EINVAL), (dict(g=WS), EINVAL),
     (dict(ldg=1 << 40), EINVAL), (dict(rows=1 << 15, cols=1 << 15, ldg=1 << 15, ldo=1 << 15, batch=1), EUNSUPPORTED),
     (dict(coef=(9.0, 9.0, 9.0) * 5), EINVAL),
     # (each step takes what the one before can leave, 1.34, 2.1 and 10, further from 1)
