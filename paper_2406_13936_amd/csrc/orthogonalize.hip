@@ -98,14 +98,19 @@ struct OrthGemmP {
 };
 
 // Tiles BM x BN x BK with WM x WN wavefronts, NS stages of direct global -> LDS loads; operands k-contiguous or row-contiguous as
-// in gemm_bf16.hip.  SPLIT: the reduction runs three times over k, with (hi, lo), (lo, hi) and (hi, hi) as operands.
+// in gemm_bf16.hip.  PP: its pipelined loop of 256 x 256 tiles (eight 16 KB units of LDS, each refilled seven phases before it is
+// read, four wavefronts half a phase behind the others; the reasons stand there).  SPLIT: the reduction runs three times over
+// k, with (hi, lo), (lo, hi) and (hi, hi) as operands.
 enum { DIAG_NONE = 0, DIAG_OUT, DIAG_ROWS, DIAG_COLS };
+enum { KIND_SYM = 0, KIND_APPLY = 1, KIND_LAST = 2 };   // A and B; X'; X' of the last step
+constexpr int BAND = 8;                  // columns of 256-wide tiles that stand side by side (gemm_bf16.hip)
 
-template <int BM, int BN, int BK, int WM, int WN, int NS, bool AT, bool BT, bool SPLIT>
+template <int BM, int BN, int BK, int WM, int WN, int NS, bool PP, bool AT, bool BT, bool SPLIT, int KIND>
 __global__ void __launch_bounds__(WM * WN * 64) orth_gemm_kernel(const OrthGemmP p, const int tilesM, const int tilesN, const int nblk, const int chunk) {
   constexpr int NW = WM * WN;
   constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 32, NI = TN / 32;
   constexpr int STAGE = (BM + BN) * BK, NPART = BK / 16;
+  static_assert(!PP || (BM == 256 && BN == 256 && BK == 64 && WM == 2 && WN == 4), "the pipelined loop");
   typedef Operand<BM, BK, AT, NW> OpA;
   typedef Operand<BN, BK, BT, NW> OpB;
   constexpr int NL = OpA::NI + OpB::NI;
@@ -128,7 +133,13 @@ __global__ void __launch_bounds__(WM * WN * 64) orth_gemm_kernel(const OrthGemmP
     const int per = tilesM * tilesN;
     z = lb / per;
     const int t = lb - z * per;
-    tm = t / tilesN; tn = t - tm * tilesN;
+    if (BM == 256 && tilesN > BAND) {             // bands of columns, row by row inside a band
+      const int nb = (tilesN + BAND - 1) / BAND, bw = (tilesN + nb - 1) / nb, b = t / (bw * tilesM);
+      const int w = min(bw, tilesN - b * bw), r = t - b * bw * tilesM;
+      tm = r / w; tn = b * bw + r - tm * w;
+    } else {
+      tm = t / tilesN; tn = t - tm * tilesN;
+    }
   }
   const int m0 = tm * BM, n0 = tn * BN;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -140,15 +151,134 @@ __global__ void __launch_bounds__(WM * WN * 64) orth_gemm_kernel(const OrthGemmP
   const __amdgpu_buffer_rsrc_t rah = rsrc(p.A + z * p.sA, abytes), rbh = rsrc(p.B + z * p.sB, bbytes);
   const __amdgpu_buffer_rsrc_t ral = rsrc(SPLIT ? p.Al + z * p.sA : p.A, abytes), rbl = rsrc(SPLIT ? p.Bl + z * p.sB : p.B, bbytes);
 
-  f32x16 acc[MI][NI];
+  f32x16 acc[PP ? 1 : MI][PP ? 1 : NI];
+  f32x4 acc16[PP ? TM / 16 : 1][PP ? TN / 16 : 1];
+  if constexpr (PP) {
 #pragma unroll
-  for (int i = 0; i < MI; ++i)
+    for (int i = 0; i < TM / 16; ++i)
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
+      for (int j = 0; j < TN / 16; ++j) acc16[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  } else {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+  }
 
   const int KT1 = (p.Kd + BK - 1) / BK, KT = SPLIT ? 3 * KT1 : KT1;
+  if constexpr (PP) {
+    typedef Operand<128, 64, AT, NW, 32> UA;                 // A unit h: rows 128 h .. 128 h + 127 of the tile, 64 k
+    typedef Operand<BT ? 256 : 128, BT ? 32 : 64, BT, NW, 32> UB;   // B unit c: k 32 c .. (BT), or columns 64 j + 32 c ..
+    constexpr int UNIT = 8192;                               // elements of a unit (16 KB)
+    UA ua[2];
+    UB ub[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      ua[h].init(wave, lane, m0 + h * 128, p.Md, p.lda);
+      if constexpr (BT) ub[h].init(wave, lane, n0, p.Nd, p.ldb);
+      else ub[h].template init<true>(wave, lane, n0 + h * 32, p.Nd, p.ldb);
+    }
+    // (k-tiles beyond the last bring zeros)
+    auto load_a = [&](int kt, int slot, int h) {
+      const int seg = SPLIT ? (kt >= KT1) + (kt >= 2 * KT1) : 2, k = SPLIT ? kt - seg * KT1 : kt;
+      ua[h].load_all(SPLIT && seg == 1 ? ral : rah, smem + (slot * 2 + h) * UNIT, wave, k * 64, 0, p.Kd, p.lda);
+    };
+    auto load_b = [&](int kt, int slot, int c) {
+      const int seg = SPLIT ? (kt >= KT1) + (kt >= 2 * KT1) : 2, k = SPLIT ? kt - seg * KT1 : kt;
+      ub[c].load_all(SPLIT && seg == 0 ? rbl : rbh, smem + (4 + slot * 2 + c) * UNIT, wave, k * 64 + (BT ? c * 32 : 0), 0, p.Kd, p.ldb);
+    };
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
+    const int i16 = lane & 15, g16 = lane >> 4;
+    const int kq = g16 * 8 + (i16 >> 2);                     // transpose reads: k within the 32-wide step
+    uint32_t aaddr[AT ? 4 : 2], baddr[BT ? 4 : 2];           // (transpose reads: by row tile; else by k-step)
+    if constexpr (AT) {
+#pragma unroll
+      for (int ii = 0; ii < 4; ++ii) {
+        const int rr = wm * 64 + ii * 16 + 4 * (i16 & 3);
+        aaddr[ii] = lds0 + 2u * (uint32_t)(kq * 128 + ((rr >> 3) ^ tr_swizzle<32>(kq)) * 8 + (rr & 7));
+      }
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+        aaddr[kk] = lds0 + (uint32_t)((wm * 64 + i16) * 128 + (((kk * 4 + g16) ^ (i16 >> 1)) << 4));
+    }
+    if constexpr (BT) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int rr = wn * 64 + j * 16 + 4 * (i16 & 3);
+        baddr[j] = lds0 + 65536u + 2u * (uint32_t)(kq * 256 + ((rr >> 3) ^ tr_swizzle<32>(kq)) * 8 + (rr & 7));
+      }
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+        baddr[kk] = lds0 + 65536u + (uint32_t)((wn * 32 + i16) * 128 + (((kk * 4 + g16) ^ (i16 >> 1)) << 4));
+    }
+    bf16x8 fa[4][2], fb[2][4];                               // fa[row tile][k-step]; fb[unit][BT: column tile, else 2 column tile + k-step]
+    auto read_a = [&](auto SLOT, auto H) {
+      constexpr int U = (decltype(SLOT)::value * 2 + decltype(H)::value) * UNIT * 2;
+      static_for<8>([&](auto I) {
+        constexpr int kk = decltype(I)::value >> 2, ii = decltype(I)::value & 3;
+        if constexpr (AT) fa[ii][kk] = lds_read_cols<U + kk * 8192, 1024>(aaddr[ii]);
+        else fa[ii][kk] = lds_read_rows<U + ii * 2048>(aaddr[kk]);
+      });
+    };
+    auto read_b = [&](auto SLOT, auto C) {
+      constexpr int c = decltype(C)::value, U = (decltype(SLOT)::value * 2 + c) * UNIT * 2;
+      static_for<4>([&](auto I) {
+        constexpr int q = decltype(I)::value;
+        if constexpr (BT) fb[c][q] = lds_read_cols<U, 2048>(baddr[q]);
+        else fb[c][q] = lds_read_rows<U + (q >> 1) * 2048>(baddr[q & 1]);
+      });
+    };
+    auto close_reads = [&]() {                               // this wave's fragment reads are done
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) asm volatile("" : "+v"(fa[q][0]), "+v"(fa[q][1]), "+v"(fb[0][q]), "+v"(fb[1][q]));
+    };
+    auto mfma = [](bf16x8 x, bf16x8 y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0); };
+    auto phase = [&](auto SLOT, auto F, int kt) {
+      constexpr int f = decltype(F)::value, h = f >> 1, c = f & 1;
+      if constexpr (f == 0) { read_a(SLOT, Const<0>{}); load_b(kt + 2, SLOT.value, 0); }
+      if constexpr (f == 1) { read_b(SLOT, Const<1>{}); load_a(kt + 2, SLOT.value, 0); }
+      if constexpr (f == 2) { read_a(SLOT, Const<1>{}); load_b(kt + 2, SLOT.value, 1); }
+      if constexpr (f == 3) { read_b(Const<1 - decltype(SLOT)::value>{}, Const<0>{}); load_a(kt + 2, SLOT.value, 1); }
+      wait_vmcnt<12>();                                      // the unit read next phase has landed; six more stay in flight
+      close_reads();
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+      static_for<16>([&](auto I) {                           // (operands swapped: a lane owns one row of C)
+        constexpr int q = decltype(I)::value;
+        if constexpr (BT) {
+          constexpr int ii = q >> 2, j = q & 3;
+          acc16[4 * h + ii][j] = mfma(fb[c][j], fa[ii][c], acc16[4 * h + ii][j]);
+        } else {
+          constexpr int kk = q >> 3, ii = (q >> 1) & 3, j = q & 1;
+          acc16[4 * h + ii][2 * c + j] = mfma(fb[c][2 * j + kk], fa[ii][kk], acc16[4 * h + ii][2 * c + j]);
+        }
+      });
+      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_barrier();
+    };
+    auto ktile = [&](auto SLOT, int kt) { static_for<4>([&](auto F) { phase(SLOT, F, kt); }); };
+#pragma unroll
+    for (int s = 0; s < 2; ++s) { load_b(s, s, 0); load_a(s, s, 0); load_b(s, s, 1); load_a(s, s, 1); }
+    wait_vmcnt<12>();
+    __builtin_amdgcn_s_barrier();
+    read_b(Const<0>{}, Const<0>{});
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_s_barrier();
+    if (wm == 1) __builtin_amdgcn_s_barrier();               // these four waves run half a phase behind
+    for (int kt = 0; kt < KT; kt += 2) {
+      ktile(Const<0>{}, kt);
+      if (kt + 1 < KT) ktile(Const<1>{}, kt + 1);
+    }
+    if (wm == 0) __builtin_amdgcn_s_barrier();
+    wait_vmcnt<0>();                                         // (zeros beyond K still on their way to LDS)
+  } else {
   OpA oa;
   OpB ob;
   oa.init(wave, lane, m0, p.Md, p.lda);
@@ -216,98 +346,131 @@ __global__ void __launch_bounds__(WM * WN * 64) orth_gemm_kernel(const OrthGemmP
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+  }
   __syncthreads();                                // the stages are dead
 
-  // ---- epilogue: 32 rows x TN columns of a wave at a time through its own fp32 slice of LDS, so that global accesses are whole
-  // 16-byte vectors; the mirror image of a symmetric tile is read from the slice by columns
+  // ---- epilogue: slices of 32 rows x TN columns of a wavefront, one after the other, through its own fp32 piece of LDS, so that
+  // global accesses are whole 16-byte vectors; the mirror image of a symmetric tile is read from there by columns.  The loads of
+  // E for the next slice are in flight while a slice is finished (one work-group to a CU: nobody else would cover them).
   constexpr int SLD = TN + 4, CPR = TN / 8, SIT = 32 * CPR / 64;
   float *stg = reinterpret_cast<float *>(smem_raw) + wave * (32 * SLD);
-  const int lrow = lane & 31, lq = lane >> 5;
-  const bool mirror = p.sym && tm != tn;
-  float lr = p.out.lr;
-  if (!p.C && p.out.scal) lr = p.out.scal[0];
-  const float decay = 1.0f - lr * p.out.wd, gain = lr * p.out.scale;
+  auto slice_row = [&](int i) -> int { return PP ? (i >> 1) * 128 + wm * 64 + (i & 1) * 32 : wm * TM + i * 32; };
+  uint4 eh[2][SIT], el[2][SIT];
+  const bool two = KIND != KIND_SYM || SPLIT;     // E is hi + lo
+  auto load_e = [&](int i, uint4 (&h)[SIT], uint4 (&l)[SIT]) {
 #pragma unroll
-  for (int i = 0; i < MI; ++i) {
+    for (int it = 0; it < SIT; ++it) {
+      const int q = it * 64 + lane, r = q / CPR, cc = (q % CPR) * 8;
+      const int m = m0 + slice_row(i) + r, n = n0 + wn * TN + cc;
+      h[it] = l[it] = make_uint4(0, 0, 0, 0);
+      if (m < p.Md && n < p.Nd) {                 // (Nd is a multiple of 8)
+        const long long at = z * p.sE + (long long)m * p.lde + n;
+        h[it] = *reinterpret_cast<const uint4 *>(p.E + at);
+        if (two) l[it] = *reinterpret_cast<const uint4 *>(p.El + at);
+      }
+    }
+  };
+  const bool has_e = KIND != KIND_SYM || p.E;
+  const bool mirror = KIND == KIND_SYM && tm != tn;
+  float decay = 1.0f, gain = -1.0f;
+  if (KIND == KIND_LAST && p.out.update) {
+    const float lr = p.out.scal ? p.out.scal[0] : p.out.lr;
+    decay = 1.0f - lr * p.out.wd;
+    gain = lr * p.out.scale;
+  }
+  if (has_e) load_e(0, eh[0], el[0]);
+  static_for<MI>([&](auto SLICE) {
+    constexpr int i = decltype(SLICE)::value;
+    if constexpr (PP) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        *reinterpret_cast<float4 *>(stg + lrow * SLD + j * 32 + c * 8 + lq * 4) =
-            make_float4(acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]);
+        for (int c = 0; c < TN / 16; ++c)
+          *reinterpret_cast<f32x4 *>(stg + (h * 16 + (lane & 15)) * SLD + c * 16 + (lane >> 4) * 4) = acc16[2 * i + h][c];
+    } else {
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          *reinterpret_cast<float4 *>(stg + (lane & 31) * SLD + j * 32 + c * 8 + (lane >> 5) * 4) =
+              make_float4(acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]);
+    }
+    if (has_e && i + 1 < MI) load_e(i + 1, eh[(i + 1) & 1], el[(i + 1) & 1]);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int it = 0; it < SIT; ++it) {
       const int q = it * 64 + lane, r = q / CPR, cc = (q % CPR) * 8;
-      const int m = m0 + wm * TM + i * 32 + r, n = n0 + wn * TN + cc;
-      if (m >= p.Md || n >= p.Nd) continue;       // (Nd is a multiple of 8)
+      const int m = m0 + slice_row(i) + r, n = n0 + wn * TN + cc;
+      if (m >= p.Md || n >= p.Nd) continue;
       float v[8];
       {
         const float4 x = *reinterpret_cast<const float4 *>(stg + r * SLD + cc), y = *reinterpret_cast<const float4 *>(stg + r * SLD + cc + 4);
         v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
       }
-      if (p.E) {
-        const long long at = z * p.sE + (long long)m * p.lde + n;
-        float h[8], l[8];
-        load8(p.E, TYPE_F16, at, h);
-        if (p.diag_of == DIAG_ROWS) {
-          const float d = p.diag[(long long)z * p.Md + m];
+      if (has_e) {
+        float h[8];
+        unpack8(eh[i & 1][it], TYPE_F16, h);
+        if (!SPLIT && KIND != KIND_SYM) {         // B's diagonal
+          if (p.diag_of == DIAG_ROWS) {
+            const float d = p.diag[(long long)z * p.Md + m];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = fmaf(d, h[e], v[e]);
-        } else if (p.diag_of == DIAG_COLS) {
-          float d[8];
-          load8(p.diag, TYPE_F32, (long long)z * p.Nd + n, d);
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(d, h[e], v[e]);
+          } else {
+            float d[8];
+            load8(p.diag, TYPE_F32, (long long)z * p.Nd + n, d);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = fmaf(d[e], h[e], v[e]);
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(d[e], h[e], v[e]);
+          }
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= p.beta;
-        if (p.El) {
-          load8(p.El, TYPE_F16, at, l);
+        if (two) {
+          float l[8];
+          unpack8(el[i & 1][it], TYPE_F16, l);
 #pragma unroll
           for (int e = 0; e < 8; ++e) h[e] += l[e];
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fmaf(p.alpha, h[e], v[e]);
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(p.alpha, h[e], p.beta * v[e]);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= p.beta;
       }
-      if (p.diag_of == DIAG_OUT) {
+      if constexpr (KIND != KIND_LAST) {
+        if (KIND == KIND_SYM && p.diag_of == DIAG_OUT) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (n + e == m) { p.diag[(long long)z * p.Md + m] = v[e]; v[e] = 0.0f; }
-      }
-      if (p.C) {
+          for (int e = 0; e < 8; ++e)
+            if (n + e == m) { p.diag[(long long)z * p.Md + m] = v[e]; v[e] = 0.0f; }
+        }
         const long long at = z * p.sC + (long long)m * p.ldc + n;
         uint4 h, l;
         split8(v, h, l);
         *reinterpret_cast<uint4 *>(p.C + at) = h;
-        if (p.Cl) *reinterpret_cast<uint4 *>(p.Cl + at) = l;
+        if (two) *reinterpret_cast<uint4 *>(p.Cl + at) = l;
         if (mirror) {
           *reinterpret_cast<float4 *>(stg + r * SLD + cc) = make_float4(v[0], v[1], v[2], v[3]);
           *reinterpret_cast<float4 *>(stg + r * SLD + cc + 4) = make_float4(v[4], v[5], v[6], v[7]);
         }
-        continue;
-      }
-      if (m >= p.rows) continue;
-      const long long at = z * p.out.so + (long long)m * p.out.ldo + n, sat = z * p.out.sshadow + (long long)m * p.out.ldo + n;
-      if (p.vec) {                                // (cols is a multiple of 8)
-        if (p.out.update) {
-          float x[8];
-          load8(p.out.o, p.out.type, at, x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = fmaf(decay, x[e], -gain * v[e]);
-        }
-        store8(p.out.o, p.out.type, at, v);
-        if (p.out.shadow) store8(p.out.shadow, TYPE_BF16, sat, v);
       } else {
+        if (m >= p.rows) continue;
+        const long long at = z * p.out.so + (long long)m * p.out.ldo + n, sat = z * p.out.sshadow + (long long)m * p.out.ldo + n;
+        if (p.vec) {                              // (cols is a multiple of 8)
+          if (p.out.update) {
+            float x[8];
+            load8(p.out.o, p.out.type, at, x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (n + e >= p.cols) continue;
-          const float x = p.out.update ? fmaf(decay, load_as_f32(p.out.o, p.out.type, at + e), -gain * v[e]) : v[e];
-          store_from_f32(p.out.o, p.out.type, at + e, x);
-          if (p.out.shadow) p.out.shadow[sat + e] = f2bf(x);
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(decay, x[e], -gain * v[e]);
+          }
+          store8(p.out.o, p.out.type, at, v);
+          if (p.out.shadow) store8(p.out.shadow, TYPE_BF16, sat, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) stg[r * SLD + cc + e] = v[e];
+#pragma unroll 1
+          for (int e = 0; e < 8 && n + e < p.cols; ++e) {
+            float x = stg[r * SLD + cc + e];
+            if (p.out.update) x = fmaf(decay, load_as_f32(p.out.o, p.out.type, at + e), -gain * x);
+            store_from_f32(p.out.o, p.out.type, at + e, x);
+            if (p.out.shadow) p.out.shadow[sat + e] = f2bf(x);
+          }
         }
       }
     }
@@ -316,7 +479,7 @@ __global__ void __launch_bounds__(WM * WN * 64) orth_gemm_kernel(const OrthGemmP
 #pragma unroll
       for (int it = 0; it < TN * 4 / 64; ++it) {
         const int q = it * 64 + lane, c = q >> 2, r0 = (q & 3) * 8;
-        const int m = m0 + wm * TM + i * 32 + r0, n = n0 + wn * TN + c;       // C[n][m ..]
+        const int m = m0 + slice_row(i) + r0, n = n0 + wn * TN + c;       // C[n][m ..]
         if (m >= p.Md || n >= p.Nd) continue;
         float v[8];
 #pragma unroll
@@ -325,21 +488,21 @@ __global__ void __launch_bounds__(WM * WN * 64) orth_gemm_kernel(const OrthGemmP
         split8(v, h, l);
         const long long at = z * p.sC + (long long)n * p.ldc + m;
         *reinterpret_cast<uint4 *>(p.C + at) = h;
-        if (p.Cl) *reinterpret_cast<uint4 *>(p.Cl + at) = l;
+        if (SPLIT) *reinterpret_cast<uint4 *>(p.Cl + at) = l;
       }
     }
     __builtin_amdgcn_wave_barrier();
-  }
+  });
 }
 
-template <int BM, int BN, int BK, int WM, int WN, int NS, bool AT, bool BT, bool SPLIT>
+template <int BM, int BN, int BK, int WM, int WN, int NS, bool PP, bool AT, bool BT, bool SPLIT, int KIND>
 hipError_t launch_cfg(const OrthGemmP &p, hipStream_t s) {
   constexpr size_t tiles = (size_t)NS * (BM + BN) * BK * 2, epi = (size_t)WM * WN * 32 * (BN / WN + 4) * 4;
   constexpr size_t lds = tiles > epi ? tiles : epi;
   static_assert(lds <= 160 * 1024, "LDS budget");
-  auto kern = orth_gemm_kernel<BM, BN, BK, WM, WN, NS, AT, BT, SPLIT>;
+  auto kern = orth_gemm_kernel<BM, BN, BK, WM, WN, NS, PP, AT, BT, SPLIT, KIND>;
   const int tm = (p.Md + BM - 1) / BM, tn = (p.Nd + BN - 1) / BN;
-  if (p.sym && (BM != BN || p.Md != p.Nd)) return hipErrorInvalidValue;
+  if ((KIND == KIND_SYM) != (p.sym != 0) || (p.sym && (BM != BN || p.Md != p.Nd))) return hipErrorInvalidValue;
   const long long nblk = (p.sym ? (long long)tn * (tn + 1) / 2 : (long long)tm * tn) * p.batch;
   if (nblk > 0x3fffffff) return hipErrorInvalidValue;
   if (lds > 64 * 1024) {
@@ -353,12 +516,33 @@ hipError_t launch_cfg(const OrthGemmP &p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <bool AT, bool BT>
+long long tile_count(const OrthGemmP &p, int e) {
+  const long long tm = (p.Md + e - 1) / e, tn = (p.Nd + e - 1) / e;
+  return (p.sym ? tn * (tn + 1) / 2 : tm * tn) * p.batch;
+}
+
+// Time of `blocks` 128 x 128 tiles per k-tile: full rounds of two work-groups to a CU and the last one (as in gemm_bf16.hip)
+double rounds_128(long long blocks) {
+  const long long full = blocks / 512, rem = blocks - full * 512;
+  const double last = rem > 256 ? 1.42 : rem == 0 ? 0.0 : full == 0 ? 1.13 : 1.13 + 0.29 * (double)rem / 256;
+  return 1.42 * (double)full + last;
+}
+
+template <bool AT, bool BT, bool SPLIT, int KIND>
+hipError_t launch_shape(const OrthGemmP &p, hipStream_t s) {
+  const long long t256 = tile_count(p, 256), t128 = tile_count(p, 128);
+  if (p.Md > 128 && p.Nd > 128 && p.Kd * (SPLIT ? 3 : 1) >= 512 && 1.5 * (double)((t256 + 255) / 256) <= rounds_128(t128))
+    return launch_cfg<256, 256, 64, 2, 4, 2, true, AT, BT, SPLIT, KIND>(p, s);
+  if (t128 <= 256) return launch_cfg<128, 128, 64, 2, 2, 4, false, AT, BT, SPLIT, KIND>(p, s);
+  return launch_cfg<128, 128, 64, 2, 2, 2, false, AT, BT, SPLIT, KIND>(p, s);
+}
+
+template <bool AT, bool BT, int KIND>
 hipError_t launch_product(const OrthGemmP &p, hipStream_t s) {
   // operand checks the kernel relies on: 16-byte aligned rows of whole chunks, operands below 2 GiB per matrix
   if (((p.lda | p.ldb | p.Md | p.Nd | p.Kd) & 7) || ((p.sA | p.sB) & 7)) return hipErrorInvalidValue;
   if ((long long)(AT ? p.Kd : p.Md) * p.lda * 2 >= (1LL << 31) || (long long)(BT ? p.Kd : p.Nd) * p.ldb * 2 >= (1LL << 31)) return hipErrorInvalidValue;
-  return p.Al ? launch_cfg<128, 128, 64, 2, 2, 2, AT, BT, true>(p, s) : launch_cfg<128, 128, 64, 2, 2, 2, AT, BT, false>(p, s);
+  return p.Al ? launch_shape<AT, BT, true, KIND>(p, s) : launch_shape<AT, BT, false, KIND>(p, s);
 }
 
 // Few rows average little of what 16-bit operands round away (relative error up to 1.6e-2 for 2 x 2, 4.4e-3 for 8 x 8, 3.2e-3 for 17 x 33)
@@ -462,7 +646,7 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
     if (pl.split) p.Al = p.Bl = xl;
     p.C = at(pl.o_a); p.Cl = pl.split ? at(pl.o_al) : nullptr; p.sC = sa; p.ldc = pl.mp;
     p.beta = pl.scale(k).gram;
-    e = pl.wide ? launch_product<false, false>(p, s) : launch_product<true, true>(p, s);
+    e = pl.wide ? launch_product<false, false, KIND_SYM>(p, s) : launch_product<true, true, KIND_SYM>(p, s);
     if (e != hipSuccess) return e;
     // B 2^eb = (b A + c A A) 2^eb
     std::memset(&p, 0, sizeof(p));
@@ -473,7 +657,7 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
     p.alpha = pl.scale(k).poly_a; p.beta = pl.scale(k).poly_aa;
     float *diag = reinterpret_cast<float *>(ws + pl.o_diag);
     if (!pl.split) { p.diag = diag; p.diag_of = DIAG_OUT; }
-    e = launch_product<false, false>(p, s);
+    e = launch_product<false, false, KIND_SYM>(p, s);
     if (e != hipSuccess) return e;
     // X' = a X + B X, or a X + X B
     std::memset(&p, 0, sizeof(p));
@@ -493,11 +677,11 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
     if (pl.wide) {
       p.A = at(pl.o_b); p.sA = sa; p.lda = pl.mp; p.B = x; p.sB = sx; p.ldb = pl.cp;
       if (pl.split) { p.Al = at(pl.o_bl); p.Bl = xl; }
-      e = launch_product<false, true>(p, s);
+      e = last ? launch_product<false, true, KIND_LAST>(p, s) : launch_product<false, true, KIND_APPLY>(p, s);
     } else {
       p.A = x; p.sA = sx; p.lda = pl.cp; p.B = at(pl.o_b); p.sB = sa; p.ldb = pl.mp;
       if (pl.split) { p.Al = xl; p.Bl = at(pl.o_bl); }
-      e = launch_product<false, false>(p, s);
+      e = last ? launch_product<false, false, KIND_LAST>(p, s) : launch_product<false, false, KIND_APPLY>(p, s);
     }
     if (e != hipSuccess) return e;
   }
