@@ -337,7 +337,7 @@ enum { ABS_TYPE_F32 = 0, ABS_TYPE_BF16 = 1, ABS_TYPE_F16 = 2 };
  *                  (Up to 128 rows or columns the products are those of ABS_PREC_F32 all the same.)
  *                  ABS_PREC_F32: as exact as fp32 products, at three times the operations.
  * Asynchronous on the stream; sums are in a fixed order (the same bits every time).  workspace: device, 256-byte aligned,
- * abs_orthogonalize_workspace_bytes, used until the call's work has run.  A matrix of 2^30 values or more: ABS_EUNSUPPORTED.
+ * abs_orthogonalize_workspace_bytes, used until the call's work has run.  A matrix of 2^29 values or more (its sides rounded up to 32): ABS_EUNSUPPORTED.
  */
 abs_status abs_orthogonalize_workspace_bytes(int batch, int rows, int cols, int prec, size_t *bytes /*host*/);
 abs_status abs_orthogonalize(const void *g_dev, int g_type, int64_t ldg, int64_t stride_g, void *o_dev, int o_type, int64_t ldo,

@@ -85,8 +85,8 @@ abs_status check_cfg(const abs_config *c) {
   if (c->opt == ABS_OPT_MUON) {
     if (c->n_layers < 2) return fail(ABS_EINVAL, "ABS_OPT_MUON needs a hidden layer");
     for (int l = 1; l < c->n_layers; ++l)
-      if (((long long)c->dims[l] + 7) * ((long long)c->dims[l - 1] + 7) >= (1LL << 30))
-        return fail(ABS_EUNSUPPORTED, "ABS_OPT_MUON: a weight matrix must hold fewer than 2^30 values");
+      if (((long long)c->dims[l] + 31) * ((long long)c->dims[l - 1] + 31) >= (1LL << 29))
+        return fail(ABS_EUNSUPPORTED, "ABS_OPT_MUON: a weight matrix must hold fewer than 2^29 values");
   }
   return ABS_OK;
 }

@@ -64,6 +64,17 @@ struct Operand {
       }
     }
   }
+  // row-contiguous: chunk ch of a k-row holds the eight values from column col_of(ch) on
+  template <class F>
+  __device__ __forceinline__ void init_cols(int wave, int lane, int cols, int ld, F col_of) {
+    static_assert(TRANS, "columns of a row-contiguous operand");
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int c = (wave * NI + i) * 64 + lane, kq = c / CH, col = col_of((c % CH) ^ (tr_swizzle<KR>(kq) & (CH - 1)));
+      kofs[i] = kq;
+      voff[i] = col < cols ? (uint32_t)(kq * ld + col) * 2u : OOB;
+    }
+  }
   // rows from elsewhere: matrix row r at row_of(r) of the operand (k-contiguous)
   template <class F>
   __device__ __forceinline__ void init_rows(int wave, int lane, int row0, int rows, int ld, F row_of) {

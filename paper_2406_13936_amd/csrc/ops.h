@@ -23,11 +23,11 @@ struct OrthScale { float gram, poly_a, poly_aa, apply_x, apply_bx; };
 struct OrthPlan {
   int batch, rows, cols, steps, split;   // split: operands as sums of two fp16 values (fp32-class products)
   int wide;                              // rows <= cols: the products A = X X^T, else A = X^T X
-  int rp, cp, mp;                        // rows, columns and the smaller side rounded up to 8
+  int rp, cp, mp;                        // rows, columns and the smaller side rounded up to 8 (32 with split)
   int nparts;                            // partial sums of a matrix's norm
   float a[ORTH_MAX_STEPS], b[ORTH_MAX_STEPS], c[ORTH_MAX_STEPS];
   int ex[ORTH_MAX_STEPS + 1], ea[ORTH_MAX_STEPS], eb[ORTH_MAX_STEPS];   // powers of two that X, A and B are stored with
-  size_t o_part, o_x[2], o_xl[2], o_a, o_al, o_b, o_bl, o_diag, total;          // pieces of the workspace
+  size_t o_part, o_x[2], o_xl, o_a, o_b, o_diag, total;          // pieces of the workspace
   OrthScale scale(int k) const;
 };
 

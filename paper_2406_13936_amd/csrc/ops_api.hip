@@ -33,7 +33,7 @@ abs_status hip_status(hipError_t e, const char *what) {
 abs_status check_matrices(int batch, int rows, int cols, int prec) {
   if (batch < 1 || rows < 1 || cols < 1) return set_error(ABS_EINVAL, "batch, rows and cols must be at least 1");
   if (prec != ABS_PREC_F32 && prec != ABS_PREC_BF16) return set_error(ABS_EINVAL, "unknown precision");
-  if (((int64_t)rows + 7) * ((int64_t)cols + 7) >= (1LL << 30)) return set_error(ABS_EUNSUPPORTED, "a matrix must hold fewer than 2^30 values");
+  if (((int64_t)rows + 31) * ((int64_t)cols + 31) >= (1LL << 29)) return set_error(ABS_EUNSUPPORTED, "a matrix must hold fewer than 2^29 values");
   return ABS_OK;
 }
 abs_status check_orth(int batch, int rows, int cols, int steps, const float *coef, float eps, int prec, const void *workspace,

@@ -195,7 +195,7 @@ def _check_orth(got, G, prec, out, tol=None, **k):
 @gpu
 @pytest.mark.parametrize("batch,rows,cols", [(1, 1, 1), (2, 1, 7), (3, 5, 1), (2, 8, 8), (3, 17, 33), (4, 64, 96), (1, 66, 65), (2, 130, 70),
                                              (3, 72, 129), (2, 333, 129), (1, 127, 128), (2, 256, 512), (1, 520, 264), (2, 300, 1100),
-                                             (1, 1030, 515), (1, 640, 640), (17, 40, 24)])
+                                             (1, 1030, 515), (1, 640, 640), (17, 40, 24), (4, 1288, 1032), (2, 600, 2056)])
 @pytest.mark.parametrize("dtype,prec", [("bf16", 1), ("f32", 0), ("f16", None)])
 @pytest.mark.parametrize("kind", ["full", "low"])
 def test_orthogonalize_against_the_definition(batch, rows, cols, dtype, prec, kind):
@@ -229,22 +229,24 @@ def test_orthogonalize_types_of_input_and_result():
 
 
 @gpu
-@pytest.mark.parametrize("rows,cols", [(24, 40), (40, 24), (100, 72), (65, 203)])
+@pytest.mark.parametrize("rows,cols", [(24, 40), (40, 24), (100, 72), (65, 203), (200, 136), (136, 200), (150, 161), (300, 264)])
 def test_orthogonalize_of_strided_and_unaligned_matrices(rows, cols):
     import torch
     A = _A()
     gen = torch.Generator().manual_seed(2)
-    for off, ld in ((0, cols + 8), (3, cols + 5), (1, cols)):
+    for off, ld in ((0, cols + 8), (3, cols + 5), (1, cols), (0, cols)):
         buf = torch.zeros(off + 3 * (rows * ld + 11), dtype=torch.float32, device="cuda")
         g = buf[off:].as_strided((3, rows, cols), (rows * ld + 11, ld, 1))
         g.copy_(_matrix("full", 3, rows, cols, gen))
-        obuf = torch.full((off + 3 * (rows * ld + 11),), 7.0, device="cuda", dtype=torch.bfloat16)
-        o = obuf[off:].as_strided((3, rows, cols), (rows * ld + 11, ld, 1))
-        A.orthogonalize(g, out=o)
-        _check_orth(o, g, 1, "bf16")
-        mask = torch.ones_like(obuf, dtype=torch.bool)
-        mask[off:].as_strided((3, rows, cols), (rows * ld + 11, ld, 1)).fill_(False)
-        assert (obuf[mask] == 7.0).all()                                # nothing outside the matrices is written
+        for dtype, prec in (("bf16", 1), ("f32", 0)):
+            for step in (rows * ld + 11, rows * ld + 16):
+                obuf = torch.full((off + 3 * step,), 7.0, device="cuda", dtype=_dt(dtype))
+                o = obuf[off:].as_strided((3, rows, cols), (step, ld, 1))
+                A.orthogonalize(g, out=o)
+                _check_orth(o, g, prec, dtype)
+                mask = torch.ones_like(obuf, dtype=torch.bool)
+                mask[off:].as_strided((3, rows, cols), (step, ld, 1)).fill_(False)
+                assert (obuf[mask] == 7.0).all()                        # nothing outside the matrices is written
         want = A.orthogonalize(g.contiguous())
         A.orthogonalize(g, out=g)                                       # in place
         assert torch.equal(g, want)
