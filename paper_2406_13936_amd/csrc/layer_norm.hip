@@ -38,11 +38,11 @@ template <int G> __device__ __forceinline__ float lanes_sum(float v) {
 // Sums of N values over the group.  G = 256: through LDS, one barrier a call (`turn` picks one of two buffers, so that the
 // next call's values do not meet this one's readers); every thread of the block takes part.
 template <int G, int N>
-__device__ __forceinline__ void group_sums(float (&v)[N], float (*sm)[N * 4], int turn) {
+__device__ __forceinline__ void group_sums(float (&v)[N], float *sm, int turn) {      // sm: 8 N floats
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = lanes_sum<(G < 64 ? G : 64)>(v[i]);
   if (G <= 64) return;
-  float *s = sm[turn & 1];
+  float *s = sm + (turn & 1) * N * 4;
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) {
 #pragma unroll
@@ -56,50 +56,59 @@ __device__ __forceinline__ void group_sums(float (&v)[N], float (*sm)[N * 4], in
   }
 }
 
-// Columns of lane l in a row: VEC: vectors of eight, (v G + l) 8 + e; else single values, (8 v + e) G + l (rows that do not start
-// on 16 bytes or end inside a vector).
-template <int G, bool VEC> __device__ __forceinline__ int col_of(int v, int e, int l) { return VEC ? (v * G + l) * 8 + e : (v * 8 + e) * G + l; }
+// Columns of lane l in a row.  VEC: 16-byte vectors that lie side by side over the lanes: of 16-bit values (v G + l) 8 + e, of fp32
+// ((2 v + e / 4) G + l) 4 + e % 4.  Else single values, (8 v + e) G + l (rows that do not start on 16 bytes or end inside a vector).
+template <int TYPE, int G, bool VEC> __device__ __forceinline__ int col_of(int v, int e, int l) {
+  if (!VEC) return (8 * v + e) * G + l;
+  return TYPE == TYPE_F32 ? ((2 * v + (e >> 2)) * G + l) * 4 + (e & 3) : (v * G + l) * 8 + e;
+}
+
+// Results are not read again here: non-temporal stores (16-bit rows of 2048: forward 116 -> 101 us for 134 M values, backward 204 -> 194;
+// non-temporal loads cost more than they give where the inputs are still in a cache).
+__device__ __forceinline__ void st_once(void *p, uint4 v) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4 w = {v.x, v.y, v.z, v.w};
+  __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
+}
 
 // What a lane holds of a row as it comes from memory
 template <int TYPE, int V> struct Raw { uint4 q[V * (TYPE == TYPE_F32 ? 2 : 1)]; };
 
+// (Every lane loads, from the row's first column where it has none, and zeros take the place of what it got: loads behind branches
+// wait for each other.)
 template <int TYPE, int G, int V, bool VEC>
 __device__ __forceinline__ void load_raw(Raw<TYPE, V> &r, const void *p, long long at, int D, int l) {
+  constexpr int PER = TYPE == TYPE_F32 ? 2 : 1, N = 8 / PER;        // vectors of a lane's eight, values of a vector
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    if constexpr (TYPE == TYPE_F32) {
-      const float *f = static_cast<const float *>(p) + at;
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int h = 0; h < PER; ++h) {
+      uint4 &q = r.q[v * PER + h];
       if constexpr (VEC) {
-        const int c = col_of<G, true>(v, 0, l);
+        const int c = col_of<TYPE, G, true>(v, N * h, l);
         const bool in = c < D;
-        r.q[2 * v] = in ? *reinterpret_cast<const uint4 *>(f + c) : make_uint4(0, 0, 0, 0);
-        r.q[2 * v + 1] = in ? *reinterpret_cast<const uint4 *>(f + c + 4) : make_uint4(0, 0, 0, 0);
+        q = *reinterpret_cast<const uint4 *>(static_cast<const unsigned char *>(p) + (at + (in ? c : 0)) * (16 / N));
+        q = make_uint4(in ? q.x : 0u, in ? q.y : 0u, in ? q.z : 0u, in ? q.w : 0u);
       } else {
-        uint32_t w[8];
+        uint32_t w[N];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = col_of<G, false>(v, e, l);
-          w[e] = c < D ? __float_as_uint(f[c]) : 0u;
+        for (int e = 0; e < N; ++e) {
+          const int c = col_of<TYPE, G, false>(v, N * h + e, l);
+          const bool in = c < D;
+          const long long i = at + (in ? c : 0);
+          const uint32_t got = TYPE == TYPE_F32 ? static_cast<const uint32_t *>(p)[i] : (uint32_t)static_cast<const uint16_t *>(p)[i];
+          w[e] = in ? got : 0u;
         }
-        r.q[2 * v] = make_uint4(w[0], w[1], w[2], w[3]);
-        r.q[2 * v + 1] = make_uint4(w[4], w[5], w[6], w[7]);
-      }
-    } else {
-      const uint16_t *h = static_cast<const uint16_t *>(p) + at;
-      if constexpr (VEC) {
-        const int c = col_of<G, true>(v, 0, l);
-        r.q[v] = c < D ? *reinterpret_cast<const uint4 *>(h + c) : make_uint4(0, 0, 0, 0);
-      } else {
-        uint32_t w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = col_of<G, false>(v, e, l);
-          w[e] = c < D ? h[c] : 0u;
-        }
-        r.q[v] = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4] | (w[5] << 16), w[6] | (w[7] << 16));
+        if constexpr (TYPE == TYPE_F32) q = make_uint4(w[0], w[1], w[2], w[3]);
+        else q = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4 % N] | (w[5 % N] << 16), w[6 % N] | (w[7 % N] << 16));
       }
     }
-  }
+}
+
+// From here on the values count as unknown, so that what was computed from them is computed again and not kept in registers.
+template <int TYPE, int V> __device__ __forceinline__ void forget(Raw<TYPE, V> &r) {
+#pragma unroll
+  for (auto &q : r.q) asm volatile("" : "+v"(q.x), "+v"(q.y), "+v"(q.z), "+v"(q.w));
 }
 template <int TYPE, int V> __device__ __forceinline__ void raw_vals(const Raw<TYPE, V> &r, int v, float (&f)[8]) {
   if constexpr (TYPE == TYPE_F32) {
@@ -113,25 +122,66 @@ template <int TYPE, int V> __device__ __forceinline__ void raw_vals(const Raw<TY
 template <int TYPE, int G, bool VEC>
 __device__ __forceinline__ void store_vals(void *p, long long at, int D, int l, int v, const float (&f)[8]) {
   if constexpr (VEC) {
-    const int c = col_of<G, true>(v, 0, l);
-    if (c < D) store8(p, TYPE, at + c, f);
+    if constexpr (TYPE == TYPE_F32) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int c = col_of<TYPE, G, true>(v, 4 * h, l);
+        if (c < D) st_once(static_cast<float *>(p) + at + c, make_uint4(__float_as_uint(f[4 * h]), __float_as_uint(f[4 * h + 1]), __float_as_uint(f[4 * h + 2]), __float_as_uint(f[4 * h + 3])));
+      }
+    } else {
+      const int c = col_of<TYPE, G, true>(v, 0, l);
+      if (c < D) st_once(static_cast<uint16_t *>(p) + at + c, pack8(TYPE, f));
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int c = col_of<G, false>(v, e, l);
+      const int c = col_of<TYPE, G, false>(v, e, l);
       if (c < D) store_from_f32(p, TYPE, at + c, f[e]);
     }
   }
 }
-template <int G, int V, bool VEC>
-__device__ __forceinline__ void load_param(float (&f)[V][8], const void *p, int type, long long at, int D, int l, float none) {
+// Gains, biases or batch gradients (fp32, or with PARAM == TYPE the rows' type) of a lane's columns; null: zeros
+template <int TYPE, int PARAM, int G, int V, bool VEC>
+__device__ __forceinline__ void load_param_as(float (&f)[V][8], const void *p, long long at, int D, int l) {
+  const bool whole = VEC && !((reinterpret_cast<uintptr_t>(p) + at * (PARAM == TYPE_F32 ? 4 : 2)) & 15);
+  if (whole && PARAM == TYPE) {
+    Raw<TYPE, V> r;
+    load_raw<TYPE, G, V, true>(r, p, at, D, l);
 #pragma unroll
-  for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v) raw_vals<TYPE, V>(r, v, f[v]);
+  } else if (whole) {                             // fp32 beside 16-bit rows: two vectors to one of theirs
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = col_of<G, VEC>(v, e, l);
-      f[v][e] = p && c < D ? load_as_f32(p, type, at + c) : none;
+    for (int v = 0; v < V; ++v) {
+      const int c = col_of<TYPE, G, VEC>(v, 0, l);
+      const bool in = c < D;
+      load8(p, TYPE_F32, at + (in ? c : 0), f[v]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[v][e] = in ? f[v][e] : 0.0f;
     }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = col_of<TYPE, G, VEC>(v, e, l);
+        const bool in = c < D;
+        const float got = load_as_f32(p, PARAM, at + (in ? c : 0));
+        f[v][e] = in ? got : 0.0f;
+      }
+  }
+}
+template <int TYPE, int G, int V, bool VEC>
+__device__ __forceinline__ void load_param(float (&f)[V][8], const void *p, int type, long long at, int D, int l) {
+  if (!p) {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[v][e] = 0.0f;
+  } else if (type == TYPE_F32) {
+    load_param_as<TYPE, TYPE_F32, G, V, VEC>(f, p, at, D, l);
+  } else {
+    load_param_as<TYPE, TYPE, G, V, VEC>(f, p, at, D, l);
+  }
 }
 
 // ---- forward -------------------------------------------------------------------------------------------------------
@@ -140,18 +190,22 @@ __device__ __forceinline__ void load_param(float (&f)[V][8], const void *p, int 
 template <int TYPE, int G, int V, bool VEC>
 __global__ void __launch_bounds__(256) ln_forward_kernel(const LayerNormP p, const int nb) {
   constexpr int GP = 256 / G;
-  __shared__ __attribute__((aligned(16))) float sm[2][4];
+  __shared__ __attribute__((aligned(16))) float sm[8];
   const int m = blockIdx.x / nb, j = blockIdx.x - m * nb, gid = threadIdx.x / G, l = threadIdx.x % G;
   const long long rows = (long long)p.b * p.T;
   const int D = p.D;
   const float n = (float)D;                       // (divided by, not multiplied with its inverse: rows of one value have variance 0)
-  float ga[V][8], be[V][8];
-  load_param<G, V, VEC>(ga, p.gamma, p.ptype, (long long)m * D, D, l, 0.0f);
-  load_param<G, V, VEC>(be, p.beta, p.ptype, (long long)m * D, D, l, 0.0f);
   int turn = 0;
-  for (long long r = (long long)j * GP + gid; r < rows; r += (long long)nb * GP) {
-    Raw<TYPE, V> raw;
-    load_raw<TYPE, G, V, VEC>(raw, p.x, m * p.sx + r * p.ldx, D, l);
+  const long long step = (long long)nb * GP;
+  long long r = (long long)j * GP + gid;
+  Raw<TYPE, V> next;                              // (the next row is on its way while a row is worked on)
+  if (r < rows) load_raw<TYPE, G, V, VEC>(next, p.x, m * p.sx + r * p.ldx, D, l);
+  float ga[V][8], be[V][8];
+  load_param<TYPE, G, V, VEC>(ga, p.gamma, p.ptype, (long long)m * D, D, l);
+  load_param<TYPE, G, V, VEC>(be, p.beta, p.ptype, (long long)m * D, D, l);
+  for (; r < rows; r += step) {
+    const Raw<TYPE, V> raw = next;
+    if (r + step < rows) load_raw<TYPE, G, V, VEC>(next, p.x, m * p.sx + (r + step) * p.ldx, D, l);
     float x[V][8], s[1] = {0.0f};
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -166,7 +220,7 @@ __global__ void __launch_bounds__(256) ln_forward_kernel(const LayerNormP p, con
     for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float d = col_of<G, VEC>(v, e, l) < D ? x[v][e] - mean : 0.0f;
+        const float d = col_of<TYPE, G, VEC>(v, e, l) < D ? x[v][e] - mean : 0.0f;
         x[v][e] = d;
         s[0] = fmaf(d, d, s[0]);
       }
@@ -187,7 +241,7 @@ __global__ void __launch_bounds__(256) ln_forward_kernel(const LayerNormP p, con
 
 // Rows longer than the registers of a block hold: three passes over the row, the later two out of the caches
 __global__ void __launch_bounds__(256) ln_forward_long_kernel(const LayerNormP p) {
-  __shared__ __attribute__((aligned(16))) float sm[2][4];
+  __shared__ __attribute__((aligned(16))) float sm[8];
   const long long rows = (long long)p.b * p.T, m = blockIdx.x / rows, r = blockIdx.x - m * rows;
   const long long xa = m * p.sx + r * p.ldx, ya = m * p.sy + r * p.ldy, pa = m * p.D;
   const float n = (float)p.D;
@@ -227,11 +281,11 @@ struct LnSplit {
 };
 
 template <int TYPE, int G, int V, bool VEC, int R, int STAT, bool LONG>
-__global__ void __launch_bounds__(256) ln_backward_kernel(const LayerNormP p, const LnSplit w) {
+__global__ void __launch_bounds__(256, V == 1 && TYPE != TYPE_F32 && STAT != STAT_SAMPLE ? 4 : 1) ln_backward_kernel(const LayerNormP p, const LnSplit w) {
   constexpr int GP = 256 / G;
   constexpr int NS = STAT == STAT_NONE ? 2 : 3;
   static_assert(!LONG || G == 256, "a tile of a long row is a block's");
-  __shared__ __attribute__((aligned(16))) float sm[2][R * NS * 4];
+  __shared__ __attribute__((aligned(16))) float sm[2 * R * NS * 4];
   __shared__ float comb[GP > 1 ? GP * G * V * 8 : 1];
   const int bid = LONG ? blockIdx.x / w.tiles : blockIdx.x, tile = LONG ? blockIdx.x - bid * w.tiles : 0;
   const int m = bid / w.nb, j = bid - m * w.nb, gid = threadIdx.x / G, l = threadIdx.x % G;
@@ -254,7 +308,7 @@ __global__ void __launch_bounds__(256) ln_backward_kernel(const LayerNormP p, co
     hop = 0;                                      // rows of a sample, then the sample GP further on
   }
   float ga[V][8], tw[V][8], tb[V][8], gw[STAT == STAT_SAMPLE ? V : 1][8], gb[STAT == STAT_SAMPLE ? V : 1][8];
-  load_param<G, V, VEC>(ga, p.gamma, p.ptype, (long long)m * p.D + c0, D, l, 0.0f);
+  load_param<TYPE, G, V, VEC>(ga, p.gamma, p.ptype, (long long)m * p.D + c0, D, l);
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -265,6 +319,8 @@ __global__ void __launch_bounds__(256) ln_backward_kernel(const LayerNormP p, co
   const bool bias = p.dbeta != nullptr;
   int turn = 0, t = 0;
   long long row = first;
+  // R rows at a time: their loads are under way together (of the first row again where there are fewer), and one exchange adds up what
+  // all of them need
   for (long long q = 0; q < count; q += R, ++turn) {
     Raw<TYPE, V> rx[R], ry[R];
     float mean[R], rstd[R], s[R * NS];
@@ -273,23 +329,21 @@ __global__ void __launch_bounds__(256) ln_backward_kernel(const LayerNormP p, co
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const bool in = q + k < count;
+      const long long from = in ? row : first;
+      load_raw<TYPE, G, V, VEC>(rx[k], p.x, m * p.sx + from * p.ldx + c0, D, l);
+      load_raw<TYPE, G, V, VEC>(ry[k], p.dy, m * p.sy + from * p.ldy + c0, D, l);
+      mean[k] = p.mean[m * rows + from];
+      rstd[k] = p.rstd[m * rows + from];
       at[k] = in ? row : -1;
-      ends[k] = false;
-      if (in) {
-        load_raw<TYPE, G, V, VEC>(rx[k], p.x, m * p.sx + row * p.ldx + c0, D, l);
-        load_raw<TYPE, G, V, VEC>(ry[k], p.dy, m * p.sy + row * p.ldy + c0, D, l);
-        mean[k] = p.mean[m * rows + row];
-        rstd[k] = p.rstd[m * rows + row];
-        ends[k] = t == T - 1;
-        if (hop) row += hop;
-        else if (ends[k]) { t = 0; row += (long long)(GP - 1) * T + 1; }
-        else { ++t; ++row; }
-      }
+      ends[k] = in && t == T - 1;
+      if (hop) row += hop;
+      else if (ends[k]) { t = 0; row += (long long)(GP - 1) * T + 1; }
+      else { ++t; ++row; }
     }
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       float s1 = 0.0f, s2 = 0.0f, sn = 0.0f;
-      if (at[k] >= 0) {
+      if (at[k] >= 0) {                           // (a branch, so that rows are worked on one after the other: all at once take twice the registers)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           float x[8], dy[8];
@@ -329,6 +383,7 @@ __global__ void __launch_bounds__(256) ln_backward_kernel(const LayerNormP p, co
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       if (at[k] < 0) continue;
+      if (V <= 2) { forget(rx[k]); forget(ry[k]); }      // (two work-groups to a CU and more: 205 -> 190 us; rows of 8192 have one either way, 120 -> 171)
       float a = s[k * NS] * inv, c = s[k * NS + 1] * inv;
       if (LONG) { a = w.sums[(m * rows + at[k]) * 2]; c = w.sums[(m * rows + at[k]) * 2 + 1]; }
       if (STAT != STAT_NONE && ends[k] && l == 0) {
@@ -359,7 +414,7 @@ __global__ void __launch_bounds__(256) ln_backward_kernel(const LayerNormP p, co
       for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int c = col_of<G, VEC>(v, e, l);
+          const int c = col_of<TYPE, G, VEC>(v, e, l);
           if (c < D) out[(long long)h * p.D + c] = h ? tb[v][e] : tw[v][e];
         }
     } else {
@@ -367,7 +422,7 @@ __global__ void __launch_bounds__(256) ln_backward_kernel(const LayerNormP p, co
 #pragma unroll
       for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) comb[gid * G * V * 8 + col_of<G, VEC>(v, e, l)] = h ? tb[v][e] : tw[v][e];
+        for (int e = 0; e < 8; ++e) comb[gid * G * V * 8 + col_of<TYPE, G, VEC>(v, e, l)] = h ? tb[v][e] : tw[v][e];
       __syncthreads();
       for (int c = threadIdx.x; c < D; c += 256) {
         float a = 0.0f;
@@ -381,7 +436,7 @@ __global__ void __launch_bounds__(256) ln_backward_kernel(const LayerNormP p, co
 
 // mean_d h and mean_d(h xh) of long rows
 __global__ void __launch_bounds__(256) ln_row_sums_kernel(const LayerNormP p, float *sums) {
-  __shared__ __attribute__((aligned(16))) float sm[2][8];
+  __shared__ __attribute__((aligned(16))) float sm[16];
   const long long rows = (long long)p.b * p.T, m = blockIdx.x / rows, r = blockIdx.x - m * rows;
   const float mean = p.mean[m * rows + r], rstd = p.rstd[m * rows + r], inv = 1.0f / (float)p.D;
   float s[2] = {0.0f, 0.0f};
@@ -450,23 +505,56 @@ __global__ void __launch_bounds__(256) ln_inner_partials_kernel(const LayerNormP
   if (threadIdx.x == 0) p.q[i] = (float)a;
 }
 
-// q_i from a second look at the rows: sum_t sum_d dy (xh gbar_gamma + gbar_beta).  A group of G lanes per sample.
-template <int G> __global__ void __launch_bounds__(256) ln_inner_rows_kernel(const LayerNormP p) {
+// q_i from a second look at the rows: sum_t sum_d dy (xh gbar_gamma + gbar_beta).  gbar stays in a group's registers, which takes
+// every (nb 256 / G)-th sample of a replica.
+template <int TYPE, int G, int V, bool VEC>
+__global__ void __launch_bounds__(256) ln_inner_rows_kernel(const LayerNormP p, const int nb) {
   constexpr int GP = 256 / G;
-  const long long i = (long long)blockIdx.x * GP + threadIdx.x / G, rows = (long long)p.b * p.T;
+  __shared__ __attribute__((aligned(16))) float sm[8];
+  const int m = blockIdx.x / nb, j = blockIdx.x - m * nb, gid = threadIdx.x / G, l = threadIdx.x % G, D = p.D;
+  const long long rows = (long long)p.b * p.T;
+  float gw[V][8], gb[V][8];
+  load_param<TYPE, G, V, VEC>(gw, p.dgamma, TYPE_F32, (long long)m * D, D, l);
+  load_param<TYPE, G, V, VEC>(gb, p.dbeta, TYPE_F32, (long long)m * D, D, l);
+  int turn = 0;
+  for (int i = j * GP + gid; i < p.b; i += nb * GP) {
+    float s[1] = {0.0f};
+    for (int t = 0; t < p.T; ++t) {
+      const long long r = (long long)i * p.T + t;
+      Raw<TYPE, V> rx, ry;
+      load_raw<TYPE, G, V, VEC>(rx, p.x, m * p.sx + r * p.ldx, D, l);
+      load_raw<TYPE, G, V, VEC>(ry, p.dy, m * p.sy + r * p.ldy, D, l);
+      const float mean = p.mean[m * rows + r], rstd = p.rstd[m * rows + r];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float x[8], dy[8];
+        raw_vals<TYPE, V>(rx, v, x);
+        raw_vals<TYPE, V>(ry, v, dy);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[0] = fmaf(dy[e], fmaf((x[e] - mean) * rstd, gw[v][e], gb[v][e]), s[0]);
+      }
+    }
+    group_sums<G, 1>(s, sm, turn++);
+    if (l == 0) p.q[(long long)m * p.b + i] = s[0];
+  }
+}
+
+// The same of long rows, a wavefront to a sample
+__global__ void __launch_bounds__(256) ln_inner_long_kernel(const LayerNormP p) {
+  const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long long)p.b * p.T;
   if (i >= (long long)p.M * p.b) return;
-  const int l = threadIdx.x % G;
+  const int l = threadIdx.x & 63;
   const long long m = i / p.b, r0 = (i - m * p.b) * p.T;
   float a = 0.0f;
   for (int t = 0; t < p.T; ++t) {
     const long long r = r0 + t, xa = m * p.sx + r * p.ldx, ya = m * p.sy + r * p.ldy;
     const float mean = p.mean[m * rows + r], rstd = p.rstd[m * rows + r];
-    for (int c = l; c < p.D; c += G) {
+    for (int c = l; c < p.D; c += 64) {
       const float xh = (load_as_f32(p.x, p.type, xa + c) - mean) * rstd;
       a = fmaf(load_as_f32(p.dy, p.type, ya + c), fmaf(xh, p.dgamma[m * p.D + c], p.dbeta ? p.dbeta[m * p.D + c] : 0.0f), a);
     }
   }
-  a = lanes_sum<G>(a);
+  a = lanes_sum<64>(a);
   if (l == 0) p.q[i] = a;
 }
 
@@ -475,20 +563,24 @@ template <int G> __global__ void __launch_bounds__(256) ln_inner_rows_kernel(con
 constexpr int LN_MAX_D = 8192;           // longest row that a block's registers hold
 constexpr int LN_BLOCKS = 1024;          // blocks of 256 threads that fill the chip
 
-// lanes and vectors to a row: 16 x 1, 64 x 1, 256 x 1, 2, 4
-int ln_shape(int D) { return D <= 128 ? 0 : D <= 512 ? 1 : D <= 2048 ? 2 : D <= 4096 ? 3 : 4; }
-int ln_groups(int D) { return D <= 128 ? 16 : D <= 512 ? 4 : 1; }       // to a block
+// lanes and vectors to a row: 16 x 1, 64 x 1, 64 x 2, 256 x 1, 256 x 2, 256 x 4
+int ln_shape(int D) { return D <= 128 ? 0 : D <= 512 ? 1 : D <= 1024 ? 2 : D <= 2048 ? 3 : D <= 4096 ? 4 : 5; }
+int ln_groups(int D) { return D <= 128 ? 16 : D <= 1024 ? 4 : 1; }      // to a block
+
+// Blocks of the backward pass that are on the chip together
+int ln_backward_blocks(const LayerNormP &p) { return p.type != TYPE_F32 && (p.D <= 512 || (p.D > 1024 && p.D <= 2048)) ? LN_BLOCKS : LN_BLOCKS / 2; }
 
 LnSplit ln_split(const LayerNormP &p, bool want) {
   LnSplit w;
   std::memset(&w, 0, sizeof(w));
   const long long rows = (long long)p.b * p.T;
   w.tiles = p.D > LN_MAX_D ? (p.D + 2047) / 2048 : 1;
-  const long long most = std::max(1, LN_BLOCKS / std::min(LN_BLOCKS, p.M * w.tiles));
-  const long long few = 16LL * ln_groups(p.D);                          // rows that pay for a partial
+  const int fill = ln_backward_blocks(p);
+  const long long most = std::max(1, fill / std::min(fill, p.M * w.tiles));
+  const long long few = (p.D <= 512 || p.D > 1024 ? 4LL : 2LL) * ln_groups(p.D);       // rows of a block at least: one round of its groups' loads
   w.samples = want ? p.b : (int)rows; w.T = want ? p.T : 1; w.chunks = 1;
-  if (want && w.T >= 2 * few && p.b * 2LL <= most) {                    // few long samples: several blocks to each
-    w.chunks = (int)std::max(1LL, std::min((w.T + few - 1) / few, most / p.b));
+  if (want && w.T >= 8 * few && p.b * 2LL <= most) {                    // few long samples: several blocks to each
+    w.chunks = (int)std::max(1LL, std::min((w.T + 4 * few - 1) / (4 * few), most / p.b));
     w.per = (w.T + w.chunks - 1) / w.chunks;
     w.chunks = (w.T + w.per - 1) / w.per;
     if (w.chunks > 1) { w.nb = w.samples * w.chunks; return w; }
@@ -528,26 +620,46 @@ hipError_t backward_shape(const LayerNormP &p, const LnSplit &w, bool want_n, hi
   switch (ln_shape(p.D)) {
     case 0: return backward_stat<TYPE, 16, 1, VEC, 4, false>(p, w, want_n, s);
     case 1: return backward_stat<TYPE, 64, 1, VEC, 4, false>(p, w, want_n, s);
-    case 2: return backward_stat<TYPE, 256, 1, VEC, 4, false>(p, w, want_n, s);
-    case 3: return backward_stat<TYPE, 256, 2, VEC, 2, false>(p, w, want_n, s);
+    case 2: return backward_stat<TYPE, 64, 2, VEC, 2, false>(p, w, want_n, s);
+    case 3: return backward_stat<TYPE, 256, 1, VEC, 4, false>(p, w, want_n, s);
+    case 4: return backward_stat<TYPE, 256, 2, VEC, 2, false>(p, w, want_n, s);
     default: return backward_stat<TYPE, 256, 4, VEC, 1, false>(p, w, want_n, s);
   }
 }
 
-template <int TYPE, int G, int V, bool VEC> hipError_t forward_cfg(const LayerNormP &p, hipStream_t s) {
-  const long long rows = (long long)p.b * p.T, gp = 256 / G;
-  const long long nb = std::max(1LL, std::min((rows + gp - 1) / gp, (2LL * LN_BLOCKS + p.M - 1) / p.M));
-  hipLaunchKernelGGL((ln_forward_kernel<TYPE, G, V, VEC>), dim3((unsigned)(nb * p.M)), dim3(256), 0, s, p, (int)nb);
-  return hipGetLastError();
+// Blocks per replica of the kernels whose groups take one row or sample after the other
+int ln_row_blocks(const LayerNormP &p, long long items, int groups) {
+  return (int)std::max(1LL, std::min((items + groups - 1) / groups, (2LL * LN_BLOCKS + p.M - 1) / p.M));
 }
-template <int TYPE, bool VEC> hipError_t forward_shape(const LayerNormP &p, hipStream_t s) {
-  switch (ln_shape(p.D)) {
-    case 0: return forward_cfg<TYPE, 16, 1, VEC>(p, s);
-    case 1: return forward_cfg<TYPE, 64, 1, VEC>(p, s);
-    case 2: return forward_cfg<TYPE, 256, 1, VEC>(p, s);
-    case 3: return forward_cfg<TYPE, 256, 2, VEC>(p, s);
-    default: return forward_cfg<TYPE, 256, 4, VEC>(p, s);
+struct Forward {
+  template <int TYPE, int G, int V, bool VEC> static void go(const LayerNormP &p, hipStream_t s) {
+    const int nb = ln_row_blocks(p, (long long)p.b * p.T, 256 / G);
+    hipLaunchKernelGGL((ln_forward_kernel<TYPE, G, V, VEC>), dim3((unsigned)((long long)nb * p.M)), dim3(256), 0, s, p, nb);
   }
+};
+struct Inner {
+  template <int TYPE, int G, int V, bool VEC> static void go(const LayerNormP &p, hipStream_t s) {
+    const int nb = ln_row_blocks(p, p.b, 256 / G);
+    hipLaunchKernelGGL((ln_inner_rows_kernel<TYPE, G, V, VEC>), dim3((unsigned)((long long)nb * p.M)), dim3(256), 0, s, p, nb);
+  }
+};
+template <class K, int TYPE, bool VEC> void by_shape(const LayerNormP &p, hipStream_t s) {
+  switch (ln_shape(p.D)) {
+    case 0: return K::template go<TYPE, 16, 1, VEC>(p, s);
+    case 1: return K::template go<TYPE, 64, 1, VEC>(p, s);
+    case 2: return K::template go<TYPE, 64, 2, VEC>(p, s);
+    case 3: return K::template go<TYPE, 256, 1, VEC>(p, s);
+    case 4: return K::template go<TYPE, 256, 2, VEC>(p, s);
+    default: return K::template go<TYPE, 256, 4, VEC>(p, s);
+  }
+}
+template <class K> hipError_t by_type(const LayerNormP &p, bool vec, hipStream_t s) {
+  switch (p.type) {
+    case TYPE_F32: vec ? by_shape<K, TYPE_F32, true>(p, s) : by_shape<K, TYPE_F32, false>(p, s); break;
+    case TYPE_BF16: vec ? by_shape<K, TYPE_BF16, true>(p, s) : by_shape<K, TYPE_BF16, false>(p, s); break;
+    default: vec ? by_shape<K, TYPE_F16, true>(p, s) : by_shape<K, TYPE_F16, false>(p, s);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -564,12 +676,7 @@ hipError_t launch_layer_norm(const LayerNormP &p, hipStream_t s) {
     hipLaunchKernelGGL(ln_forward_long_kernel, dim3((unsigned)(rows * p.M)), dim3(256), 0, s, p);
     return hipGetLastError();
   }
-  const bool vec = rows_of_vectors(p.x, p.type, p.sx, p.ldx, p.D) && rows_of_vectors(p.y, p.type, p.sy, p.ldy, p.D);
-  switch (p.type) {
-    case TYPE_F32: return vec ? forward_shape<TYPE_F32, true>(p, s) : forward_shape<TYPE_F32, false>(p, s);
-    case TYPE_BF16: return vec ? forward_shape<TYPE_BF16, true>(p, s) : forward_shape<TYPE_BF16, false>(p, s);
-    default: return vec ? forward_shape<TYPE_F16, true>(p, s) : forward_shape<TYPE_F16, false>(p, s);
-  }
+  return by_type<Forward>(p, rows_of_vectors(p.x, p.type, p.sx, p.ldx, p.D) && rows_of_vectors(p.y, p.type, p.sy, p.ldy, p.D), s);
 }
 
 hipError_t launch_layer_norm_backward(const LayerNormP &p, void *workspace, hipStream_t s) {
@@ -609,8 +716,8 @@ hipError_t launch_layer_norm_backward(const LayerNormP &p, void *workspace, hipS
   hipLaunchKernelGGL(ln_finish_kernel, dim3((unsigned)(colblocks * p.M + nblocks)), dim3(256), 0, s, p, w, count, w.chunks, colblocks, nshares);
   if (p.q) {
     if (w.chunks > 1) hipLaunchKernelGGL(ln_inner_partials_kernel, dim3((unsigned)((long long)p.M * p.b)), dim3(256), 0, s, p, w);
-    else if (p.D <= 128) hipLaunchKernelGGL(ln_inner_rows_kernel<16>, dim3((unsigned)(((long long)p.M * p.b + 15) / 16)), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL(ln_inner_rows_kernel<64>, dim3((unsigned)(((long long)p.M * p.b + 3) / 4)), dim3(256), 0, s, p);
+    else if (p.D > LN_MAX_D) hipLaunchKernelGGL(ln_inner_long_kernel, dim3((unsigned)(((long long)p.M * p.b + 3) / 4)), dim3(256), 0, s, p);
+    else return by_type<Inner>(p, vec, s);
   }
   return hipGetLastError();
 }

@@ -653,8 +653,8 @@ const char *orth_plan(int batch, int rows, int cols, int split, int steps, const
     pl.ex[k + 1] = exponent_for(s);
   }
   if (orth_small_fits(rows, cols)) { pl.total = 256; return nullptr; }     // (all of it is in LDS)
-  // about 16 chunks of 8 values to a thread of the norm's pass, as long as a matrix has them
-  pl.nparts = (int)std::min<long long>(ORTH_PARTS, ((long long)rows * cols + 256 * 128 - 1) / (256 * 128));
+  // two chunks of 8 values to a thread of the norm's pass, until there are as many blocks as one block of the next pass adds up
+  pl.nparts = (int)std::min<long long>(ORTH_PARTS, ((long long)rows * cols + 4095) / 4096);
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t r = o; o = (o + bytes + 255) / 256 * 256; return r; };
   const size_t xb = (size_t)batch * pl.rp * pl.cp * (pl.split ? 4 : 2), ab = (size_t)batch * pl.mp * pl.mp * (pl.split ? 4 : 2);
