@@ -464,11 +464,12 @@ __global__ void __launch_bounds__(256) ln_sample_kernel(const LayerNormP p, cons
 }
 
 // gbar = (1 / b) sum of the partials j step, j < count, in order; further blocks add n_i's shares.
-__global__ void __launch_bounds__(256) ln_finish_kernel(const LayerNormP p, const LnSplit w, const int count, const int step, const int colblocks, const int nshares) {
-  __shared__ float sm[4][64];
+constexpr int FIN = 8;                   // wavefronts of a block, each with a part of the partials
+__global__ void __launch_bounds__(FIN * 64) ln_finish_kernel(const LayerNormP p, const LnSplit w, const int count, const int step, const int colblocks, const int nshares) {
+  __shared__ float sm[FIN][64];
   const int nfin = colblocks * p.M;
   if ((int)blockIdx.x >= nfin) {
-    const long long i = (blockIdx.x - nfin) * 256LL + threadIdx.x, n = (long long)p.M * p.b;
+    const long long i = (blockIdx.x - nfin) * (FIN * 64LL) + threadIdx.x, n = (long long)p.M * p.b;
     if (i >= n) return;
     float a = 0.0f;
     for (int k = 0; k < nshares; ++k) a += w.npart[k * n + i];
@@ -476,16 +477,21 @@ __global__ void __launch_bounds__(256) ln_finish_kernel(const LayerNormP p, cons
     return;
   }
   const int m = blockIdx.x / colblocks, c = (blockIdx.x - m * colblocks) * 64 + (threadIdx.x & 63), q = threadIdx.x >> 6;
-  const int per = (count + 3) / 4, j1 = min(count, (q + 1) * per);
+  const int per = (count + FIN - 1) / FIN, j1 = min(count, (q + 1) * per);
   const float *part = w.part + (long long)m * w.nb * 2 * p.D + c;
   float a = 0.0f;
-  if (c < 2 * p.D)
+  if (c < 2 * p.D) {
+#pragma unroll 8
     for (int j = q * per; j < j1; ++j) a += part[(long long)j * step * 2 * p.D];
+  }
   sm[q][threadIdx.x & 63] = a;
   __syncthreads();
   if (q == 0 && c < 2 * p.D) {
     const int k = threadIdx.x & 63;
-    const float g = ((sm[0][k] + sm[1][k]) + (sm[2][k] + sm[3][k])) * (1.0f / (float)p.b);
+    float g = 0.0f;
+#pragma unroll
+    for (int f = 0; f < FIN; ++f) g += sm[f][k];
+    g *= 1.0f / (float)p.b;
     if (c < p.D) p.dgamma[(long long)m * p.D + c] = g;
     else if (p.dbeta) p.dbeta[(long long)m * p.D + c - p.D] = g;
   }
@@ -561,22 +567,21 @@ __global__ void __launch_bounds__(256) ln_inner_long_kernel(const LayerNormP p) 
 // ---- choices -------------------------------------------------------------------------------------------------------
 
 constexpr int LN_MAX_D = 8192;           // longest row that a block's registers hold
-constexpr int LN_BLOCKS = 1024;          // blocks of 256 threads that fill the chip
+// Blocks of 256 threads of the backward pass: two to a CU.  Their loads keep memory as busy as those of more blocks, which leave
+// more partials and, where registers hold only two or three of them on a CU, a last round (8 x 8192 rows of 2048: 512 blocks 170 us, 768
+// 184, 1024 176; 4 x 4096 rows of 4096 98, 107, 118).
+constexpr int LN_BLOCKS = 512;
 
 // lanes and vectors to a row: 16 x 1, 64 x 1, 64 x 2, 256 x 1, 256 x 2, 256 x 4
 int ln_shape(int D) { return D <= 128 ? 0 : D <= 512 ? 1 : D <= 1024 ? 2 : D <= 2048 ? 3 : D <= 4096 ? 4 : 5; }
 int ln_groups(int D) { return D <= 128 ? 16 : D <= 1024 ? 4 : 1; }      // to a block
-
-// Blocks of the backward pass that are on the chip together
-int ln_backward_blocks(const LayerNormP &p) { return p.type != TYPE_F32 && (p.D <= 512 || (p.D > 1024 && p.D <= 2048)) ? LN_BLOCKS : LN_BLOCKS / 2; }
 
 LnSplit ln_split(const LayerNormP &p, bool want) {
   LnSplit w;
   std::memset(&w, 0, sizeof(w));
   const long long rows = (long long)p.b * p.T;
   w.tiles = p.D > LN_MAX_D ? (p.D + 2047) / 2048 : 1;
-  const int fill = ln_backward_blocks(p);
-  const long long most = std::max(1, fill / std::min(fill, p.M * w.tiles));
+  const long long most = std::max(1, LN_BLOCKS / std::min(LN_BLOCKS, p.M * w.tiles));
   const long long few = (p.D <= 512 || p.D > 1024 ? 4LL : 2LL) * ln_groups(p.D);       // rows of a block at least: one round of its groups' loads
   w.samples = want ? p.b : (int)rows; w.T = want ? p.T : 1; w.chunks = 1;
   if (want && w.T >= 8 * few && p.b * 2LL <= most) {                    // few long samples: several blocks to each
@@ -629,7 +634,7 @@ hipError_t backward_shape(const LayerNormP &p, const LnSplit &w, bool want_n, hi
 
 // Blocks per replica of the kernels whose groups take one row or sample after the other
 int ln_row_blocks(const LayerNormP &p, long long items, int groups) {
-  return (int)std::max(1LL, std::min((items + groups - 1) / groups, (2LL * LN_BLOCKS + p.M - 1) / p.M));
+  return (int)std::max(1LL, std::min((items + groups - 1) / groups, (4LL * LN_BLOCKS + p.M - 1) / p.M));
 }
 struct Forward {
   template <int TYPE, int G, int V, bool VEC> static void go(const LayerNormP &p, hipStream_t s) {
@@ -712,8 +717,8 @@ hipError_t launch_layer_norm_backward(const LayerNormP &p, void *workspace, hipS
   }
   const int colblocks = (2 * p.D + 63) / 64;
   const int count = w.chunks > 1 ? w.samples : w.nb;
-  const long long nblocks = nshares ? ((long long)p.M * p.b + 255) / 256 : 0;
-  hipLaunchKernelGGL(ln_finish_kernel, dim3((unsigned)(colblocks * p.M + nblocks)), dim3(256), 0, s, p, w, count, w.chunks, colblocks, nshares);
+  const long long nblocks = nshares ? ((long long)p.M * p.b + FIN * 64 - 1) / (FIN * 64) : 0;
+  hipLaunchKernelGGL(ln_finish_kernel, dim3((unsigned)((long long)colblocks * p.M + nblocks)), dim3(FIN * 64), 0, s, p, w, count, w.chunks, colblocks, nshares);
   if (p.q) {
     if (w.chunks > 1) hipLaunchKernelGGL(ln_inner_partials_kernel, dim3((unsigned)((long long)p.M * p.b)), dim3(256), 0, s, p, w);
     else if (p.D > LN_MAX_D) hipLaunchKernelGGL(ln_inner_long_kernel, dim3((unsigned)(((long long)p.M * p.b + 3) / 4)), dim3(256), 0, s, p);
