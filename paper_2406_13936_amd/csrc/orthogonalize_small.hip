@@ -1,7 +1,11 @@
 // Orthogonalisation of matrices that a work-group's LDS holds (the formulas and number formats of orthogonalize.hip, operands as
 // hi + lo): one launch, one work-group of eight wavefronts to a matrix, which takes the momentum's step, the norm, all
 // Newton-Schulz steps and the update.  Such matrices are latency: launch by launch every product is a handful of k-tiles
-// behind 8 us (4 of 64 x 96: 132 us for 17 launches, here 33).
+// behind a launch's 3 to 8 us.  5 steps, replayed from a graph, this kernel against the launches of orthogonalize.hip: 4 of 64 x 96
+// 25 us against 61, 4 of 16 x 1000 37 / 93, 4 of 128 x 128 70 / 75, 4 of 64 x 512 75 / 76, 512 of 64 x 512 169 / 384, 512 of
+// 128 x 128 151 / 281, 2048 of 16 x 16 46 / 293; so every matrix that fits is taken here.  What bounds it is the chain of LDS reads,
+// dependent MFMAs and barriers of one work-group (3.3 us a step of 64 x 96, 1.3 of 16 x 16, 10 of 128 x 128); the number of
+// tiles is a template's, so that their loops are straight code (4 of 64 x 96 with run-time loops: 35 us).
 //
 // LDS: X [mp][np + 8] and A [mp][mp + 8] as two fp16 values each, m = the smaller side, sides rounded up to 32 with zeros
 // (rows 16 bytes off a multiple of 64 bytes: the 16 rows of a fragment read meet different banks).
@@ -22,12 +26,18 @@ namespace absk {
 namespace {
 
 constexpr int SM_WAVES = 8, SM_THREADS = SM_WAVES * 64;
-constexpr int SM_MAX_M = 128, SM_TILES = SM_MAX_M / 16;
+constexpr int SM_MAX_M = 128;
+constexpr size_t SM_LDS = 160 * 1024 - 1024;               // (what a work-group has less the kernel's own few arrays)
 constexpr size_t SM_RED = SM_WAVES * 256 * sizeof(float);          // partial tiles of reductions shared by wavefronts
 
 int up(int v, int a) { return (v + a - 1) / a * a; }
+// tiles of 16 that hold the smaller side, as there are kernels for
+int small_tiles(int rows, int cols) {
+  const int t = (std::min(rows, cols) + 15) / 16;
+  return t <= 2 ? t : t <= 4 ? 4 : t <= 6 ? 6 : 8;
+}
 size_t small_lds(int rows, int cols) {
-  const size_t m = up(std::min(rows, cols), 32), n = up(std::max(rows, cols), 32);
+  const size_t m = std::max(32, 16 * small_tiles(rows, cols)), n = up(std::max(rows, cols), 32);
   return (m * (n + 8) + m * (m + 8)) * 4 + SM_RED;
 }
 
@@ -64,112 +74,171 @@ __device__ __forceinline__ void get4(const uint16_t *hi, const uint16_t *lo, flo
   v[2] = f16_val(h.y & 0xffffu) + f16_val(l.y & 0xffffu); v[3] = f16_val(h.y >> 16) + f16_val(l.y >> 16);
 }
 
-// C = alpha C_old + beta R R^T for the nt x nt tiles of 16 x 16, R = rh + rl with K values (a multiple of 32) to a row.
-// A wavefront has tiles of one row of tiles (the fragments of that row are read once), or, where there are fewer tiles than
-// wavefronts, a share of a tile's reduction; shares are added in order.  C may be R: it is written behind a barrier.
-__device__ __forceinline__ void gram(const uint16_t *rh, const uint16_t *rl, int ldr, int K, uint16_t *ch, uint16_t *cl, int ldc, int nt,
+// hi + lo of both operands, the small products first
+__device__ __forceinline__ f32x4 mfma_split(f16x8 ph, f16x8 pl, f16x8 qh, f16x8 ql, f32x4 c) { return mfma16(ph, qh, mfma16(pl, qh, mfma16(ph, ql, c))); }
+
+// C = alpha C_old + beta R R^T for the NT x NT tiles of 16 x 16, R = rh + rl with K values (a multiple of 32) to a row.  SELF: C is R, and
+// its old value counts.  A wavefront has tiles of one row of tiles (the fragments of that row are read once), or, where there are
+// fewer tiles than wavefronts, a share of a tile's reduction; shares are added in order.
+template <int NT, bool SELF>
+__device__ __forceinline__ void gram(const uint16_t *rh, const uint16_t *rl, int ldr, int K, uint16_t *ch, uint16_t *cl, int ldc,
                                      float alpha, float beta, float *red) {
+  constexpr int SHARES = NT == 1 ? 8 : NT == 2 ? 2 : 1;    // of a reduction
+  constexpr int PER = NT == 4 ? 2 : 1;                     // wavefronts to a row of tiles
+  constexpr int TILES = SHARES > 1 ? 1 : NT / PER;         // of a wavefront, PER apart
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = lane & 15, g16 = lane >> 4;
-  const int per = nt >= 4 ? SM_WAVES / nt : 1;             // wavefronts to a row of tiles
-  const int shares = nt == 1 ? 8 : nt == 2 ? 2 : 1;        // of a reduction
-  f32x4 acc[SM_TILES];
-  int ti, t0, dt, k0 = 0, k1 = K;
-  if (shares > 1) {
-    const int tile = wave / shares, s = wave - tile * shares, kc = (K / 32 + shares - 1) / shares * 32;
-    ti = tile / nt; t0 = tile - ti * nt; dt = SM_TILES;
-    k0 = min(K, s * kc); k1 = min(K, k0 + kc);
-  } else if (nt == 3) {                                    // nine tiles: row by row, one wavefront to each
-    ti = wave; t0 = 0; dt = 1;
-  } else {
-    ti = wave / per; t0 = wave - ti * per; dt = per;
-  }
-  const bool on = ti < nt;
+  const int tile = wave / SHARES, s = wave % SHARES;
+  const int ti = SHARES > 1 ? tile / NT : wave / PER, t0 = SHARES > 1 ? tile % NT : wave % PER;
+  const bool on = ti < NT;
+  f32x4 acc[TILES];
 #pragma unroll
-  for (int j = 0; j < SM_TILES; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int j = 0; j < TILES; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   if (on) {
-    const int own = (ti * 16 + i16) * ldr + g16 * 8;
+    const int kc = SHARES > 1 ? (K / 32 + SHARES - 1) / SHARES * 32 : K, k0 = SHARES > 1 ? s * kc : 0, k1 = min(K, k0 + kc);
+    const int own = (ti * 16 + i16) * ldr + g16 * 8, other = (t0 * 16 + i16) * ldr + g16 * 8;
     for (int k = k0; k < k1; k += 32) {
       const f16x8 qh = rows8(rh + own + k), ql = rows8(rl + own + k);
 #pragma unroll
-      for (int j = 0; j < SM_TILES; ++j) {
-        const int tj = t0 + j * dt;
-        if (tj >= nt) break;
-        const int o = (tj * 16 + i16) * ldr + g16 * 8 + k;
-        const f16x8 ph = rows8(rh + o), pl = rows8(rl + o);
-        acc[j] = mfma16(ph, ql, acc[j]);
-        acc[j] = mfma16(pl, qh, acc[j]);
-        acc[j] = mfma16(ph, qh, acc[j]);
+      for (int j = 0; j < TILES; ++j) {
+        const int o = other + j * PER * 16 * ldr + k;
+        acc[j] = mfma_split(rows8(rh + o), rows8(rl + o), qh, ql, acc[j]);
       }
     }
   }
-  if (shares > 1) {
+  if (SHARES > 1) {
     *reinterpret_cast<f32x4 *>(red + (wave * 64 + lane) * 4) = acc[0];
     __syncthreads();
-    if (wave % shares == 0)
-      for (int s = 1; s < shares; ++s) acc[0] += *reinterpret_cast<const f32x4 *>(red + ((wave + s) * 64 + lane) * 4);
-  }
-  // (a lane has four consecutive columns of one row)
-  const bool writes = on && (shares == 1 || wave % shares == 0);
-  if (writes && alpha != 0.0f) {
+    if (s == 0) {
 #pragma unroll
-    for (int j = 0; j < SM_TILES; ++j) {
-      const int tj = t0 + j * dt;
-      if (tj >= nt) break;
-      const int o = (ti * 16 + i16) * ldc + tj * 16 + g16 * 4;
-      float c[4];
-      get4(ch + o, cl + o, c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(alpha, c[e], beta * acc[j][e]);
+      for (int h = 1; h < SHARES; ++h) acc[0] += *reinterpret_cast<const f32x4 *>(red + ((wave + h) * 64 + lane) * 4);
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < SM_TILES; ++j) acc[j] *= beta;
   }
-  __syncthreads();                                         // every read of R is done
+  const bool writes = on && s == 0;
+  const int at = (ti * 16 + i16) * ldc + t0 * 16 + g16 * 4;          // (a lane has four consecutive columns of one row)
+#pragma unroll
+  for (int j = 0; j < TILES; ++j) {
+    acc[j] *= beta;
+    if (SELF && writes) {
+      float c[4];
+      get4(ch + at + j * PER * 16, cl + at + j * PER * 16, c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(alpha, c[e], acc[j][e]);
+    }
+  }
+  if (SELF) __syncthreads();                               // every read of R is done
   if (writes) {
 #pragma unroll
-    for (int j = 0; j < SM_TILES; ++j) {
-      const int tj = t0 + j * dt;
-      if (tj >= nt) break;
-      const int o = (ti * 16 + i16) * ldc + tj * 16 + g16 * 4;
+    for (int j = 0; j < TILES; ++j) {
       const float v[4] = {acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
-      put4(ch + o, cl + o, v);
+      put4(ch + at + j * PER * 16, cl + at + j * PER * 16, v);
     }
   }
   __syncthreads();
 }
 
+// X' = ax X + bx B X, or the result of the last step.  SHARE wavefronts to a block of 16 columns, each with some of its tiles.
+template <int NT, int SHARE>
+__device__ __forceinline__ void apply(const OrthSmallP &p, int z, uint16_t *xh, uint16_t *xl, int ldx, const uint16_t *bh, const uint16_t *bl,
+                                      int ldb, int m, int n, int mp, float ax, float bx, bool last) {
+  constexpr int TILES = (NT + SHARE - 1) / SHARE;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = lane & 15, g16 = lane >> 4, nb = (n + 15) >> 4, t0 = wave % SHARE * TILES;
+  for (int cb = wave / SHARE; SHARE > 1 || cb < nb; cb += SM_WAVES / SHARE) {
+    f32x4 acc[TILES];
+#pragma unroll
+    for (int j = 0; j < TILES; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const bool on = (SHARE == 1 || cb < nb) && t0 < NT;
+    const int xt = (t0 * 16 + i16) * ldx + cb * 16 + g16 * 4;        // X[i][c ..], i = 16 (t0 + j) + i16
+    if (on) {
+      const int xo = (g16 * 8 + (i16 >> 2)) * ldx + cb * 16 + 4 * (i16 & 3), bo = (t0 * 16 + i16) * ldb + g16 * 8;
+      for (int k = 0; k < mp; k += 32) {
+        const f16x8 ph = cols8(xh + xo + k * ldx, ldx), pl = cols8(xl + xo + k * ldx, ldx);
+#pragma unroll
+        for (int j = 0; j < TILES; ++j) {
+          const int o = bo + j * 16 * ldb + k;
+          acc[j] = mfma_split(ph, pl, rows8(bh + o), rows8(bl + o), acc[j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < TILES; ++j) {
+        float x[4];
+        get4(xh + xt + j * 16 * ldx, xl + xt + j * 16 * ldx, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(ax, x[e], bx * acc[j][e]);
+      }
+    }
+    if (SHARE > 1) __syncthreads();                        // others read these columns too
+    if (on && !last) {
+#pragma unroll
+      for (int j = 0; j < TILES; ++j) {
+        const float v[4] = {acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
+        put4(xh + xt + j * 16 * ldx, xl + xt + j * 16 * ldx, v);
+      }
+    } else if (on) {
+      const float lr = p.out.scal ? p.out.scal[0] : p.out.lr, decay = 1.0f - lr * p.out.wd, gain = lr * p.out.scale;
+#pragma unroll
+      for (int j = 0; j < TILES; ++j) {
+        const int i = (t0 + j) * 16 + i16, c = cb * 16 + g16 * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (i >= m || c + e >= n) continue;
+          const int r = p.wide ? i : c + e, q = p.wide ? c + e : i;
+          const long long at = z * p.out.so + (long long)r * p.out.ldo + q;
+          const float v = p.out.update ? fmaf(decay, load_as_f32(p.out.o, p.out.type, at), -gain * acc[j][e]) : acc[j][e];
+          store_from_f32(p.out.o, p.out.type, at, v);
+          if (p.out.shadow) p.out.shadow[z * p.out.sshadow + (long long)r * p.out.ldo + q] = f2bf(v);
+        }
+      }
+    }
+    if (SHARE > 1) break;                                  // (there are no more columns than one round takes)
+  }
+  __syncthreads();
+}
+
+// NT: tiles of 16 that hold the smaller side (LDS has at least 32 rows, the k of one MFMA)
+template <int NT>
 __global__ void __launch_bounds__(SM_THREADS) orth_small_kernel(const OrthSmallP p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
   __shared__ double sm[SM_WAVES];
   __shared__ double norm2;
-  const int z = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int i16 = lane & 15, g16 = lane >> 4;
+  __shared__ OrthScale sc[ORTH_MAX_STEPS];
+  constexpr int mp = NT == 1 ? 32 : NT * 16, lda = mp + 8, HELD = 4;
+  const int z = blockIdx.x, tid = threadIdx.x;
   const int m = min(p.rows, p.cols), n = max(p.rows, p.cols);
-  const int mp = (m + 31) & ~31, np = (n + 31) & ~31, ldx = np + 8, lda = mp + 8;
+  const int np = (n + 31) & ~31, ldx = np + 8;
   uint16_t *xh = reinterpret_cast<uint16_t *>(smem_raw), *xl = xh + mp * ldx, *ah = xl + mp * ldx, *al = ah + mp * lda;
   float *red = reinterpret_cast<float *>(al + mp * lda);
 
-  // zeros where the sides are rounded up; the norm, and the momentum's step
-  for (int i = tid; i < (mp * ldx + mp * lda) / 4; i += SM_THREADS) reinterpret_cast<uint4 *>(xh)[i] = make_uint4(0, 0, 0, 0);
+  // the norm, and the momentum's step; up to HELD chunks of eight values to a thread stay in registers for what follows
   const int cc = (p.cols + 7) >> 3, chunks = p.rows * cc;
+  float held[HELD][8];
   double sum = 0.0;
-  for (int i = tid; i < chunks; i += SM_THREADS) {
-    const int r = i / cc, c = (i - r * cc) * 8;
+#pragma unroll
+  for (int h = 0; h < HELD; ++h) {
+    const int i = tid + h * SM_THREADS;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) held[h][e] = 0.0f;
+    if (i < chunks) load_u8<true>(p.in, p.rows, p.cols, p.vec, z, i / cc, i % cc * 8, held[h]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fma((double)held[h][e], (double)held[h][e], sum);
+  }
+  for (int i = tid + HELD * SM_THREADS; i < chunks; i += SM_THREADS) {
     float u[8];
-    load_u8<true>(p.in, p.rows, p.cols, p.vec, z, r, c, u);
+    load_u8<true>(p.in, p.rows, p.cols, p.vec, z, i / cc, i % cc * 8, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = fma((double)u[e], (double)u[e], sum);
   }
+  // zeros where the sides are rounded up, and the steps' factors where they are at hand
+  for (int i = tid; i < (mp * ldx + mp * lda) / 4; i += SM_THREADS) reinterpret_cast<uint4 *>(xh)[i] = make_uint4(0, 0, 0, 0);
+  if (tid == 0)
+    for (int k = 0; k < p.steps; ++k) sc[k] = p.sc[k];
   sum = block_sum<SM_WAVES>(sum, sm);
   if (tid == 0) norm2 = sum;
   __syncthreads();
   const double scale = (double)p.first / (sqrt(norm2) + (double)p.eps);
-  for (int i = tid; i < chunks; i += SM_THREADS) {         // (a thread meets the values of v that it has written)
+  auto put = [&](int i, const float (&u)[8]) {
     const int r = i / cc, c = (i - r * cc) * 8;
-    float u[8];
-    load_u8<false>(p.in, p.rows, p.cols, p.vec, z, r, c, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if (c + e >= p.cols) break;
@@ -179,76 +248,42 @@ __global__ void __launch_bounds__(SM_THREADS) orth_small_kernel(const OrthSmallP
       xh[o] = h;
       xl[o] = f16_bits(v - f16_val(h));
     }
+  };
+#pragma unroll
+  for (int h = 0; h < HELD; ++h)
+    if (tid + h * SM_THREADS < chunks) put(tid + h * SM_THREADS, held[h]);
+  for (int i = tid + HELD * SM_THREADS; i < chunks; i += SM_THREADS) {       // (a thread meets the values of v that it has written)
+    float u[8];
+    load_u8<false>(p.in, p.rows, p.cols, p.vec, z, i / cc, i % cc * 8, u);
+    put(i, u);
   }
   __syncthreads();
 
-  const int nt = (m + 15) >> 4, nb = (n + 15) >> 4;
-  // wavefronts to a block of 16 columns, each with some of its tiles: one where there are enough blocks
-  const int share = nb <= 1 ? 8 : nb <= 2 ? 4 : nb <= 4 ? 2 : 1, tiles = (nt + share - 1) / share;
-  float lr = p.out.lr;
-  if (p.out.scal) lr = p.out.scal[0];
-  const float decay = 1.0f - lr * p.out.wd, gain = lr * p.out.scale;
   for (int k = 0; k < p.steps; ++k) {
-    const OrthScale s = p.sc[k];
-    gram(xh, xl, ldx, np, ah, al, lda, nt, 0.0f, s.gram, red);
-    gram(ah, al, lda, mp, ah, al, lda, nt, s.poly_a, s.poly_aa, red);
+    const OrthScale s = sc[k];
     const bool last = k + 1 == p.steps;
-    for (int cb0 = 0; cb0 < nb; cb0 += SM_WAVES / share) {
-      const int cb = cb0 + wave / share, t0 = wave % share * tiles, t1 = min(nt, t0 + tiles);
-      f32x4 acc[SM_TILES];
-#pragma unroll
-      for (int j = 0; j < SM_TILES; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      if (cb < nb) {
-        const int xo = (g16 * 8 + (i16 >> 2)) * ldx + cb * 16 + 4 * (i16 & 3);
-        for (int kk = 0; kk < mp; kk += 32) {
-          const f16x8 ph = cols8(xh + xo + kk * ldx, ldx), pl = cols8(xl + xo + kk * ldx, ldx);
-#pragma unroll
-          for (int j = 0; j < SM_TILES; ++j) {
-            if (t0 + j >= t1) break;
-            const int o = ((t0 + j) * 16 + i16) * lda + g16 * 8 + kk;
-            const f16x8 qh = rows8(ah + o), ql = rows8(al + o);
-            acc[j] = mfma16(ph, ql, acc[j]);
-            acc[j] = mfma16(pl, qh, acc[j]);
-            acc[j] = mfma16(ph, qh, acc[j]);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < SM_TILES; ++j) {
-          if (t0 + j >= t1) break;
-          const int o = ((t0 + j) * 16 + i16) * ldx + cb * 16 + g16 * 4;
-          float x[4];
-          get4(xh + o, xl + o, x);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(s.apply_x, x[e], s.apply_bx * acc[j][e]);
-        }
-      }
-      if (share > 1) __syncthreads();                      // others read these columns too (then there is one round)
-      if (cb >= nb) continue;
-#pragma unroll
-      for (int j = 0; j < SM_TILES; ++j) {
-        if (t0 + j >= t1) break;
-        const int i = (t0 + j) * 16 + i16, c = cb * 16 + g16 * 4;          // X'[i][c ..]
-        float v[4] = {acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
-        if (!last) { put4(xh + i * ldx + c, xl + i * ldx + c, v); continue; }
-        if (i >= m) continue;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (c + e >= n) continue;
-          const int r = p.wide ? i : c + e, q = p.wide ? c + e : i;
-          const long long at = z * p.out.so + (long long)r * p.out.ldo + q;
-          const float x = p.out.update ? fmaf(decay, load_as_f32(p.out.o, p.out.type, at), -gain * v[e]) : v[e];
-          store_from_f32(p.out.o, p.out.type, at, x);
-          if (p.out.shadow) p.out.shadow[z * p.out.sshadow + (long long)r * p.out.ldo + q] = f2bf(x);
-        }
-      }
-    }
-    __syncthreads();
+    gram<NT, false>(xh, xl, ldx, np, ah, al, lda, 0.0f, s.gram, red);
+    gram<NT, true>(ah, al, lda, mp, ah, al, lda, s.poly_a, s.poly_aa, red);
+    // as many wavefronts to a block of 16 columns as leave none idle
+    if (NT >= 8 && n <= 16) apply<NT, NT >= 8 ? 8 : 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
+    else if (NT >= 4 && n <= 32) apply<NT, NT >= 4 ? 4 : 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
+    else if (NT >= 2 && n <= 64) apply<NT, NT >= 2 ? 2 : 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
+    else apply<NT, 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
   }
+}
+
+template <int NT> hipError_t launch_nt(const OrthSmallP &p, int batch, size_t lds, hipStream_t s) {
+  static std::once_flag once;
+  static hipError_t err = hipSuccess;
+  std::call_once(once, [&] { err = hipFuncSetAttribute(reinterpret_cast<const void *>(orth_small_kernel<NT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)SM_LDS); });
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL(orth_small_kernel<NT>, dim3(batch), dim3(SM_THREADS), lds, s, p);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-bool orth_small_fits(int rows, int cols) { return std::min(rows, cols) <= SM_MAX_M && std::max(rows, cols) <= 8192 && small_lds(rows, cols) <= 160 * 1024 - 256; }
+bool orth_small_fits(int rows, int cols) { return std::min(rows, cols) <= SM_MAX_M && std::max(rows, cols) <= 8192 && small_lds(rows, cols) <= SM_LDS; }
 
 hipError_t launch_orth_small(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, hipStream_t s) {
   OrthSmallP p;
@@ -257,12 +292,14 @@ hipError_t launch_orth_small(const OrthPlan &pl, const OrthIn &in, const OrthOut
   p.vec = rows_of_vectors(in.g, in.type, in.sg, in.ldg, pl.cols) && (!in.v || rows_of_vectors(in.v, TYPE_F32, in.sv, pl.cols, pl.cols));
   p.first = (float)(1u << pl.ex[0]);
   for (int k = 0; k < pl.steps; ++k) p.sc[k] = pl.scale(k);
-  static std::once_flag once;
-  static hipError_t err = hipSuccess;
-  std::call_once(once, [&] { err = hipFuncSetAttribute(reinterpret_cast<const void *>(orth_small_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - 256); });
-  if (err != hipSuccess) return err;
-  hipLaunchKernelGGL(orth_small_kernel, dim3(pl.batch), dim3(SM_THREADS), small_lds(pl.rows, pl.cols), s, p);
-  return hipGetLastError();
+  const size_t lds = small_lds(pl.rows, pl.cols);
+  switch (small_tiles(pl.rows, pl.cols)) {
+    case 1: return launch_nt<1>(p, pl.batch, lds, s);
+    case 2: return launch_nt<2>(p, pl.batch, lds, s);
+    case 4: return launch_nt<4>(p, pl.batch, lds, s);
+    case 6: return launch_nt<6>(p, pl.batch, lds, s);
+    default: return launch_nt<8>(p, pl.batch, lds, s);
+  }
 }
 
 }  // namespace absk
