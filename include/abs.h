@@ -336,6 +336,8 @@ enum { ABS_TYPE_F32 = 0, ABS_TYPE_BF16 = 1, ABS_TYPE_F16 = 2 };
  *                  in 32 bits): relative error of the result 0.5 to 1.6e-3, no more than a bf16 result's own rounding adds.
  *                  (Up to 128 rows or columns the products are those of ABS_PREC_F32 all the same.)
  *                  ABS_PREC_F32: as exact as fp32 products, at three times the operations.
+ *   eps          : X is held to 2^-40 of the largest singular value that it can have (1 at first), so a matrix whose norm is below 1e-3 eps
+ *                  loses precision: 1e-6 of the result at a million values and a norm of 1e-3 eps, and in proportion below that.
  * Asynchronous on the stream; sums are in a fixed order (the same bits every time).  workspace: device, 256-byte aligned,
  * abs_orthogonalize_workspace_bytes, used until the call's work has run.  A matrix of 2^29 values or more (its sides rounded up to 32): ABS_EUNSUPPORTED.
  */
@@ -359,6 +361,7 @@ abs_status abs_muon_step(void *x_dev, int x_type, const void *g_dev, int g_type,
 /*
  * Layer norm over the last dimension, M replicas with gains and biases of their own (fp32 arithmetic, one rounding at the end):
  *   mu = mean_d x,  r = 1 / sqrt(mean_d (x - mu)^2 + eps),  y = (x - mu) r gamma + beta
+ * At most 2^20 replicas, 2^27 gains (M D) and 2^31 - 1 rows (M b T); beyond: ABS_EUNSUPPORTED.
  */
 typedef struct {
   int M, b, T, D;             /* replicas, samples of each, rows of a sample (tokens), values of a row; all >= 1 */

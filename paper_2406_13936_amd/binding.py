@@ -502,6 +502,12 @@ def _like(t):
     return _torch.empty_like(t) if t.is_contiguous() else _torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
+def _fits(what: str, *sizes):
+    """The C entries take sizes of 31 bits."""
+    if max(sizes) > 0x7fffffff:
+        raise AbsError(f"{what} is too large: {max(sizes)} along a dimension")
+
+
 @functools.lru_cache(maxsize=512)
 def _rows(shape, stride, what: str):
     """(stride of the first dimension, stride of a row) of a tensor whose dimensions between the first and the last are one
@@ -537,6 +543,7 @@ def _matrices(shape, stride, what: str):
         elif st != step * batch:
             raise AbsError(f"{what}: matrices must be equally spaced")
         batch *= n
+    _fits(what, batch, rows, cols)
     return batch, rows, cols, (step or 0), (stride[-2] if rows > 1 else cols)
 
 
@@ -615,6 +622,7 @@ def _norm_shape(shape, stride, kind: int, param_kind: int, other_shape, other_st
     T = 1
     for n in shape[2:-1]:
         T *= n
+    _fits("x", M, b, T, D)
     sx, ldx = _rows(shape, stride, "x")
     sy, ldy = _rows(other_shape, other_stride, other)
     s = LayerNormShape(M, b, T, D, kind, param_kind, ldx, sx, ldy, sy, D, b * T * D)

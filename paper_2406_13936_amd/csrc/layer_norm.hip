@@ -523,10 +523,10 @@ __global__ void __launch_bounds__(256) ln_inner_rows_kernel(const LayerNormP p, 
   load_param<TYPE, G, V, VEC>(gw, p.dgamma, TYPE_F32, (long long)m * D, D, l);
   load_param<TYPE, G, V, VEC>(gb, p.dbeta, TYPE_F32, (long long)m * D, D, l);
   int turn = 0;
-  for (int i = j * GP + gid; i < p.b; i += nb * GP) {
+  for (long long i = j * GP + gid; i < p.b; i += nb * GP) {
     float s[1] = {0.0f};
     for (int t = 0; t < p.T; ++t) {
-      const long long r = (long long)i * p.T + t;
+      const long long r = i * p.T + t;
       Raw<TYPE, V> rx, ry;
       load_raw<TYPE, G, V, VEC>(rx, p.x, m * p.sx + r * p.ldx, D, l);
       load_raw<TYPE, G, V, VEC>(ry, p.dy, m * p.sy + r * p.ldy, D, l);
@@ -587,12 +587,12 @@ LnSplit ln_split(const LayerNormP &p, bool want) {
   if (want && w.T >= 8 * few && p.b * 2LL <= most) {                    // few long samples: several blocks to each
     w.chunks = (int)std::max(1LL, std::min((w.T + 4 * few - 1) / (4 * few), most / p.b));
     w.per = (w.T + w.chunks - 1) / w.chunks;
-    w.chunks = (w.T + w.per - 1) / w.per;
+    w.chunks = (int)((w.T + (long long)w.per - 1) / w.per);
     if (w.chunks > 1) { w.nb = w.samples * w.chunks; return w; }
   }
   const long long nb = std::max(1LL, std::min(most, (rows + few - 1) / few));
   w.per = (int)((w.samples + nb - 1) / nb);
-  w.nb = (w.samples + w.per - 1) / w.per;
+  w.nb = (int)((w.samples + (long long)w.per - 1) / w.per);
   return w;
 }
 int ln_sample_tiles(const LayerNormP &p) { return (2 * p.D + 255) / 256; }

@@ -4,11 +4,23 @@
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
+#include <atomic>
 #include "abs_internal.h"
 
 namespace absk {
 
 enum { TYPE_F32 = 0, TYPE_BF16 = 1, TYPE_F16 = 2 };
+// Lets a kernel take more than 64 KB of LDS on the current device (`done`: the kernel's own, a bit per device)
+inline hipError_t allow_lds(const void *kernel, size_t bytes, std::atomic<uint64_t> &done) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
 inline int type_bytes(int t) { return t == TYPE_F32 ? 4 : 2; }
 
 // ---- orthogonalisation ---------------------------------------------------------------------------------------------

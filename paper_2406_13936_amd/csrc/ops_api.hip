@@ -54,7 +54,9 @@ abs_status check_shape(const abs_layer_norm_shape *s, bool backward) {
   if (!known_type(s->type)) return set_error(ABS_EINVAL, "unknown type");
   if (s->param_type != s->type && s->param_type != ABS_TYPE_F32) return set_error(ABS_EINVAL, "param_type must be ABS_TYPE_F32 or type");
   const int64_t rows = (int64_t)s->b * s->T;
-  if (rows > 0x7fffffff / s->M || (int64_t)s->M * s->D > 0x7fffffff) return set_error(ABS_EUNSUPPORTED, "too many rows or values");
+  // (a grid counts its threads in 32 bits, and 512 of them add the partial gradients of 64 gains or biases)
+  if (s->M > 1 << 20 || (int64_t)s->M * s->D > 1 << 27 || rows > 0x7fffffff / s->M)
+    return set_error(ABS_EUNSUPPORTED, "more than 2^20 replicas, 2^27 gains or 2^31 - 1 rows");
   if (!strides_ok(s->M, s->stride_x, rows, s->ldx, s->D) || !strides_ok(s->M, s->stride_y, rows, s->ldy, s->D) ||
       (backward && !strides_ok(s->M, s->stride_dx, rows, s->lddx, s->D)))
     return set_error(ABS_EINVAL, "strides: ld >= D, and replicas must not run into each other");
@@ -177,6 +179,8 @@ abs_status abs_layer_norm_backward(const abs_layer_norm_shape *shape, const void
   const int64_t ey = extent(shape->M, shape->stride_y, rows, shape->ldy, shape->D, shape->type);
   const int64_t ed = extent(shape->M, shape->stride_dx, rows, shape->lddx, shape->D, shape->type);
   if (overlap(dx_dev, ed, x_dev, ex) || overlap(dx_dev, ed, dy_dev, ey)) return set_error(ABS_EINVAL, "dx_dev must not overlap x_dev or dy_dev");
+  if (overlap(workspace, (int64_t)need, x_dev, ex) || overlap(workspace, (int64_t)need, dy_dev, ey) || overlap(workspace, (int64_t)need, dx_dev, ed))
+    return set_error(ABS_EINVAL, "the workspace must not overlap x_dev, dy_dev or dx_dev");
   p.x = x_dev; p.gamma = gamma_dev; p.mean = const_cast<float *>(mean_dev); p.rstd = const_cast<float *>(rstd_dev);
   p.dy = dy_dev; p.dx = dx_dev; p.dgamma = dgamma_dev; p.dbeta = dbeta_dev; p.n = n_dev; p.q = q_dev;
   return hip_status(launch_layer_norm_backward(p, workspace, static_cast<hipStream_t>(hip_stream)), "abs_layer_norm_backward");

@@ -25,7 +25,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <mutex>
 #include "device_utils.h"
 #include "mfma_tile.h"
 #include "ops.h"
@@ -540,11 +539,10 @@ hipError_t launch_cfg(const OrthGemmP &p, hipStream_t s) {
   const int tm = (p.Md + BM - 1) / BM, tn = (p.Nd + BN - 1) / BN;
   if ((KIND == KIND_SYM) != (p.sym != 0) || (p.sym && (BM != BN || p.Md != p.Nd))) return hipErrorInvalidValue;
   const long long nblk = (p.sym ? (long long)tn * (tn + 1) / 2 : (long long)tm * tn) * p.batch;
-  if (nblk > 0x3fffffff) return hipErrorInvalidValue;
+  if ((nblk + 7) * (WM * WN * WK * 64) > 0xffffffffLL) return hipErrorInvalidValue;      // (a grid counts its threads in 32 bits)
   if (lds > 64 * 1024) {
-    static std::once_flag once;
-    static hipError_t err = hipSuccess;
-    std::call_once(once, [&] { err = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); });
+    static std::atomic<uint64_t> done{0};
+    const hipError_t err = allow_lds(reinterpret_cast<const void *>(kern), lds, done);
     if (err != hipSuccess) return err;
   }
   const int chunk = (int)((nblk + 7) / 8);

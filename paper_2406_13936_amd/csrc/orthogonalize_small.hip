@@ -15,7 +15,6 @@
 //                  only, so one wavefront reads and replaces them without waiting for the others
 #include <algorithm>
 #include <cstring>
-#include <mutex>
 #include "device_utils.h"
 #include "mfma_tile.h"
 #include "ops.h"
@@ -264,21 +263,27 @@ __global__ void __launch_bounds__(SM_THREADS) orth_small_kernel(const OrthSmallP
     const bool last = k + 1 == p.steps;
     gram<NT, false>(xh, xl, ldx, np, ah, al, lda, 0.0f, s.gram, red);
     gram<NT, true>(ah, al, lda, mp, ah, al, lda, s.poly_a, s.poly_aa, red);
-    // as many wavefronts to a block of 16 columns as leave none idle
-    if (NT >= 8 && n <= 16) apply<NT, NT >= 8 ? 8 : 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
-    else if (NT >= 4 && n <= 32) apply<NT, NT >= 4 ? 4 : 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
-    else if (NT >= 2 && n <= 64) apply<NT, NT >= 2 ? 2 : 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
+    // two wavefronts to a block of 16 columns where there are no more than four of these
+    constexpr bool TWO = NT == 2 || NT == 4;
+    if (TWO && n <= 64) apply<NT, TWO ? 2 : 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
     else apply<NT, 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
   }
 }
 
 template <int NT> hipError_t launch_nt(const OrthSmallP &p, int batch, size_t lds, hipStream_t s) {
-  static std::once_flag once;
-  static hipError_t err = hipSuccess;
-  std::call_once(once, [&] { err = hipFuncSetAttribute(reinterpret_cast<const void *>(orth_small_kernel<NT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)SM_LDS); });
-  if (err != hipSuccess) return err;
-  hipLaunchKernelGGL(orth_small_kernel<NT>, dim3(batch), dim3(SM_THREADS), lds, s, p);
-  return hipGetLastError();
+  static std::atomic<uint64_t> done{0};
+  hipError_t err = allow_lds(reinterpret_cast<const void *>(orth_small_kernel<NT>), SM_LDS, done);
+  constexpr int MOST = 1 << 22;                            // matrices of a launch: a grid counts its threads in 32 bits
+  for (int z0 = 0; z0 < batch && err == hipSuccess; z0 += std::min(MOST, batch - z0)) {
+    OrthSmallP q = p;
+    q.in.g = static_cast<const unsigned char *>(p.in.g) + z0 * p.in.sg * type_bytes(p.in.type);
+    if (p.in.v) q.in.v = p.in.v + z0 * p.in.sv;
+    q.out.o = static_cast<unsigned char *>(p.out.o) + z0 * p.out.so * type_bytes(p.out.type);
+    if (p.out.shadow) q.out.shadow = p.out.shadow + z0 * p.out.sshadow;
+    hipLaunchKernelGGL(orth_small_kernel<NT>, dim3(std::min(MOST, batch - z0)), dim3(SM_THREADS), lds, s, q);
+    err = hipGetLastError();
+  }
+  return err;
 }
 
 }  // namespace

@@ -94,7 +94,8 @@ def _shape(**k):
 @pytest.mark.parametrize("change,status", [
     (dict(M=0), EINVAL), (dict(b=0), EINVAL), (dict(T=0), EINVAL), (dict(D=0), EINVAL), (dict(type=3), EINVAL),
     (dict(param_type=1), EINVAL), (dict(ldx=15), EINVAL), (dict(stride_x=100), EINVAL), (dict(ldy=-16), EINVAL), (dict(stride_y=0), EINVAL),
-    (dict(b=1 << 20, T=1 << 12, stride_x=1 << 40, stride_y=1 << 40), EUNSUPPORTED)])
+    (dict(b=1 << 20, T=1 << 12, stride_x=1 << 40, stride_y=1 << 40), EUNSUPPORTED), (dict(M=(1 << 20) + 1), EUNSUPPORTED),
+    (dict(D=1 << 27, ldx=1 << 27, ldy=1 << 27, stride_x=1 << 32, stride_y=1 << 32), EUNSUPPORTED)])
 def test_layer_norm_refuses_shapes(change, status):
     lib = _lib()
     s = _shape(**change)
@@ -124,6 +125,8 @@ def test_layer_norm_refuses_arguments():
         assert bwd(**{name: far[0] + 2}) == EINVAL, name
     assert bwd(ws=None) == EINVAL and bwd(ws=WS + 16) == EINVAL and bwd(nbytes=16) == ENOMEM
     assert bwd(dx=far[1]) == EINVAL and bwd(dx=far[0] + 64) == EINVAL
+    for name in ("dy", "x", "dx"):
+        assert bwd(**{name: WS + 128}) == EINVAL, name
     assert lib.abs_layer_norm_backward_workspace_bytes(C.byref(s), 0, 0, None) == EINVAL
 
 
@@ -139,6 +142,19 @@ def test_tensors_on_the_host_are_refused():
         A.layer_norm(x, x[:, 0])
     with pytest.raises(A.AbsError, match="float32, bfloat16 or float16"):
         A.orthogonalize(x.double())
+
+
+def test_sizes_beyond_31_bits_are_refused():
+    """(The C entries take 31 bits, and ctypes would drop the rest.)"""
+    import torch
+    from paper_2406_13936_amd import binding as B
+    big = 1 << 32
+    with pytest.raises(B.AbsError, match="too large"):
+        B._matrices((big + 1, 1, 1), (1, 1, 1), "g")
+    with pytest.raises(B.AbsError, match="too large"):
+        B._matrices((1 << 16, 1 << 16, 1, 1), (1 << 16, 1, 1, 1), "g")
+    with pytest.raises(B.AbsError, match="too large"):
+        B._norm_shape(torch.Size((1, big + 2, 4)), (4 * (big + 2), 4, 1), 0, 0, torch.Size((1, big + 2, 4)), (4 * (big + 2), 4, 1), "dy")
 
 
 # ---- orthogonalisation ----------------------------------------------------------------------------------------------------
@@ -279,6 +295,42 @@ def test_orthogonalize_of_zeros_infinities_and_extreme_sizes():
         # with the usual eps a tiny matrix stays small: its norm does not reach it
         out = A.orthogonalize(G[5:6].cuda() * 1e24)
         _check_orth(out, G[5:6] * 1e24, 0, "f32", tol=1e-4)
+
+
+@gpu
+def test_orthogonalize_of_very_many_matrices():
+    """More than one launch has places for, and more values than 32 bits count."""
+    import torch
+    A = _A()
+    gen = torch.Generator("cuda").manual_seed(5)
+    G = torch.randn((4194304 + 3, 1, 1), generator=gen, device="cuda")
+    p = G.double() / (G.double().abs() + 1e-7)
+    for _ in range(5):
+        p = COEF[0] * p + COEF[1] * p ** 3 + COEF[2] * p ** 5
+    v, x = torch.zeros_like(G), torch.full_like(G, 2.0)
+    assert (A.orthogonalize(G).double() - p).abs().max() <= (TOL32 + U["f32"]) * p.abs().max()
+    A.muon_step(x, G, v, 0.5, momentum=0.0, scale=1.0)
+    assert torch.equal(v, G) and (x.double() - (2.0 - 0.5 * p)).abs().max() <= 0.5 * TOL32 * p.abs().max() + 2 * 2.5 * U["f32"]
+    del G, p, v, x
+    G = torch.randn((32771, 264, 256), generator=gen, device="cuda", dtype=torch.bfloat16)
+    assert G.numel() > 1 << 31
+    out = A.orthogonalize(G)
+    some = [0, 1, 32767, 32768, 32770]
+    _check_orth(out[some], G[some], 1, "bf16")
+
+
+@gpu
+def test_orthogonalize_with_strides_beyond_32_bits():
+    import torch
+    A = _A()
+    for rows, cols, ld in ((33, 40, 1 << 26), (140, 136, (1 << 24) + 3)):
+        step = rows * ld
+        buf = torch.empty(step + rows * ld, device="cuda", dtype=torch.bfloat16)
+        g = buf.as_strided((2, rows, cols), (step, ld, 1))
+        g.copy_(_matrix("full", 2, rows, cols, torch.Generator().manual_seed(6)))
+        want = A.orthogonalize(g.contiguous())
+        A.orthogonalize(g, out=g)
+        assert torch.equal(g, want)
 
 
 @gpu
@@ -594,6 +646,40 @@ def test_layer_norm_of_strided_rows():
         A.layer_norm(torch.zeros((2, 4, 8, 6), device="cuda").transpose(2, 3), torch.zeros((2, 8), device="cuda"))
     with pytest.raises(A.AbsError, match=r"\[M, D\]"):
         A.layer_norm(torch.zeros((2, 4, 8), device="cuda"), torch.zeros((2, 9), device="cuda"))
+
+
+@gpu
+def test_layer_norm_beyond_32_bits():
+    """Strides, and numbers of values, that 32 bits do not hold."""
+    import torch
+    A = _A()
+    gen = torch.Generator("cuda").manual_seed(7)
+    for D in (40, 1000, 9000):
+        M, b, ld, step = 2, 3, 1 << 29, 1 << 31
+        bufs = [torch.empty(step + 2 * ld + D, device="cuda", dtype=torch.bfloat16) for _ in range(3)]
+        x, dy, y = (t.as_strided((M, b, 1, D), (step, ld, ld, 1)) for t in bufs)
+        for t in (x, dy):
+            t.copy_(torch.randn((M, b, 1, D), generator=gen, device="cuda"))
+        w, bias = torch.randn((M, D), generator=gen, device="cuda"), torch.randn((M, D), generator=gen, device="cuda")
+        want = A.layer_norm(x.contiguous(), w, bias)
+        got = A.layer_norm(x, w, bias, out=y)
+        assert all(torch.equal(p, r) for p, r in zip(got, want))
+        ref = A.layer_norm_backward(dy.contiguous(), x.contiguous(), w, *want[1:], want_norms=True, want_inner=True)
+        got = A.layer_norm_backward(dy, x, w, *want[1:], want_norms=True, want_inner=True)
+        assert all(torch.equal(p, r) for p, r in zip(got, ref))
+        del bufs, x, dy, y
+    n, D = (1 << 20) + 5, 2056
+    x = torch.randn((1, n, D), generator=gen, device="cuda", dtype=torch.bfloat16)
+    dy = torch.randn((1, n, D), generator=gen, device="cuda", dtype=torch.bfloat16)
+    w, bias = torch.randn((1, D), generator=gen, device="cuda"), torch.randn((1, D), generator=gen, device="cuda")
+    y, mean, rstd = A.layer_norm(x, w, bias)
+    dx, _, _, ni, _ = A.layer_norm_backward(dy, x, w, mean, rstd, want_norms=True)
+    tail = slice(n - 7, n)
+    assert y.numel() > 1 << 31
+    for p, r in zip((y, mean, rstd), A.layer_norm(x[:, tail], w, bias)):
+        assert torch.equal(p[:, tail], r)
+    part = A.layer_norm_backward(dy[:, tail], x[:, tail], w, mean[:, tail].contiguous(), rstd[:, tail].contiguous(), want_norms=True)
+    assert torch.equal(dx[:, tail], part[0]) and torch.equal(ni[:, tail], part[3])
 
 
 @gpu
