@@ -5,13 +5,14 @@
 //   sample i (T rows):  g_i = (sum_t dy xh, sum_t dy),   gbar = mean_i g_i,   n_i = ||g_i||^2,   q_i = <g_i, gbar>
 //
 // All of it is bound by memory: forward reads x and writes y, backward reads x and dy and writes dx.  A row lives in the
-// registers of a group of G lanes (16, 64 or 256, V vectors of 8 values to a lane), so it is read once; gains, biases and
+// registers of a group of G lanes (16 to 512, V vectors of 8 values to a lane), so it is read once; gains, biases and
 // the sums for gbar stay in the registers of the lanes that own their columns, over all rows of a block.  A block leaves
 // one partial of (sum dy xh, sum dy), and a second launch adds the partials in order: no atomics, the same bits every time.
 // The gradient of a gain is no outer product, so n_i has no factored form: samples of several rows are summed in
 // registers by the block that has all of their rows, or from the partials where a sample is spread over blocks.
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 #include "device_utils.h"
 #include "ops.h"
 #include "typed_mem.h"
@@ -35,74 +36,100 @@ template <int G> __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
-// Sums of N values over the group.  G = 256: through LDS, one barrier a call (`turn` picks one of two buffers, so that the
+constexpr int ln_threads(int G) { return G > 256 ? G : 256; }      // of a block
+
+// Sums of N values over the group.  G >= 256: through LDS, one barrier a call (`turn` picks one of two buffers, so that the
 // next call's values do not meet this one's readers); every thread of the block takes part.
 template <int G, int N>
-__device__ __forceinline__ void group_sums(float (&v)[N], float *sm, int turn) {      // sm: 8 N floats
+__device__ __forceinline__ void group_sums(float (&v)[N], float *sm, int turn) {      // sm: 2 N floats to a wavefront
+  constexpr int W = G > 64 ? G / 64 : 4;
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = lanes_sum<(G < 64 ? G : 64)>(v[i]);
   if (G <= 64) return;
-  float *s = sm + (turn & 1) * N * 4;
+  float *s = sm + (turn & 1) * N * W;
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) s[i * 4 + wave] = v[i];
+    for (int i = 0; i < N; ++i) s[i * W + wave] = v[i];
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const float4 f = *reinterpret_cast<const float4 *>(s + i * 4);
-    v[i] = (f.x + f.y) + (f.z + f.w);
+    v[i] = 0.0f;
+#pragma unroll
+    for (int h = 0; h < W; h += 4) {
+      const float4 f = *reinterpret_cast<const float4 *>(s + i * W + h);
+      v[i] += (f.x + f.y) + (f.z + f.w);
+    }
   }
 }
 
-// Columns of lane l in a row.  VEC: 16-byte vectors that lie side by side over the lanes: of 16-bit values (v G + l) 8 + e, of fp32
-// ((2 v + e / 4) G + l) 4 + e % 4.  Else single values, (8 v + e) G + l (rows that do not start on 16 bytes or end inside a vector).
-template <int TYPE, int G, bool VEC> __device__ __forceinline__ int col_of(int v, int e, int l) {
-  if (!VEC) return (8 * v + e) * G + l;
+// Columns of lane l in a row: 16-byte vectors that lie side by side over the lanes, of 16-bit values (v G + l) 8 + e, of fp32
+// ((2 v + e / 4) G + l) 4 + e % 4.
+template <int TYPE, int G> __device__ __forceinline__ int col_of(int v, int e, int l) {
   return TYPE == TYPE_F32 ? ((2 * v + (e >> 2)) * G + l) * 4 + (e & 3) : (v * G + l) * 8 + e;
 }
 
 // Results are not read again here: non-temporal stores (16-bit rows of 2048: forward 116 -> 101 us for 134 M values, backward 204 -> 194;
 // non-temporal loads cost more than they give where the inputs are still in a cache).
-__device__ __forceinline__ void st_once(void *p, uint4 v) {
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));       // 16 bytes that start anywhere a 16-bit value may
+template <bool VEC> __device__ __forceinline__ void st_once(void *p, uint4 v) {
   const u32x4 w = {v.x, v.y, v.z, v.w};
-  __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
+  if constexpr (VEC) __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
+  else __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any *>(p));
+}
+
+// q without its first k values of BYTES, moved down, zeros behind them (k <= 16 / BYTES)
+template <int BYTES> __device__ __forceinline__ uint4 move_down(uint4 q, int k) {
+  if (BYTES == 2) {
+    const uint32_t s = 16 * (k & 1);
+    q = make_uint4(__builtin_amdgcn_alignbit(q.y, q.x, s), __builtin_amdgcn_alignbit(q.z, q.y, s), __builtin_amdgcn_alignbit(q.w, q.z, s), q.w >> s);
+    k >>= 1;
+  }
+  const bool one = k & 1, two = k & 2, all = k & 4;        // words
+  q = make_uint4(one ? q.y : q.x, one ? q.z : q.y, one ? q.w : q.z, one ? 0u : q.w);
+  q = make_uint4(two ? q.z : q.x, two ? q.w : q.y, two ? 0u : q.z, two ? 0u : q.w);
+  return make_uint4(all ? 0u : q.x, all ? 0u : q.y, all ? 0u : q.z, all ? 0u : q.w);
+}
+
+// 16 bytes of a row of D values of BYTES from column c on, zeros beyond the row; nothing outside the row is read.  VEC: whole vectors at
+// 16-byte places.  Else a vector that would pass the row's end is the row's last one, moved down.
+// (Every lane loads, from a column of the row where it has none: loads behind branches wait for each other.)
+template <int BYTES, bool VEC> __device__ __forceinline__ uint4 load16(const void *p, long long at, int c, int D) {
+  constexpr int N = 16 / BYTES;
+  if constexpr (VEC) {
+    const bool in = c < D;
+    const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const unsigned char *>(p) + (at + (in ? c : 0)) * BYTES);
+    return make_uint4(in ? q.x : 0u, in ? q.y : 0u, in ? q.z : 0u, in ? q.w : 0u);
+  }
+  const unsigned char *row = static_cast<const unsigned char *>(p) + at * BYTES;
+  if (D < N) {                                    // (no row this short has such a vector)
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (c + e < D) {
+        if constexpr (BYTES == 4) w[e] = reinterpret_cast<const uint32_t *>(row)[c + e];
+        else w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[c + e] << (16 * (e & 1));
+      }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+    const int from = min(c, D - N), k = min(c - from, N);
+    const u32x4 q = *reinterpret_cast<const u32x4_any *>(row + (long long)from * BYTES);
+    return move_down<BYTES>(make_uint4(q.x, q.y, q.z, q.w), k);
+  }
 }
 
 // What a lane holds of a row as it comes from memory
 template <int TYPE, int V> struct Raw { uint4 q[V * (TYPE == TYPE_F32 ? 2 : 1)]; };
 
-// (Every lane loads, from the row's first column where it has none, and zeros take the place of what it got: loads behind branches
-// wait for each other.)
 template <int TYPE, int G, int V, bool VEC>
 __device__ __forceinline__ void load_raw(Raw<TYPE, V> &r, const void *p, long long at, int D, int l) {
   constexpr int PER = TYPE == TYPE_F32 ? 2 : 1, N = 8 / PER;        // vectors of a lane's eight, values of a vector
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int h = 0; h < PER; ++h) {
-      uint4 &q = r.q[v * PER + h];
-      if constexpr (VEC) {
-        const int c = col_of<TYPE, G, true>(v, N * h, l);
-        const bool in = c < D;
-        q = *reinterpret_cast<const uint4 *>(static_cast<const unsigned char *>(p) + (at + (in ? c : 0)) * (16 / N));
-        q = make_uint4(in ? q.x : 0u, in ? q.y : 0u, in ? q.z : 0u, in ? q.w : 0u);
-      } else {
-        uint32_t w[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const int c = col_of<TYPE, G, false>(v, N * h + e, l);
-          const bool in = c < D;
-          const long long i = at + (in ? c : 0);
-          const uint32_t got = TYPE == TYPE_F32 ? static_cast<const uint32_t *>(p)[i] : (uint32_t)static_cast<const uint16_t *>(p)[i];
-          w[e] = in ? got : 0u;
-        }
-        if constexpr (TYPE == TYPE_F32) q = make_uint4(w[0], w[1], w[2], w[3]);
-        else q = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4 % N] | (w[5 % N] << 16), w[6 % N] | (w[7 % N] << 16));
-      }
-    }
+    for (int h = 0; h < PER; ++h) r.q[v * PER + h] = load16<16 / N, VEC>(p, at, col_of<TYPE, G>(v, N * h, l), D);
 }
 
 // From here on the values count as unknown, so that what was computed from them is computed again and not kept in registers.
@@ -121,22 +148,19 @@ template <int TYPE, int V> __device__ __forceinline__ void raw_vals(const Raw<TY
 }
 template <int TYPE, int G, bool VEC>
 __device__ __forceinline__ void store_vals(void *p, long long at, int D, int l, int v, const float (&f)[8]) {
-  if constexpr (VEC) {
-    if constexpr (TYPE == TYPE_F32) {
+  constexpr int PER = TYPE == TYPE_F32 ? 2 : 1, N = 8 / PER;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = col_of<TYPE, G, true>(v, 4 * h, l);
-        if (c < D) st_once(static_cast<float *>(p) + at + c, make_uint4(__float_as_uint(f[4 * h]), __float_as_uint(f[4 * h + 1]), __float_as_uint(f[4 * h + 2]), __float_as_uint(f[4 * h + 3])));
-      }
-    } else {
-      const int c = col_of<TYPE, G, true>(v, 0, l);
-      if (c < D) st_once(static_cast<uint16_t *>(p) + at + c, pack8(TYPE, f));
-    }
-  } else {
+  for (int h = 0; h < PER; ++h) {
+    const int c = col_of<TYPE, G>(v, N * h, l);
+    if (VEC ? c < D : c + N <= D) {
+      if constexpr (TYPE == TYPE_F32)
+        st_once<VEC>(static_cast<float *>(p) + at + c, make_uint4(__float_as_uint(f[4 * h]), __float_as_uint(f[4 * h + 1]), __float_as_uint(f[4 * h + 2]), __float_as_uint(f[4 * h + 3])));
+      else
+        st_once<VEC>(static_cast<uint16_t *>(p) + at + c, pack8(TYPE, f));
+    } else if (!VEC) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = col_of<TYPE, G, false>(v, e, l);
-      if (c < D) store_from_f32(p, TYPE, at + c, f[e]);
+      for (int e = 0; e < N; ++e)
+        if (c + e < D) store_from_f32(p, TYPE, at + c + e, f[N * h + e]);
     }
   }
 }
@@ -144,26 +168,33 @@ __device__ __forceinline__ void store_vals(void *p, long long at, int D, int l, 
 template <int TYPE, int PARAM, int G, int V, bool VEC>
 __device__ __forceinline__ void load_param_as(float (&f)[V][8], const void *p, long long at, int D, int l) {
   const bool whole = VEC && !((reinterpret_cast<uintptr_t>(p) + at * (PARAM == TYPE_F32 ? 4 : 2)) & 15);
-  if (whole && PARAM == TYPE) {
-    Raw<TYPE, V> r;
-    load_raw<TYPE, G, V, true>(r, p, at, D, l);
+  auto load = [&](auto W) {
+    constexpr bool w = decltype(W)::value;
+    if constexpr (PARAM == TYPE) {
+      Raw<TYPE, V> r;
+      load_raw<TYPE, G, V, w>(r, p, at, D, l);
 #pragma unroll
-    for (int v = 0; v < V; ++v) raw_vals<TYPE, V>(r, v, f[v]);
-  } else if (whole) {                             // fp32 beside 16-bit rows: two vectors to one of theirs
+      for (int v = 0; v < V; ++v) raw_vals<TYPE, V>(r, v, f[v]);
+    } else {                                      // fp32 beside 16-bit rows: two vectors to one of theirs
+      Raw<TYPE_F32, V> r;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = col_of<TYPE, G, VEC>(v, 0, l);
-      const bool in = c < D;
-      load8(p, TYPE_F32, at + (in ? c : 0), f[v]);
+      for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[v][e] = in ? f[v][e] : 0.0f;
+        for (int h = 0; h < 2; ++h) r.q[2 * v + h] = load16<4, w>(p, at, col_of<TYPE, G>(v, 4 * h, l), D);
+#pragma unroll
+      for (int v = 0; v < V; ++v) raw_vals<TYPE_F32, V>(r, v, f[v]);
     }
-  } else {
+  };
+  if constexpr (!VEC) {
+    load(std::false_type{});
+  } else if (whole) {
+    load(std::true_type{});
+  } else {                                        // (whole vectors of rows beside unaligned gains)
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int c = col_of<TYPE, G, VEC>(v, e, l);
+        const int c = col_of<TYPE, G>(v, e, l);
         const bool in = c < D;
         const float got = load_as_f32(p, PARAM, at + (in ? c : 0));
         f[v][e] = in ? got : 0.0f;
@@ -186,11 +217,11 @@ __device__ __forceinline__ void load_param(float (&f)[V][8], const void *p, int 
 
 // ---- forward -------------------------------------------------------------------------------------------------------
 
-// nb blocks per replica; a group takes every (nb 256 / G)-th row
+// nb blocks per replica; a group takes every (nb GP)-th row
 template <int TYPE, int G, int V, bool VEC>
-__global__ void __launch_bounds__(256) ln_forward_kernel(const LayerNormP p, const int nb) {
-  constexpr int GP = 256 / G;
-  __shared__ __attribute__((aligned(16))) float sm[8];
+__global__ void __launch_bounds__(ln_threads(G)) ln_forward_kernel(const LayerNormP p, const int nb) {
+  constexpr int GP = ln_threads(G) / G;
+  __shared__ __attribute__((aligned(16))) float sm[ln_threads(G) / 32];
   const int m = blockIdx.x / nb, j = blockIdx.x - m * nb, gid = threadIdx.x / G, l = threadIdx.x % G;
   const long long rows = (long long)p.b * p.T;
   const int D = p.D;
@@ -220,7 +251,7 @@ __global__ void __launch_bounds__(256) ln_forward_kernel(const LayerNormP p, con
     for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float d = col_of<TYPE, G, VEC>(v, e, l) < D ? x[v][e] - mean : 0.0f;
+        const float d = col_of<TYPE, G>(v, e, l) < D ? x[v][e] - mean : 0.0f;
         x[v][e] = d;
         s[0] = fmaf(d, d, s[0]);
       }
@@ -270,22 +301,22 @@ __global__ void __launch_bounds__(256) ln_forward_long_kernel(const LayerNormP p
 
 enum { STAT_NONE = 0, STAT_ROW = 1, STAT_SAMPLE = 2 };   // n_i: not here; of samples that are one row; of samples of several
 
-// How the rows of a replica are dealt to its nb blocks: `per` whole samples each (chunks == 1; without statistics every row is a
-// sample), or a sample's rows in `chunks` blocks of `per` rows.
+// How the rows of a replica are dealt to its nb blocks: `per` whole samples each, a sample to a group (chunks == 0; without statistics
+// every row is a sample), or a sample's rows in `chunks` blocks of `per` rows.
 struct LnSplit {
   int samples, T, nb, chunks, per;
   int tiles;             // column tiles of a row longer than a block's registers
   float *part;           // [M nb][2][D] partial sums of dy xh and dy
-  float *npart;          // [tiles][M samples] partial n (tiles > 1 or chunks > 1)
+  float *npart;          // [tiles][M samples] partial n (tiles > 1 or chunks > 0)
   const float *sums;     // [M rows][2] mean_d h, mean_d(h xh) of long rows
 };
 
 template <int TYPE, int G, int V, bool VEC, int R, int STAT, bool LONG>
-__global__ void __launch_bounds__(256, V == 1 && TYPE != TYPE_F32 && STAT != STAT_SAMPLE ? 4 : 1) ln_backward_kernel(const LayerNormP p, const LnSplit w) {
-  constexpr int GP = 256 / G;
+__global__ void __launch_bounds__(ln_threads(G), V == 1 && TYPE != TYPE_F32 && STAT != STAT_SAMPLE ? 4 : 1) ln_backward_kernel(const LayerNormP p, const LnSplit w) {
+  constexpr int GP = ln_threads(G) / G;
   constexpr int NS = STAT == STAT_NONE ? 2 : 3;
   static_assert(!LONG || G == 256, "a tile of a long row is a block's");
-  __shared__ __attribute__((aligned(16))) float sm[2 * R * NS * 4];
+  __shared__ __attribute__((aligned(16))) float sm[2 * R * NS * (ln_threads(G) / 64)];
   __shared__ float comb[GP > 1 ? GP * G * V * 8 : 1];
   const int bid = LONG ? blockIdx.x / w.tiles : blockIdx.x, tile = LONG ? blockIdx.x - bid * w.tiles : 0;
   const int m = bid / w.nb, j = bid - m * w.nb, gid = threadIdx.x / G, l = threadIdx.x % G;
@@ -295,7 +326,7 @@ __global__ void __launch_bounds__(256, V == 1 && TYPE != TYPE_F32 && STAT != STA
   // the group's rows: count of them, the q-th at row(q); samples end where t == T - 1
   long long first, count, hop;
   const int T = w.T;
-  if (w.chunks > 1) {
+  if (w.chunks > 0) {
     const int i = j / w.chunks, ch = j - i * w.chunks;
     const long long r0 = (long long)i * T + (long long)ch * w.per, r1 = min(r0 + w.per, (long long)(i + 1) * T);
     first = r0 + gid;
@@ -383,7 +414,8 @@ __global__ void __launch_bounds__(256, V == 1 && TYPE != TYPE_F32 && STAT != STA
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       if (at[k] < 0) continue;
-      if (V <= 2) { forget(rx[k]); forget(ry[k]); }      // (two work-groups to a CU and more: 205 -> 190 us; rows of 8192 have one either way, 120 -> 171)
+      forget(rx[k]);                              // (more work-groups to a CU: rows of 2048 205 -> 190 us)
+      forget(ry[k]);
       float a = s[k * NS] * inv, c = s[k * NS + 1] * inv;
       if (LONG) { a = w.sums[(m * rows + at[k]) * 2]; c = w.sums[(m * rows + at[k]) * 2 + 1]; }
       if (STAT != STAT_NONE && ends[k] && l == 0) {
@@ -414,7 +446,7 @@ __global__ void __launch_bounds__(256, V == 1 && TYPE != TYPE_F32 && STAT != STA
       for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int c = col_of<TYPE, G, VEC>(v, e, l);
+          const int c = col_of<TYPE, G>(v, e, l);
           if (c < D) out[(long long)h * p.D + c] = h ? tb[v][e] : tw[v][e];
         }
     } else {
@@ -422,7 +454,7 @@ __global__ void __launch_bounds__(256, V == 1 && TYPE != TYPE_F32 && STAT != STA
 #pragma unroll
       for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) comb[gid * G * V * 8 + col_of<TYPE, G, VEC>(v, e, l)] = h ? tb[v][e] : tw[v][e];
+        for (int e = 0; e < 8; ++e) comb[gid * G * V * 8 + col_of<TYPE, G>(v, e, l)] = h ? tb[v][e] : tw[v][e];
       __syncthreads();
       for (int c = threadIdx.x; c < D; c += 256) {
         float a = 0.0f;
@@ -456,6 +488,7 @@ __global__ void __launch_bounds__(256) ln_sample_kernel(const LayerNormP p, cons
   float *part = w.part + (long long)i * w.chunks * 2 * p.D;
   float g = 0.0f;
   if (c < 2 * p.D) {
+#pragma unroll 8
     for (int k = 0; k < w.chunks; ++k) g += part[(long long)k * 2 * p.D + c];
     part[c] = g;
   }
@@ -512,11 +545,11 @@ __global__ void __launch_bounds__(256) ln_inner_partials_kernel(const LayerNormP
 }
 
 // q_i from a second look at the rows: sum_t sum_d dy (xh gbar_gamma + gbar_beta).  gbar stays in a group's registers, which takes
-// every (nb 256 / G)-th sample of a replica.
+// every (nb GP)-th sample of a replica.
 template <int TYPE, int G, int V, bool VEC>
-__global__ void __launch_bounds__(256) ln_inner_rows_kernel(const LayerNormP p, const int nb) {
-  constexpr int GP = 256 / G;
-  __shared__ __attribute__((aligned(16))) float sm[8];
+__global__ void __launch_bounds__(ln_threads(G)) ln_inner_rows_kernel(const LayerNormP p, const int nb) {
+  constexpr int GP = ln_threads(G) / G;
+  __shared__ __attribute__((aligned(16))) float sm[ln_threads(G) / 32];
   const int m = blockIdx.x / nb, j = blockIdx.x - m * nb, gid = threadIdx.x / G, l = threadIdx.x % G, D = p.D;
   const long long rows = (long long)p.b * p.T;
   float gw[V][8], gb[V][8];
@@ -567,35 +600,50 @@ __global__ void __launch_bounds__(256) ln_inner_long_kernel(const LayerNormP p) 
 // ---- choices -------------------------------------------------------------------------------------------------------
 
 constexpr int LN_MAX_D = 8192;           // longest row that a block's registers hold
-// Blocks of 256 threads of the backward pass: two to a CU.  Their loads keep memory as busy as those of more blocks, which leave
+// Blocks of the backward pass: two to a CU of 256 threads, one of 512.  Their loads keep memory as busy as those of more blocks, which leave
 // more partials and, where registers hold only two or three of them on a CU, a last round (8 x 8192 rows of 2048: 512 blocks 170 us, 768
 // 184, 1024 176; 4 x 4096 rows of 4096 98, 107, 118).
 constexpr int LN_BLOCKS = 512;
 
-// lanes and vectors to a row: 16 x 1, 64 x 1, 64 x 2, 256 x 1, 256 x 2, 256 x 4
+// lanes and vectors to a row: 16 x 1, 64 x 1, 64 x 2, 256 x 1, 256 x 2, 512 x 2 (256 x 4 fill the registers with one row: gradients of
+// 2 x 8 x 512 rows of 8192 in bf16 114 us, here 99; 5 x 219 x 13 of 4507 in fp16 with q_i 465, here 280)
 int ln_shape(int D) { return D <= 128 ? 0 : D <= 512 ? 1 : D <= 1024 ? 2 : D <= 2048 ? 3 : D <= 4096 ? 4 : 5; }
 int ln_groups(int D) { return D <= 128 ? 16 : D <= 1024 ? 4 : 1; }      // to a block
+int ln_rows_at_once(int D) { return D > LN_MAX_D ? 4 : D > 2048 ? 2 : D > 1024 ? 4 : D > 512 ? 2 : 4; }      // of a group, backward
 
-LnSplit ln_split(const LayerNormP &p, bool want) {
+int ln_sample_tiles(const LayerNormP &p) { return (2 * p.D + 255) / 256; }
+
+LnSplit ln_split(const LayerNormP &p, bool want, bool want_q) {
   LnSplit w;
   std::memset(&w, 0, sizeof(w));
-  const long long rows = (long long)p.b * p.T;
+  const long long rows = (long long)p.b * p.T, all = (long long)p.M * p.b;
+  const int groups = ln_groups(p.D), once = ln_rows_at_once(p.D);
   w.tiles = p.D > LN_MAX_D ? (p.D + 2047) / 2048 : 1;
-  const long long most = std::max(1, LN_BLOCKS / std::min(LN_BLOCKS, p.M * w.tiles));
-  const long long few = (p.D <= 512 || p.D > 1024 ? 4LL : 2LL) * ln_groups(p.D);       // rows of a block at least: one round of its groups' loads
-  w.samples = want ? p.b : (int)rows; w.T = want ? p.T : 1; w.chunks = 1;
-  if (want && w.T >= 8 * few && p.b * 2LL <= most) {                    // few long samples: several blocks to each
-    w.chunks = (int)std::max(1LL, std::min((w.T + 4 * few - 1) / (4 * few), most / p.b));
-    w.per = (w.T + w.chunks - 1) / w.chunks;
+  // (blocks of 512 threads are alone on their CU)
+  const long long blocks = std::max(1, LN_BLOCKS / (w.tiles > 1 ? w.tiles : p.D > 4096 ? 2 : 1)), most = std::max(1LL, blocks / p.M);
+  const long long few = (long long)once * groups;            // rows of a block at least: one round of its groups' loads
+  w.samples = want ? p.b : (int)rows; w.T = want ? p.T : 1;
+  // Blocks to a sample, whose partials a further launch adds, or samples to a group: what the partials cost (a launch, and bytes as five rows
+  // have) against groups left idle, and against the second look at the rows that q_i takes otherwise.  us, blocks to a sample against samples
+  // to a group: n_i of 5 x 2 samples of 124 rows of 345 14 / 106, 12 x 90 of 227 of 251 172 / 325, 16 x 64 of 64 of 512 42 / 52, but 8 x 32 of
+  // 16 of 2048 28 / 22 and 16 x 512 of 64 of 96 66 / 60; with q_i 16 x 512 of 32 of 512 191 / 255, 16 x 128 of 64 of 512 85 / 119, but
+  // 16 x 1024 of 32 of 96 98 / 91.
+  const bool idle = w.T >= 4 * once && all * (w.T >= 32 || groups > 1 ? 2 : 4) <= blocks * groups, less = w.T >= 128 && all <= blocks * groups;
+  const bool fits = all * ln_sample_tiles(p) <= 1 << 23;     // (a grid counts its threads in 32 bits)
+  if (want && fits && (idle || less || (want_q && w.T >= 32 && w.T >= few))) {
+    // one round of rows to each of sixteen blocks, then up to four
+    const long long rounds = (w.T + few - 1) / few;
+    w.chunks = (int)std::max(1LL, std::min(blocks / all, std::min(rounds, std::max(16LL, (rounds + 3) / 4))));
+    w.per = (int)((w.T + (long long)w.chunks - 1) / w.chunks);
     w.chunks = (int)((w.T + (long long)w.per - 1) / w.per);
-    if (w.chunks > 1) { w.nb = w.samples * w.chunks; return w; }
+    w.nb = w.samples * w.chunks;
+    return w;
   }
   const long long nb = std::max(1LL, std::min(most, (rows + few - 1) / few));
   w.per = (int)((w.samples + nb - 1) / nb);
   w.nb = (int)((w.samples + (long long)w.per - 1) / w.per);
   return w;
 }
-int ln_sample_tiles(const LayerNormP &p) { return (2 * p.D + 255) / 256; }
 
 struct LnPieces { size_t part, npart, sums, total; };
 LnPieces ln_pieces(const LayerNormP &p, const LnSplit &w, bool want_n) {
@@ -603,7 +651,7 @@ LnPieces ln_pieces(const LayerNormP &p, const LnSplit &w, bool want_n) {
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t r = o; o = (o + bytes + 255) / 256 * 256; return r; };
   q.part = take((size_t)p.M * w.nb * 2 * p.D * 4);
-  q.npart = take(want_n ? (size_t)p.M * p.b * 4 * (w.chunks > 1 ? ln_sample_tiles(p) : w.tiles > 1 ? w.tiles : 0) : 0);
+  q.npart = take(want_n ? (size_t)p.M * p.b * 4 * (w.chunks > 0 ? ln_sample_tiles(p) : w.tiles > 1 ? w.tiles : 0) : 0);
   q.sums = take(w.tiles > 1 ? (size_t)p.M * p.b * p.T * 8 : 0);
   q.total = o;
   return q;
@@ -613,8 +661,8 @@ template <int TYPE, int G, int V, bool VEC, int R, bool LONG>
 hipError_t backward_stat(const LayerNormP &p, const LnSplit &w, bool want_n, hipStream_t s) {
   const long long blocks = (long long)p.M * w.nb * w.tiles;
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks), block(256);
-  if (!want_n || w.chunks > 1) hipLaunchKernelGGL((ln_backward_kernel<TYPE, G, V, VEC, R, STAT_NONE, LONG>), grid, block, 0, s, p, w);
+  const dim3 grid((unsigned)blocks), block(ln_threads(G));
+  if (!want_n || w.chunks > 0) hipLaunchKernelGGL((ln_backward_kernel<TYPE, G, V, VEC, R, STAT_NONE, LONG>), grid, block, 0, s, p, w);
   else if (w.T == 1) hipLaunchKernelGGL((ln_backward_kernel<TYPE, G, V, VEC, R, STAT_ROW, LONG>), grid, block, 0, s, p, w);
   else hipLaunchKernelGGL((ln_backward_kernel<TYPE, G, V, VEC, R, STAT_SAMPLE, LONG>), grid, block, 0, s, p, w);
   return hipGetLastError();
@@ -628,7 +676,7 @@ hipError_t backward_shape(const LayerNormP &p, const LnSplit &w, bool want_n, hi
     case 2: return backward_stat<TYPE, 64, 2, VEC, 2, false>(p, w, want_n, s);
     case 3: return backward_stat<TYPE, 256, 1, VEC, 4, false>(p, w, want_n, s);
     case 4: return backward_stat<TYPE, 256, 2, VEC, 2, false>(p, w, want_n, s);
-    default: return backward_stat<TYPE, 256, 4, VEC, 1, false>(p, w, want_n, s);
+    default: return backward_stat<TYPE, 512, 2, VEC, 2, false>(p, w, want_n, s);
   }
 }
 
@@ -638,14 +686,14 @@ int ln_row_blocks(const LayerNormP &p, long long items, int groups) {
 }
 struct Forward {
   template <int TYPE, int G, int V, bool VEC> static void go(const LayerNormP &p, hipStream_t s) {
-    const int nb = ln_row_blocks(p, (long long)p.b * p.T, 256 / G);
-    hipLaunchKernelGGL((ln_forward_kernel<TYPE, G, V, VEC>), dim3((unsigned)((long long)nb * p.M)), dim3(256), 0, s, p, nb);
+    const int nb = ln_row_blocks(p, (long long)p.b * p.T, ln_threads(G) / G);
+    hipLaunchKernelGGL((ln_forward_kernel<TYPE, G, V, VEC>), dim3((unsigned)((long long)nb * p.M)), dim3(ln_threads(G)), 0, s, p, nb);
   }
 };
 struct Inner {
   template <int TYPE, int G, int V, bool VEC> static void go(const LayerNormP &p, hipStream_t s) {
-    const int nb = ln_row_blocks(p, p.b, 256 / G);
-    hipLaunchKernelGGL((ln_inner_rows_kernel<TYPE, G, V, VEC>), dim3((unsigned)((long long)nb * p.M)), dim3(256), 0, s, p, nb);
+    const int nb = ln_row_blocks(p, p.b, ln_threads(G) / G);
+    hipLaunchKernelGGL((ln_inner_rows_kernel<TYPE, G, V, VEC>), dim3((unsigned)((long long)nb * p.M)), dim3(ln_threads(G)), 0, s, p, nb);
   }
 };
 template <class K, int TYPE, bool VEC> void by_shape(const LayerNormP &p, hipStream_t s) {
@@ -655,7 +703,7 @@ template <class K, int TYPE, bool VEC> void by_shape(const LayerNormP &p, hipStr
     case 2: return K::template go<TYPE, 64, 2, VEC>(p, s);
     case 3: return K::template go<TYPE, 256, 1, VEC>(p, s);
     case 4: return K::template go<TYPE, 256, 2, VEC>(p, s);
-    default: return K::template go<TYPE, 256, 4, VEC>(p, s);
+    default: return K::template go<TYPE, 512, 2, VEC>(p, s);
   }
 }
 template <class K> hipError_t by_type(const LayerNormP &p, bool vec, hipStream_t s) {
@@ -670,7 +718,7 @@ template <class K> hipError_t by_type(const LayerNormP &p, bool vec, hipStream_t
 }  // namespace
 
 size_t layer_norm_backward_bytes(const LayerNormP &p, bool want_n, bool want_q) {
-  return ln_pieces(p, ln_split(p, want_n || want_q), want_n).total;
+  return ln_pieces(p, ln_split(p, want_n || want_q, want_q), want_n).total;
 }
 
 hipError_t launch_layer_norm(const LayerNormP &p, hipStream_t s) {
@@ -688,7 +736,7 @@ hipError_t launch_layer_norm_backward(const LayerNormP &p, void *workspace, hipS
   const long long rows = (long long)p.b * p.T;
   if (rows * p.M > 0x7fffffff) return hipErrorInvalidValue;
   const bool want_n = p.n != nullptr, want = want_n || p.q;
-  LnSplit w = ln_split(p, want);
+  LnSplit w = ln_split(p, want, p.q != nullptr);
   const LnPieces at = ln_pieces(p, w, want_n);
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   w.part = reinterpret_cast<float *>(ws + at.part);
@@ -708,7 +756,7 @@ hipError_t launch_layer_norm_backward(const LayerNormP &p, void *workspace, hipS
   }
   if (e != hipSuccess) return e;
   int nshares = 0;
-  if (w.chunks > 1) {
+  if (w.chunks > 0) {
     nshares = ln_sample_tiles(p);
     hipLaunchKernelGGL(ln_sample_kernel, dim3((unsigned)((long long)p.M * p.b * nshares)), dim3(256), 0, s, p, w, nshares);
     if (!want_n) nshares = 0;
@@ -716,11 +764,11 @@ hipError_t launch_layer_norm_backward(const LayerNormP &p, void *workspace, hipS
     nshares = w.tiles;
   }
   const int colblocks = (2 * p.D + 63) / 64;
-  const int count = w.chunks > 1 ? w.samples : w.nb;
+  const int count = w.chunks > 0 ? w.samples : w.nb, step = std::max(1, w.chunks);
   const long long nblocks = nshares ? ((long long)p.M * p.b + FIN * 64 - 1) / (FIN * 64) : 0;
-  hipLaunchKernelGGL(ln_finish_kernel, dim3((unsigned)((long long)colblocks * p.M + nblocks)), dim3(FIN * 64), 0, s, p, w, count, w.chunks, colblocks, nshares);
+  hipLaunchKernelGGL(ln_finish_kernel, dim3((unsigned)((long long)colblocks * p.M + nblocks)), dim3(FIN * 64), 0, s, p, w, count, step, colblocks, nshares);
   if (p.q) {
-    if (w.chunks > 1) hipLaunchKernelGGL(ln_inner_partials_kernel, dim3((unsigned)((long long)p.M * p.b)), dim3(256), 0, s, p, w);
+    if (w.chunks > 0) hipLaunchKernelGGL(ln_inner_partials_kernel, dim3((unsigned)((long long)p.M * p.b)), dim3(256), 0, s, p, w);
     else if (p.D > LN_MAX_D) hipLaunchKernelGGL(ln_inner_long_kernel, dim3((unsigned)(((long long)p.M * p.b + 3) / 4)), dim3(256), 0, s, p);
     else return by_type<Inner>(p, vec, s);
   }

@@ -622,7 +622,8 @@ def test_layer_norm_gradient_against_differences():
 def test_layer_norm_of_strided_rows():
     import torch
     A = _A()
-    for D, ld, off in ((24, 24, 1), (40, 48, 0), (33, 37, 2), (264, 272, 8), (600, 601, 0)):
+    for D, ld, off in ((24, 24, 1), (40, 48, 0), (33, 37, 2), (264, 272, 8), (600, 601, 0),
+                       (3, 5, 1), (7, 7, 3), (9, 11, 1), (1501, 1503, 1), (5001, 5001, 2), (8190, 8191, 1)):
         M, b, T = 2, 3, 4
         big = torch.randn(off + M * (b * T * ld + 5), device="cuda", generator=torch.Generator("cuda").manual_seed(D)).to(torch.bfloat16)
         x = big[off:].as_strided((M, b, T, D), (b * T * ld + 5, T * ld, ld, 1))
