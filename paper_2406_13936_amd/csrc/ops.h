@@ -63,6 +63,10 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
 // orthogonalize_small.hip: a work-group's LDS holds the matrix
 bool orth_small_fits(int rows, int cols);
 hipError_t launch_orth_small(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, hipStream_t s);
+// or not, but the smaller side is short: the norm's partial sums are there already
+bool orth_slices_fit(int batch, int rows, int cols);
+size_t orth_slices_bytes(const OrthPlan &pl, size_t &o_x, size_t &o_a, size_t &o_part);
+hipError_t launch_orth_slices(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, const double *norm, unsigned char *ws, hipStream_t s);
 
 // ---- layer norm ----------------------------------------------------------------------------------------------------
 

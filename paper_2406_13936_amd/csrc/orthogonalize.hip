@@ -573,7 +573,7 @@ struct OrthShape { int tile, groups, ring; };
 OrthShape choose_shape(int Md, int Nd, int K, int batch, int sym) {
   const long long t256 = tile_count(Md, Nd, batch, sym, 256), t128 = tile_count(Md, Nd, batch, sym, 128), t64 = tile_count(Md, Nd, batch, sym, 64);
   if (t64 <= 384) return {64, 2, t64 <= 256 ? 4 : 2};
-  if (Md > 128 && Nd > 128 && K >= 512 && 1.5 * (double)((t256 + 255) / 256) <= rounds_128(t128)) return {256, 1, 2};
+  if (K >= 512 && 1.5 * (double)((t256 + 255) / 256) <= rounds_128(t128)) return {256, 1, 2};
   return {128, t128 <= 256 ? 2 : 1, 2};
 }
 
@@ -657,6 +657,12 @@ const char *orth_plan(int batch, int rows, int cols, int split, int steps, const
   auto take = [&](size_t bytes) { const size_t r = o; o = (o + bytes + 255) / 256 * 256; return r; };
   const size_t xb = (size_t)batch * pl.rp * pl.cp * (pl.split ? 4 : 2), ab = (size_t)batch * pl.mp * pl.mp * (pl.split ? 4 : 2);
   pl.o_part = take((size_t)batch * pl.nparts * 8);
+  if (orth_slices_fit(batch, rows, cols)) {
+    size_t x, a, part;
+    pl.o_x[0] = take(orth_slices_bytes(pl, x, a, part));
+    pl.total = o;
+    return nullptr;
+  }
   for (int i = 0; i < 2; ++i) pl.o_x[i] = take(xb);
   pl.o_xl = pl.split ? 0 : take(xb);                // (no product reads it: each entry is replaced where it was read)
   pl.o_a = take(ab); pl.o_b = take(ab);
@@ -667,6 +673,7 @@ const char *orth_plan(int batch, int rows, int cols, int split, int steps, const
 
 hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, void *workspace, hipStream_t s) {
   if (orth_small_fits(pl.rows, pl.cols)) return launch_orth_small(pl, in, out, eps, s);
+  const bool slices = orth_slices_fit(pl.batch, pl.rows, pl.cols);
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   auto at = [&](size_t off) { return reinterpret_cast<uint16_t *>(ws + off); };
   const int f = pl.split ? 2 : 1, ldx = f * pl.cp, lda = f * pl.mp;
@@ -684,10 +691,11 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
     b.part += (long long)z0 * pl.nparts; b.xh += z0 * sx;
     if (b.xl) b.xl += z0 * sx;
     hipLaunchKernelGGL(orth_norm_kernel, dim3(pl.nparts, nz), dim3(256), 0, s, b);
-    hipLaunchKernelGGL(orth_prep_kernel, dim3((pl.rp * (pl.cp / 8) + 1023) / 1024, nz), dim3(256), 0, s, b);
+    if (!slices) hipLaunchKernelGGL(orth_prep_kernel, dim3((pl.rp * (pl.cp / 8) + 1023) / 1024, nz), dim3(256), 0, s, b);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
+  if (slices) return launch_orth_slices(pl, in, out, eps, q.part, ws + pl.o_x[0], s);
   for (int k = 0; k < pl.steps; ++k) {
     const uint16_t *x = at(pl.o_x[k & 1]);
     OrthGemmP p;

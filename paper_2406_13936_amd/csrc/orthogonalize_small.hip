@@ -77,11 +77,13 @@ __device__ __forceinline__ void get4(const uint16_t *hi, const uint16_t *lo, flo
 __device__ __forceinline__ f32x4 mfma_split(f16x8 ph, f16x8 pl, f16x8 qh, f16x8 ql, f32x4 c) { return mfma16(ph, qh, mfma16(pl, qh, mfma16(ph, ql, c))); }
 
 // C = alpha C_old + beta R R^T for the NT x NT tiles of 16 x 16, R = rh + rl with K values (a multiple of 32) to a row.  SELF: C is R, and
-// its old value counts.  A wavefront has tiles of one row of tiles (the fragments of that row are read once), or, where there are
+// its old value counts.  PART: C is fp32 in memory, 16 NT values to a row.  A wavefront has tiles of one row of tiles (the fragments of that row are read once), or, where there are
 // fewer tiles than wavefronts, a share of a tile's reduction; shares are added in order.
-template <int NT, bool SELF>
+enum { GRAM_NEW = 0, GRAM_SELF = 1, GRAM_PART = 2 };
+template <int NT, int KIND>
 __device__ __forceinline__ void gram(const uint16_t *rh, const uint16_t *rl, int ldr, int K, uint16_t *ch, uint16_t *cl, int ldc,
-                                     float alpha, float beta, float *red) {
+                                     float alpha, float beta, float *red, float *part = nullptr) {
+  constexpr bool SELF = KIND == GRAM_SELF;
   constexpr int SHARES = NT == 1 ? 8 : NT == 2 ? 2 : 1;    // of a reduction
   constexpr int PER = NT == 4 ? 2 : 1;                     // wavefronts to a row of tiles
   constexpr int TILES = SHARES > 1 ? 1 : NT / PER;         // of a wavefront, PER apart
@@ -129,6 +131,10 @@ __device__ __forceinline__ void gram(const uint16_t *rh, const uint16_t *rl, int
   if (writes) {
 #pragma unroll
     for (int j = 0; j < TILES; ++j) {
+      if (KIND == GRAM_PART) {
+        *reinterpret_cast<f32x4 *>(part + (ti * 16 + i16) * (NT * 16) + (t0 + j * PER) * 16 + g16 * 4) = acc[j];
+        continue;
+      }
       const float v[4] = {acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
       put4(ch + at + j * PER * 16, cl + at + j * PER * 16, v);
     }
@@ -136,10 +142,11 @@ __device__ __forceinline__ void gram(const uint16_t *rh, const uint16_t *rl, int
   __syncthreads();
 }
 
-// X' = ax X + bx B X, or the result of the last step.  SHARE wavefronts to a block of 16 columns, each with some of its tiles.
+// X' = ax X + bx B X, or the result of the last step, for n columns that are columns n0 .. of the matrix.  SHARE wavefronts to a block of
+// 16 columns, each with some of its tiles.
 template <int NT, int SHARE>
 __device__ __forceinline__ void apply(const OrthSmallP &p, int z, uint16_t *xh, uint16_t *xl, int ldx, const uint16_t *bh, const uint16_t *bl,
-                                      int ldb, int m, int n, int mp, float ax, float bx, bool last) {
+                                      int ldb, int m, int n, int n0, int mp, float ax, float bx, bool last) {
   constexpr int TILES = (NT + SHARE - 1) / SHARE;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = lane & 15, g16 = lane >> 4, nb = (n + 15) >> 4, t0 = wave % SHARE * TILES;
@@ -182,7 +189,7 @@ __device__ __forceinline__ void apply(const OrthSmallP &p, int z, uint16_t *xh, 
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if (i >= m || c + e >= n) continue;
-          const int r = p.wide ? i : c + e, q = p.wide ? c + e : i;
+          const int r = p.wide ? i : n0 + c + e, q = p.wide ? n0 + c + e : i;
           const long long at = z * p.out.so + (long long)r * p.out.ldo + q;
           const float v = p.out.update ? fmaf(decay, load_as_f32(p.out.o, p.out.type, at), -gain * acc[j][e]) : acc[j][e];
           store_from_f32(p.out.o, p.out.type, at, v);
@@ -261,13 +268,23 @@ __global__ void __launch_bounds__(SM_THREADS) orth_small_kernel(const OrthSmallP
   for (int k = 0; k < p.steps; ++k) {
     const OrthScale s = sc[k];
     const bool last = k + 1 == p.steps;
-    gram<NT, false>(xh, xl, ldx, np, ah, al, lda, 0.0f, s.gram, red);
-    gram<NT, true>(ah, al, lda, mp, ah, al, lda, s.poly_a, s.poly_aa, red);
+    gram<NT, GRAM_NEW>(xh, xl, ldx, np, ah, al, lda, 0.0f, s.gram, red);
+    gram<NT, GRAM_SELF>(ah, al, lda, mp, ah, al, lda, s.poly_a, s.poly_aa, red);
     // two wavefronts to a block of 16 columns where there are no more than four of these
     constexpr bool TWO = NT == 2 || NT == 4;
-    if (TWO && n <= 64) apply<NT, TWO ? 2 : 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
-    else apply<NT, 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, mp, s.apply_x, s.apply_bx, last);
+    if (TWO && n <= 64) apply<NT, TWO ? 2 : 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, 0, mp, s.apply_x, s.apply_bx, last);
+    else apply<NT, 1>(p, z, xh, xl, ldx, ah, al, lda, m, n, 0, mp, s.apply_x, s.apply_bx, last);
   }
+}
+
+// The same from matrix z0 on
+OrthSmallP from_matrix(const OrthSmallP &p, int z0) {
+  OrthSmallP q = p;
+  q.in.g = static_cast<const unsigned char *>(p.in.g) + z0 * p.in.sg * type_bytes(p.in.type);
+  if (p.in.v) q.in.v = p.in.v + z0 * p.in.sv;
+  q.out.o = static_cast<unsigned char *>(p.out.o) + z0 * p.out.so * type_bytes(p.out.type);
+  if (p.out.shadow) q.out.shadow = p.out.shadow + z0 * p.out.sshadow;
+  return q;
 }
 
 template <int NT> hipError_t launch_nt(const OrthSmallP &p, int batch, size_t lds, hipStream_t s) {
@@ -275,12 +292,124 @@ template <int NT> hipError_t launch_nt(const OrthSmallP &p, int batch, size_t ld
   hipError_t err = allow_lds(reinterpret_cast<const void *>(orth_small_kernel<NT>), SM_LDS, done);
   constexpr int MOST = 1 << 22;                            // matrices of a launch: a grid counts its threads in 32 bits
   for (int z0 = 0; z0 < batch && err == hipSuccess; z0 += std::min(MOST, batch - z0)) {
-    OrthSmallP q = p;
-    q.in.g = static_cast<const unsigned char *>(p.in.g) + z0 * p.in.sg * type_bytes(p.in.type);
-    if (p.in.v) q.in.v = p.in.v + z0 * p.in.sv;
-    q.out.o = static_cast<unsigned char *>(p.out.o) + z0 * p.out.so * type_bytes(p.out.type);
-    if (p.out.shadow) q.out.shadow = p.out.shadow + z0 * p.out.sshadow;
-    hipLaunchKernelGGL(orth_small_kernel<NT>, dim3(std::min(MOST, batch - z0)), dim3(SM_THREADS), lds, s, q);
+    hipLaunchKernelGGL(orth_small_kernel<NT>, dim3(std::min(MOST, batch - z0)), dim3(SM_THREADS), lds, s, from_matrix(p, z0));
+    err = hipGetLastError();
+  }
+  return err;
+}
+
+// ---- few rows, many columns ----------------------------------------------------------------------------------------
+//
+// A smaller side of up to 128 beside one that LDS does not hold: slices of SLICE columns (of the longer side), a work-group to each.  A
+// step needs A of all slices and leaves every slice to itself otherwise, so it is two launches: one adds the slices' shares of A,
+// in order; the other forms B (every work-group for itself: its A is in LDS, and 64 MFMAs of a wavefront are shorter than a launch),
+// replaces its columns of X and leaves their share of the next A.  5 steps, replayed from a graph, against the tiles of
+// orthogonalize.hip: 10 of 36 x 2972 80 us against 207, 1 of 25 x 2365 46 / 143, 3 of 2858 x 50 68 / 169, 2 of 16 x 100000 144 / 3627.
+// Bound by its launches (4 to 5 us each); 512 of 32 x 2048 (453 / 860) by reading and writing X once a step.
+constexpr int SLICE = 128, SLICE_LD = SLICE + 8;
+
+struct OrthSliceP {
+  OrthSmallP q;
+  int slices, nparts, k;                                   // k: the step; -1: X_0 and its share of A
+  const double *norm;                                      // [batch][nparts]
+  uint16_t *x, *a;                                         // [batch][slices][2][mp][SLICE_LD], [batch][2][mp][mp + 8], as in LDS
+  float *part;                                             // [batch][slices][16 NT][16 NT]
+};
+
+template <int NT>
+__global__ void __launch_bounds__(SM_THREADS) orth_slice_kernel(const OrthSliceP p) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+  __shared__ double sm[SM_WAVES];
+  __shared__ double norm2;
+  constexpr int mp = NT == 1 ? 32 : NT * 16, lda = mp + 8, ldx = SLICE_LD, XB = mp * ldx / 4, AB = mp * lda / 4;      // 16-byte pieces of both parts
+  const int z = blockIdx.x / p.slices, j = blockIdx.x - z * p.slices, tid = threadIdx.x;
+  const int m = min(p.q.rows, p.q.cols), n0 = j * SLICE, n = min(SLICE, max(p.q.rows, p.q.cols) - n0);
+  uint16_t *xh = reinterpret_cast<uint16_t *>(smem_raw), *xl = xh + mp * ldx, *ah = xl + mp * ldx, *al = ah + mp * lda;
+  float *red = reinterpret_cast<float *>(al + mp * lda);
+  uint4 *xs = reinterpret_cast<uint4 *>(xh), *xg = reinterpret_cast<uint4 *>(p.x) + (long long)blockIdx.x * XB;
+  const bool last = p.k + 1 == p.q.steps;
+  if (p.k < 0) {
+    for (int i = tid; i < XB; i += SM_THREADS) xs[i] = make_uint4(0, 0, 0, 0);
+    const double sum = block_sum<SM_WAVES>(tid < p.nparts ? p.norm[(long long)z * p.nparts + tid] : 0.0, sm);
+    if (tid == 0) norm2 = sum;
+    __syncthreads();
+    const double scale = (double)p.q.first / (sqrt(norm2) + (double)p.q.eps);
+    const int r0 = p.q.wide ? 0 : n0, c0 = p.q.wide ? n0 : 0;
+    const int cc = p.q.wide ? SLICE / 8 : (p.q.cols + 7) >> 3, chunks = (p.q.wide ? p.q.rows : n) * cc;
+    for (int i = tid; i < chunks; i += SM_THREADS) {
+      const int r = i / cc, c = (i - r * cc) * 8;
+      float u[8];
+      load_u8<false>(p.q.in, p.q.rows, p.q.cols, p.q.vec, z, r0 + r, c0 + c, u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (c0 + c + e >= p.q.cols) break;
+        const float v = (float)((double)u[e] * scale);
+        const uint16_t h = f16_bits(v);
+        const int o = p.q.wide ? r * ldx + c + e : (c + e) * ldx + r;
+        xh[o] = h;
+        xl[o] = f16_bits(v - f16_val(h));
+      }
+    }
+  } else {
+    uint4 *as = reinterpret_cast<uint4 *>(ah);
+    const uint4 *ag = reinterpret_cast<const uint4 *>(p.a) + (long long)z * AB;
+#pragma unroll 4
+    for (int i = tid; i < AB; i += SM_THREADS) as[i] = ag[i];
+#pragma unroll 4
+    for (int i = tid; i < XB; i += SM_THREADS) xs[i] = xg[i];
+    __syncthreads();
+    const OrthScale s = p.q.sc[p.k];
+    gram<NT, GRAM_SELF>(ah, al, lda, mp, ah, al, lda, s.poly_a, s.poly_aa, red);
+    apply<NT, 1>(p.q, z, xh, xl, ldx, ah, al, lda, m, n, n0, mp, s.apply_x, s.apply_bx, last);
+    if (last) return;
+  }
+  __syncthreads();
+  for (int i = tid; i < XB; i += SM_THREADS) xg[i] = xs[i];
+  gram<NT, GRAM_PART>(xh, xl, ldx, SLICE, nullptr, nullptr, 0, 0.0f, 1.0f, red, p.part + (long long)blockIdx.x * (NT * NT * 256));
+}
+
+// A = gram times the slices' shares, added in order (by four wavefronts a quarter each), as hi + lo where LDS will have it
+template <int NT>
+__global__ void __launch_bounds__(256) orth_slice_sum_kernel(const OrthSliceP p) {
+  constexpr int mp = NT == 1 ? 32 : NT * 16, lda = mp + 8, side = NT * 16;
+  __shared__ f32x4 sm[4][64];
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, z = blockIdx.x / (mp * mp / 256);
+  const int at = (blockIdx.x - z * (mp * mp / 256)) * 256 + lane * 4, r = at / mp, c = at % mp;
+  const bool in = r < side && c < side;
+  const int per = (p.slices + 3) / 4, j1 = min(p.slices, (q + 1) * per);
+  f32x4 v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (in) {
+    const float *part = p.part + (long long)z * p.slices * side * side + r * side + c;
+#pragma unroll 8
+    for (int j = q * per; j < j1; ++j) v += *reinterpret_cast<const f32x4 *>(part + (long long)j * side * side);
+  }
+  sm[q][lane] = v;
+  __syncthreads();
+  if (q) return;
+  v = ((sm[0][lane] + sm[1][lane]) + sm[2][lane]) + sm[3][lane];
+  v *= p.q.sc[p.k].gram;
+  const float f[4] = {v[0], v[1], v[2], v[3]};
+  uint16_t *a = p.a + (long long)z * 2 * mp * lda + r * lda + c;
+  put4(a, a + mp * lda, f);
+}
+
+template <int NT> hipError_t launch_slices(const OrthSliceP &p, int batch, hipStream_t s) {
+  constexpr int mp = NT == 1 ? 32 : NT * 16;
+  constexpr size_t lds = (size_t)mp * (SLICE_LD + mp + 8) * 4 + SM_RED;
+  static_assert(lds <= SM_LDS, "LDS budget");
+  static std::atomic<uint64_t> done{0};
+  hipError_t err = allow_lds(reinterpret_cast<const void *>(orth_slice_kernel<NT>), lds, done);
+  const int most = std::max(1, (1 << 22) / std::max(p.slices, mp * mp / 256));      // matrices of a launch: a grid counts its threads in 32 bits
+  for (int z0 = 0; z0 < batch && err == hipSuccess; z0 += std::min(most, batch - z0)) {
+    const int nz = std::min(most, batch - z0);
+    OrthSliceP b = p;
+    b.q = from_matrix(p.q, z0);
+    b.norm += (long long)z0 * p.nparts;
+    b.x += (long long)z0 * p.slices * 2 * mp * SLICE_LD; b.a += (long long)z0 * 2 * mp * (mp + 8); b.part += (long long)z0 * p.slices * NT * NT * 256;
+    for (b.k = -1; b.k < p.q.steps; ++b.k) {
+      if (b.k >= 0) hipLaunchKernelGGL(orth_slice_sum_kernel<NT>, dim3(nz * (mp * mp / 256)), dim3(256), 0, s, b);
+      hipLaunchKernelGGL(orth_slice_kernel<NT>, dim3(nz * p.slices), dim3(SM_THREADS), lds, s, b);
+    }
     err = hipGetLastError();
   }
   return err;
@@ -290,13 +419,35 @@ template <int NT> hipError_t launch_nt(const OrthSmallP &p, int batch, size_t ld
 
 bool orth_small_fits(int rows, int cols) { return std::min(rows, cols) <= SM_MAX_M && std::max(rows, cols) <= 8192 && small_lds(rows, cols) <= SM_LDS; }
 
-hipError_t launch_orth_small(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, hipStream_t s) {
+// Always up to 64; from 65 on (whose LDS leaves a CU one work-group) while all slices are resident at once, and beyond 96, where B takes
+// a work-group longest, only of longer rows.  us, this against tiles: 64 of 64 x 640 98 / 125, 1024 of 64 x 1024 1222 / 1499; 64 of 96 x 512
+// 121 / 129, of 96 x 1024 202 / 172; 1 of 128 x 512 101 / 88, 1 of 128 x 1024 103 / 108, 16 of 128 x 2048 152 / 190, 32 270 / 229.
+bool orth_slices_fit(int batch, int rows, int cols) {
+  const int m = std::min(rows, cols), n = std::max(rows, cols);
+  return m <= 64 || (m <= SM_MAX_M && (long long)batch * ((n + SLICE - 1) / SLICE) <= 256 && (m <= 96 || n >= 1024));
+}
+
+size_t orth_slices_bytes(const OrthPlan &pl, size_t &o_x, size_t &o_a, size_t &o_part) {
+  const size_t nt = small_tiles(pl.rows, pl.cols), mp = std::max<size_t>(32, 16 * nt), slices = (std::max(pl.rows, pl.cols) + SLICE - 1) / SLICE;
+  auto up256 = [](size_t b) { return (b + 255) / 256 * 256; };
+  o_x = 0;
+  o_a = up256(pl.batch * slices * 2 * mp * SLICE_LD * 2);
+  o_part = o_a + up256(pl.batch * 2 * mp * (mp + 8) * 2);
+  return o_part + up256(pl.batch * slices * nt * nt * 256 * 4);
+}
+
+static OrthSmallP small_args(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps) {
   OrthSmallP p;
   std::memset(&p, 0, sizeof(p));
   p.in = in; p.out = out; p.rows = pl.rows; p.cols = pl.cols; p.wide = pl.wide; p.steps = pl.steps; p.eps = eps;
   p.vec = rows_of_vectors(in.g, in.type, in.sg, in.ldg, pl.cols) && (!in.v || rows_of_vectors(in.v, TYPE_F32, in.sv, pl.cols, pl.cols));
   p.first = (float)(1u << pl.ex[0]);
   for (int k = 0; k < pl.steps; ++k) p.sc[k] = pl.scale(k);
+  return p;
+}
+
+hipError_t launch_orth_small(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, hipStream_t s) {
+  const OrthSmallP p = small_args(pl, in, out, eps);
   const size_t lds = small_lds(pl.rows, pl.cols);
   switch (small_tiles(pl.rows, pl.cols)) {
     case 1: return launch_nt<1>(p, pl.batch, lds, s);
@@ -304,6 +455,23 @@ hipError_t launch_orth_small(const OrthPlan &pl, const OrthIn &in, const OrthOut
     case 4: return launch_nt<4>(p, pl.batch, lds, s);
     case 6: return launch_nt<6>(p, pl.batch, lds, s);
     default: return launch_nt<8>(p, pl.batch, lds, s);
+  }
+}
+
+hipError_t launch_orth_slices(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, const double *norm, unsigned char *ws, hipStream_t s) {
+  size_t o_x, o_a, o_part;
+  (void)orth_slices_bytes(pl, o_x, o_a, o_part);
+  OrthSliceP p;
+  std::memset(&p, 0, sizeof(p));
+  p.q = small_args(pl, in, out, eps);
+  p.slices = (std::max(pl.rows, pl.cols) + SLICE - 1) / SLICE; p.nparts = pl.nparts; p.norm = norm;
+  p.x = reinterpret_cast<uint16_t *>(ws + o_x); p.a = reinterpret_cast<uint16_t *>(ws + o_a); p.part = reinterpret_cast<float *>(ws + o_part);
+  switch (small_tiles(pl.rows, pl.cols)) {
+    case 1: return launch_slices<1>(p, pl.batch, s);
+    case 2: return launch_slices<2>(p, pl.batch, s);
+    case 4: return launch_slices<4>(p, pl.batch, s);
+    case 6: return launch_slices<6>(p, pl.batch, s);
+    default: return launch_slices<8>(p, pl.batch, s);
   }
 }
 

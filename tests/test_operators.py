@@ -211,7 +211,8 @@ def _check_orth(got, G, prec, out, tol=None, **k):
 @gpu
 @pytest.mark.parametrize("batch,rows,cols", [(1, 1, 1), (2, 1, 7), (3, 5, 1), (2, 8, 8), (3, 17, 33), (4, 64, 96), (1, 66, 65), (2, 130, 70),
                                              (3, 72, 129), (2, 333, 129), (1, 127, 128), (2, 256, 512), (1, 520, 264), (2, 300, 1100),
-                                             (1, 1030, 515), (1, 640, 640), (17, 40, 24), (4, 1288, 1032), (2, 600, 2056)])
+                                             (1, 1030, 515), (1, 640, 640), (17, 40, 24), (4, 1288, 1032), (2, 600, 2056),
+                                             (2, 13, 1500), (3, 1300, 30), (2, 50, 1409), (2, 1025, 90), (1, 125, 1100), (1, 2000, 128), (40, 1100, 70)])
 @pytest.mark.parametrize("dtype,prec", [("bf16", 1), ("f32", 0), ("f16", None)])
 @pytest.mark.parametrize("kind", ["full", "low"])
 def test_orthogonalize_against_the_definition(batch, rows, cols, dtype, prec, kind):
@@ -245,7 +246,7 @@ def test_orthogonalize_types_of_input_and_result():
 
 
 @gpu
-@pytest.mark.parametrize("rows,cols", [(24, 40), (40, 24), (100, 72), (65, 203), (200, 136), (136, 200), (150, 161), (300, 264)])
+@pytest.mark.parametrize("rows,cols", [(24, 40), (40, 24), (100, 72), (65, 203), (200, 136), (136, 200), (150, 161), (300, 264), (9, 1301), (1290, 61)])
 def test_orthogonalize_of_strided_and_unaligned_matrices(rows, cols):
     import torch
     A = _A()
@@ -393,7 +394,7 @@ def test_orthogonalize_on_a_stream_and_in_a_graph():
 # ---- the step with orthogonalised momentum ------------------------------------------------------------------------------------
 
 @gpu
-@pytest.mark.parametrize("batch,rows,cols", [(1, 1, 9), (3, 33, 50), (2, 128, 64), (2, 264, 136), (1, 70, 515)])
+@pytest.mark.parametrize("batch,rows,cols", [(1, 1, 9), (3, 33, 50), (2, 128, 64), (2, 264, 136), (1, 70, 515), (2, 1201, 27)])
 @pytest.mark.parametrize("xt,gt", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "bf16"), ("f32", "bf16")])
 @pytest.mark.parametrize("nesterov", [True, False])
 def test_muon_step_against_the_definition(batch, rows, cols, xt, gt, nesterov):
