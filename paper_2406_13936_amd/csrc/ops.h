@@ -61,7 +61,7 @@ const char *orth_plan(int batch, int rows, int cols, int split, int steps, const
 hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, void *workspace, hipStream_t s);
 
 // orthogonalize_small.hip: a work-group's LDS holds the matrix
-bool orth_small_fits(int rows, int cols);
+bool orth_small_fits(int batch, int rows, int cols);
 hipError_t launch_orth_small(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, hipStream_t s);
 // or not, but the smaller side is short: the norm's partial sums are there already
 bool orth_slices_fit(int batch, int rows, int cols);

@@ -650,7 +650,7 @@ const char *orth_plan(int batch, int rows, int cols, int split, int steps, const
     pl.eb[k] = exponent_for(std::max(inner, 1.0 / 256) * (1.0 + 1.0 / 32));
     pl.ex[k + 1] = exponent_for(s);
   }
-  if (orth_small_fits(rows, cols)) { pl.total = 256; return nullptr; }     // (all of it is in LDS)
+  if (orth_small_fits(batch, rows, cols)) { pl.total = 256; return nullptr; }     // (all of it is in LDS)
   // two chunks of 8 values to a thread of the norm's pass, until there are as many blocks as one block of the next pass adds up
   pl.nparts = (int)std::min<long long>(ORTH_PARTS, ((long long)rows * cols + 4095) / 4096);
   size_t o = 0;
@@ -672,7 +672,7 @@ const char *orth_plan(int batch, int rows, int cols, int split, int steps, const
 }
 
 hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, void *workspace, hipStream_t s) {
-  if (orth_small_fits(pl.rows, pl.cols)) return launch_orth_small(pl, in, out, eps, s);
+  if (orth_small_fits(pl.batch, pl.rows, pl.cols)) return launch_orth_small(pl, in, out, eps, s);
   const bool slices = orth_slices_fit(pl.batch, pl.rows, pl.cols);
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   auto at = [&](size_t off) { return reinterpret_cast<uint16_t *>(ws + off); };

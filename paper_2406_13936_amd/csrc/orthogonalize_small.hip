@@ -2,8 +2,8 @@
 // hi + lo): one launch, one work-group of eight wavefronts to a matrix, which takes the momentum's step, the norm, all
 // Newton-Schulz steps and the update.  Such matrices are latency: launch by launch every product is a handful of k-tiles
 // behind a launch's 3 to 8 us.  5 steps, replayed from a graph, this kernel against the launches of orthogonalize.hip: 4 of 64 x 96
-// 25 us against 61, 4 of 16 x 1000 37 / 93, 4 of 128 x 128 70 / 75, 4 of 64 x 512 75 / 76, 512 of 64 x 512 169 / 384, 512 of
-// 128 x 128 151 / 281, 2048 of 16 x 16 46 / 293; so every matrix that fits is taken here.  What bounds it is the chain of LDS reads,
+// 25 us against 61, 4 of 16 x 1000 37 / 93, 4 of 128 x 128 70 / 75, 512 of 64 x 512 169 / 384, 512 of
+// 128 x 128 151 / 281, 2048 of 16 x 16 46 / 293; so every matrix that fits is taken here, or by the slices below.  What bounds it is the chain of LDS reads,
 // dependent MFMAs and barriers of one work-group (3.3 us a step of 64 x 96, 1.3 of 16 x 16, 10 of 128 x 128); the number of
 // tiles is a template's, so that their loops are straight code (4 of 64 x 96 with run-time loops: 35 us).
 //
@@ -417,7 +417,13 @@ template <int NT> hipError_t launch_slices(const OrthSliceP &p, int batch, hipSt
 
 }  // namespace
 
-bool orth_small_fits(int rows, int cols) { return std::min(rows, cols) <= SM_MAX_M && std::max(rows, cols) <= 8192 && small_lds(rows, cols) <= SM_LDS; }
+// ... and which slices that are few do not take in less time.  us, one launch against slices: 4 of 32 x 768 53 / 42, of 64 x 256 44 / 54, of
+// 64 x 512 75 / 55, of 96 x 224 73 / 78, of 96 x 280 91 / 78; 30 of 32 x 1000 68 / 47, 80 of 64 x 384 63 / 79.
+bool orth_small_fits(int batch, int rows, int cols) {
+  const int m = std::min(rows, cols), n = std::max(rows, cols);
+  if (m > SM_MAX_M || n > 8192 || small_lds(rows, cols) > SM_LDS) return false;
+  return m <= 16 || m > 96 || m * n <= 22000 || (long long)batch * ((n + SLICE - 1) / SLICE) > (m <= 32 ? 256 : 128);
+}
 
 // Always up to 64; from 65 on (whose LDS leaves a CU one work-group) while all slices are resident at once, and beyond 96, where B takes
 // a work-group longest, only of longer rows.  us, this against tiles: 64 of 64 x 640 98 / 125, 1024 of 64 x 1024 1222 / 1499; 64 of 96 x 512

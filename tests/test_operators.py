@@ -212,7 +212,7 @@ def _check_orth(got, G, prec, out, tol=None, **k):
 @pytest.mark.parametrize("batch,rows,cols", [(1, 1, 1), (2, 1, 7), (3, 5, 1), (2, 8, 8), (3, 17, 33), (4, 64, 96), (1, 66, 65), (2, 130, 70),
                                              (3, 72, 129), (2, 333, 129), (1, 127, 128), (2, 256, 512), (1, 520, 264), (2, 300, 1100),
                                              (1, 1030, 515), (1, 640, 640), (17, 40, 24), (4, 1288, 1032), (2, 600, 2056),
-                                             (2, 13, 1500), (3, 1300, 30), (2, 50, 1409), (2, 1025, 90), (1, 125, 1100), (1, 2000, 128), (40, 1100, 70)])
+                                             (2, 13, 1500), (3, 1300, 30), (2, 50, 1409), (2, 1025, 90), (1, 125, 1100), (1, 2000, 128), (40, 1100, 70), (2, 64, 500), (300, 24, 960)])
 @pytest.mark.parametrize("dtype,prec", [("bf16", 1), ("f32", 0), ("f16", None)])
 @pytest.mark.parametrize("kind", ["full", "low"])
 def test_orthogonalize_against_the_definition(batch, rows, cols, dtype, prec, kind):
