@@ -4,7 +4,8 @@
 //   h = dy gamma,  dx = r (h - mean_d h - xh mean_d(h xh))
 //   sample i (T rows):  g_i = (sum_t dy xh, sum_t dy),   gbar = mean_i g_i,   n_i = ||g_i||^2,   q_i = <g_i, gbar>
 //
-// All of it is bound by memory: forward reads x and writes y, backward reads x and dy and writes dx.  A row lives in the
+// All of it is bound by memory: forward reads x and writes y, backward reads x and dy and writes dx (8 x 8192 rows of 2048 in bf16: 108 us
+// and 168, 5.0 and 4.8 TB/s; 90 us where half of x is still in a cache).  A row lives in the
 // registers of a group of G lanes (16 to 512, V vectors of 8 values to a lane), so it is read once; gains, biases and
 // the sums for gbar stay in the registers of the lanes that own their columns, over all rows of a block.  A block leaves
 // one partial of (sum dy xh, sum dy), and a second launch adds the partials in order: no atomics, the same bits every time.
