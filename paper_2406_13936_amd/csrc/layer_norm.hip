@@ -74,7 +74,6 @@ template <int TYPE, int G> __device__ __forceinline__ int col_of(int v, int e, i
 // Results are not read again here: non-temporal stores (16-bit rows of 2048: forward 116 -> 101 us for 134 M values, backward 204 -> 194;
 // non-temporal loads cost more than they give where the inputs are still in a cache).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef u32x4 u32x4_any __attribute__((aligned(2)));       // 16 bytes that start anywhere a 16-bit value may
 template <bool VEC> __device__ __forceinline__ void st_once(void *p, uint4 v) {
   const u32x4 w = {v.x, v.y, v.z, v.w};
   if constexpr (VEC) __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
@@ -116,8 +115,7 @@ template <int BYTES, bool VEC> __device__ __forceinline__ uint4 load16(const voi
     return make_uint4(w[0], w[1], w[2], w[3]);
   } else {
     const int from = min(c, D - N), k = min(c - from, N);
-    const u32x4 q = *reinterpret_cast<const u32x4_any *>(row + (long long)from * BYTES);
-    return move_down<BYTES>(make_uint4(q.x, q.y, q.z, q.w), k);
+    return move_down<BYTES>(load16_any(row + (long long)from * BYTES), k);
   }
 }
 

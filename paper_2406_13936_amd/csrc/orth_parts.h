@@ -24,23 +24,22 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4 &hi, uint4 &lo
   lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
-// Values (r, c) .. (r, c + 7) of what is orthogonalised, matrix z; zeros outside the matrix.  vec: rows of G (and v) start on
-// 16 bytes and hold whole vectors.  ADVANCE: v takes its step first (each value must be visited once so); else v is the new one.
+// Values (r, c) .. (r, c + 7) of what is orthogonalised, matrix z; zeros outside the matrix.  ADVANCE: v takes its step first (each value must be visited once so); else v is the new one.
 template <bool ADVANCE>
-__device__ __forceinline__ void load_u8(const OrthIn &in, int rows, int cols, bool vec, int z, int r, int c, float (&u)[8]) {
+__device__ __forceinline__ void load_u8(const OrthIn &in, int rows, int cols, int z, int r, int c, float (&u)[8]) {
   const long long g0 = z * in.sg + (long long)r * in.ldg + c, v0 = z * in.sv + (long long)r * cols + c;
   const float mu = in.momentum;
-  if (vec && r < rows && c < cols) {
-    load8(in.g, in.type, g0, u);
+  if (r < rows && c + 8 <= cols) {
+    load8_any(in.g, in.type, g0, u);
     if (in.v) {
       float v[8];
-      load8(in.v, TYPE_F32, v0, v);
+      load8_any(in.v, TYPE_F32, v0, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (ADVANCE) v[e] = fmaf(mu, v[e], u[e]);
         u[e] = in.nesterov ? fmaf(mu, v[e], u[e]) : v[e];
       }
-      if (ADVANCE) store8(in.v, TYPE_F32, v0, v);
+      if (ADVANCE) store8_any(in.v, TYPE_F32, v0, v);
     }
     return;
   }

@@ -42,7 +42,7 @@ __device__ __forceinline__ int paired(int c) { return 2 * (c & ~31) + (c & 31); 
 
 struct OrthPrepP {
   OrthIn in;
-  int rows, cols, rp, cp, nparts, vec, ex;   // vec: all rows start on 16 bytes, cols is a multiple of 8
+  int rows, cols, rp, cp, nparts, ex;
   double *part; uint16_t *xh, *xl;       // (split: xl null, both parts in xh)
   float eps;
 };
@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(const OrthPrepP p) {
   for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
     const int r = i / cc, c = (i - r * cc) * 8;
     float u[8];
-    load_u8<true>(p.in, p.rows, p.cols, p.vec, z, r, c, u);
+    load_u8<true>(p.in, p.rows, p.cols, z, r, c, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = fma((double)u[e], (double)u[e], sum);
   }
@@ -64,7 +64,8 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(const OrthPrepP p) {
   if (threadIdx.x == 0) p.part[(long long)z * p.nparts + blockIdx.x] = t;
 }
 
-// X_0 2^ex as two fp16 values, zeros in the rows and columns that round the sides up to 8
+// X_0 2^ex as two fp16 values, zeros in the rows and columns that round the sides up to 8.  (Loads of all of a thread's chunks before the
+// scale is known: 18 -> 30 us for 4096 x 4096.)
 __global__ void __launch_bounds__(256) orth_prep_kernel(const OrthPrepP p) {
   __shared__ double sm[4];
   __shared__ double scale;
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(256) orth_prep_kernel(const OrthPrepP p) {
   for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
     const int r = i / cc, c = (i - r * cc) * 8;
     float u[8];
-    load_u8<false>(p.in, p.rows, p.cols, p.vec, z, r, c, u);
+    load_u8<false>(p.in, p.rows, p.cols, z, r, c, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) u[e] = (float)((double)u[e] * sc);
     uint4 h, l;
@@ -101,7 +102,7 @@ struct OrthGemmP {
   int sym;                               // C is symmetric: tiles below the diagonal are written from those above it
   float *diag; int diag_of;              // [z][mp] fp32 diagonal: DIAG_OUT: C's, which is stored as zeros there; DIAG_ROWS, DIAG_COLS:
                                          //   beta diag[m] (or [n]) times E's first part is added
-  OrthOut out; int rows, cols, vec;      // the last step (C null)
+  OrthOut out; int rows, cols;           // the last step (C null)
 };
 
 // Tiles BM x BN x BK with WM x WN wavefronts, NS stages of direct global -> LDS loads; operands k-contiguous or row-contiguous as
@@ -486,15 +487,15 @@ __global__ void __launch_bounds__(WM * WN * WK * 64) orth_gemm_kernel(const Orth
       } else {
         if (m >= p.rows || n >= p.cols) continue;
         const long long at = z * p.out.so + (long long)m * p.out.ldo + n, sat = z * p.out.sshadow + (long long)m * p.out.ldo + n;
-        if (p.vec) {                              // (cols is a multiple of 8: all of the vector is inside)
+        if (n + 8 <= p.cols) {
           if (p.out.update) {
             float x[8];
-            load8(p.out.o, p.out.type, at, x);
+            load8_any(p.out.o, p.out.type, at, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = fmaf(decay, x[e], -gain * v[e]);
           }
-          store8(p.out.o, p.out.type, at, v);
-          if (p.out.shadow) store8(p.out.shadow, TYPE_BF16, sat, v);
+          store8_any(p.out.o, p.out.type, at, v);
+          if (p.out.shadow) store8_any(p.out.shadow, TYPE_BF16, sat, v);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) sum[r * SLD + cc + e] = v[e];
@@ -681,7 +682,6 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
   OrthPrepP q;
   std::memset(&q, 0, sizeof(q));
   q.in = in; q.rows = pl.rows; q.cols = pl.cols; q.rp = pl.rp; q.cp = pl.cp; q.nparts = pl.nparts; q.ex = pl.ex[0]; q.eps = eps;
-  q.vec = rows_of_vectors(in.g, in.type, in.sg, in.ldg, pl.cols) && (!in.v || rows_of_vectors(in.v, TYPE_F32, in.sv, pl.cols, pl.cols));
   q.part = reinterpret_cast<double *>(ws + pl.o_part); q.xh = at(pl.o_x[0]); q.xl = pl.split ? nullptr : at(pl.o_xl);
   for (int z0 = 0; z0 < pl.batch; z0 += 32768) {  // (grids have 65535 places along y)
     OrthPrepP b = q;
@@ -728,8 +728,6 @@ hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const Orth
     p.alpha = pl.scale(k).apply_x; p.beta = pl.scale(k).apply_bx;
     if (last) {
       p.out = out; p.rows = pl.rows; p.cols = pl.cols;
-      p.vec = rows_of_vectors(out.o, out.type, out.so, out.ldo, pl.cols) &&
-              (!out.shadow || rows_of_vectors(out.shadow, TYPE_BF16, out.sshadow, out.ldo, pl.cols));
     } else {
       p.C = at(pl.o_x[~k & 1]); p.Cl = pl.split ? nullptr : at(pl.o_xl); p.sC = sx; p.ldc = ldx;
     }

@@ -42,7 +42,7 @@ size_t small_lds(int rows, int cols) {
 
 struct OrthSmallP {
   OrthIn in; OrthOut out;
-  int rows, cols, vec, wide, steps;
+  int rows, cols, wide, steps;
   float eps, first;                      // first: the power of two that X_0 is stored with
   OrthScale sc[ORTH_MAX_STEPS];
 };
@@ -225,13 +225,13 @@ __global__ void __launch_bounds__(SM_THREADS) orth_small_kernel(const OrthSmallP
     const int i = tid + h * SM_THREADS;
 #pragma unroll
     for (int e = 0; e < 8; ++e) held[h][e] = 0.0f;
-    if (i < chunks) load_u8<true>(p.in, p.rows, p.cols, p.vec, z, i / cc, i % cc * 8, held[h]);
+    if (i < chunks) load_u8<true>(p.in, p.rows, p.cols, z, i / cc, i % cc * 8, held[h]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = fma((double)held[h][e], (double)held[h][e], sum);
   }
   for (int i = tid + HELD * SM_THREADS; i < chunks; i += SM_THREADS) {
     float u[8];
-    load_u8<true>(p.in, p.rows, p.cols, p.vec, z, i / cc, i % cc * 8, u);
+    load_u8<true>(p.in, p.rows, p.cols, z, i / cc, i % cc * 8, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = fma((double)u[e], (double)u[e], sum);
   }
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(SM_THREADS) orth_small_kernel(const OrthSmallP
     if (tid + h * SM_THREADS < chunks) put(tid + h * SM_THREADS, held[h]);
   for (int i = tid + HELD * SM_THREADS; i < chunks; i += SM_THREADS) {       // (a thread meets the values of v that it has written)
     float u[8];
-    load_u8<false>(p.in, p.rows, p.cols, p.vec, z, i / cc, i % cc * 8, u);
+    load_u8<false>(p.in, p.rows, p.cols, z, i / cc, i % cc * 8, u);
     put(i, u);
   }
   __syncthreads();
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(SM_THREADS) orth_slice_kernel(const OrthSliceP
     for (int i = tid; i < chunks; i += SM_THREADS) {
       const int r = i / cc, c = (i - r * cc) * 8;
       float u[8];
-      load_u8<false>(p.q.in, p.q.rows, p.q.cols, p.q.vec, z, r0 + r, c0 + c, u);
+      load_u8<false>(p.q.in, p.q.rows, p.q.cols, z, r0 + r, c0 + c, u);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (c0 + c + e >= p.q.cols) break;
@@ -446,7 +446,6 @@ static OrthSmallP small_args(const OrthPlan &pl, const OrthIn &in, const OrthOut
   OrthSmallP p;
   std::memset(&p, 0, sizeof(p));
   p.in = in; p.out = out; p.rows = pl.rows; p.cols = pl.cols; p.wide = pl.wide; p.steps = pl.steps; p.eps = eps;
-  p.vec = rows_of_vectors(in.g, in.type, in.sg, in.ldg, pl.cols) && (!in.v || rows_of_vectors(in.v, TYPE_F32, in.sv, pl.cols, pl.cols));
   p.first = (float)(1u << pl.ex[0]);
   for (int k = 0; k < pl.steps; ++k) p.sc[k] = pl.scale(k);
   return p;

@@ -52,6 +52,35 @@ __device__ __forceinline__ void store8(void *p, int type, long long i, const flo
     *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + i) = pack8(type, v);
   }
 }
+// The same at places of the type's own alignment (the machine takes 16 bytes from anywhere)
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ uint4 load16_any(const void *p) {
+  const u32x4_any q = *static_cast<const u32x4_any *>(p);
+  return make_uint4(q.x, q.y, q.z, q.w);
+}
+__device__ __forceinline__ void store16_any(void *p, uint4 v) {
+  const u32x4_any q = {v.x, v.y, v.z, v.w};
+  *static_cast<u32x4_any *>(p) = q;
+}
+__device__ __forceinline__ void load8_any(const void *p, int type, long long i, float (&v)[8]) {
+  if (type == TYPE_F32) {
+    const uint4 a = load16_any(static_cast<const float *>(p) + i), b = load16_any(static_cast<const float *>(p) + i + 4);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(w[e]);
+  } else {
+    unpack8(load16_any(static_cast<const uint16_t *>(p) + i), type, v);
+  }
+}
+__device__ __forceinline__ void store8_any(void *p, int type, long long i, const float (&v)[8]) {
+  if (type == TYPE_F32) {
+    float *f = static_cast<float *>(p) + i;
+    store16_any(f, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+    store16_any(f + 4, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+  } else {
+    store16_any(static_cast<uint16_t *>(p) + i, pack8(type, v));
+  }
+}
 
 }  // namespace
 
