@@ -60,6 +60,9 @@ struct OrthOut {
 const char *orth_plan(int batch, int rows, int cols, int split, int steps, const float *coef, OrthPlan &pl);
 hipError_t launch_orthogonalize(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, void *workspace, hipStream_t s);
 
+// the rule for a product's tiles (tests ask it too, to reach every kind)
+int orth_product_shape(int Md, int Nd, int K, int batch, int sym);
+
 // orthogonalize_small.hip: a work-group's LDS holds the matrix
 bool orth_small_fits(int batch, int rows, int cols);
 hipError_t launch_orth_small(const OrthPlan &pl, const OrthIn &in, const OrthOut &out, float eps, hipStream_t s);

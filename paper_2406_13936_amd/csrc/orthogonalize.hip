@@ -563,25 +563,9 @@ long long tile_count(int Md, int Nd, int batch, int sym, int e) {
   return (sym ? tn * (tn + 1) / 2 : tm * tn) * batch;
 }
 
-// Tile, groups of wavefronts to a tile and ring of stages of a product whose reduction is K places of memory long.  us a product, 128 x 128
-// tiles of four wavefronts with a ring of four -> this, measured over whole calls:
-//   one tile of 64 x 64 to a CU: A and B of 12 of 1001 x 333 (252 tiles) in fp32 34 -> 13 and 21 -> 11, of one 1024 x 1024 (136) 40 -> 21,
-//   of one 300 x 300 (15) 18 -> 9; two groups instead of one 3 to 8 % less, four no more
-//   up to one and a half: 8 of 512 x 784 (288) 21 -> 10; 2 of 4096 x 1024 (272) 100 -> 50.  Beyond, 64 x 64 tiles bring too many bytes: one
-//   2048 x 2048 (528 tiles; 136 of 128 x 128) 2 longer
-//   up to one tile of 128 x 128 to a CU, two groups: one 2048 x 2048 (136, 256 tiles) 5 less, 8 of 512 x 784 (224) 3 less
-struct OrthShape { int tile, groups, ring; };
-OrthShape choose_shape(int Md, int Nd, int K, int batch, int sym) {
-  const long long t256 = tile_count(Md, Nd, batch, sym, 256), t128 = tile_count(Md, Nd, batch, sym, 128), t64 = tile_count(Md, Nd, batch, sym, 64);
-  if (t64 <= 384) return {64, 2, t64 <= 256 ? 4 : 2};
-  if (K >= 512 && 1.5 * (double)((t256 + 255) / 256) <= rounds_128(t128)) return {256, 1, 2};
-  return {128, t128 <= 256 ? 2 : 1, 2};
-}
-
 template <bool AT, bool BT, bool SPLIT, int KIND>
 hipError_t launch_shape(const OrthGemmP &p, hipStream_t s) {
-  const OrthShape c = choose_shape(p.Md, p.Nd, p.Kd * (SPLIT ? 2 : 1), p.batch, p.sym);
-  switch (c.tile * 100 + c.groups * 10 + c.ring) {
+  switch (orth_product_shape(p.Md, p.Nd, p.Kd * (SPLIT ? 2 : 1), p.batch, p.sym)) {
     case 25612: return launch_cfg<256, 256, 64, 2, 4, 1, 2, true, AT, BT, SPLIT, KIND>(p, s);
     case 12812: return launch_cfg<128, 128, 64, 2, 2, 1, 2, false, AT, BT, SPLIT, KIND>(p, s);
     case 12822: return launch_cfg<128, 128, 128, 2, 2, 2, 2, false, AT, BT, SPLIT, KIND>(p, s);
@@ -606,6 +590,20 @@ constexpr int SPLIT_ALWAYS = 128;
 int exponent_for(double bound) { return 15 - (int)std::ceil(std::log2(bound)); }
 
 }  // namespace
+
+// Tile, groups of wavefronts to a tile and ring of stages (tile * 100 + groups * 10 + ring) of a product whose reduction is K places of
+// memory long.  us a product, 128 x 128 tiles of four wavefronts with a ring of four -> this, measured over whole calls:
+//   one tile of 64 x 64 to a CU: A and B of 12 of 1001 x 333 (252 tiles) in fp32 34 -> 13 and 21 -> 11, of one 1024 x 1024 (136) 40 -> 21,
+//   of one 300 x 300 (15) 18 -> 9; two groups instead of one 3 to 8 % less, four no more
+//   up to one and a half: 8 of 512 x 784 (288) 21 -> 10; 2 of 4096 x 1024 (272) 100 -> 50.  Beyond, 64 x 64 tiles bring too many bytes: one
+//   2048 x 2048 (528 tiles; 136 of 128 x 128) 2 longer
+//   up to one tile of 128 x 128 to a CU, two groups: one 2048 x 2048 (136, 256 tiles) 5 less, 8 of 512 x 784 (224) 3 less
+int orth_product_shape(int Md, int Nd, int K, int batch, int sym) {
+  const long long t256 = tile_count(Md, Nd, batch, sym, 256), t128 = tile_count(Md, Nd, batch, sym, 128), t64 = tile_count(Md, Nd, batch, sym, 64);
+  if (t64 <= 384) return t64 <= 256 ? 6424 : 6422;
+  if (K >= 512 && 1.5 * (double)((t256 + 255) / 256) <= rounds_128(t128)) return 25612;
+  return t128 <= 256 ? 12822 : 12812;
+}
 
 OrthScale OrthPlan::scale(int k) const {
   const int to = k + 1 == steps ? 0 : ex[k + 1];           // (the result itself is not scaled)
