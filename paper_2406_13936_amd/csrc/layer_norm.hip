@@ -145,6 +145,12 @@ template <int TYPE, int V> __device__ __forceinline__ void raw_vals(const Raw<TY
     unpack8(r.q[v], TYPE, f);
   }
 }
+// What a column's value is centred with: the row's mean, and beyond the row, where values are zeros, nothing: 1 / sqrt(eps) times a large
+// mean may be infinite, and its product with dy = 0 NaN
+template <int TYPE, int G, bool VEC> __device__ __forceinline__ float mean_at(int v, int e, int l, int D, float mean) {
+  constexpr int N = TYPE == TYPE_F32 ? 4 : 8;              // (whole vectors are in the row or not)
+  return col_of<TYPE, G>(v, VEC ? e & ~(N - 1) : e, l) < D ? mean : 0.0f;
+}
 template <int TYPE, int G, bool VEC>
 __device__ __forceinline__ void store_vals(void *p, long long at, int D, int l, int v, const float (&f)[8]) {
   constexpr int PER = TYPE == TYPE_F32 ? 2 : 1, N = 8 / PER;
@@ -381,8 +387,7 @@ __global__ void __launch_bounds__(ln_threads(G), V == 1 && TYPE != TYPE_F32 && S
           raw_vals<TYPE, V>(ry[k], v, dy);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            // (beyond the row dy is zero; x - mean is not, so nothing but products with dy may use it)
-            const float xh = (x[e] - mean[k]) * rstd[k], h = dy[e] * ga[v][e], dw = dy[e] * xh;
+            const float xh = (x[e] - mean_at<TYPE, G, VEC>(v, e, l, D, mean[k])) * rstd[k], h = dy[e] * ga[v][e], dw = dy[e] * xh;
             s1 += h;
             s2 = fmaf(h, xh, s2);
             if (STAT == STAT_SAMPLE) { gw[v][e] += dw; gb[v][e] += dy[e]; }
@@ -569,7 +574,7 @@ __global__ void __launch_bounds__(ln_threads(G)) ln_inner_rows_kernel(const Laye
         raw_vals<TYPE, V>(rx, v, x);
         raw_vals<TYPE, V>(ry, v, dy);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[0] = fmaf(dy[e], fmaf((x[e] - mean) * rstd, gw[v][e], gb[v][e]), s[0]);
+        for (int e = 0; e < 8; ++e) s[0] = fmaf(dy[e], fmaf((x[e] - mean_at<TYPE, G, VEC>(v, e, l, D, mean)) * rstd, gw[v][e], gb[v][e]), s[0]);
       }
     }
     group_sums<G, 1>(s, sm, turn++);
