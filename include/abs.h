@@ -326,8 +326,9 @@ enum { ABS_TYPE_F32 = 0, ABS_TYPE_BF16 = 1, ABS_TYPE_F16 = 2 };
  * (with A = X^T X on the right where rows > cols: the same X).  A zero matrix gives zeros, one with an infinity or NaN gives NaN
  * and leaves the others alone.
  *   g_dev, o_dev : device, [batch][rows][cols]; ldg, ldo: values from row to row (>= cols), stride_g, stride_o: from matrix to
- *                  matrix.  Any alignment of the type; rows that start on 16 bytes and hold a multiple of 8 values are faster.
- *                  o_dev may be g_dev (same type and strides); it must not overlap it otherwise.
+ *                  matrix, whose rows do not overlap: matrix after matrix, or interleaved by rows.  Any alignment of the type; rows that start on 16 bytes and hold a multiple of 8 values are faster.
+ *                  o_dev may be g_dev (same type and strides); it must not overlap it otherwise
+ *                  (columns of the same rows that are apart do not).
  *   steps        : 1 .. 32.
  *   coef         : host, 3 * steps floats a, b, c, step by step, or NULL: (3.4445, -4.7750, 2.0315) in all, which takes singular
  *                  values from 0.01 on to about 0.7 .. 1.2 in five steps.  Coefficients that let a singular value of at most 1 grow
@@ -367,7 +368,8 @@ typedef struct {
   int M, b, T, D;             /* replicas, samples of each, rows of a sample (tokens), values of a row; all >= 1 */
   int type;                   /* ABS_TYPE_* of x, y, dy and dx */
   int param_type;             /* ABS_TYPE_* of gamma and beta [M x D]: ABS_TYPE_F32 or `type` */
-  int64_t ldx, stride_x;      /* x: values from row to row (>= D) and from replica to replica */
+  int64_t ldx, stride_x;      /* x: values from row to row (>= D) and from replica to replica; rows do not overlap: replica after replica,
+                                 or interleaved by rows */
   int64_t ldy, stride_y;      /* y, or dy */
   int64_t lddx, stride_dx;    /* dx (backward) */
 } abs_layer_norm_shape;

@@ -1,6 +1,7 @@
 // C ABI of the operators beside the replicas' step (declared in include/abs.h): argument checks and launches.
 #include <cmath>
 #include <cstring>
+#include <numeric>
 
 #include "../../include/abs.h"
 #include "api_status.h"
@@ -13,18 +14,33 @@ namespace {
 bool known_type(int t) { return t >= ABS_TYPE_F32 && t <= ABS_TYPE_F16; }
 bool aligned_to(const void *p, int bytes) { return !(reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)); }
 
-// bytes from the first value of a [n][rows][cols] block to behind its last
-int64_t extent(int64_t n, int64_t stride, int64_t rows, int64_t ld, int64_t cols, int type) {
-  return ((n - 1) * stride + (rows - 1) * ld + cols) * type_bytes(type);
+// A [n][rows][cols] block in memory, `bytes` to a value
+struct Block {
+  const void *p;
+  int64_t n, stride, rows, ld, cols;
+  int bytes;
+  uintptr_t at() const { return reinterpret_cast<uintptr_t>(p); }
+  uintptr_t extent() const { return (uintptr_t)(((n - 1) * stride + (rows - 1) * ld + cols) * bytes); }       // from the first value to behind the last
+};
+Block piece(const void *p, int64_t values, int bytes) { return {p, 1, 0, 1, 0, values, bytes}; }
+bool overlap(const Block &a, const Block &b) {
+  const uintptr_t p = a.at(), q = b.at();
+  if (p + a.extent() <= q || q + b.extent() <= p) return false;
+  // every row of either begins a multiple of `pitch` behind its first one: apart if the rows are within one such space
+  int64_t pitch = 0;
+  for (const Block *x : {&a, &b}) {
+    if (x->n > 1) pitch = std::gcd(pitch, x->stride * x->bytes);
+    if (x->rows > 1) pitch = std::gcd(pitch, x->ld * x->bytes);
+  }
+  if (!pitch) return true;
+  const uintptr_t space = (uintptr_t)pitch, d = q >= p ? (q - p) % space : (space - (p - q) % space) % space;
+  return !(d >= (uintptr_t)(a.cols * a.bytes) && d + (uintptr_t)(b.cols * b.bytes) <= space);
 }
-bool overlap(const void *a, int64_t an, const void *b, int64_t bn) {
-  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
-  return p < q + (uintptr_t)bn && q < p + (uintptr_t)an;
-}
-// rows that do not run into each other, offsets that 64 bits hold
+// rows that do not overlap, matrix after matrix or interleaved; offsets that 64 bits hold
 bool strides_ok(int64_t n, int64_t stride, int64_t rows, int64_t ld, int64_t cols) {
   const int64_t big = (int64_t)1 << 46;
-  return ld >= cols && ld < big / rows && stride >= 0 && stride < big / n && (n == 1 || stride >= (rows - 1) * ld + cols);
+  if (ld < cols || ld >= big / rows || stride < 0 || stride >= big / n) return false;
+  return n == 1 || stride >= (rows - 1) * ld + cols || (stride >= cols && ld >= (n - 1) * stride + cols);
 }
 abs_status hip_status(hipError_t e, const char *what) {
   return e == hipSuccess ? ABS_OK : set_error(ABS_EHIP, std::string(what) + ": " + hipGetErrorString(e));
@@ -59,7 +75,7 @@ abs_status check_shape(const abs_layer_norm_shape *s, bool backward) {
     return set_error(ABS_EUNSUPPORTED, "more than 2^20 replicas, 2^27 gains or 2^31 - 1 rows");
   if (!strides_ok(s->M, s->stride_x, rows, s->ldx, s->D) || !strides_ok(s->M, s->stride_y, rows, s->ldy, s->D) ||
       (backward && !strides_ok(s->M, s->stride_dx, rows, s->lddx, s->D)))
-    return set_error(ABS_EINVAL, "strides: ld >= D, and replicas must not run into each other");
+    return set_error(ABS_EINVAL, "strides: ld >= D, and rows must not overlap");
   return ABS_OK;
 }
 LayerNormP layer_norm_args(const abs_layer_norm_shape *s) {
@@ -93,11 +109,12 @@ abs_status abs_orthogonalize(const void *g_dev, int g_type, int64_t ldg, int64_t
   abs_status st = check_orth(batch, rows, cols, steps, coef, eps, prec, workspace, workspace_bytes, pl);
   if (st != ABS_OK) return st;
   if (!strides_ok(batch, stride_g, rows, ldg, cols) || !strides_ok(batch, stride_o, rows, ldo, cols) || ldg > 0x7fffffff || ldo > 0x7fffffff)
-    return set_error(ABS_EINVAL, "strides: ld >= cols, and matrices must not run into each other");
+    return set_error(ABS_EINVAL, "strides: ld >= cols, and rows must not overlap");
   if (!aligned_to(g_dev, type_bytes(g_type)) || !aligned_to(o_dev, type_bytes(o_type))) return set_error(ABS_EINVAL, "pointers must be aligned to their type");
   const bool same = g_dev == o_dev && g_type == o_type && ldg == ldo && stride_g == stride_o;
-  const int64_t ge = extent(batch, stride_g, rows, ldg, cols, g_type), oe = extent(batch, stride_o, rows, ldo, cols, o_type);
-  if ((!same && overlap(g_dev, ge, o_dev, oe)) || overlap(workspace, (int64_t)pl.total, g_dev, ge) || overlap(workspace, (int64_t)pl.total, o_dev, oe))
+  const Block g = {g_dev, batch, stride_g, rows, ldg, cols, type_bytes(g_type)}, o = {o_dev, batch, stride_o, rows, ldo, cols, type_bytes(o_type)};
+  const Block ws = piece(workspace, (int64_t)pl.total, 1);
+  if ((!same && overlap(g, o)) || overlap(ws, g) || overlap(ws, o))
     return set_error(ABS_EINVAL, "o_dev must be g_dev or not overlap it, and the workspace neither");
   const OrthIn in = {g_dev, g_type, stride_g, (int)ldg, nullptr, 0, 0.0f, 0};
   OrthOut out;
@@ -119,11 +136,11 @@ abs_status abs_muon_step(void *x_dev, int x_type, const void *g_dev, int g_type,
   if (!aligned_to(x_dev, type_bytes(x_type)) || !aligned_to(g_dev, type_bytes(g_type)) || !aligned_to(v_dev, 4))
     return set_error(ABS_EINVAL, "pointers must be aligned to their type");
   const int64_t n = (int64_t)rows * cols;
-  const struct { const void *p; int64_t bytes; } used[4] = {{x_dev, batch * n * type_bytes(x_type)}, {g_dev, batch * n * type_bytes(g_type)},
-                                                            {v_dev, batch * n * 4}, {workspace, (int64_t)pl.total}};
+  const Block used[4] = {piece(x_dev, batch * n, type_bytes(x_type)), piece(g_dev, batch * n, type_bytes(g_type)), piece(v_dev, batch * n, 4),
+                         piece(workspace, (int64_t)pl.total, 1)};
   for (int i = 0; i < 4; ++i)
     for (int j = 0; j < i; ++j)
-      if (overlap(used[i].p, used[i].bytes, used[j].p, used[j].bytes)) return set_error(ABS_EINVAL, "x, g, v and the workspace must not overlap");
+      if (overlap(used[i], used[j])) return set_error(ABS_EINVAL, "x, g, v and the workspace must not overlap");
   const OrthIn in = {g_dev, g_type, n, cols, v_dev, n, momentum, nesterov != 0};
   OrthOut out;
   std::memset(&out, 0, sizeof(out));
@@ -143,8 +160,8 @@ abs_status abs_layer_norm(const abs_layer_norm_shape *shape, const void *x_dev, 
     return set_error(ABS_EINVAL, "pointers must be aligned to their type");
   const int64_t rows = (int64_t)shape->b * shape->T;
   const bool same = x_dev == y_dev && shape->ldx == shape->ldy && shape->stride_x == shape->stride_y;
-  if (!same && overlap(x_dev, extent(shape->M, shape->stride_x, rows, shape->ldx, shape->D, shape->type), y_dev,
-                       extent(shape->M, shape->stride_y, rows, shape->ldy, shape->D, shape->type)))
+  const Block x = {x_dev, shape->M, shape->stride_x, rows, shape->ldx, shape->D, e}, y = {y_dev, shape->M, shape->stride_y, rows, shape->ldy, shape->D, e};
+  if (!same && overlap(x, y))
     return set_error(ABS_EINVAL, "y_dev must be x_dev or not overlap it");
   LayerNormP p = layer_norm_args(shape);
   p.x = x_dev; p.gamma = gamma_dev; p.beta = beta_dev; p.eps = eps; p.y = y_dev; p.mean = mean_dev; p.rstd = rstd_dev;
@@ -175,12 +192,10 @@ abs_status abs_layer_norm_backward(const abs_layer_norm_shape *shape, const void
   for (const void *f : {(const void *)mean_dev, (const void *)rstd_dev, (const void *)dgamma_dev, (const void *)dbeta_dev, (const void *)n_dev, (const void *)q_dev})
     if (!aligned_to(f, 4)) return set_error(ABS_EINVAL, "pointers must be aligned to their type");
   const int64_t rows = (int64_t)shape->b * shape->T;
-  const int64_t ex = extent(shape->M, shape->stride_x, rows, shape->ldx, shape->D, shape->type);
-  const int64_t ey = extent(shape->M, shape->stride_y, rows, shape->ldy, shape->D, shape->type);
-  const int64_t ed = extent(shape->M, shape->stride_dx, rows, shape->lddx, shape->D, shape->type);
-  if (overlap(dx_dev, ed, x_dev, ex) || overlap(dx_dev, ed, dy_dev, ey)) return set_error(ABS_EINVAL, "dx_dev must not overlap x_dev or dy_dev");
-  if (overlap(workspace, (int64_t)need, x_dev, ex) || overlap(workspace, (int64_t)need, dy_dev, ey) || overlap(workspace, (int64_t)need, dx_dev, ed))
-    return set_error(ABS_EINVAL, "the workspace must not overlap x_dev, dy_dev or dx_dev");
+  const Block x = {x_dev, shape->M, shape->stride_x, rows, shape->ldx, shape->D, e}, dy = {dy_dev, shape->M, shape->stride_y, rows, shape->ldy, shape->D, e};
+  const Block dx = {dx_dev, shape->M, shape->stride_dx, rows, shape->lddx, shape->D, e}, ws = piece(workspace, (int64_t)need, 1);
+  if (overlap(dx, x) || overlap(dx, dy)) return set_error(ABS_EINVAL, "dx_dev must not overlap x_dev or dy_dev");
+  if (overlap(ws, x) || overlap(ws, dy) || overlap(ws, dx)) return set_error(ABS_EINVAL, "the workspace must not overlap x_dev, dy_dev or dx_dev");
   p.x = x_dev; p.gamma = gamma_dev; p.mean = const_cast<float *>(mean_dev); p.rstd = const_cast<float *>(rstd_dev);
   p.dy = dy_dev; p.dx = dx_dev; p.dgamma = dgamma_dev; p.dbeta = dbeta_dev; p.n = n_dev; p.q = q_dev;
   return hip_status(launch_layer_norm_backward(p, workspace, static_cast<hipStream_t>(hip_stream)), "abs_layer_norm_backward");

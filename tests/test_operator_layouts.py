@@ -1,0 +1,116 @@
+"""Layouts that the operators take: replicas or matrices interleaved by rows, results in other columns of the rows that are read."""
+import ctypes as C
+
+import pytest
+
+from test_operators import EINVAL, FAKE, WS, _A, _lib, _matrix, _orth, _shape
+
+gpu = pytest.mark.gpu
+
+
+# M = 2 replicas of 3 x 4 rows of 16
+@pytest.mark.parametrize("ld,stride,ok", [(32, 16, 1), (35, 17, 1), (33, 17, 1), (32, 17, 0), (31, 16, 0), (32, 15, 0), (32, 0, 0), (16, 192, 1),
+                                          (16, 191, 0), (20, 236, 1), (20, 235, 0), (16, 1 << 44, 1), (1 << 41, 16, 1), (16, 1 << 46, 0)])
+def test_which_rows_are_apart(ld, stride, ok):
+    lib, n = _lib(), C.c_size_t(0)
+    for names in (("ldx", "stride_x"), ("ldy", "stride_y"), ("lddx", "stride_dx")):
+        s = _shape(**dict(zip(names, (ld, stride))))
+        assert lib.abs_layer_norm_backward_workspace_bytes(C.byref(s), 1, 1, C.byref(n)) == (0 if ok else EINVAL), names
+
+
+# x: 2 x 12 rows of 16 floats, 40 floats from row to row; y begins `at` floats behind x (refused before a launch)
+@pytest.mark.parametrize("at,ldy", [(0, 44), (1, 40), (15, 40), (25, 40), (39, 40), (40, 40), (-16, 44), (480, 40), (16, 44), (16, 20), (55, 40)])
+def test_results_that_meet_what_is_read_are_refused(at, ldy):
+    lib = _lib()
+    s = _shape(ldx=40, stride_x=480, ldy=ldy, stride_y=12 * ldy, lddx=ldy, stride_dx=12 * ldy)
+    x, far = FAKE, [FAKE + (1 << 20) * i for i in range(1, 9)]
+    assert lib.abs_layer_norm(C.byref(s), x, far[0], None, 1e-5, x + 4 * at, None, None, None) == EINVAL
+    s.ldy, s.stride_y = 16, 192
+    assert lib.abs_layer_norm_backward(C.byref(s), far[0], x, *far[1:4], x + 4 * at, *far[4:8], WS, 1 << 20, None) == EINVAL
+    assert _orth(lib, g=x, o=x + 4 * at, rows=12, cols=16, ldg=40, sg=480, ldo=ldy, so=12 * ldy) == EINVAL
+
+
+def _interleaved(shape, ld, dtype, offset=0):
+    """A [M, ..., D] tensor whose rows lie side by side, `ld` values from one replica's to the next's, and the memory that it is in."""
+    import torch
+    M, D = shape[0], shape[-1]
+    rows = 1
+    for n in shape[1:-1]:
+        rows *= n
+    buf = torch.full((offset + rows * M * ld,), 5.0, device="cuda", dtype=dtype)
+    strides, step = [], M * ld
+    for n in reversed(shape[1:-1]):
+        strides.insert(0, step)
+        step *= n
+    return buf[offset:].as_strided(shape, (ld, *strides, 1)), buf
+
+
+@gpu
+@pytest.mark.parametrize("D,pad,offset", [(24, 0, 0), (33, 2, 1), (264, 8, 8), (600, 1, 0), (2056, 0, 0), (5001, 3, 1), (9000, 8, 0)])
+def test_layer_norm_of_interleaved_replicas(D, pad, offset):
+    import torch
+    A = _A()
+    for shape in ((3, 5, 4, D), (3, 2, 150, D), (4, 1, 1, D)):
+        for dtype in (torch.float32, torch.bfloat16):
+            gen = torch.Generator("cuda").manual_seed(D)
+            x, dy, out = (_interleaved(shape, D + pad, dtype, offset) for _ in range(3))
+            for t, _ in (x, dy):
+                t.copy_(torch.randn(shape, generator=gen, device="cuda"))
+            w, bias = (torch.randn((shape[0], D), generator=gen, device="cuda") for _ in range(2))
+            want = A.layer_norm(x[0].contiguous(), w, bias)
+            for p, r in zip(A.layer_norm(x[0], w, bias, out=out[0]), want):
+                assert torch.equal(p, r)
+            ref = A.layer_norm_backward(dy[0].contiguous(), x[0].contiguous(), w, *want[1:], want_norms=True, want_inner=True)
+            got = A.layer_norm_backward(dy[0], x[0], w, *want[1:], want_norms=True, want_inner=True)
+            for p, r in zip(got, ref):
+                assert torch.equal(p, r)
+            A.layer_norm(x[0], w, bias, out=x[0])                       # in place
+            assert torch.equal(x[0], want[0])
+            for t, buf in (x, dy, out):
+                t.fill_(5.0)
+                assert (buf == 5.0).all()                               # nothing between the rows is written
+
+
+@gpu
+@pytest.mark.parametrize("batch,rows,cols", [(3, 24, 40), (3, 40, 24), (4, 24, 1300), (2, 1290, 61), (3, 150, 161), (2, 300, 264), (40, 65, 203)])
+def test_orthogonalize_of_interleaved_matrices(batch, rows, cols):
+    import torch
+    A = _A()
+    G = _matrix("full", batch, rows, cols, torch.Generator().manual_seed(rows)).float().cuda()
+    want = A.orthogonalize(G)
+    for pad, offset in ((0, 0), (3, 1)):
+        g, out = (_interleaved((batch, rows, cols), cols + pad, torch.float32, offset) for _ in range(2))
+        g[0].copy_(G)
+        assert torch.equal(A.orthogonalize(g[0], out=out[0]), want)
+        assert torch.equal(g[0], G)
+        A.orthogonalize(g[0], out=g[0])
+        assert torch.equal(g[0], want)
+        for t, buf in (g, out):
+            t.fill_(5.0)
+            assert (buf == 5.0).all()
+
+
+@gpu
+def test_results_beside_what_is_read():
+    """The other half of the same rows."""
+    import torch
+    A = _A()
+    for D in (40, 1001):
+        both = torch.randn((3, 5, 4, 2 * D), device="cuda")
+        x, y = both[..., :D], both[..., D:]
+        keep, w = x.clone(), torch.randn((3, D), device="cuda")
+        want = A.layer_norm(keep, w)[0]
+        for src, dst in ((x, y), (y, x)):
+            src.copy_(keep)
+            A.layer_norm(src, w, out=dst)
+            assert torch.equal(dst, want) and torch.equal(src, keep)
+        with pytest.raises(A.AbsError, match="overlap"):
+            A.layer_norm(x, w, out=both[..., D - 1:2 * D - 1])
+    for rows, cols in ((40, 24), (24, 1300), (150, 161)):
+        both = torch.randn((2, rows, 2 * cols), device="cuda")
+        g, o = both[..., :cols], both[..., cols:]
+        keep = g.clone()
+        A.orthogonalize(g, out=o)
+        assert torch.equal(o, A.orthogonalize(keep)) and torch.equal(g, keep)
+        with pytest.raises(A.AbsError, match="overlap"):
+            A.orthogonalize(g, out=both[..., 1:cols + 1])
