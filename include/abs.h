@@ -375,7 +375,7 @@ typedef struct {
 } abs_layer_norm_shape;
 
 /*   beta_dev may be NULL (no bias); mean_dev, rstd_dev : device, float [M x b x T], each may be NULL.  y_dev may be x_dev with the
- *   same strides.  0 <= eps.  Asynchronous on the stream. */
+ *   same strides; no output overlaps an input or another output otherwise.  0 <= eps.  Asynchronous on the stream. */
 abs_status abs_layer_norm(const abs_layer_norm_shape *shape /*host*/, const void *x_dev, const void *gamma_dev, const void *beta_dev,
                           float eps, void *y_dev, float *mean_dev, float *rstd_dev, void *hip_stream);
 
@@ -387,7 +387,7 @@ abs_status abs_layer_norm(const abs_layer_norm_shape *shape /*host*/, const void
  *   n_i = ||g_i||^2,  q_i = <g_i, gbar>    (without beta: of the gamma part alone)
  * n_i and q_i add to those of other layers (abs_layer_stats): S1 = sum_i n_i, S2 = ||gbar||^2, S3 = sum_i q_i^2, S4 = sum_i q_i.
  *   mean_dev, rstd_dev : device, float [M x b x T], of the forward pass.
- *   dx_dev : overlaps neither x nor dy.   dgamma_dev, dbeta_dev : device, float [M x D]; dbeta_dev NULL: the layer has no bias.
+ *   No output overlaps an input, another output or the workspace.   dgamma_dev, dbeta_dev : device, float [M x D]; dbeta_dev NULL: the layer has no bias.
  *   n_dev, q_dev : device, float [M x b], either may be NULL.
  * Asynchronous on the stream; sums in a fixed order.  workspace: device, 256-byte aligned, of the size the other call tells for
  * the same shape and the same outputs asked for, used until the call's work has run.

@@ -36,6 +36,17 @@ bool overlap(const Block &a, const Block &b) {
   const uintptr_t space = (uintptr_t)pitch, d = q >= p ? (q - p) % space : (space - (p - q) % space) % space;
   return !(d >= (uintptr_t)(a.cols * a.bytes) && d + (uintptr_t)(b.cols * b.bytes) <= space);
 }
+// Any of the outputs over an input or another output (absent ones: null)
+template <size_t NO, size_t NI> bool outputs_overlap(const Block (&out)[NO], const Block (&in)[NI]) {
+  for (size_t i = 0; i < NO; ++i) {
+    if (!out[i].p) continue;
+    for (const Block &x : in)
+      if (x.p && overlap(out[i], x)) return true;
+    for (size_t j = 0; j < i; ++j)
+      if (out[j].p && overlap(out[i], out[j])) return true;
+  }
+  return false;
+}
 // rows that do not overlap, matrix after matrix or interleaved; offsets that 64 bits hold
 bool strides_ok(int64_t n, int64_t stride, int64_t rows, int64_t ld, int64_t cols) {
   const int64_t big = (int64_t)1 << 46;
@@ -161,8 +172,11 @@ abs_status abs_layer_norm(const abs_layer_norm_shape *shape, const void *x_dev, 
   const int64_t rows = (int64_t)shape->b * shape->T;
   const bool same = x_dev == y_dev && shape->ldx == shape->ldy && shape->stride_x == shape->stride_y;
   const Block x = {x_dev, shape->M, shape->stride_x, rows, shape->ldx, shape->D, e}, y = {y_dev, shape->M, shape->stride_y, rows, shape->ldy, shape->D, e};
-  if (!same && overlap(x, y))
-    return set_error(ABS_EINVAL, "y_dev must be x_dev or not overlap it");
+  if (!same && overlap(x, y)) return set_error(ABS_EINVAL, "y_dev must be x_dev or not overlap it");
+  const int64_t all = shape->M * rows, gains = (int64_t)shape->M * shape->D;
+  const Block out[] = {y, piece(mean_dev, all, 4), piece(rstd_dev, all, 4)}, params[] = {piece(gamma_dev, gains, pe), piece(beta_dev, gains, pe)};
+  if (outputs_overlap(out, params) || outputs_overlap({out[1], out[2]}, {x}))
+    return set_error(ABS_EINVAL, "y_dev, mean_dev and rstd_dev must not overlap an input or each other");
   LayerNormP p = layer_norm_args(shape);
   p.x = x_dev; p.gamma = gamma_dev; p.beta = beta_dev; p.eps = eps; p.y = y_dev; p.mean = mean_dev; p.rstd = rstd_dev;
   return hip_status(launch_layer_norm(p, static_cast<hipStream_t>(hip_stream)), "abs_layer_norm");
@@ -192,10 +206,12 @@ abs_status abs_layer_norm_backward(const abs_layer_norm_shape *shape, const void
   for (const void *f : {(const void *)mean_dev, (const void *)rstd_dev, (const void *)dgamma_dev, (const void *)dbeta_dev, (const void *)n_dev, (const void *)q_dev})
     if (!aligned_to(f, 4)) return set_error(ABS_EINVAL, "pointers must be aligned to their type");
   const int64_t rows = (int64_t)shape->b * shape->T;
-  const Block x = {x_dev, shape->M, shape->stride_x, rows, shape->ldx, shape->D, e}, dy = {dy_dev, shape->M, shape->stride_y, rows, shape->ldy, shape->D, e};
-  const Block dx = {dx_dev, shape->M, shape->stride_dx, rows, shape->lddx, shape->D, e}, ws = piece(workspace, (int64_t)need, 1);
-  if (overlap(dx, x) || overlap(dx, dy)) return set_error(ABS_EINVAL, "dx_dev must not overlap x_dev or dy_dev");
-  if (overlap(ws, x) || overlap(ws, dy) || overlap(ws, dx)) return set_error(ABS_EINVAL, "the workspace must not overlap x_dev, dy_dev or dx_dev");
+  const int64_t all = shape->M * rows, gains = (int64_t)shape->M * shape->D, samples = (int64_t)shape->M * shape->b;
+  const Block in[] = {{x_dev, shape->M, shape->stride_x, rows, shape->ldx, shape->D, e}, {dy_dev, shape->M, shape->stride_y, rows, shape->ldy, shape->D, e},
+                      piece(gamma_dev, gains, type_bytes(shape->param_type)), piece(mean_dev, all, 4), piece(rstd_dev, all, 4)};
+  const Block out[] = {{dx_dev, shape->M, shape->stride_dx, rows, shape->lddx, shape->D, e}, piece(dgamma_dev, gains, 4), piece(dbeta_dev, gains, 4),
+                       piece(n_dev, samples, 4), piece(q_dev, samples, 4), piece(workspace, (int64_t)need, 1)};
+  if (outputs_overlap(out, in)) return set_error(ABS_EINVAL, "outputs and the workspace must not overlap an input or each other");
   p.x = x_dev; p.gamma = gamma_dev; p.mean = const_cast<float *>(mean_dev); p.rstd = const_cast<float *>(rstd_dev);
   p.dy = dy_dev; p.dx = dx_dev; p.dgamma = dgamma_dev; p.dbeta = dbeta_dev; p.n = n_dev; p.q = q_dev;
   return hip_status(launch_layer_norm_backward(p, workspace, static_cast<hipStream_t>(hip_stream)), "abs_layer_norm_backward");

@@ -30,6 +30,36 @@ def test_results_that_meet_what_is_read_are_refused(at, ldy):
     assert _orth(lib, g=x, o=x + 4 * at, rows=12, cols=16, ldg=40, sg=480, ldo=ldy, so=12 * ldy) == EINVAL
 
 
+def test_outputs_that_meet_an_operand_are_refused():
+    """Each output of the gradients over each input, another output or the workspace, and of the forward pass; by one value."""
+    lib = _lib()
+    s = _shape()                                      # x, dy, dx: 384 values; gains 32; statistics of rows 24, of samples 6
+    names = ("dy", "x", "gamma", "mean", "rstd", "dx", "dgamma", "dbeta", "n", "q")
+    size = dict(dy=384, x=384, gamma=32, mean=24, rstd=24, dx=384, dgamma=32, dbeta=32, n=6, q=6)
+    for o in names[5:]:
+        for other in names:
+            if other == o:
+                continue
+            at = {name: FAKE + (1 << 20) * i for i, name in enumerate(names)}
+            at[o] = at[other] + 4 * (size[other] - 1)
+            assert lib.abs_layer_norm_backward(C.byref(s), *[at[name] for name in names], WS, 1 << 20, None) == EINVAL, (o, other)
+            assert b"overlap" in lib.abs_last_error(None)
+    for o in names:
+        at = {name: FAKE + (1 << 20) * i for i, name in enumerate(names)}
+        at[o] = WS - 4 * (size[o] - 1)
+        assert lib.abs_layer_norm_backward(C.byref(s), *[at[name] for name in names], WS, 1 << 20, None) == EINVAL, o
+        assert b"overlap" in lib.abs_last_error(None)
+    names, size = ("x", "gamma", "beta", "y", "mean", "rstd"), dict(size, beta=32, y=384)
+    for o in names[3:]:
+        for other in names:
+            if other == o:
+                continue
+            at = {name: FAKE + (1 << 20) * i for i, name in enumerate(names)}
+            at[o] = at[other] + 4 * (size[other] - 1)
+            assert lib.abs_layer_norm(C.byref(s), at["x"], at["gamma"], at["beta"], 1e-5, at["y"], at["mean"], at["rstd"], None) == EINVAL, (o, other)
+            assert b"overlap" in lib.abs_last_error(None)
+
+
 def _interleaved(shape, ld, dtype, offset=0):
     """A [M, ..., D] tensor whose rows lie side by side, `ld` values from one replica's to the next's, and the memory that it is in."""
     import torch
