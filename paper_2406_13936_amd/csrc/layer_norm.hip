@@ -275,10 +275,12 @@ __global__ void __launch_bounds__(ln_threads(G)) ln_forward_kernel(const LayerNo
   }
 }
 
-// Rows longer than the registers of a block hold: three passes over the row, the later two out of the caches
-__global__ void __launch_bounds__(256) ln_forward_long_kernel(const LayerNormP p) {
+// Rows longer than the registers of a block hold: three passes over the row, the later two out of the caches.  A launch takes LN_LONG_ROWS rows:
+// a grid counts its threads in 32 bits.  (Blocks that take several rows one after the other need 1.1 to 1.2 times as long.)
+constexpr int LN_LONG_ROWS = 1 << 18;
+__global__ void __launch_bounds__(256) ln_forward_long_kernel(const LayerNormP p, const long long first) {
   __shared__ __attribute__((aligned(16))) float sm[8];
-  const long long rows = (long long)p.b * p.T, m = blockIdx.x / rows, r = blockIdx.x - m * rows;
+  const long long rows = (long long)p.b * p.T, i = first + blockIdx.x, m = i / rows, r = i - m * rows;
   const long long xa = m * p.sx + r * p.ldx, ya = m * p.sy + r * p.ldy, pa = m * p.D;
   const float n = (float)p.D;
   float s[1] = {0.0f};
@@ -730,7 +732,8 @@ hipError_t launch_layer_norm(const LayerNormP &p, hipStream_t s) {
   if (rows == 0) return hipSuccess;
   if (rows * p.M > 0x7fffffff) return hipErrorInvalidValue;
   if (p.D > LN_MAX_D) {
-    hipLaunchKernelGGL(ln_forward_long_kernel, dim3((unsigned)(rows * p.M)), dim3(256), 0, s, p);
+    for (long long first = 0; first < rows * p.M; first += LN_LONG_ROWS)
+      hipLaunchKernelGGL(ln_forward_long_kernel, dim3((unsigned)std::min<long long>(rows * p.M - first, LN_LONG_ROWS)), dim3(256), 0, s, p, first);
     return hipGetLastError();
   }
   return by_type<Forward>(p, rows_of_vectors(p.x, p.type, p.sx, p.ldx, p.D) && rows_of_vectors(p.y, p.type, p.sy, p.ldy, p.D), s);

@@ -21,3 +21,20 @@ def test_constant_rows_of_huge_values(D, dtype):
         assert torch.equal(y, bias[:, None, None].to(y.dtype).expand_as(y)) and (mean == 2.0 ** 113).all() and (rstd > 9e5).all()
         got = A.layer_norm_backward(dy, x, w, mean, rstd, want_norms=True, want_inner=True)
         _check_backward(got, dy, x, w, mean, rstd, True, dtype)
+
+
+@gpu
+def test_more_long_rows_than_a_launch_takes():
+    """(A block to a row would be more threads than a grid counts from 2^24 rows on, which fit the card in place.)"""
+    import torch
+    A = _A()
+    M, b, D = 2, (1 << 17) + 5, 8193
+    gen = torch.Generator("cuda").manual_seed(1)
+    x = torch.randn((M, b, D), generator=gen, device="cuda", dtype=torch.bfloat16)
+    w, bias = (torch.randn((M, D), generator=gen, device="cuda") for _ in range(2))
+    keep = x.clone()
+    y, mean, rstd = A.layer_norm(x, w, bias, out=x)
+    for i in (slice(0, 3), slice(b - 12, b)):
+        for p, r in zip((y, mean, rstd), A.layer_norm(keep[:, i], w, bias)):
+            assert torch.equal(p[:, i], r)
+    _check_forward(y[:, -9:, None], mean[:, -9:, None], rstd[:, -9:, None], keep[:, -9:, None], w, bias, 1e-5, "bf16")
