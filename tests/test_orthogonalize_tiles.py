@@ -188,3 +188,27 @@ def test_short_sides_take_products_of_both_parts(rows, cols):
             want = _orth(G[i].double())
             assert (out[i].double() - want).norm() <= (TOL32 + U32) * want.norm(), i
         assert torch.equal(out, B.orthogonalize(G, prec=B.PREC_F32))
+
+
+@gpu
+@pytest.mark.parametrize("batch,rows,cols", [(3, 48, 80), (2, 128, 100), (3, 40, 1200), (2, 1100, 20), (3, 200, 144), (1, 264, 600), (1, 1000, 1000)])
+@pytest.mark.parametrize("prec", [B.PREC_BF16, B.PREC_F32])
+def test_matrices_whose_norm_is_about_eps_or_below(batch, rows, cols, prec):
+    """X_k is held to 2^-40 (later, where its bound is above 1, 2^-39) of 1, an entry; N entries are off by sqrt(N) times that, which each later
+    step multiplies by 3.4445 like X itself: 2^-40 sqrt(N) / |X_0| (1 + 2 / 3.4 + 2 / 3.4^2 + ..) of the result, at most 2 of the first term."""
+    import torch
+    gen = torch.Generator().manual_seed(rows)
+    G = _matrix("full", batch, rows, cols, gen).cuda()
+    G /= torch.linalg.vector_norm(G, dim=(1, 2), keepdim=True)
+    for eps in (1e-7, 1e-3):
+        for ratio in (1.0, 1e-3, 1e-6):
+            g = (G * (eps * ratio)).float()
+            out = B.orthogonalize(g, prec=prec, eps=eps)
+            for i in range(batch):
+                x = g[i].double() / (torch.linalg.vector_norm(g[i].double()) + eps)
+                held = 2.0 * 2.0 ** -40 * math.sqrt(rows * cols) / float(x.norm())
+                for _ in range(5):
+                    k = x @ x.T.contiguous()
+                    x = COEF[0] * x + (COEF[1] * k + COEF[2] * (k @ k)) @ x
+                err = float((out[i].double() - x).norm() / x.norm())
+                assert err <= _tol(prec, rows, cols) + U32 + held, (eps, ratio, i, err, held)
