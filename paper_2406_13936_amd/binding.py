@@ -557,6 +557,8 @@ def _orth_bytes(batch: int, rows: int, cols: int, prec: int) -> int:
 def _coefficients(coefficients, steps: int):
     if coefficients is None:
         return None
+    if int(steps) < 1:
+        raise AbsError("steps must be in [1, 32]")
     flat = np.ascontiguousarray(coefficients, dtype=np.float32).reshape(-1)
     if flat.size == 3:
         flat = np.tile(flat, int(steps))
@@ -630,7 +632,9 @@ def _norm_shape(shape, stride, kind: int, param_kind: int, other_shape, other_st
 
 
 def _norm_params(x, p, what: str) -> int:
-    if p.shape[0] != x.shape[0] or p.shape[-1] != x.shape[-1] or p.dim() != 2 or not p.is_contiguous():
+    if x.dim() < 3:
+        raise AbsError("x must be [M, b, ..., D]")
+    if p.dim() != 2 or p.shape[0] != x.shape[0] or p.shape[1] != x.shape[-1] or not p.is_contiguous():
         raise AbsError(f"{what} must be a contiguous [M, D] tensor")
     return _type_of(p, what)
 

@@ -60,6 +60,21 @@ def test_outputs_that_meet_an_operand_are_refused():
             assert b"overlap" in lib.abs_last_error(None)
 
 
+def test_wrong_dimensions_and_numbers_of_steps_are_refused_like_all_else():
+    import torch
+    from paper_2406_13936_amd import binding as B
+    x = torch.zeros(2, 3, 8)
+    for y, p in ((x, torch.zeros(())), (x, torch.zeros(8)), (x, torch.zeros(2, 1, 8)), (x, torch.zeros(2, 7)), (torch.zeros(()), torch.zeros(2, 8)),
+                 (torch.zeros(8), torch.zeros(8, 8)), (torch.zeros(2, 8), torch.zeros(2, 8))):
+        with pytest.raises(B.AbsError):
+            B._norm_params(y, p, "weight")
+    for steps in (0, -1):
+        with pytest.raises(B.AbsError, match="steps"):
+            B._coefficients((1.5, -0.5, 0.0), steps)
+    with pytest.raises(B.AbsError, match="two dimensions"):
+        B._matrices((8,), (1,), "g")
+
+
 def _interleaved(shape, ld, dtype, offset=0):
     """A [M, ..., D] tensor whose rows lie side by side, `ld` values from one replica's to the next's, and the memory that it is in."""
     import torch
