@@ -451,6 +451,9 @@ def average_bf16_static(params):
 # Single-token calls run for a few microseconds on the GPU, so the host's part is kept short: checks go by shapes, strides and
 # types and their outcome is kept by these, the device is only switched where it has to be, and the stream is asked for as a
 # plain handle.
+#
+# Like every call here they are outside autograd: results never require a gradient, whatever their inputs do.  What a call changes in
+# place counts as changed (saved for a backward pass, it makes that pass raise).
 
 _torch = None
 _TYPES = {}
@@ -489,6 +492,11 @@ def _call(dev: int, fn, *args):
     else:
         with _torch.cuda.device(dev):
             _check(fn(*args, _torch._C._cuda_getCurrentRawStream(dev)))
+
+
+def _written(*tensors):
+    """Lets autograd know that kernels have changed tensors of the caller in place."""
+    _torch.autograd.graph.increment_version(tensors)
 
 
 def _workspace(nbytes: int, device):
@@ -573,7 +581,8 @@ def orthogonalize(g, steps: int = 5, coefficients=None, eps: float = 1e-7, prec:
     type can tell apart, PREC_BF16 for bfloat16 only."""
     lib, _ = _lib_and_torch()
     gt = _type_of(g, "g")
-    if out is None:
+    given = out is not None
+    if not given:
         out, ot = _like(g), gt
     else:
         ot = _type_of(out, "out")
@@ -588,13 +597,15 @@ def orthogonalize(g, steps: int = 5, coefficients=None, eps: float = 1e-7, prec:
     keep, ws = _workspace(nbytes, g.device)
     _call(dev, lib.abs_orthogonalize, g.data_ptr(), gt, ldg, sg, out.data_ptr(), ot, ldo, so, batch, rows, cols, int(steps),
           None if coef is None else coef.ctypes.data, eps, prec, ws, nbytes)
+    if given:
+        _written(out)
     return out
 
 
 def muon_step(x, g, v, lr: float, momentum: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
               scale: Optional[float] = None, steps: int = 5, coefficients=None, eps: float = 1e-7, prec: Optional[int] = None):
     """One step with orthogonalised momentum on [..., rows, cols] device matrices, in place on x and on the fp32 momentum v
-    (abs_muon_step).  scale defaults to 0.2 sqrt(max(rows, cols)); prec to PREC_F32 where x is float32."""
+    (abs_muon_step), as an optimizer does under no_grad.  scale defaults to 0.2 sqrt(max(rows, cols)); prec to PREC_F32 where x is float32."""
     lib, _ = _lib_and_torch()
     xt, gt = _type_of(x, "x"), _type_of(g, "g")
     if _type_of(v, "v") != 0:
@@ -613,6 +624,7 @@ def muon_step(x, g, v, lr: float, momentum: float = 0.95, weight_decay: float = 
     keep, ws = _workspace(nbytes, x.device)
     _call(dev, lib.abs_muon_step, x.data_ptr(), xt, g.data_ptr(), gt, v.data_ptr(), batch, rows, cols, lr, momentum,
           1 if nesterov else 0, weight_decay, scale, int(steps), None if coef is None else coef.ctypes.data, eps, prec, ws, nbytes)
+    _written(x, v)
 
 
 @functools.lru_cache(maxsize=512)
@@ -641,7 +653,8 @@ def _norm_params(x, p, what: str) -> int:
 
 def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None):
     """Layer norm of [M, b, ..., D] over the last dimension with weights and biases [M, D] (fp32 or x's type), one set per
-    replica.  Returns (y, mean, rstd), the latter two fp32 [M, b, ...]; `out` may be x itself."""
+    replica.  Returns (y, mean, rstd), the latter two fp32 [M, b, ...]; `out` may be x itself.  No autograd graph is kept: gradients
+    are layer_norm_backward's."""
     lib, torch = _lib_and_torch()
     kind = _type_of(x, "x")
     pt = _norm_params(x, weight, "weight")
@@ -656,6 +669,8 @@ def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None):
     rstd = torch.empty_like(mean)
     _call(dev, lib.abs_layer_norm, shape, x.data_ptr(), weight.data_ptr(), bias.data_ptr() if bias is not None else None, eps,
           y.data_ptr(), mean.data_ptr(), rstd.data_ptr())
+    if out is not None:
+        _written(y)
     return y, mean, rstd
 
 
