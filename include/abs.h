@@ -326,13 +326,13 @@ enum { ABS_TYPE_F32 = 0, ABS_TYPE_BF16 = 1, ABS_TYPE_F16 = 2 };
  * (with A = X^T X on the right where rows > cols: the same X).  A zero matrix gives zeros, one with an infinity or NaN gives NaN
  * and leaves the others alone.
  *   g_dev, o_dev : device, [batch][rows][cols]; ldg, ldo: values from row to row (>= cols), stride_g, stride_o: from matrix to
- *                  matrix, whose rows do not overlap: matrix after matrix, or interleaved by rows.  Any alignment of the type; rows that start on 16 bytes and hold a multiple of 8 values are faster.
+ *                  matrix, whose rows do not overlap: matrix after matrix, or interleaved by rows.  Any alignment of the type.
  *                  o_dev may be g_dev (same type and strides); it must not overlap it otherwise
  *                  (columns of the same rows that are apart do not).
  *   steps        : 1 .. 32.
  *   coef         : host, 3 * steps floats a, b, c, step by step, or NULL: (3.4445, -4.7750, 2.0315) in all, which takes singular
- *                  values from 0.01 on to about 0.7 .. 1.2 in five steps.  Coefficients that let a singular value of at most 1 grow
- *                  beyond 256 are refused.
+ *                  values from 0.01 on to about 0.7 .. 1.2 in five steps.  Coefficients are refused that let a singular value of at
+ *                  most 1 grow beyond 256, or b s^2 + c s^4 beyond 4096, or that leave none above 1/256.
  *   prec         : ABS_PREC_BF16: products of 16-bit operands (fp16 with powers of two that keep them in range; X itself is held
  *                  in 32 bits): relative error of the result 0.5 to 1.6e-3, no more than a bf16 result's own rounding adds.
  *                  (Up to 128 rows or columns the products are those of ABS_PREC_F32 all the same.)
@@ -385,7 +385,9 @@ abs_status abs_layer_norm(const abs_layer_norm_shape *shape /*host*/, const void
  *   xh = (x - mu) r,  h = dy gamma,  dx = r (h - mean_d h - xh mean_d(h xh))
  *   g_i = (sum_t dy xh, sum_t dy) over the T rows of sample i;  (dgamma, dbeta) = gbar = (1 / b) sum_i g_i
  *   n_i = ||g_i||^2,  q_i = <g_i, gbar>    (without beta: of the gamma part alone)
- * n_i and q_i add to those of other layers (abs_layer_stats): S1 = sum_i n_i, S2 = ||gbar||^2, S3 = sum_i q_i^2, S4 = sum_i q_i.
+ * n_i and q_i add to those of the same samples' other parameters: S1 = sum_i n_i, S2 = ||gbar||^2, S3 = sum_i q_i^2, S4 = sum_i q_i.
+ * (Linear layers': abs_layer_stats with T = 1, as it takes one row to a sample; a sample of several rows has no factored norm there,
+ * so with T > 1 these are the statistics of the norms' parameters alone.)
  *   mean_dev, rstd_dev : device, float [M x b x T], of the forward pass.
  *   No output overlaps an input, another output or the workspace.   dgamma_dev, dbeta_dev : device, float [M x D]; dbeta_dev NULL: the layer has no bias.
  *   n_dev, q_dev : device, float [M x b], either may be NULL.

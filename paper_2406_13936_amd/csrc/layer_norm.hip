@@ -608,7 +608,8 @@ __global__ void __launch_bounds__(256) ln_inner_long_kernel(const LayerNormP p) 
 constexpr int LN_MAX_D = 8192;           // longest row that a block's registers hold
 // Blocks of the backward pass: two to a CU of 256 threads, one of 512.  Their loads keep memory as busy as those of more blocks, which leave
 // more partials and, where registers hold only two or three of them on a CU, a last round (8 x 8192 rows of 2048: 512 blocks 170 us, 768
-// 184, 1024 176; 4 x 4096 rows of 4096 98, 107, 118).
+// 184, 1024 176; 4 x 4096 rows of 4096 98, 107, 118).  Whole samples make fewer where their number is just past a multiple of the blocks
+// (n_i of 512 samples of 64 rows of 2048 79 us, of 513 in 257 blocks of two 106, of 600 121).
 constexpr int LN_BLOCKS = 512;
 
 // lanes and vectors to a row: 16 x 1, 64 x 1, 64 x 2, 256 x 1, 256 x 2, 512 x 2 (256 x 4 fill the registers with one row: gradients of
