@@ -212,3 +212,33 @@ def test_matrices_whose_norm_is_about_eps_or_below(batch, rows, cols, prec):
                     x = COEF[0] * x + (COEF[1] * k + COEF[2] * (k @ k)) @ x
                 err = float((out[i].double() - x).norm() / x.norm())
                 assert err <= _tol(prec, rows, cols) + U32 + held, (eps, ratio, i, err, held)
+
+
+@gpu
+@pytest.mark.parametrize("rows,cols,blocks", [(23000, 23000, 92), (13000, 41000, 50), (41000, 13000, 50)])
+@pytest.mark.parametrize("prec", [B.PREC_BF16, B.PREC_F32])
+def test_matrices_of_almost_as_many_values_as_are_taken(rows, cols, blocks, prec):
+    """Blocks that meet in no row or column, scattered over the matrix: each is taken for itself, with the norm of all of them, and what
+    lies in none stays zero."""
+    import torch
+    gen = torch.Generator("cuda").manual_seed(rows)
+    r, c = rows // blocks, cols // blocks
+    P = torch.randn((blocks, r, c), generator=gen, device="cuda")
+    ri = torch.randperm(rows, generator=gen, device="cuda").view(blocks, r)
+    ci = torch.randperm(cols, generator=gen, device="cuda").view(blocks, c)
+    G = torch.zeros((rows, cols), device="cuda")
+    for k in range(blocks):
+        G[ri[k][:, None], ci[k]] = P[k]
+    x = P.double() / (torch.linalg.vector_norm(P.double()) + 1e-7)
+    for _ in range(5):
+        k = torch.matmul(x, x.transpose(1, 2).contiguous())
+        x = COEF[0] * x + torch.matmul(COEF[1] * k + COEF[2] * torch.matmul(k, k), x)
+    out = B.orthogonalize(G[None], prec=prec)[0]
+    del G
+    got = torch.stack([out[ri[k][:, None], ci[k]] for k in range(blocks)])
+    assert (got.double() - x).norm() <= (_tol(prec, rows, cols) + U32) * x.norm()
+    for k in range(blocks):
+        out[ri[k][:, None], ci[k]] = 0.0
+    assert int(torch.count_nonzero(out)) == 0
+    with pytest.raises(B.AbsError, match="2\\^29"):
+        B.orthogonalize(torch.empty((1, 1 << 15, 1 << 14), device="cuda"))
