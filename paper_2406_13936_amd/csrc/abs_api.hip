@@ -1281,7 +1281,10 @@ static abs_status local_step_impl(abs_ctx *c, const int32_t *idx_dev, int ldi, i
   up.beta1 = c->cfg.beta1; up.beta2 = c->cfg.beta2; up.eps = c->cfg.eps; up.wd = c->cfg.weight_decay;
   up.c1 = ph.c1; up.c2 = ph.c2; up.scal = ph.scal;
   if (s2_in_update) up.sq_wave = c->at<float>(pl.o_sqwave);
-  { ProfScope ps_(c, T_UPDATE, 0.0, muon ? 4.0 * M * pl.P : 1.0 * M * pl.P * (c->cfg.opt == ABS_OPT_SGD ? 12 : c->cfg.opt == ABS_OPT_ADAMW ? 28 : 20) + (pl.bf16 ? 2.0 * M * pl.P : 0.0));
+  double stepped = (double)pl.P;         // values that the update's launch steps (Muon: of the others it reads the gradient for ||gbar||^2)
+  for (int l = 1; l < L && muon; ++l) stepped -= (double)pl.dims[l] * pl.dims[l - 1];
+  const double step_bytes = (c->cfg.opt == ABS_OPT_SGD ? 12 : has_first_moment(c->cfg.opt) ? 28 : 20) + (pl.bf16 ? 2 : 0);
+  { ProfScope ps_(c, T_UPDATE, 0.0, M * (stepped * step_bytes + (s2_in_update ? 4.0 * (pl.P - stepped) : 0.0)));
   if (muon) {
     MuonRestP mr;                        // biases and the last layer take AdamW's step
     std::memset(&mr, 0, sizeof(mr));
