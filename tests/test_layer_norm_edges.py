@@ -38,3 +38,41 @@ def test_more_long_rows_than_a_launch_takes():
         for p, r in zip((y, mean, rstd), A.layer_norm(keep[:, i], w, bias)):
             assert torch.equal(p[:, i], r)
     _check_forward(y[:, -9:, None], mean[:, -9:, None], rstd[:, -9:, None], keep[:, -9:, None], w, bias, 1e-5, "bf16")
+
+
+@gpu
+@pytest.mark.parametrize("D", [8, 40, 256, 1024, 2048, 4096, 8192, 8200])
+@pytest.mark.parametrize("dtype,ptype", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+def test_gains_and_sums_that_no_vector_begins_on(D, dtype, ptype):
+    """Rows of whole vectors beside gains, biases, batch gradients and statistics one value off any; and without the outputs that may be absent."""
+    import ctypes as C
+    import torch
+    from paper_2406_13936_amd import binding as B
+    A = _A()
+    M, b, T = 2, 5, 3
+    x, w, bias, dy = _ln_inputs(M, b, T, D, dtype, ptype)
+
+    def off(t):
+        buf = torch.zeros(t.numel() + 1, device="cuda", dtype=t.dtype)
+        v = buf[1:].view(t.shape)
+        return v.copy_(t)
+    y, mean, rstd = A.layer_norm(x, w, bias)
+    for p, r in zip(A.layer_norm(x, off(w), off(bias)), (y, mean, rstd)):
+        assert torch.equal(p, r)
+    want = A.layer_norm_backward(dy, x, w, mean, rstd, want_norms=True, want_inner=True)
+    got = [off(torch.zeros_like(t)) for t in want]
+    got[0] = torch.empty_like(want[0])
+    lib = B.load_library()
+    kind = lambda s: {"f32": 0, "bf16": 1, "f16": 2}[s]  # noqa: E731
+    s = B.LayerNormShape(M, b, T, D, kind(dtype), kind(ptype), D, b * T * D, D, b * T * D, D, b * T * D)
+    n = C.c_size_t(0)
+    assert lib.abs_layer_norm_backward_workspace_bytes(C.byref(s), 1, 1, C.byref(n)) == 0
+    keep, ws = B._workspace(n.value, x.device)
+    stream = torch.cuda.current_stream().cuda_stream
+    ins = [dy, x, off(w), off(mean), off(rstd)]
+    assert lib.abs_layer_norm_backward(C.byref(s), *[t.data_ptr() for t in ins + got], ws, n.value, stream) == 0
+    for p, r in zip(got, want):
+        assert torch.equal(p, r)
+    z = torch.empty_like(y)
+    assert lib.abs_layer_norm(C.byref(s), x.data_ptr(), w.data_ptr(), bias.data_ptr(), 1e-5, z.data_ptr(), None, None, stream) == 0
+    assert torch.equal(z, y)
