@@ -679,8 +679,8 @@ def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None):
 def layer_norm_backward(dy, x, weight, mean, rstd, has_bias: bool = True, want_norms: bool = False, want_inner: bool = False):
     """Gradients of layer_norm from the signals dy [M, b, ..., D] of the per-sample losses, and the batch tests' statistics of
     the gradient of weight and bias.  Returns (dx, dweight, dbias, n, q): batch gradients fp32 [M, D] (means over the b
-    samples; dbias None without a bias), n_i = ||g_i||^2 and q_i = <g_i, gbar> fp32 [M, b], None unless asked for.  They add to layer_stats' of linear
-    layers, which take one row to a sample: samples of several rows have no such partner here."""
+    samples; dbias None without a bias), n_i = ||g_i||^2 and q_i = <g_i, gbar> fp32 [M, b], None unless asked for.  They add
+    to layer_stats' of linear layers, which take one row to a sample: samples of several rows have no such partner here."""
     lib, torch = _lib_and_torch()
     kind = _type_of(x, "x")
     pt = _norm_params(x, weight, "weight")

@@ -30,6 +30,30 @@ def test_results_that_meet_what_is_read_are_refused(at, ldy):
     assert _orth(lib, g=x, o=x + 4 * at, rows=12, cols=16, ldg=40, sg=480, ldo=ldy, so=12 * ldy) == EINVAL
 
 
+def test_no_layouts_that_meet_are_taken_for_apart():
+    """Random blocks of both kinds, value by value: what meets is refused (before a launch; the others are not called)."""
+    import random
+    lib, rng, met = _lib(), random.Random(4), 0
+
+    def block(M, rows, D):
+        while True:
+            ld, stride = rng.randint(1, 40), rng.randint(0, 90)
+            if M == 1 or stride >= (rows - 1) * ld + D or (stride >= D and ld >= (M - 1) * stride + D):
+                if ld >= D:
+                    return ld, stride, {m * stride + r * ld + c for m in range(M) for r in range(rows) for c in range(D)}
+    for _ in range(20000):
+        M, rows, D = rng.randint(1, 3), rng.randint(1, 4), rng.randint(1, 6)
+        (ldx, sx, x), (ldy, sy, y) = block(M, rows, D), block(M, rows, D)
+        at = rng.randint(-150, 150)
+        if (at == 0 and (ldx, sx) == (ldy, sy)) or x.isdisjoint(v + at for v in y):
+            continue
+        met += 1
+        s = _shape(M=M, b=rows, T=1, D=D, ldx=ldx, stride_x=sx, ldy=ldy, stride_y=sy)
+        assert lib.abs_layer_norm(C.byref(s), FAKE, FAKE + (1 << 20), None, 1e-5, FAKE + 4 * at, None, None, None) == EINVAL, (M, rows, D, ldx, sx, ldy, sy, at)
+        assert b"overlap" in lib.abs_last_error(None)
+    assert met > 2000
+
+
 def test_outputs_that_meet_an_operand_are_refused():
     """Each output of the gradients over each input, another output or the workspace, and of the forward pass; by one value."""
     lib = _lib()
@@ -159,3 +183,34 @@ def test_results_beside_what_is_read():
         assert torch.equal(o, A.orthogonalize(keep)) and torch.equal(g, keep)
         with pytest.raises(A.AbsError, match="overlap"):
             A.orthogonalize(g, out=both[..., 1:cols + 1])
+
+
+@gpu
+def test_results_between_the_replicas_that_are_read():
+    """Each replica with memory of its own, in which operands and results follow each other; statistics in a gap between replicas."""
+    import torch
+    A = _A()
+    for M, b, D in ((3, 6, 40), (2, 5, 1001)):
+        n = b * D
+        arena = torch.randn((M, 3 * n + 7), device="cuda")
+        x, y = (arena[:, i * n:(i + 1) * n].view(M, b, D) for i in (0, 2))
+        keep, w = x.clone(), torch.randn((M, D), device="cuda")
+        want = A.layer_norm(keep, w)
+        for src, dst in ((x, y), (y, x)):
+            src.copy_(keep)
+            assert torch.equal(A.layer_norm(src, w, out=dst)[0], want[0]) and torch.equal(src, keep)
+        gains = arena[0, n:n + M * D].view(M, D)                        # (as many as fit between two pieces)
+        if M * D <= n:
+            x.copy_(keep)
+            gains.copy_(w)
+            assert torch.equal(A.layer_norm(x, gains, out=y)[0], want[0])
+        mid = arena[:, n - 1:2 * n - 1].as_strided((M, b, D), (3 * n + 7, D, 1), arena.storage_offset() + n - 1)
+        with pytest.raises(A.AbsError, match="overlap"):
+            A.layer_norm(x, w, out=mid)
+    for rows, cols in ((40, 24), (24, 1300), (150, 161)):
+        n = rows * cols
+        arena = torch.randn((3, 2 * n), device="cuda")
+        g, o = (arena[:, i * n:(i + 1) * n].view(3, rows, cols) for i in (0, 1))
+        keep = g.clone()
+        A.orthogonalize(g, out=o)
+        assert torch.equal(o, A.orthogonalize(keep)) and torch.equal(g, keep)
