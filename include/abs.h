@@ -400,6 +400,83 @@ abs_status abs_layer_norm_backward(const abs_layer_norm_shape *shape /*host*/, c
                                    float *dgamma_dev, float *dbeta_dev, float *n_dev, float *q_dev, void *workspace,
                                    size_t workspace_bytes, void *hip_stream);
 
+/* Types of whole numbers in device memory. */
+enum { ABS_TYPE_I32 = 16, ABS_TYPE_I64 = 17 };
+
+/*
+ * Token embedding of M replicas with tables of their own:  y_t = scale table[token_t]   (one rounding, to y's type).
+ * A token outside [0, V) is padding: its row of y is zeros, and it has no part in any gradient.
+ * At most 2^20 replicas, 2^25 samples (M b), 2^31 - 1 tokens (M b T) and 2^30 words; beyond: ABS_EUNSUPPORTED.
+ */
+typedef struct {
+  int M, b, T, V, D;          /* replicas, samples of each, tokens of a sample, words of a table, values of a row; all >= 1 */
+  int token_type;             /* ABS_TYPE_I32 or ABS_TYPE_I64; tokens are [M x b x T] without gaps */
+  int type;                   /* ABS_TYPE_* of y, or of dy */
+  int table_type;             /* ABS_TYPE_* of the table [M x V x D] (forward) */
+  int64_t ldy, stride_y;      /* y or dy: values from row to row (>= D) and from replica to replica; rows do not overlap: replica after
+                                 replica, or interleaved by rows */
+} abs_embedding_shape;
+
+/*   y_dev overlaps no input.  Asynchronous on the stream. */
+abs_status abs_embedding(const abs_embedding_shape *shape /*host*/, const void *tokens_dev, const void *table_dev, float scale,
+                         void *y_dev, void *hip_stream);
+
+/*
+ * Its gradient, from the backprop signals dy of the per-sample losses (as elsewhere here, not divided by the batch size), and the batch
+ * tests' statistics of it:
+ *   g_i = scale sum_t dy_t e(token_t)^T over the T tokens of sample i,   dtable = gbar = (1 / b) sum_i g_i,   n_i = ||g_i||^2,  q_i = <g_i, gbar>
+ * They add to those of the same samples' other parameters, as abs_layer_norm_backward's do.
+ *   dtable_dev   : device, float [M x V x D], written whole (zeros for words that no token names).
+ *   n_dev, q_dev : device, float [M x b], either may be NULL.
+ * No output overlaps an input, another output or the workspace.  Asynchronous on the stream; sums in fp32 in a fixed order (the same bits
+ * every time), of the tokens of a word in the order of the samples.  workspace: device, 256-byte aligned, of the size the other call tells
+ * for the same shape and the same outputs asked for, used until the call's work has run.
+ */
+abs_status abs_embedding_backward_workspace_bytes(const abs_embedding_shape *shape /*host*/, int want_n, int want_q, size_t *bytes /*host*/);
+abs_status abs_embedding_backward(const abs_embedding_shape *shape /*host*/, const void *dy_dev, const void *tokens_dev, float scale,
+                                  float *dtable_dev, float *n_dev, float *q_dev, void *workspace, size_t workspace_bytes,
+                                  void *hip_stream);
+
+/*
+ * Root-mean-square norm over the last dimension behind the addition of a residual, M replicas with gains of their own (fp32 arithmetic):
+ *   h = x + residual, rounded to its type;   r = 1 / sqrt(mean_d h^2 + eps),   y = h r w      (of h as it is stored)
+ * or, with scale_dev, in 8 bits:   c = max(max_d |y| / 448, 2^-100) of each row,   y / c rounded to e4m3 (four exponent and three
+ * mantissa bits, no infinities); a row with an infinity or NaN has c = NaN.
+ * At most 2^20 replicas, 2^27 gains (M D) and 2^31 - 1 rows (M b T); beyond: ABS_EUNSUPPORTED.
+ */
+typedef struct {
+  int M, b, T, D;             /* replicas, samples of each, rows of a sample (tokens), values of a row; all >= 1 */
+  int type;                   /* ABS_TYPE_* of x, residual, h, y (without scale_dev), dy, dh and dx */
+  int param_type;             /* ABS_TYPE_* of w [M x D]: ABS_TYPE_F32 or `type` */
+  /* values from row to row (>= D) and from replica to replica; rows do not overlap: replica after replica, or interleaved by rows */
+  int64_t ldx, stride_x;      /* x;          backward: h */
+  int64_t ldr, stride_r;      /* residual;   backward: dh (looked at where there is one) */
+  int64_t ldh, stride_h;      /* h (looked at where there is a residual);   backward: dx */
+  int64_t ldy, stride_y;      /* y;          backward: dy */
+} abs_rms_norm_shape;
+
+/*   residual_dev and h_dev: both, or both NULL (h = x).  h_dev and y_dev may be x_dev or residual_dev with the same strides (not both the
+ *   same); no output overlaps an input or another output otherwise.
+ *   scale_dev : device, float [M x b x T], or NULL: y in `type`.   rstd_dev : device, float [M x b x T], may be NULL.   0 <= eps.
+ *   Asynchronous on the stream. */
+abs_status abs_rms_norm(const abs_rms_norm_shape *shape /*host*/, const void *x_dev, const void *residual_dev, const void *w_dev, float eps,
+                        void *h_dev, void *y_dev, float *scale_dev, float *rstd_dev, void *hip_stream);
+
+/*
+ * Its gradients, from the signals dy of the per-sample losses at y and, where there is one, dh at h (the residual's way on), and the batch
+ * tests' statistics of the gain's gradient:
+ *   hh = h r,  u = dy w,  dx = dh + r (u - hh mean_d(u hh))    (of x and of the residual alike)
+ *   g_i = sum_t dy hh over the T rows of sample i;  dw = gbar = (1 / b) sum_i g_i;   n_i = ||g_i||^2,  q_i = <g_i, gbar>
+ *   dh_dev may be NULL.   rstd_dev : device, float [M x b x T], of the forward pass.   dw_dev : device, float [M x D].
+ *   n_dev, q_dev : device, float [M x b], either may be NULL.
+ * No output overlaps an input, another output or the workspace.  Asynchronous on the stream; sums in a fixed order.  workspace: device,
+ * 256-byte aligned, of the size the other call tells for the same shape and the same outputs asked for, used until the call's work has run.
+ */
+abs_status abs_rms_norm_backward_workspace_bytes(const abs_rms_norm_shape *shape /*host*/, int want_n, int want_q, size_t *bytes /*host*/);
+abs_status abs_rms_norm_backward(const abs_rms_norm_shape *shape /*host*/, const void *dy_dev, const void *h_dev, const void *dh_dev,
+                                 const void *w_dev, const float *rstd_dev, void *dx_dev, float *dw_dev, float *n_dev, float *q_dev,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /*
  * Per-kernel timing (measurement aid; not part of the method).  While enabled, every kernel
  * launch of abs_local_step / abs_average_replicas is bracketed by two HIP events on the

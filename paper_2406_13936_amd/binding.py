@@ -32,6 +32,8 @@ EXPORTS = [
     "abs_set_fused_update", "abs_set_gram_ip_max_batch",
     "abs_orthogonalize", "abs_orthogonalize_workspace_bytes", "abs_muon_step",
     "abs_layer_norm", "abs_layer_norm_backward", "abs_layer_norm_backward_workspace_bytes",
+    "abs_embedding", "abs_embedding_backward", "abs_embedding_backward_workspace_bytes",
+    "abs_rms_norm", "abs_rms_norm_backward", "abs_rms_norm_backward_workspace_bytes",
 ]
 
 
@@ -66,6 +68,16 @@ class LayerNormShape(C.Structure):
     _fields_ = [("M", C.c_int), ("b", C.c_int), ("T", C.c_int), ("D", C.c_int), ("type", C.c_int),
                 ("param_type", C.c_int), ("ldx", C.c_int64), ("stride_x", C.c_int64), ("ldy", C.c_int64),
                 ("stride_y", C.c_int64), ("lddx", C.c_int64), ("stride_dx", C.c_int64)]
+
+
+class EmbeddingShape(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("M", "b", "T", "V", "D", "token_type", "type", "table_type")] + \
+               [(n, C.c_int64) for n in ("ldy", "stride_y")]
+
+
+class RmsNormShape(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("M", "b", "T", "D", "type", "param_type")] + \
+               [(n, C.c_int64) for n in ("ldx", "stride_x", "ldr", "stride_r", "ldh", "stride_h", "ldy", "stride_y")]
 
 
 def load_library(reload: bool = False):
@@ -136,6 +148,12 @@ def load_library(reload: bool = False):
                                    C.c_void_p, C.c_void_p, C.c_void_p]
     lib.abs_layer_norm_backward_workspace_bytes.argtypes = [C.POINTER(LayerNormShape), C.c_int, C.c_int, C.POINTER(C.c_size_t)]
     lib.abs_layer_norm_backward.argtypes = [C.POINTER(LayerNormShape)] + [C.c_void_p] * 11 + [C.c_size_t, C.c_void_p]
+    lib.abs_embedding.argtypes = [C.POINTER(EmbeddingShape), C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p]
+    lib.abs_embedding_backward_workspace_bytes.argtypes = [C.POINTER(EmbeddingShape), C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+    lib.abs_embedding_backward.argtypes = [C.POINTER(EmbeddingShape), C.c_void_p, C.c_void_p, C.c_float] + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+    lib.abs_rms_norm.argtypes = [C.POINTER(RmsNormShape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_float] + [C.c_void_p] * 5
+    lib.abs_rms_norm_backward_workspace_bytes.argtypes = [C.POINTER(RmsNormShape), C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+    lib.abs_rms_norm_backward.argtypes = [C.POINTER(RmsNormShape)] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]
     _lib = lib
     return lib
 
@@ -708,3 +726,173 @@ def layer_norm_backward(dy, x, weight, mean, rstd, has_bias: bool = True, want_n
           dx.data_ptr(), dw.data_ptr(), db.data_ptr() if has_bias else None, n.data_ptr() if want_norms else None,
           q.data_ptr() if want_inner else None, ws, nbytes)
     return dx, dw, db, n, q
+
+
+# -- operators of a language model's blocks ----------------------------------------------------------------------------
+
+def _product(sizes) -> int:
+    n = 1
+    for v in sizes:
+        n *= v
+    return n
+
+
+def _token_type(tokens) -> int:
+    kind = {_torch.int32: 16, _torch.int64: 17}.get(tokens.dtype)
+    if kind is None:
+        raise AbsError(f"tokens must be int32 or int64, not {tokens.dtype}")
+    if not tokens.is_cuda:
+        raise AbsError("tokens must be in device memory")
+    if tokens.dim() < 2 or not tokens.is_contiguous():
+        raise AbsError("tokens must be a contiguous [M, b, ...] tensor")
+    return kind
+
+
+@functools.lru_cache(maxsize=512)
+def _embedding_shape(shape, V: int, token_kind: int, kind: int, table_kind: int, other_shape, other_stride, other: str):
+    """(struct for tokens and the tensor y or dy beside them, reference to it, workspace bytes by outputs asked for)"""
+    M, b, T, D = shape[0], shape[1], _product(shape[2:]), other_shape[-1]
+    if min(shape + other_shape) < 1:
+        raise AbsError(f"tokens and {other} must not be empty")
+    _fits("tokens", M, b, T, V, D)
+    sy, ldy = _rows(other_shape, other_stride, other)
+    s = EmbeddingShape(M, b, T, V, D, token_kind, kind, table_kind, ldy, sy)
+    return s, C.byref(s), {}
+
+
+def embedding(tokens, table, scale: float = 1.0, dtype=None, out=None):
+    """scale * table[m, token] for int32 or int64 tokens [M, b, ...] and tables [M, V, D], one to a replica: [M, b, ..., D] of type
+    `dtype` (default: the table's).  A token outside [0, V) is padding: zeros.  Gradients are embedding_backward's."""
+    lib, torch = _lib_and_torch()
+    token_kind, table_kind = _token_type(tokens), _type_of(table, "table")
+    if table.dim() != 3 or table.shape[0] != tokens.shape[0] or not table.is_contiguous():
+        raise AbsError("table must be a contiguous [M, V, D] tensor")
+    if out is None:
+        y = torch.empty(tokens.shape + table.shape[-1:], dtype=table.dtype if dtype is None else dtype, device=tokens.device)
+    else:
+        y = out
+        if y.shape != tokens.shape + table.shape[-1:] or (dtype is not None and y.dtype != dtype):
+            raise AbsError("out must be [M, b, ..., D] of the type asked for")
+    kind = _type_of(y, "the result")
+    dev = _same_device(tokens, table, y)
+    _, shape, _ = _embedding_shape(tokens.shape, table.shape[1], token_kind, kind, table_kind, y.shape, y.stride(), "out")
+    _call(dev, lib.abs_embedding, shape, tokens.data_ptr(), table.data_ptr(), scale, y.data_ptr())
+    if out is not None:
+        _written(y)
+    return y
+
+
+def embedding_backward(dy, tokens, vocab: int, scale: float = 1.0, want_norms: bool = False, want_inner: bool = False):
+    """Gradient of embedding's tables from the signals dy [M, b, ..., D] of the per-sample losses, and the batch tests' statistics of
+    it.  Returns (dtable, n, q): the batch gradient fp32 [M, vocab, D] (mean over the b samples), n_i = ||g_i||^2 and
+    q_i = <g_i, gbar> fp32 [M, b], None unless asked for."""
+    lib, torch = _lib_and_torch()
+    token_kind, kind = _token_type(tokens), _type_of(dy, "dy")
+    if dy.shape[:-1] != tokens.shape:
+        raise AbsError("dy must be [M, b, ..., D] beside tokens [M, b, ...]")
+    dev = _same_device(tokens, dy)
+    s, shape, sizes = _embedding_shape(tokens.shape, int(vocab), token_kind, kind, kind, dy.shape, dy.stride(), "dy")
+    wants = (bool(want_norms), bool(want_inner))
+    nbytes = sizes.get(wants)
+    if nbytes is None:
+        size = C.c_size_t(0)
+        _check(lib.abs_embedding_backward_workspace_bytes(shape, int(wants[0]), int(wants[1]), C.byref(size)))
+        nbytes = sizes[wants] = size.value
+    dtable = torch.empty((s.M, s.V, s.D), dtype=torch.float32, device=dy.device)
+    n = torch.empty((s.M, s.b), dtype=torch.float32, device=dy.device) if want_norms else None
+    q = torch.empty((s.M, s.b), dtype=torch.float32, device=dy.device) if want_inner else None
+    keep, ws = _workspace(nbytes, dy.device)
+    _call(dev, lib.abs_embedding_backward, shape, dy.data_ptr(), tokens.data_ptr(), scale, dtable.data_ptr(),
+          n.data_ptr() if want_norms else None, q.data_ptr() if want_inner else None, ws, nbytes)
+    return dtable, n, q
+
+
+@functools.lru_cache(maxsize=512)
+def _rms_shape(shape, kind: int, param_kind: int, x, r, h, y):
+    """(struct, reference to it, workspace bytes by outputs asked for); x, r, h, y: (strides, name) of the tensors beside each other, or None"""
+    M, b, T, D = shape[0], shape[1], _product(shape[2:-1]), shape[-1]
+    _fits("x", M, b, T, D)
+    f = []
+    for t in (x, r, h, y):
+        stride, ld = _rows(shape, t[0], t[1]) if t is not None else (b * T * D, D)
+        f += [ld, stride]
+    s = RmsNormShape(M, b, T, D, kind, param_kind, *f)
+    return s, C.byref(s), {}
+
+
+def _beside(x, t, what: str):
+    if t.shape != x.shape or t.dtype != x.dtype:
+        raise AbsError(f"{what} must have the shape and type of the rows beside it")
+    return t.stride(), what
+
+
+def _rms_norm(x, weight, residual, eps, out, residual_out, eight):
+    lib, torch = _lib_and_torch()
+    kind = _type_of(x, "x")
+    pt = _norm_params(x, weight, "weight")
+    if residual is None and residual_out is not None:
+        raise AbsError("residual_out without a residual")
+    h = None if residual is None else _like(x) if residual_out is None else residual_out
+    if eight:
+        y = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device) if out is None else out
+        if y.shape != x.shape or y.dtype != torch.float8_e4m3fn:
+            raise AbsError("out must have x's shape and type float8_e4m3fn")
+        beside = (y.stride(), "out")
+    else:
+        y = _like(x) if out is None else out
+        beside = _beside(x, y, "out")
+    dev = _same_device(x, weight, residual, h, y)
+    _, shape, _ = _rms_shape(x.shape, kind, pt, (x.stride(), "x"), None if residual is None else _beside(x, residual, "residual"),
+                             None if h is None else _beside(x, h, "residual_out"), beside)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    scales = torch.empty_like(rstd) if eight else None
+    _call(dev, lib.abs_rms_norm, shape, x.data_ptr(), residual.data_ptr() if residual is not None else None, weight.data_ptr(), eps,
+          h.data_ptr() if h is not None else None, y.data_ptr(), scales.data_ptr() if eight else None, rstd.data_ptr())
+    if out is not None:
+        _written(out)
+    if residual_out is not None:
+        _written(residual_out)
+    return y, scales, (x if h is None else h), rstd
+
+
+def rms_norm(x, weight, residual=None, eps: float = 1e-6, out=None, residual_out=None):
+    """Root-mean-square norm of h = x + residual, rounded to its type, for [M, b, ..., D] over the last dimension with gains [M, D] (fp32 or
+    x's type), one set per replica.  Returns (y, h, rstd): h is x where there is no residual, rstd fp32 [M, b, ...]; `out` and
+    `residual_out` may be x or residual.  No autograd graph is kept: gradients are rms_norm_backward's."""
+    y, _, h, rstd = _rms_norm(x, weight, residual, eps, out, residual_out, False)
+    return y, h, rstd
+
+
+def rms_norm_8bit(x, weight, residual=None, eps: float = 1e-6, out=None, residual_out=None):
+    """rms_norm with its result in 8 bits: returns (y8, scales, h, rstd) with y = y8 * scales[..., None], y8 float8_e4m3fn, scales fp32
+    [M, b, ...]: a row's largest magnitude over 448, at least 2^-100."""
+    return _rms_norm(x, weight, residual, eps, out, residual_out, True)
+
+
+def rms_norm_backward(dy, h, weight, rstd, dh=None, want_norms: bool = False, want_inner: bool = False):
+    """Gradients of rms_norm from the signals dy [M, b, ..., D] of the per-sample losses at its result and dh at its h (None: nothing else
+    reads h), and the batch tests' statistics of the gain's gradient.  Returns (dx, dweight, n, q): dx is the gradient of x and of the
+    residual alike, dweight the batch gradient fp32 [M, D] (mean over the b samples), n_i = ||g_i||^2 and q_i = <g_i, gbar> fp32 [M, b],
+    None unless asked for."""
+    lib, torch = _lib_and_torch()
+    kind = _type_of(h, "h")
+    pt = _norm_params(h, weight, "weight")
+    if rstd.dtype != torch.float32 or rstd.shape != h.shape[:-1] or not rstd.is_contiguous():
+        raise AbsError("rstd must be a contiguous float32 tensor [M, b, ...]")
+    dx = _like(h)
+    dev = _same_device(h, dy, weight, rstd, dh)
+    s, shape, sizes = _rms_shape(h.shape, kind, pt, (h.stride(), "h"), None if dh is None else _beside(h, dh, "dh"), (dx.stride(), "dx"),
+                                 _beside(h, dy, "dy"))
+    wants = (bool(want_norms), bool(want_inner))
+    nbytes = sizes.get(wants)
+    if nbytes is None:
+        size = C.c_size_t(0)
+        _check(lib.abs_rms_norm_backward_workspace_bytes(shape, int(wants[0]), int(wants[1]), C.byref(size)))
+        nbytes = sizes[wants] = size.value
+    dw = torch.empty((s.M, s.D), dtype=torch.float32, device=h.device)
+    n = torch.empty((s.M, s.b), dtype=torch.float32, device=h.device) if want_norms else None
+    q = torch.empty((s.M, s.b), dtype=torch.float32, device=h.device) if want_inner else None
+    keep, ws = _workspace(nbytes, h.device)
+    _call(dev, lib.abs_rms_norm_backward, shape, dy.data_ptr(), h.data_ptr(), dh.data_ptr() if dh is not None else None, weight.data_ptr(),
+          rstd.data_ptr(), dx.data_ptr(), dw.data_ptr(), n.data_ptr() if want_norms else None, q.data_ptr() if want_inner else None, ws, nbytes)
+    return dx, dw, n, q

@@ -88,4 +88,43 @@ size_t layer_norm_backward_bytes(const LayerNormP &p, bool want_n, bool want_q);
 hipError_t launch_layer_norm(const LayerNormP &p, hipStream_t s);
 hipError_t launch_layer_norm_backward(const LayerNormP &p, void *workspace, hipStream_t s);
 
+// ---- root-mean-square norm -------------------------------------------------------------------------------------------
+
+constexpr int RMS_MAX_D = 8192;          // longest row that a block's registers hold
+constexpr int RMS_BLOCKS = 512;          // of the backward pass, as layer norm's
+// lanes and vectors to a row: 16 x 1, 64 x 1, 64 x 2, 256 x 1, 256 x 2, 512 x 2
+inline int rms_shape(int D) { return D <= 128 ? 0 : D <= 512 ? 1 : D <= 1024 ? 2 : D <= 2048 ? 3 : D <= 4096 ? 4 : 5; }
+
+// M replicas with gains of their own [M x D]; each has b samples of T rows of D values.  Strides: values from row to row and from replica
+// to replica.
+struct RmsNormP {
+  int M, b, T, D, type, ptype;
+  long long ldx, sx, ldr, sr, ldh, sh, ldy, sy;
+  const void *x, *res, *w;                 // forward: x (ldx), residual (ldr, may be null); backward: h (ldx), dh (ldr, may be null)
+  float eps;
+  void *h, *y; float *scale;               // forward: h (ldh; with a residual), y (ldy; e4m3 if there is a scale)
+  float *rstd;                             // forward: output (may be null); backward: input
+  const void *dy; void *dx;                // backward: dy (ldy), dx (ldh)
+  float *dw, *n, *q;                       // n, q may be null
+};
+size_t rms_norm_backward_bytes(const RmsNormP &p, bool want_n, bool want_q);
+hipError_t launch_rms_norm(const RmsNormP &p, hipStream_t s);
+hipError_t launch_rms_norm_backward(const RmsNormP &p, void *workspace, hipStream_t s);
+
+// ---- token embedding -------------------------------------------------------------------------------------------------
+
+// M replicas with tables of their own [M][V][D]; each has b samples of T tokens.
+struct EmbeddingP {
+  int M, b, T, V, D;
+  int wide;                                // tokens of 64 bits, not 32
+  int type, ttype;                         // of y or dy; of the table (forward)
+  long long ldy, sy;                       // y or dy: values from row to row and from replica to replica
+  const void *tokens, *table; float scale;
+  void *y; const void *dy;
+  float *dtable, *n, *q;                   // n, q may be null
+};
+size_t embedding_backward_bytes(const EmbeddingP &p, bool want_n, bool want_q);
+hipError_t launch_embedding(const EmbeddingP &p, hipStream_t s);
+hipError_t launch_embedding_backward(const EmbeddingP &p, void *workspace, hipStream_t s);
+
 }  // namespace absk

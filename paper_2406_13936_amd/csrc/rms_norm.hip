@@ -1,0 +1,225 @@
+// Root-mean-square norm behind the addition of a residual, with a result of the rows' type or in 8 bits (e4m3) with a scale to a row.
+//
+//   h = x + residual, rounded to its type (what the next layers add to);  r = 1 / sqrt(mean_d h^2 + eps),  y = h r w
+//   in 8 bits:  c = max(max_d |y| / 448, 2^-100),  y / c rounded to e4m3
+//
+// y is made of the h that is stored, so that the backward pass, which reads h, differentiates what was computed.  Bound by memory: x and
+// the residual are read, h and y written, once each.  A row lives in the registers of 16 to 512 lanes as in layer_norm.hip; the sum of
+// squares and the largest |h w| are exchanged together, as r only scales them: one exchange a row.
+#include <algorithm>
+#include <cstring>
+#include "device_utils.h"
+#include "ops.h"
+#include "row_groups.h"
+
+namespace absk {
+namespace {
+
+constexpr float E4M3_MAX = 448.0f;
+constexpr float SMALLEST_SCALE = 0x1p-100f;      // (its inverse is finite)
+
+__device__ __forceinline__ float scale_of(float rstd, float most) {
+  const float c = rstd * most / E4M3_MAX;        // NaN of a row with NaN or infinities stays
+  return c < SMALLEST_SCALE ? SMALLEST_SCALE : c;
+}
+// four values in e4m3, to the nearest, ties to even (the machine's conversion)
+__device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+template <int G> __device__ __forceinline__ float lanes_max(float v) {
+  v = fmaxf(v, dpp<0xB1>(v));
+  v = fmaxf(v, dpp<0x4E>(v));
+  v = fmaxf(v, dpp<0x141>(v));
+  v = fmaxf(v, dpp<0x140>(v));
+  if (G == 64) {
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    v = fmaxf(v, __shfl_xor(v, 32, 64));
+  }
+  return v;
+}
+// Sum and, if MAX, maximum over the group; sm: 4 floats to a wavefront, `turn` as in group_sums
+template <int G, bool MAX> __device__ __forceinline__ void group_sum_max(float &s, float &m, float *sm, int turn) {
+  if (!MAX) {
+    float v[1] = {s};
+    group_sums<G, 1>(v, sm, turn);
+    s = v[0];
+    return;
+  }
+  constexpr int W = G > 64 ? G / 64 : 4;
+  s = lanes_sum<(G < 64 ? G : 64)>(s);
+  m = lanes_max<(G < 64 ? G : 64)>(m);
+  if (G <= 64) return;
+  float *at = sm + (turn & 1) * 2 * W;
+  if ((threadIdx.x & 63) == 0) { at[threadIdx.x >> 6] = s; at[W + (threadIdx.x >> 6)] = m; }
+  __syncthreads();
+  s = m = 0.0f;
+#pragma unroll
+  for (int h = 0; h < W; h += 4) {
+    const float4 f = *reinterpret_cast<const float4 *>(at + h), g = *reinterpret_cast<const float4 *>(at + W + h);
+    s += (f.x + f.y) + (f.z + f.w);
+    m = fmaxf(m, fmaxf(fmaxf(g.x, g.y), fmaxf(g.z, g.w)));
+  }
+}
+
+// The lane's eight values v of a row in e4m3; whole: vectors of a row that are all in it or not, at places that their stores may take
+template <int TYPE, int G>
+__device__ __forceinline__ void store_e4m3(void *p, long long at, int D, int l, int v, const float (&f)[8], bool whole) {
+  uint8_t *row = static_cast<uint8_t *>(p) + at;
+  const uint32_t lo = pack4_e4m3(f[0], f[1], f[2], f[3]), hi = pack4_e4m3(f[4], f[5], f[6], f[7]);
+  const int c0 = col_of<TYPE, G>(v, 0, l), c4 = col_of<TYPE, G>(v, 4, l);
+  if (whole) {
+    if (TYPE != TYPE_F32) {
+      if (c0 < D) *reinterpret_cast<uint2 *>(row + c0) = make_uint2(lo, hi);
+    } else {
+      if (c0 < D) *reinterpret_cast<uint32_t *>(row + c0) = lo;
+      if (c4 < D) *reinterpret_cast<uint32_t *>(row + c4) = hi;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (c0 + e < D) row[c0 + e] = (uint8_t)(lo >> (8 * e));
+      if (c4 + e < D) row[c4 + e] = (uint8_t)(hi >> (8 * e));
+    }
+  }
+}
+
+// nb blocks per replica; a group takes every (nb GP)-th row
+template <int TYPE, int G, int V, bool VEC, bool ADD, bool EIGHT>
+__global__ void __launch_bounds__(ln_threads(G)) rms_forward_kernel(const RmsNormP p, const int nb) {
+  constexpr int GP = ln_threads(G) / G;
+  __shared__ __attribute__((aligned(16))) float sm[ln_threads(G) / 16];
+  const int m = blockIdx.x / nb, j = blockIdx.x - m * nb, gid = threadIdx.x / G, l = threadIdx.x % G;
+  const long long rows = (long long)p.b * p.T, step = (long long)nb * GP;
+  const int D = p.D;
+  const float n = (float)D;
+  const bool whole = VEC && !(((reinterpret_cast<uintptr_t>(p.y) | (uintptr_t)p.sy | (uintptr_t)p.ldy)) & 7);
+  int turn = 0;
+  long long r = (long long)j * GP + gid;
+  Raw<TYPE, V> nx, nr;                            // (the next row is on its way while a row is worked on)
+  if (r < rows) {
+    load_raw<TYPE, G, V, VEC>(nx, p.x, m * p.sx + r * p.ldx, D, l);
+    if (ADD) load_raw<TYPE, G, V, VEC>(nr, p.res, m * p.sr + r * p.ldr, D, l);
+  }
+  float w[V][8];
+  load_param<TYPE, G, V, VEC>(w, p.w, p.ptype, (long long)m * D, D, l);
+  // G >= 256: every thread of the block goes through every exchange (one group to a block: they agree on r)
+  for (; r < rows; r += step) {
+    const Raw<TYPE, V> rx = nx, rr = nr;
+    if (r + step < rows) {
+      load_raw<TYPE, G, V, VEC>(nx, p.x, m * p.sx + (r + step) * p.ldx, D, l);
+      if (ADD) load_raw<TYPE, G, V, VEC>(nr, p.res, m * p.sr + (r + step) * p.ldr, D, l);
+    }
+    float h[V][8], s = 0.0f, most = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      raw_vals<TYPE, V>(rx, v, h[v]);
+      if (ADD) {
+        float q[8];
+        raw_vals<TYPE, V>(rr, v, q);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[v][e] += q[e];
+        if (TYPE != TYPE_F32) unpack8(pack8(TYPE, h[v]), TYPE, h[v]);
+        store_vals<TYPE, G, VEC>(p.h, m * p.sh + r * p.ldh, D, l, v, h[v]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {               // (zeros beyond the row)
+        s = fmaf(h[v][e], h[v][e], s);
+        if (EIGHT) most = fmaxf(most, fabsf(h[v][e] * w[v][e]));
+      }
+    }
+    group_sum_max<G, EIGHT>(s, most, sm, turn++);
+    const float rstd = 1.0f / sqrtf(s / n + p.eps);
+    float c = 0.0f, by = rstd;
+    if (EIGHT) { c = scale_of(rstd, most); by = rstd * (1.0f / c); }
+    if (l == 0) {
+      if (p.rstd) p.rstd[m * rows + r] = rstd;
+      if (EIGHT) p.scale[m * rows + r] = c;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[v][e] = EIGHT ? (h[v][e] * w[v][e]) * by : (h[v][e] * rstd) * w[v][e];
+      if (EIGHT) store_e4m3<TYPE, G>(p.y, m * p.sy + r * p.ldy, D, l, v, h[v], whole);
+      else store_vals<TYPE, G, VEC>(p.y, m * p.sy + r * p.ldy, D, l, v, h[v]);
+    }
+  }
+}
+
+// Rows longer than the registers of a block hold: a second pass over h as it was stored, out of the caches (a thread reads what it wrote).
+// A launch takes RMS_LONG_ROWS rows: a grid counts its threads in 32 bits.
+constexpr int RMS_LONG_ROWS = 1 << 18;
+__global__ void __launch_bounds__(256) rms_forward_long_kernel(const RmsNormP p, const int eight, const long long first) {
+  __shared__ __attribute__((aligned(16))) float sm[16];
+  const long long rows = (long long)p.b * p.T, i = first + blockIdx.x, m = i / rows, r = i - m * rows;
+  const long long xa = m * p.sx + r * p.ldx, ra = m * p.sr + r * p.ldr, ha = m * p.sh + r * p.ldh, ya = m * p.sy + r * p.ldy, pa = m * p.D;
+  float s = 0.0f, most = 0.0f;
+  for (int c = threadIdx.x; c < p.D; c += 256) {
+    float h = load_as_f32(p.x, p.type, xa + c);
+    if (p.res) {
+      h += load_as_f32(p.res, p.type, ra + c);
+      store_from_f32(p.h, p.type, ha + c, h);
+      h = load_as_f32(p.h, p.type, ha + c);
+    }
+    s = fmaf(h, h, s);
+    if (eight) most = fmaxf(most, fabsf(h * load_as_f32(p.w, p.ptype, pa + c)));
+  }
+  group_sum_max<256, true>(s, most, sm, 0);
+  const float rstd = 1.0f / sqrtf(s / (float)p.D + p.eps), scale = scale_of(rstd, most), by = rstd * (1.0f / scale);
+  if (threadIdx.x == 0) {
+    if (p.rstd) p.rstd[m * rows + r] = rstd;
+    if (eight) p.scale[m * rows + r] = scale;
+  }
+  for (int c = threadIdx.x; c < p.D; c += 256) {
+    const float h = p.res ? load_as_f32(p.h, p.type, ha + c) : load_as_f32(p.x, p.type, xa + c), w = load_as_f32(p.w, p.ptype, pa + c);
+    if (eight) static_cast<uint8_t *>(p.y)[ya + c] = (uint8_t)pack4_e4m3((h * w) * by, 0.0f, 0.0f, 0.0f);
+    else store_from_f32(p.y, p.type, ya + c, (h * rstd) * w);
+  }
+}
+
+template <int TYPE, int G, int V, bool VEC> void forward_shape(const RmsNormP &p, hipStream_t s) {
+  const long long groups = ln_threads(G) / G, rows = (long long)p.b * p.T;
+  const int nb = (int)std::max(1LL, std::min((rows + groups - 1) / groups, (4LL * RMS_BLOCKS + p.M - 1) / p.M));
+  const dim3 grid((unsigned)((long long)nb * p.M)), block(ln_threads(G));
+  if (p.scale) {
+    if (p.res) hipLaunchKernelGGL((rms_forward_kernel<TYPE, G, V, VEC, true, true>), grid, block, 0, s, p, nb);
+    else hipLaunchKernelGGL((rms_forward_kernel<TYPE, G, V, VEC, false, true>), grid, block, 0, s, p, nb);
+  } else {
+    if (p.res) hipLaunchKernelGGL((rms_forward_kernel<TYPE, G, V, VEC, true, false>), grid, block, 0, s, p, nb);
+    else hipLaunchKernelGGL((rms_forward_kernel<TYPE, G, V, VEC, false, false>), grid, block, 0, s, p, nb);
+  }
+}
+template <int TYPE, bool VEC> void forward_by_length(const RmsNormP &p, hipStream_t s) {
+  switch (rms_shape(p.D)) {
+    case 0: return forward_shape<TYPE, 16, 1, VEC>(p, s);
+    case 1: return forward_shape<TYPE, 64, 1, VEC>(p, s);
+    case 2: return forward_shape<TYPE, 64, 2, VEC>(p, s);
+    case 3: return forward_shape<TYPE, 256, 1, VEC>(p, s);
+    case 4: return forward_shape<TYPE, 256, 2, VEC>(p, s);
+    default: return forward_shape<TYPE, 512, 2, VEC>(p, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(const RmsNormP &p, hipStream_t s) {
+  const long long rows = (long long)p.b * p.T;
+  if (rows * p.M > 0x7fffffff) return hipErrorInvalidValue;
+  if (p.D > RMS_MAX_D) {
+    for (long long first = 0; first < rows * p.M; first += RMS_LONG_ROWS)
+      hipLaunchKernelGGL(rms_forward_long_kernel, dim3((unsigned)std::min<long long>(rows * p.M - first, RMS_LONG_ROWS)), dim3(256), 0, s, p, p.scale != nullptr, first);
+    return hipGetLastError();
+  }
+  const bool vec = rows_of_vectors(p.x, p.type, p.sx, p.ldx, p.D) &&
+                   (!p.res || (rows_of_vectors(p.res, p.type, p.sr, p.ldr, p.D) && rows_of_vectors(p.h, p.type, p.sh, p.ldh, p.D))) &&
+                   (p.scale || rows_of_vectors(p.y, p.type, p.sy, p.ldy, p.D));
+  switch (p.type) {
+    case TYPE_F32: vec ? forward_by_length<TYPE_F32, true>(p, s) : forward_by_length<TYPE_F32, false>(p, s); break;
+    case TYPE_BF16: vec ? forward_by_length<TYPE_BF16, true>(p, s) : forward_by_length<TYPE_BF16, false>(p, s); break;
+    default: vec ? forward_by_length<TYPE_F16, true>(p, s) : forward_by_length<TYPE_F16, false>(p, s);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace absk
