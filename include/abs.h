@@ -478,6 +478,50 @@ abs_status abs_rms_norm_backward(const abs_rms_norm_shape *shape /*host*/, const
                                  void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * Causal attention within packed sequences, query heads in groups that share a head of keys and values:
+ *   s_ij = scale q_i . k_j for the rows j <= i of i's sequence,   o_i = sum_j softmax(s_i)_j v_j,   lse_i = log sum_j exp s_ij
+ * Sequences are runs of rows: rows offsets[s] .. offsets[s + 1] - 1 (some may be empty), or without offsets T rows each, one behind the
+ * other.  Rows of no sequence (before the first, behind the last) are not read, and are left as they are in the outputs or set to zeros.
+ * What a row's mask leaves out has no part in it, infinities and NaN included.
+ * Sums, maxima and the softmax are fp32; with 16-bit types softmax weights are rounded to that type for the product with v (and their
+ * gradients for the products with q and k).  Heads of up to 128 values, at most 2^31 - 1 rows; beyond: ABS_EUNSUPPORTED.
+ */
+typedef struct {
+  int type;                   /* ABS_TYPE_* of q, k, v, o, do, dq, dk and dv */
+  int seqs;                   /* sequences, >= 1 */
+  int T;                      /* rows of each (without offsets: rows = seqs T) */
+  int Hq, Hkv, D;             /* heads of queries (a multiple of Hkv) and of keys, values of a head, 1 .. 128 */
+  int offsets_type;           /* ABS_TYPE_I32 or ABS_TYPE_I64, or 0: no offsets */
+  int64_t rows;               /* of all tensors, >= 1 */
+  /* values from row to row (ld >= D) and from head to head; rows of heads do not overlap: [rows][heads][D], [heads][rows][D], columns of wider rows */
+  int64_t ldq, head_q, ldk, head_k, ldv, head_v, ldo, head_o;
+  int64_t lddo, head_do, lddq, head_dq, lddk, head_dk, lddv, head_dv;      /* backward */
+} abs_attention_shape;
+
+/*   offsets_dev : device, seqs + 1 values that do not fall, within 0 .. rows (they are brought into that range: a list that is none gives
+ *                 wrong results, but reads and writes nothing outside the tensors), or NULL.
+ *   scale       : positive, for instance 1 / sqrt(D).
+ *   lse_dev     : device, float [Hq][rows], may be NULL.
+ *   zero_rest   : 0: rows of no sequence are left as they are in o_dev and lse_dev; 1: zeros.
+ * No output overlaps an input, another output or the workspace.  Asynchronous on the stream; the same bits every time.  workspace: device,
+ * 256-byte aligned, of the size the other call tells (NULL where that is 0), used until the call's work has run. */
+abs_status abs_causal_attention_workspace_bytes(const abs_attention_shape *shape /*host*/, int backward, size_t *bytes /*host*/);
+abs_status abs_causal_attention(const abs_attention_shape *shape /*host*/, const void *q_dev, const void *k_dev, const void *v_dev,
+                                const void *offsets_dev, float scale, void *o_dev, float *lse_dev, int zero_rest, void *workspace,
+                                size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Its gradients, from the signals do at its result, and o and lse of the forward pass:
+ *   p_ij = exp(s_ij - lse_i),  ds_ij = scale p_ij (do_i . v_j - do_i . o_i)
+ *   dv_j = sum_i p_ij do_i,  dk_j = sum_i ds_ij q_i  over the rows and query heads that see key j,   dq_i = sum_j ds_ij k_j
+ * Arguments as above (zero_rest: of dq, dk and dv).
+ */
+abs_status abs_causal_attention_backward(const abs_attention_shape *shape /*host*/, const void *do_dev, const void *q_dev, const void *k_dev,
+                                         const void *v_dev, const void *o_dev, const float *lse_dev, const void *offsets_dev, float scale,
+                                         void *dq_dev, void *dk_dev, void *dv_dev, int zero_rest, void *workspace, size_t workspace_bytes,
+                                         void *hip_stream);
+
+/*
  * Per-kernel timing (measurement aid; not part of the method).  While enabled, every kernel
  * launch of abs_local_step / abs_average_replicas is bracketed by two HIP events on the
  * context's stream.  abs_profile_read synchronises, folds the elapsed times into per-kernel

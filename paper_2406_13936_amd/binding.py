@@ -34,6 +34,7 @@ EXPORTS = [
     "abs_layer_norm", "abs_layer_norm_backward", "abs_layer_norm_backward_workspace_bytes",
     "abs_embedding", "abs_embedding_backward", "abs_embedding_backward_workspace_bytes",
     "abs_rms_norm", "abs_rms_norm_backward", "abs_rms_norm_backward_workspace_bytes",
+    "abs_causal_attention", "abs_causal_attention_backward", "abs_causal_attention_workspace_bytes",
 ]
 
 
@@ -78,6 +79,12 @@ class EmbeddingShape(C.Structure):
 class RmsNormShape(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("M", "b", "T", "D", "type", "param_type")] + \
                [(n, C.c_int64) for n in ("ldx", "stride_x", "ldr", "stride_r", "ldh", "stride_h", "ldy", "stride_y")]
+
+
+class AttentionShape(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("type", "seqs", "T", "Hq", "Hkv", "D", "offsets_type")] + \
+               [(n, C.c_int64) for n in ("rows", "ldq", "head_q", "ldk", "head_k", "ldv", "head_v", "ldo", "head_o", "lddo", "head_do",
+                                         "lddq", "head_dq", "lddk", "head_dk", "lddv", "head_dv")]
 
 
 def load_library(reload: bool = False):
@@ -154,6 +161,11 @@ def load_library(reload: bool = False):
     lib.abs_rms_norm.argtypes = [C.POINTER(RmsNormShape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_float] + [C.c_void_p] * 5
     lib.abs_rms_norm_backward_workspace_bytes.argtypes = [C.POINTER(RmsNormShape), C.c_int, C.c_int, C.POINTER(C.c_size_t)]
     lib.abs_rms_norm_backward.argtypes = [C.POINTER(RmsNormShape)] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]
+    lib.abs_causal_attention_workspace_bytes.argtypes = [C.POINTER(AttentionShape), C.c_int, C.POINTER(C.c_size_t)]
+    lib.abs_causal_attention.argtypes = [C.POINTER(AttentionShape)] + [C.c_void_p] * 4 + [C.c_float, C.c_void_p, C.c_void_p, C.c_int,
+                                                                                          C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.abs_causal_attention_backward.argtypes = [C.POINTER(AttentionShape)] + [C.c_void_p] * 7 + [C.c_float] + [C.c_void_p] * 3 + \
+                                                 [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
     _lib = lib
     return lib
 
@@ -896,3 +908,110 @@ def rms_norm_backward(dy, h, weight, rstd, dh=None, want_norms: bool = False, wa
     _call(dev, lib.abs_rms_norm_backward, shape, dy.data_ptr(), h.data_ptr(), dh.data_ptr() if dh is not None else None, weight.data_ptr(),
           rstd.data_ptr(), dx.data_ptr(), dw.data_ptr(), n.data_ptr() if want_norms else None, q.data_ptr() if want_inner else None, ws, nbytes)
     return dx, dw, n, q
+
+
+@functools.lru_cache(maxsize=2048)
+def _heads(shape, stride, what: str):
+    """(values from row to row, from head to head) of [..., T, heads, D] whose rows, over all dimensions before the heads, are equally spaced"""
+    if stride[-1] != 1 and shape[-1] != 1:
+        raise AbsError(f"{what}: values of a head must be consecutive")
+    ld, n = None, 1
+    for size, step in zip(shape[-3::-1], stride[-3::-1]):
+        if size == 1:
+            continue
+        if ld is None:
+            ld = step
+        elif step != ld * n:
+            raise AbsError(f"{what}: rows must be equally spaced")
+        n *= size
+    heads, D = shape[-2], shape[-1]
+    head = stride[-2] if heads > 1 else D
+    return (max(heads * head, D) if ld is None else ld), head
+
+
+@functools.lru_cache(maxsize=512)
+def _attention_shape(kind: int, packed: int, seqs: int, lead, Hq: int, Hkv: int, D: int, strides):
+    """(struct, reference to it, workspace bytes: forward, or backward where strides has all eight tensors')"""
+    rows = _product(lead)
+    T = lead[-1]
+    if not packed:
+        seqs = rows // T
+    _fits("q", rows, seqs, Hq, Hkv, D)
+    s = AttentionShape(kind, seqs, 0 if packed else T, Hq, Hkv, D, packed, rows, *[v for pair in strides for v in pair])
+    size = C.c_size_t(0)
+    _check(_lib.abs_causal_attention_workspace_bytes(C.byref(s), int(len(strides) > 4), C.byref(size)))
+    return s, C.byref(s), size.value
+
+
+def _attention_operands(q, k, v, offsets):
+    """(type, type of offsets or 0, sequences of offsets, dimensions of the rows)"""
+    kind = _type_of(q, "q")
+    if q.dim() < 3 or k.dim() != q.dim() or k.shape[:-2] != q.shape[:-2] or k.shape[-1] != q.shape[-1] or v.shape != k.shape:
+        raise AbsError("q must be [..., T, Hq, D], and k and v [..., T, Hkv, D] beside it")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise AbsError("q, k and v must have the same type")
+    if q.numel() == 0 or k.numel() == 0:
+        raise AbsError("q, k and v must not be empty")
+    if offsets is None:
+        return kind, 0, 0, q.shape[:-2]
+    if q.dim() != 3:
+        raise AbsError("with offsets q, k and v must be [rows, heads, D]")
+    packed = {_torch.int32: 16, _torch.int64: 17}.get(offsets.dtype)
+    if packed is None or offsets.dim() != 1 or offsets.numel() < 2 or not offsets.is_contiguous():
+        raise AbsError("offsets must be a contiguous int32 or int64 tensor [sequences + 1]")
+    if not offsets.is_cuda:
+        raise AbsError("offsets must be in device memory")
+    return kind, packed, offsets.numel() - 1, q.shape[:-2]
+
+
+def _default_scale(scale, D: int) -> float:
+    return 1.0 / D ** 0.5 if scale is None else scale
+
+
+def causal_attention(q, k, v, offsets=None, scale: Optional[float] = None, out=None):
+    """Causal attention of q [..., T, Hq, D] over k and v [..., T, Hkv, D], each index before T a sequence of its own, or with `offsets` (int32 or
+    int64, [sequences + 1]) of [rows, heads, D] over packed sequences: rows offsets[s] .. offsets[s + 1] - 1.  Hq is a multiple of Hkv, D at most
+    128, scale 1 / sqrt(D) by default.  Returns (o, lse), lse fp32 [Hq, ..., T] (or [Hq, rows]); rows of no sequence are zeros, in a given
+    `out` they stay as they are.  q, k and v may be columns of one buffer.  No autograd graph is kept: gradients are causal_attention_backward's."""
+    lib, torch = _lib_and_torch()
+    kind, packed, seqs, lead = _attention_operands(q, k, v, offsets)
+    o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    if o.shape != q.shape or o.dtype != q.dtype:
+        raise AbsError("out must have q's shape and type")
+    dev = _same_device(q, k, v, offsets, o)
+    _, shape, nbytes = _attention_shape(kind, packed, seqs, lead, q.shape[-2], k.shape[-2], q.shape[-1],
+                                        tuple(_heads(t.shape, t.stride(), n) for t, n in ((q, "q"), (k, "k"), (v, "v"), (o, "out"))))
+    new = torch.empty if out is None or not packed else torch.zeros
+    lse = new(q.shape[-2:-1] + lead, dtype=torch.float32, device=q.device)
+    keep, ws = _workspace(nbytes, q.device) if nbytes else (None, None)
+    _call(dev, lib.abs_causal_attention, shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr() if packed else None,
+          _default_scale(scale, q.shape[-1]), o.data_ptr(), lse.data_ptr(), int(out is None), ws, nbytes)
+    if out is not None:
+        _written(out)
+    return o, lse
+
+
+def causal_attention_backward(do, q, k, v, o, lse, offsets=None, scale: Optional[float] = None, out=None):
+    """Gradients (dq, dk, dv) of causal_attention from the signals `do` at its result, and its operands and results.  Of rows of no sequence they
+    are zeros; with out = (dq, dk, dv), for instance columns of one buffer, they are written there and such rows stay as they are."""
+    lib, torch = _lib_and_torch()
+    kind, packed, seqs, lead = _attention_operands(q, k, v, offsets)
+    for t, what in ((do, "do"), (o, "o")):
+        if t.shape != q.shape or t.dtype != q.dtype:
+            raise AbsError(f"{what} must have q's shape and type")
+    if lse.dtype != torch.float32 or lse.shape != q.shape[-2:-1] + lead or not lse.is_contiguous():
+        raise AbsError("lse must be a contiguous float32 tensor [Hq, ..., T]")
+    dq, dk, dv = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)] if out is None else out
+    for t, g, what in ((q, dq, "dq"), (k, dk, "dk"), (v, dv, "dv")):
+        if g.shape != t.shape or g.dtype != t.dtype:
+            raise AbsError(f"{what} must have the shape and type of what it is the gradient of")
+    dev = _same_device(q, k, v, offsets, o, lse, do, dq, dk, dv)
+    named = ((q, "q"), (k, "k"), (v, "v"), (o, "o"), (do, "do"), (dq, "dq"), (dk, "dk"), (dv, "dv"))
+    _, shape, nbytes = _attention_shape(kind, packed, seqs, lead, q.shape[-2], k.shape[-2], q.shape[-1],
+                                        tuple(_heads(t.shape, t.stride(), n) for t, n in named))
+    keep, ws = _workspace(nbytes, q.device)
+    _call(dev, lib.abs_causal_attention_backward, shape, do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+          offsets.data_ptr() if packed else None, _default_scale(scale, q.shape[-1]), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), int(out is None), ws, nbytes)
+    if out is not None:
+        _written(dq, dk, dv)
+    return dq, dk, dv

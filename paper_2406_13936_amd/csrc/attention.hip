@@ -1,0 +1,187 @@
+// Causal attention over packed sequences with grouped heads, forward.
+//
+//   s_ij = a q_i . k_j for j <= i of one sequence,   o_i = sum_j softmax(s_i)_j v_j,   lse_i = log sum_j exp s_ij
+//
+// One pass over the keys with the running maximum and sum of the softmax.  A block takes 128 queries of a head, 32 to a wavefront, and goes through
+// the keys in tiles that it shares.  S^T = K Q^T, so that a query is a lane's column: its maximum needs one exchange between the two halves of a
+// wavefront, its sum none until the end, and exp(S^T) is, rounded, the operand of O^T += V^T P^T without leaving the registers.
+#include <algorithm>
+#include "attention_parts.h"
+
+namespace absk {
+namespace {
+
+// Tiles before each sequence, for more than 64 of them: first[s], s = 0 .. seqs
+__global__ void __launch_bounds__(256) attention_tiles_kernel(const AttentionP p, int *first, const int size) {
+  __shared__ int sums[4];
+  int before = 0;
+  for (int s0 = 0; s0 < p.seqs; s0 += 256) {
+    const int s = s0 + threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = s < p.seqs ? (span_of(p, s).len + size - 1) / size : 0;
+    int upto = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += v;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int at = before;
+    for (int w = 0; w < wave; ++w) at += sums[w];
+    if (s < p.seqs) first[s] = at + upto - n;
+    before += sums[0] + sums[1] + sums[2] + sums[3];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) first[p.seqs] = before;
+}
+
+template <int TYPE, int ND, bool VEC>
+__global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, const int blocks) {
+  constexpr int BK = TYPE == TYPE_F32 ? 32 : 64, NB = BK / 32;
+  typedef Tile<TYPE, BK, ND> KV;
+  typedef typename KV::E E;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+  __shared__ int odd[2];                               // values of a masked tile hold infinities or NaN
+  E *const lds = reinterpret_cast<E *>(lds_raw);       // [2][keys, values]
+  if ((int)blockIdx.x >= blocks) return zero_rest(p, p.o, TYPE, p.Hq, p.ldo, p.ho, p.lse, blockIdx.x - blocks, REST_BLOCKS);
+  int head, t;
+  head_and_tile(blockIdx.x, p.Hq, head, t);
+  Work w = find_tile(p, t, ATTENTION_ROWS);
+  if (w.tile < 0) return;
+  w.tile = (w.len + ATTENTION_ROWS - 1) / ATTENTION_ROWS - 1 - w.tile;      // the longest first
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int q0 = w.tile * ATTENTION_ROWS, mine = q0 + wave * 32, row = mine + (lane & 31);
+  const bool in = row < w.len;
+  const int kvh = head / (p.Hq / p.Hkv);
+  const E *q = static_cast<const E *>(p.q) + w.start * p.ldq + head * p.hq;
+  const E *k = static_cast<const E *>(p.k) + w.start * p.ldk + kvh * p.hk;
+  const E *v = static_cast<const E *>(p.v) + w.start * p.ldv + kvh * p.hv;
+  Frag8<TYPE> qf[2 * ND];
+#pragma unroll
+  for (int i = 0; i < 2 * ND; ++i) qf[i] = row_frag<TYPE, VEC>(q, (long long)row * p.ldq, in, i, p.D);
+  f32x16 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = zeros16();
+  float top = -__builtin_inff(), sum = 0.0f;
+  const float c = p.scale * LOG2E;
+  const int end = min(w.len, q0 + ATTENTION_ROWS), tiles = (end + BK - 1) / BK;
+  KV tk, tv;
+  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+  tk.template load<VEC>(k, p.ldk, 0, w.len, p.D);
+  tv.template load<VEC>(v, p.ldv, 0, w.len, p.D);
+  __syncthreads();
+  tk.store(lds);
+  tv.store(lds + KV::ELEMS);
+  if (BK > q0 && tv.any()) odd[0] = 1;
+  __syncthreads();
+  for (int j = 0; j < tiles; ++j) {
+    const int k0 = j * BK, cur = j & 1;
+    const E *lk = lds + cur * 2 * KV::ELEMS, *lv = lk + KV::ELEMS;
+    const bool more = j + 1 < tiles;
+    if (more) {
+      tk.template load<VEC>(k, p.ldk, k0 + BK, w.len, p.D);
+      tv.template load<VEC>(v, p.ldv, k0 + BK, w.len, p.D);
+    }
+    if (k0 <= mine + 31 && mine < w.len) {
+      f32x16 s[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b] = zeros16();
+#pragma unroll
+      for (int i = 0; i < 2 * ND; ++i)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) mma<TYPE>(s[b], KV::rows(lk, 32 * b, i), qf[i]);
+      const bool masked = k0 + BK - 1 > mine;
+      if (masked) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (k0 + 32 * b + 8 * (r >> 2) + 4 * h + (r & 3) > row) s[b][r] = -__builtin_inff();
+      }
+      float most = s[0][0];
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][r]);
+      most = fmaxf(most, __shfl_xor(most, 32, 64)) * c;
+      // A row's reference follows its maximum only when that is 2^8 beyond it (whatever other rows' do): results are the same, what is summed
+      // stays below 2^8 times the number of keys
+      if (__any(most > top + 8.0f)) {
+        const float next = most > top + 8.0f ? most : top, by = __builtin_amdgcn_exp2f(top - (next == -__builtin_inff() ? 0.0f : next));
+        top = next;
+        sum *= by;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= by;
+      }
+      const float ref = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -ref));
+          sum += s[b][r];
+        }
+      const bool clean = masked && odd[cur];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const Frag8<TYPE> x[2] = {as_frag<TYPE>(s[b], 0), as_frag<TYPE>(s[b], 1)};
+        add_cols<TYPE, BK, ND>(o, lv, 32 * b, x, clean);
+        if (clean) add_unusual<TYPE, BK, ND>(o, lv, 32 * b, [&](int r) { return k0 + 32 * b + r <= row; });
+      }
+    }
+    if (more) {
+      E *next = lds + (cur ^ 1) * 2 * KV::ELEMS;
+      tk.store(next);
+      tv.store(next + KV::ELEMS);
+      if (k0 + 2 * BK > q0 && tv.any()) odd[cur ^ 1] = 1;      // (a tile that some wavefront masks; the mark stays: a false one costs time alone)
+    }
+    __syncthreads();
+  }
+  sum += __shfl_xor(sum, 32, 64);
+  if (!in) return;
+  store_row<TYPE, ND, VEC>(static_cast<E *>(p.o) + w.start * p.ldo + head * p.ho, (long long)row * p.ldo, o, 1.0f / sum, p.D);
+  if (p.lse && h == 0) p.lse[head * p.rows + w.start + row] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+template <int TYPE, int ND, bool VEC> hipError_t forward_launch(const AttentionP &p, hipStream_t s) {
+  constexpr int BK = TYPE == TYPE_F32 ? 32 : 64;
+  constexpr size_t bytes = 4 * Tile<TYPE, BK, ND>::ELEMS * sizeof(typename ElemOf<TYPE>::type);
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(&attention_kernel<TYPE, ND, VEC>), bytes, done);
+  if (e != hipSuccess) return e;
+  const long long blocks = attention_tiles(p) * p.Hq, rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
+  hipLaunchKernelGGL((attention_kernel<TYPE, ND, VEC>), dim3((unsigned)(blocks + rest)), dim3(256), bytes, s, p, (int)blocks);
+  return hipGetLastError();
+}
+template <int TYPE, bool VEC> hipError_t forward_width(const AttentionP &p, hipStream_t s) {
+  switch ((p.D + 31) / 32) {
+    case 1: return forward_launch<TYPE, 1, VEC>(p, s);
+    case 2: return forward_launch<TYPE, 2, VEC>(p, s);
+    case 3: return forward_launch<TYPE, 3, VEC>(p, s);
+    default: return forward_launch<TYPE, 4, VEC>(p, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attention_tiles(const AttentionP &p, hipStream_t s) {
+  if (!p.offsets || p.seqs <= 64) return hipSuccess;
+  hipLaunchKernelGGL(attention_tiles_kernel, dim3(1), dim3(256), 0, s, p, const_cast<int *>(p.first), ATTENTION_ROWS);
+  return hipGetLastError();
+}
+
+hipError_t launch_attention(const AttentionP &p, hipStream_t s) {
+  const hipError_t e = launch_attention_tiles(p, s);
+  if (e != hipSuccess) return e;
+  const bool vec = rows_of_vectors(p.q, p.type, p.hq, p.ldq, p.D) && rows_of_vectors(p.k, p.type, p.hk, p.ldk, p.D) &&
+                   rows_of_vectors(p.v, p.type, p.hv, p.ldv, p.D) && rows_of_vectors(p.o, p.type, p.ho, p.ldo, p.D);
+  switch (p.type) {
+    case TYPE_F32: return vec ? forward_width<TYPE_F32, true>(p, s) : forward_width<TYPE_F32, false>(p, s);
+    case TYPE_BF16: return vec ? forward_width<TYPE_BF16, true>(p, s) : forward_width<TYPE_BF16, false>(p, s);
+    default: return vec ? forward_width<TYPE_F16, true>(p, s) : forward_width<TYPE_F16, false>(p, s);
+  }
+}
+
+}  // namespace absk

@@ -1,0 +1,323 @@
+// Gradients of causal attention (attention.hip).
+//
+//   p_ij = exp(s_ij - lse_i),  D_i = do_i . o_i,  ds_ij = a p_ij (do_i . v_j - D_i)
+//   dv_j = sum_i p_ij do_i,  dk_j = sum_i ds_ij q_i  (query heads that share the key head add up),  dq_i = sum_j ds_ij k_j
+//
+// Scores are formed again from q and k.  Two kernels, so that every sum has one owner and an order of its own (the same bits every time): one takes 128
+// keys, 32 to a wavefront, and goes through the queries of all heads that share them; the other takes 128 queries and goes through their keys.
+// Together seven products where one kernel would need five, but no sums of dq in memory by atomics.  Scores stay in registers: what is a result of the
+// first products is, rounded, an operand of the second ones, whose other operand is read transposed from the tile that is in LDS anyway.
+//
+// fp16 operands hold p and ds in 16 bits with powers of two: p by 2^12 (else values below 2^-14, those of a row of many keys, lose bits), ds by the power that
+// takes twice the largest |do_i| |v_j|, a bound on |ds / a|, to 2^14 at most.
+#include <algorithm>
+#include "attention_parts.h"
+
+namespace absk {
+namespace {
+
+template <int TYPE> constexpr float P_SHIFT = TYPE == TYPE_F16 ? 12.0f : 0.0f;
+
+// D_i of every row and query head, 16 lanes each; WIDE 0: any alignment.  fp16: the largest squared lengths of do_i and v_j that each block meets
+template <int TYPE, bool VEC>
+__global__ void __launch_bounds__(256) attention_inner_kernel(const AttentionP p) {
+  const int g = threadIdx.x / 16, l = threadIdx.x % 16, D = p.D;
+  const long long start = span_of(p, 0).start;
+  const Span last = span_of(p, p.seqs - 1);
+  const long long n = max(0LL, last.start + last.len - start);
+  const long long step = (long long)gridDim.x * 16;
+  float longest = 0.0f, longest_v = 0.0f;
+  typedef typename ElemOf<TYPE>::type E;
+  auto values = [&](const void *base, long long at, float (&v)[8]) {
+    const E *src = static_cast<const E *>(base) + at + l * 8;
+    if (VEC && l * 8 < D) {
+      load8(src, TYPE, 0, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = l * 8 + e < D ? load_as_f32(src, TYPE, e) : 0.0f;
+    }
+  };
+  for (long long i = (long long)blockIdx.x * 16 + g; i < n * p.Hq; i += step) {
+    const long long r = i / p.Hq, row = start + r;
+    const int h = (int)(i - r * p.Hq);
+    float a[8], b[8], s = 0.0f, t = 0.0f;
+    values(p.dout, row * p.lddo + h * p.hdo, a);
+    values(p.o, row * p.ldo + h * p.ho, b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s = fmaf(a[e], b[e], s);
+      if (TYPE == TYPE_F16) t = fmaf(a[e], a[e], t);
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      s += __shfl_xor(s, o, 16);
+      if (TYPE == TYPE_F16) t += __shfl_xor(t, o, 16);
+    }
+    if (l == 0) p.inner[h * p.rows + row] = s;
+    if (TYPE == TYPE_F16 && t < __builtin_inff()) longest = fmaxf(longest, t);
+  }
+  if constexpr (TYPE == TYPE_F16) {
+    for (long long i = (long long)blockIdx.x * 16 + g; i < n * p.Hkv; i += step) {
+      const long long r = i / p.Hkv, row = start + r;
+      float a[8], t = 0.0f;
+      values(p.v, row * p.ldv + (i - r * p.Hkv) * p.hv, a);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t = fmaf(a[e], a[e], t);
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) t += __shfl_xor(t, o, 16);
+      if (t < __builtin_inff()) longest_v = fmaxf(longest_v, t);
+    }
+    __shared__ float sm[2][16];
+    if (l == 0) { sm[0][g] = longest; sm[1][g] = longest_v; }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+      float m = 0.0f;
+      for (int k = 0; k < 16; ++k) m = fmaxf(m, sm[threadIdx.x][k]);
+      p.most[threadIdx.x * p.nmost + blockIdx.x] = m;
+    }
+  }
+}
+
+// The power of two that ds is held with
+template <int TYPE> __device__ __forceinline__ float ds_factor(const AttentionP &p) {
+  if constexpr (TYPE != TYPE_F16) return 1.0f;
+  float a = 0.0f, b = 0.0f;
+  for (int i = threadIdx.x & 63; i < p.nmost; i += 64) { a = fmaxf(a, p.most[i]); b = fmaxf(b, p.most[p.nmost + i]); }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) { a = fmaxf(a, __shfl_xor(a, o, 64)); b = fmaxf(b, __shfl_xor(b, o, 64)); }
+  const float bound = 2.0f * sqrtf(a) * sqrtf(b);
+  if (!(bound > 0.0f)) return 1.0f;
+  int e;
+  (void)frexpf(bound, &e);                             // bound < 2^e
+  return ldexpf(1.0f, max(-100, min(100, 14 - e)));
+}
+
+// dk and dv of 128 keys
+template <int TYPE, int ND, bool VEC>
+__global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) attention_keys_kernel(const AttentionP p, const int blocks) {
+  constexpr int BQ = TYPE == TYPE_F32 || ND >= 3 ? 32 : 64;
+  typedef Tile<TYPE, BQ, ND> T;
+  typedef typename T::E E;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+  __shared__ __attribute__((aligned(16))) float stat[2][2][BQ];      // lse (to base 2) and D of a tile's queries
+  __shared__ int odd[2];
+  E *const lds = reinterpret_cast<E *>(lds_raw);       // [2][queries, do]
+  if ((int)blockIdx.x >= blocks) {
+    zero_rest(p, p.dk, TYPE, p.Hkv, p.lddk, p.hdk, nullptr, blockIdx.x - blocks, REST_BLOCKS);
+    return zero_rest(p, p.dv, TYPE, p.Hkv, p.lddv, p.hdv, nullptr, blockIdx.x - blocks, REST_BLOCKS);
+  }
+  int kvh, t;
+  head_and_tile(blockIdx.x, p.Hkv, kvh, t);
+  const Work w = find_tile(p, t, ATTENTION_ROWS);      // (the first keys of a sequence, seen by most queries, come first)
+  if (w.tile < 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int k0 = w.tile * ATTENTION_ROWS, mine = k0 + wave * 32, key = mine + (lane & 31), G = p.Hq / p.Hkv;
+  const bool in = key < w.len;
+  const float f = ds_factor<TYPE>(p), g = f * __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>);
+  Frag8<TYPE> kf[2 * ND], vf[2 * ND];
+#pragma unroll
+  for (int i = 0; i < 2 * ND; ++i) {
+    kf[i] = row_frag<TYPE, VEC>(p.k, (w.start + key) * p.ldk + kvh * p.hk, in, i, p.D);
+    vf[i] = row_frag<TYPE, VEC>(p.v, (w.start + key) * p.ldv + kvh * p.hv, in, i, p.D);
+  }
+  f32x16 dk[ND], dv[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) dk[d] = dv[d] = zeros16();
+  const float c = p.scale * LOG2E;
+  const int first = k0 / BQ, each = (w.len + BQ - 1) / BQ - first, total = each * G;
+  T tq, td;
+  float lse = 0.0f, inner = 0.0f;
+  auto load = [&](int head, int j) {
+    const int r0 = j * BQ;
+    tq.template load<VEC>(static_cast<const E *>(p.q) + w.start * p.ldq + head * p.hq, p.ldq, r0, w.len, p.D);
+    td.template load<VEC>(static_cast<const E *>(p.dout) + w.start * p.lddo + head * p.hdo, p.lddo, r0, w.len, p.D);
+    if (threadIdx.x < BQ) {
+      const int r = r0 + threadIdx.x;
+      const long long at = head * p.rows + w.start + (r < w.len ? r : 0);
+      lse = r < w.len ? p.lse[at] * LOG2E - P_SHIFT<TYPE> : __builtin_inff();
+      inner = r < w.len ? p.inner[at] : 0.0f;
+    }
+  };
+  auto store = [&](int buf, int j) {
+    tq.store(lds + buf * 2 * T::ELEMS);
+    td.store(lds + buf * 2 * T::ELEMS + T::ELEMS);
+    if (threadIdx.x < BQ) { stat[buf][0][threadIdx.x] = lse; stat[buf][1][threadIdx.x] = inner; }
+    if (j * BQ < k0 + ATTENTION_ROWS && (tq.any() || td.any())) odd[buf] = 1;      // (a tile that some wavefront masks)
+  };
+  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+  int head = kvh * G, j = first;
+  load(head, j);
+  __syncthreads();
+  store(0, j);
+  __syncthreads();
+  for (int it = 0; it < total; ++it) {
+    const int cur = it & 1, r0 = j * BQ;
+    const E *lq = lds + cur * 2 * T::ELEMS, *ld = lq + T::ELEMS;
+    if (++j == first + each) { j = first; ++head; }
+    const bool more = it + 1 < total;
+    if (more) load(head, j);
+#pragma unroll
+    for (int b = 0; b < BQ / 32; ++b) {
+      const int q0 = r0 + 32 * b;
+      if (q0 + 31 < mine || q0 >= w.len || mine >= w.len) continue;
+      f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+      for (int i = 0; i < 2 * ND; ++i) {
+        mma<TYPE>(s, T::rows(lq, 32 * b, i), kf[i]);
+        mma<TYPE>(dp, T::rows(ld, 32 * b, i), vf[i]);
+      }
+      const bool masked = q0 < mine + 31;
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const float4 l4 = *reinterpret_cast<const float4 *>(&stat[cur][0][32 * b + 8 * r4 + 4 * h]);
+        const float4 d4 = *reinterpret_cast<const float4 *>(&stat[cur][1][32 * b + 8 * r4 + 4 * h]);
+        const float l[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * r4 + e;
+          float x = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[e])), y = x * ((dp[r] - dd[e]) * g);
+          if (masked && q0 + 8 * r4 + 4 * h + e < key) x = y = 0.0f;
+          s[r] = x;
+          dp[r] = y;
+        }
+      }
+      const bool clean = masked && odd[cur];
+      const Frag8<TYPE> x[2] = {as_frag<TYPE>(s, 0), as_frag<TYPE>(s, 1)}, y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
+      add_cols<TYPE, BQ, ND>(dv, ld, 32 * b, x, clean);
+      add_cols<TYPE, BQ, ND>(dk, lq, 32 * b, y, clean);
+      if (clean) {
+        add_unusual<TYPE, BQ, ND>(dv, ld, 32 * b, [&](int r) { return q0 + r >= key; });
+        add_unusual<TYPE, BQ, ND>(dk, lq, 32 * b, [&](int r) { return q0 + r >= key; });
+      }
+    }
+    if (more) store(cur ^ 1, j);
+    __syncthreads();
+  }
+  if (!in) return;
+  store_row<TYPE, ND, VEC>(p.dk, (w.start + key) * p.lddk + kvh * p.hdk, dk, p.scale / f, p.D);
+  store_row<TYPE, ND, VEC>(p.dv, (w.start + key) * p.lddv + kvh * p.hdv, dv, __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>), p.D);
+}
+
+// dq of 128 queries of a head
+template <int TYPE, int ND, bool VEC>
+__global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) attention_queries_kernel(const AttentionP p, const int blocks) {
+  constexpr int BK = TYPE == TYPE_F32 ? 32 : 64;
+  typedef Tile<TYPE, BK, ND> T;
+  typedef typename T::E E;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+  __shared__ int odd[2];
+  E *const lds = reinterpret_cast<E *>(lds_raw);       // [2][keys, values]
+  if ((int)blockIdx.x >= blocks) return zero_rest(p, p.dq, TYPE, p.Hq, p.lddq, p.hdq, nullptr, blockIdx.x - blocks, REST_BLOCKS);
+  int head, t;
+  head_and_tile(blockIdx.x, p.Hq, head, t);
+  Work w = find_tile(p, t, ATTENTION_ROWS);
+  if (w.tile < 0) return;
+  w.tile = (w.len + ATTENTION_ROWS - 1) / ATTENTION_ROWS - 1 - w.tile;      // the longest first
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int q0 = w.tile * ATTENTION_ROWS, mine = q0 + wave * 32, row = mine + (lane & 31);
+  const bool in = row < w.len;
+  const int kvh = head / (p.Hq / p.Hkv);
+  const E *k = static_cast<const E *>(p.k) + w.start * p.ldk + kvh * p.hk;
+  const E *v = static_cast<const E *>(p.v) + w.start * p.ldv + kvh * p.hv;
+  const float f = ds_factor<TYPE>(p);
+  Frag8<TYPE> qf[2 * ND], of[2 * ND];
+#pragma unroll
+  for (int i = 0; i < 2 * ND; ++i) {
+    qf[i] = row_frag<TYPE, VEC>(p.q, (w.start + row) * p.ldq + head * p.hq, in, i, p.D);
+    of[i] = row_frag<TYPE, VEC>(p.dout, (w.start + row) * p.lddo + head * p.hdo, in, i, p.D);
+  }
+  const long long at = head * p.rows + w.start + (in ? row : 0);
+  const float lse = in ? p.lse[at] * LOG2E : __builtin_inff(), inner = in ? p.inner[at] : 0.0f, c = p.scale * LOG2E;
+  f32x16 dq[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) dq[d] = zeros16();
+  const int end = min(w.len, q0 + ATTENTION_ROWS), tiles = (end + BK - 1) / BK;
+  T tk, tv;
+  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+  tk.template load<VEC>(k, p.ldk, 0, w.len, p.D);
+  tv.template load<VEC>(v, p.ldv, 0, w.len, p.D);
+  __syncthreads();
+  tk.store(lds);
+  tv.store(lds + T::ELEMS);
+  if (BK > q0 && tk.any()) odd[0] = 1;
+  __syncthreads();
+  for (int j = 0; j < tiles; ++j) {
+    const int k0 = j * BK, cur = j & 1;
+    const E *lk = lds + cur * 2 * T::ELEMS, *lv = lk + T::ELEMS;
+    const bool more = j + 1 < tiles;
+    if (more) {
+      tk.template load<VEC>(k, p.ldk, k0 + BK, w.len, p.D);
+      tv.template load<VEC>(v, p.ldv, k0 + BK, w.len, p.D);
+    }
+#pragma unroll
+    for (int b = 0; b < BK / 32; ++b) {
+      const int kb = k0 + 32 * b;
+      if (kb > mine + 31 || kb >= w.len || mine >= w.len) continue;
+      f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+      for (int i = 0; i < 2 * ND; ++i) {
+        mma<TYPE>(s, T::rows(lk, 32 * b, i), qf[i]);
+        mma<TYPE>(dp, T::rows(lv, 32 * b, i), of[i]);
+      }
+      const bool masked = kb + 31 > mine;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse));
+        dp[r] = x * ((dp[r] - inner) * f);
+        if (masked && kb + 8 * (r >> 2) + 4 * h + (r & 3) > row) dp[r] = 0.0f;
+      }
+      const bool clean = masked && odd[cur];
+      const Frag8<TYPE> y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
+      add_cols<TYPE, BK, ND>(dq, lk, 32 * b, y, clean);
+      if (clean) add_unusual<TYPE, BK, ND>(dq, lk, 32 * b, [&](int r) { return kb + r <= row; });
+    }
+    if (more) {
+      E *next = lds + (cur ^ 1) * 2 * T::ELEMS;
+      tk.store(next);
+      tv.store(next + T::ELEMS);
+      if (k0 + 2 * BK > q0 && tk.any()) odd[cur ^ 1] = 1;
+    }
+    __syncthreads();
+  }
+  if (!in) return;
+  store_row<TYPE, ND, VEC>(p.dq, (w.start + row) * p.lddq + head * p.hdq, dq, p.scale / f, p.D);
+}
+
+template <int TYPE, int ND, bool VEC> hipError_t backward_launch(const AttentionP &p, hipStream_t s) {
+  constexpr int BQ = TYPE == TYPE_F32 || ND >= 3 ? 32 : 64, BK = TYPE == TYPE_F32 ? 32 : 64;
+  constexpr size_t e = sizeof(typename ElemOf<TYPE>::type), keys = 4 * Tile<TYPE, BQ, ND>::ELEMS * e, queries = 4 * Tile<TYPE, BK, ND>::ELEMS * e;
+  static std::atomic<uint64_t> done_keys{0}, done_queries{0};
+  hipError_t err = allow_lds(reinterpret_cast<const void *>(&attention_keys_kernel<TYPE, ND, VEC>), keys, done_keys);
+  if (err == hipSuccess) err = allow_lds(reinterpret_cast<const void *>(&attention_queries_kernel<TYPE, ND, VEC>), queries, done_queries);
+  if (err != hipSuccess) return err;
+  const long long tiles = attention_tiles(p), rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
+  hipLaunchKernelGGL((attention_inner_kernel<TYPE, VEC>), dim3(p.nmost), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hkv + rest)), dim3(256), keys, s, p, (int)(tiles * p.Hkv));
+  hipLaunchKernelGGL((attention_queries_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hq + rest)), dim3(256), queries, s, p, (int)(tiles * p.Hq));
+  return hipGetLastError();
+}
+template <int TYPE, bool VEC> hipError_t backward_width(const AttentionP &p, hipStream_t s) {
+  switch ((p.D + 31) / 32) {
+    case 1: return backward_launch<TYPE, 1, VEC>(p, s);
+    case 2: return backward_launch<TYPE, 2, VEC>(p, s);
+    case 3: return backward_launch<TYPE, 3, VEC>(p, s);
+    default: return backward_launch<TYPE, 4, VEC>(p, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attention_backward(const AttentionP &p, hipStream_t s) {
+  const hipError_t e = launch_attention_tiles(p, s);
+  if (e != hipSuccess) return e;
+  const auto rows = [&](const void *t, long long h, long long ld) { return rows_of_vectors(t, p.type, h, ld, p.D); };
+  const bool vec = rows(p.q, p.hq, p.ldq) && rows(p.k, p.hk, p.ldk) && rows(p.v, p.hv, p.ldv) && rows(p.o, p.ho, p.ldo) && rows(p.dout, p.hdo, p.lddo) &&
+                   rows(p.dq, p.hdq, p.lddq) && rows(p.dk, p.hdk, p.lddk) && rows(p.dv, p.hdv, p.lddv);
+  switch (p.type) {
+    case TYPE_F32: return vec ? backward_width<TYPE_F32, true>(p, s) : backward_width<TYPE_F32, false>(p, s);
+    case TYPE_BF16: return vec ? backward_width<TYPE_BF16, true>(p, s) : backward_width<TYPE_BF16, false>(p, s);
+    default: return vec ? backward_width<TYPE_F16, true>(p, s) : backward_width<TYPE_F16, false>(p, s);
+  }
+}
+
+}  // namespace absk

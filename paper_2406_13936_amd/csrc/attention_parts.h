@@ -1,0 +1,366 @@
+// What the attention kernels share: sequences and their tiles, operand tiles in LDS, matrix-core fragments.
+//
+// Products are of 32 x 32 tiles with the reduction in steps of 16: a lane's fragment holds eight values, of row (lane & 31) of the operand and
+// of the reduction's places 8 (lane >> 5) + e; results have column (lane & 31) and rows 8 (r / 4) + 4 (lane >> 5) + r % 4, r = 0 .. 15.  The order of the
+// reduction is free as long as both operands have the same, so registers 8 b .. 8 b + 7 of a result are, rounded, a fragment of the next product
+// whose places are rows 16 b + 8 (e / 4) + 4 (lane >> 5) + e % 4: scores never go through LDS, the other operand is read in that order instead.
+// fp32 values take eight 32 x 32 x 2 products to a step, with the same fragments.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include "device_utils.h"
+#include "mfma_tile.h"
+#include "ops.h"
+#include "typed_mem.h"
+
+namespace absk {
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// ---- types -----------------------------------------------------------------------------------------------------------
+
+template <int TYPE> struct Frag8 { uint4 q; };                       // eight 16-bit values
+template <> struct Frag8<TYPE_F32> { float v[8]; };
+template <int TYPE> struct ElemOf { typedef uint16_t type; };
+template <> struct ElemOf<TYPE_F32> { typedef float type; };
+
+template <int TYPE> __device__ __forceinline__ void mma(f32x16 &c, const Frag8<TYPE> &a, const Frag8<TYPE> &b) {
+  if constexpr (TYPE == TYPE_BF16) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.q), __builtin_bit_cast(bf16x8, b.q), c, 0, 0, 0);
+  } else if constexpr (TYPE == TYPE_F16) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a.q), __builtin_bit_cast(f16x8, b.q), c, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
+  }
+}
+// registers 8 b .. 8 b + 7 of a result as a fragment
+template <int TYPE> __device__ __forceinline__ Frag8<TYPE> as_frag(const f32x16 &c, int b) {
+  Frag8<TYPE> f;
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = c[8 * b + e];
+  if constexpr (TYPE == TYPE_F32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e] = v[e];
+  } else {
+    f.q = pack8(TYPE, v);
+  }
+  return f;
+}
+__device__ __forceinline__ f32x16 zeros16() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.0f;
+  return z;
+}
+// an infinity or NaN?
+template <int TYPE> __device__ __forceinline__ bool unusual(float v) { return !(fabsf(v) < __builtin_inff()); }
+template <int TYPE> __device__ __forceinline__ uint32_t unusual_half(uint32_t w) {      // of a word's low 16 bits
+  constexpr uint32_t E = TYPE == TYPE_BF16 ? 0x7f80u : 0x7c00u;
+  return (w & E) == E;
+}
+template <int TYPE> __device__ __forceinline__ bool any_unusual(const uint4 q) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  bool any = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (TYPE == TYPE_F32) any |= unusual<TYPE>(__uint_as_float(w[e]));
+    else any |= unusual_half<TYPE>(w[e]) || unusual_half<TYPE>(w[e] >> 16);
+  }
+  return any;
+}
+// zeros in the place of infinities and NaN
+template <int TYPE> __device__ __forceinline__ Frag8<TYPE> usual(Frag8<TYPE> f) {
+  if constexpr (TYPE == TYPE_F32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e] = unusual<TYPE>(f.v[e]) ? 0.0f : f.v[e];
+  } else {
+    uint32_t w[4] = {f.q.x, f.q.y, f.q.z, f.q.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] &= (unusual_half<TYPE>(w[e]) ? 0u : 0xffffu) | (unusual_half<TYPE>(w[e] >> 16) ? 0u : 0xffff0000u);
+    f.q = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return f;
+}
+
+// ---- operand tiles in LDS ----------------------------------------------------------------------------------------------
+
+// ROWS rows of 32 ND values.  16-bit: rows of 4, 8 or 16 chunks of 16 bytes, whose places are exchanged by an XOR of the row so that neither reads
+// of 16 rows' same chunk nor transposing reads of four rows' four chunks meet in a bank.  fp32: rows four words apart from a multiple of 64.
+template <int TYPE, int ROWS, int ND> struct Tile {
+  typedef typename ElemOf<TYPE>::type E;
+  static constexpr int CH = ND == 1 ? 4 : ND == 2 ? 8 : 16;          // chunks of a row, of which 4 ND hold values
+  static constexpr int PER = TYPE == TYPE_F32 ? 4 : 8;               // values of a 16-byte vector
+  static constexpr int LD = TYPE == TYPE_F32 ? ((32 * ND + 63) / 64 * 64 + 4) : CH * 8;
+  static constexpr int ELEMS = ROWS * LD;
+  static constexpr int VECS = ROWS * 32 * ND / PER;                  // vectors of the tile
+  static constexpr int NV = (VECS + 255) / 256;                      // of a thread (of 256)
+
+  static __device__ __forceinline__ int swizzle(int row) {
+    return CH == 16 ? 4 * (row & 3) | (row >> 2 & 3) : CH == 8 ? 4 * (row >> 1 & 1) | (row >> 2 & 3) : row >> 2 & 3;
+  }
+  static __device__ __forceinline__ int place(int row, int chunk) {  // of vector `chunk` of a row, in values
+    return TYPE == TYPE_F32 ? row * LD + chunk * 4 : row * LD + (chunk ^ swizzle(row)) * 8;
+  }
+
+  // A thread's part of rows row0 .. of a sequence of `len` rows whose first value is at `base`: zeros beyond the sequence and beyond D.
+  // (Every thread loads, from a place of the tensor where it has none.)
+  uint4 q[NV];
+  template <bool VEC> __device__ __forceinline__ void load(const void *base, long long ld, int row0, int len, int D) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = threadIdx.x + i * 256, row = c / (32 * ND / PER), col = c % (32 * ND / PER) * PER;
+      const int r = row0 + row;
+      if constexpr (VEC) {
+        const bool in = r < len && col < D && (VECS % 256 == 0 || row < ROWS);
+        const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const E *>(base) + (in ? r * ld + col : 0));
+        q[i] = make_uint4(in ? w.x : 0u, in ? w.y : 0u, in ? w.z : 0u, in ? w.w : 0u);
+      } else {
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        if (r < len && (VECS % 256 == 0 || row < ROWS)) {
+          const E *p = static_cast<const E *>(base) + r * ld + col;
+#pragma unroll
+          for (int e = 0; e < PER; ++e)
+            if (col + e < D) {
+              if constexpr (TYPE == TYPE_F32) w[e] = __float_as_uint(p[e]);
+              else w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+            }
+        }
+        q[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(E *lds) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = threadIdx.x + i * 256, row = c / (32 * ND / PER), chunk = c % (32 * ND / PER);
+      if (VECS % 256 == 0 || row < ROWS) *reinterpret_cast<uint4 *>(lds + place(row, chunk)) = q[i];
+    }
+  }
+  __device__ __forceinline__ bool any() const {
+    bool a = false;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) a |= any_unusual<TYPE>(q[i]);
+    return a;
+  }
+
+  // Fragment of rows row0 .. row0 + 31 for step k of the values (16 k ..)
+  static __device__ __forceinline__ Frag8<TYPE> rows(const E *lds, int row0, int k) {
+    const int lane = threadIdx.x & 63, row = row0 + (lane & 31), h = lane >> 5;
+    Frag8<TYPE> f;
+    if constexpr (TYPE == TYPE_F32) {
+      const float4 a = *reinterpret_cast<const float4 *>(lds + place(row, 4 * k + 2 * h)), b = *reinterpret_cast<const float4 *>(lds + place(row, 4 * k + 2 * h + 1));
+      f.v[0] = a.x; f.v[1] = a.y; f.v[2] = a.z; f.v[3] = a.w; f.v[4] = b.x; f.v[5] = b.y; f.v[6] = b.z; f.v[7] = b.w;
+    } else {
+      f.q = *reinterpret_cast<const uint4 *>(lds + place(row, 2 * k + h));
+    }
+    return f;
+  }
+  // Transposed: of values 32 d .. 32 d + 31 as rows and the tile's rows row0 + 8 (e / 4) + 4 (lane >> 5) + e % 4 as the reduction's places
+  static __device__ __forceinline__ Frag8<TYPE> cols(const E *lds, int row0, int d) {
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    Frag8<TYPE> f;
+    if constexpr (TYPE == TYPE_F32) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f.v[e] = lds[(row0 + 8 * (e >> 2) + 4 * h + (e & 3)) * LD + 32 * d + (lane & 31)];
+    } else {
+      // a transposing read: lane i of 16 names four values of one row, and gets one value of each of four rows
+      const int i16 = lane & 15, col = 32 * d + (lane >> 4 & 1) * 16 + 4 * (i16 & 3), row = row0 + 4 * h + (i16 >> 2);
+      const E *a = lds + place(row, col >> 3) + (col & 7), *b = lds + place(row + 8, col >> 3) + (col & 7);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(a));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(b));
+      f.q = __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    return f;
+  }
+  static __device__ __forceinline__ float value(const E *lds, int row, int col) {
+    const E v = lds[place(row, col / PER) + col % PER];
+    if constexpr (TYPE == TYPE_F32) return v;
+    else return TYPE == TYPE_BF16 ? bf2f(v) : f16_val(v);
+  }
+};
+
+// The fragment of one row of memory for step k: the row's values 16 k + 8 (lane >> 5) + e; zeros where there is no row, and beyond D
+template <int TYPE, bool VEC>
+__device__ __forceinline__ Frag8<TYPE> row_frag(const void *base, long long at, bool in, int k, int D) {
+  typedef typename ElemOf<TYPE>::type E;
+  const int col = 16 * k + 8 * (threadIdx.x >> 5 & 1);
+  Frag8<TYPE> f;
+  float v[8];
+  const E *p = static_cast<const E *>(base) + (in && col < D ? at + col : 0);
+  const bool ok = in && col < D;
+  if constexpr (TYPE == TYPE_F32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (VEC) {
+        const bool o = ok && col + 4 * h < D;
+        const float4 a = *reinterpret_cast<const float4 *>(o ? p + 4 * h : p);
+        v[4 * h] = o ? a.x : 0.0f; v[4 * h + 1] = o ? a.y : 0.0f; v[4 * h + 2] = o ? a.z : 0.0f; v[4 * h + 3] = o ? a.w : 0.0f;
+      } else {
+#pragma unroll
+        for (int e = 4 * h; e < 4 * h + 4; ++e) v[e] = ok && col + e < D ? p[e] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e] = v[e];
+  } else if constexpr (VEC) {
+    const uint4 w = *reinterpret_cast<const uint4 *>(p);
+    f.q = make_uint4(ok ? w.x : 0u, ok ? w.y : 0u, ok ? w.z : 0u, ok ? w.w : 0u);
+  } else {
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (ok && col + e < D) w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+    f.q = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return f;
+}
+
+// acc[d] += sum over the tile's rows row0 .. of (row, place) X^T Y: the two fragments of x are rows of the reduction
+template <int TYPE, int ROWS, int ND>
+__device__ __forceinline__ void add_cols(f32x16 (&acc)[ND], const typename ElemOf<TYPE>::type *lds, int row0, const Frag8<TYPE> (&x)[2], bool clean) {
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      Frag8<TYPE> f = Tile<TYPE, ROWS, ND>::cols(lds, row0 + 16 * b, d);
+      if (clean) f = usual<TYPE>(f);
+      mma<TYPE>(acc[d], f, x[b]);
+    }
+}
+// What add_cols left out with `clean`: infinities and NaN of the tile's rows row0 .. row0 + 31, in the columns of acc (the lane's own) that the mask
+// leaves to them.  They count as they are: weights are positive or make them NaN.
+template <int TYPE, int ROWS, int ND, class F>
+__device__ __forceinline__ void add_unusual(f32x16 (&acc)[ND], const typename ElemOf<TYPE>::type *lds, int row0, F &&sees) {
+  const int h = threadIdx.x >> 5 & 1;
+  for (int r = 0; r < 32; ++r) {
+    if (!sees(r)) continue;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const float v = Tile<TYPE, ROWS, ND>::value(lds, row0 + r, 32 * d + 8 * (k >> 2) + 4 * h + (k & 3));
+        if (unusual<TYPE>(v)) acc[d][k] += v;
+      }
+  }
+}
+
+// Results to memory: the lane's row of D values from acc (its column), times `by`
+template <int TYPE, int ND, bool VEC>
+__device__ __forceinline__ void store_row(void *base, long long at, const f32x16 (&acc)[ND], float by, int D) {
+  const int h = threadIdx.x >> 5 & 1;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int col = 32 * d + 8 * k + 4 * h;
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = acc[d][4 * k + e] * by;
+      if (VEC) {
+        if (col >= D) continue;
+        if constexpr (TYPE == TYPE_F32) {
+          *reinterpret_cast<float4 *>(static_cast<float *>(base) + at + col) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+          const uint32_t lo = TYPE == TYPE_BF16 ? pack2bf(v[0], v[1]) : (uint32_t)f16_bits(v[0]) | ((uint32_t)f16_bits(v[1]) << 16);
+          const uint32_t hi = TYPE == TYPE_BF16 ? pack2bf(v[2], v[3]) : (uint32_t)f16_bits(v[2]) | ((uint32_t)f16_bits(v[3]) << 16);
+          *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(base) + at + col) = make_uint2(lo, hi);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + e < D) store_from_f32(base, TYPE, at + col + e, v[e]);
+      }
+    }
+}
+
+// ---- sequences -------------------------------------------------------------------------------------------------------
+
+struct Span { long long start; int len; };             // rows of a sequence
+
+// The s-th sequence: between its offsets, brought into [0, rows] (a list that does not rise gives empty sequences, never rows outside)
+__device__ __forceinline__ Span span_of(const AttentionP &p, int s) {
+  if (!p.offsets) return {(long long)s * p.T, p.T};
+  long long a, b;
+  if (p.wide) { a = static_cast<const long long *>(p.offsets)[s]; b = static_cast<const long long *>(p.offsets)[s + 1]; }
+  else { a = static_cast<const int *>(p.offsets)[s]; b = static_cast<const int *>(p.offsets)[s + 1]; }
+  a = max(0LL, min(a, p.rows));
+  b = max(a, min(b, p.rows));
+  return {a, (int)(b - a)};
+}
+
+struct Work { long long start; int len, tile; };       // tile < 0: none
+
+// The t-th tile of `size` rows of all sequences.  Every lane of a wavefront asks for the same t.  With more than 64 sequences p.first holds the number
+// of tiles before each (attention_tiles_kernel).
+__device__ __forceinline__ Work find_tile(const AttentionP &p, int t, int size) {
+  if (!p.offsets) {
+    const int each = (p.T + size - 1) / size, s = t / each;
+    if (s >= p.seqs) return {0, 0, -1};
+    return {(long long)s * p.T, p.T, t - s * each};
+  }
+  const int lane = threadIdx.x & 63;
+  if (p.seqs <= 64) {
+    const Span mine = lane < p.seqs ? span_of(p, lane) : Span{0, 0};
+    const int n = (mine.len + size - 1) / size;
+    int upto = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += v;
+    }
+    const uint64_t behind = __ballot(upto > t);
+    if (!behind) return {0, 0, -1};
+    const int s = __ffsll((unsigned long long)behind) - 1;
+    const int tile = t - __shfl(upto - n, s, 64);
+    const Span at = span_of(p, s);
+    return {at.start, at.len, tile};
+  }
+  // the last sequence with first <= t (of those that start alike, all but the last are empty): 64 places at a time
+  int lo = 0, n = p.seqs;                              // among lo .. lo + n - 1
+  if (t >= p.first[p.seqs]) return {0, 0, -1};
+  while (n > 1) {
+    const int step = (n + 63) / 64, at = lo + lane * step;
+    const uint64_t in = __ballot(lane * step < n && p.first[min(at, p.seqs)] <= t);
+    const int k = 63 - __clzll((unsigned long long)in);
+    n = min(step, n - k * step);
+    lo += k * step;
+  }
+  const Span at = span_of(p, lo);
+  return {at.start, at.len, t - p.first[lo]};
+}
+
+// Heads and tiles of a block: neighbouring heads share keys and values, so they go to one XCD (blocks are dealt to the eight in turn)
+__device__ __forceinline__ void head_and_tile(int block, int heads, int &head, int &tile) {
+  if (heads % 8 == 0) {
+    const int each = heads / 8, r = block / 8;
+    head = block % 8 * each + r % each;
+    tile = r / each;
+  } else {
+    head = block % heads;
+    tile = block / heads;
+  }
+}
+
+// Zeros in rows before the first and behind the last sequence: `part` of `parts` blocks
+__device__ __forceinline__ void zero_rest(const AttentionP &p, void *out, int type, int heads, long long ld, long long sh, float *lse, int part, int parts) {
+  const Span first = span_of(p, 0), last = span_of(p, p.seqs - 1);
+  const long long head = first.start, from = last.start + last.len, n = head + max(0LL, p.rows - from), D = p.D;
+  for (long long i = (long long)part * 256 + threadIdx.x; i < n * heads * D; i += (long long)parts * 256) {
+    const long long r = i / (heads * D), rest = i - r * heads * D, h = rest / D, row = r < head ? r : from + (r - head);
+    store_from_f32(out, type, row * ld + h * sh + (rest - h * D), 0.0f);
+  }
+  if (lse)
+    for (long long i = (long long)part * 256 + threadIdx.x; i < n * heads; i += (long long)parts * 256) {
+      const long long h = i / n, r = i - h * n;
+      lse[h * p.rows + (r < head ? r : from + (r - head))] = 0.0f;
+    }
+}
+constexpr int REST_BLOCKS = 64;
+
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.69314718055994531f;
+
+}  // namespace
+}  // namespace absk

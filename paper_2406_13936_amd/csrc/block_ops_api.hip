@@ -58,6 +58,63 @@ RmsNormP rms_args(const abs_rms_norm_shape *s) {
   return p;
 }
 
+// ---- causal attention ------------------------------------------------------------------------------------------------
+
+// Heads of rows of D values: blocks of [heads][rows][D], head after head or (as projections leave them) interleaved by rows
+Block heads_of(const void *t, const abs_attention_shape *s, int heads, int64_t ld, int64_t head) {
+  return {t, heads, head, s->rows, ld, s->D, type_bytes(s->type)};
+}
+struct AttentionPieces { size_t first, inner, most, total; };
+constexpr int MOST_BLOCKS = 1024;
+AttentionPieces attention_pieces(const abs_attention_shape *s, bool backward) {
+  AttentionPieces q;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t r = at; at = (at + bytes + 255) / 256 * 256; return r; };
+  q.first = take(s->offsets_type && s->seqs > 64 ? ((size_t)s->seqs + 1) * 4 : 0);
+  q.inner = take(backward ? (size_t)s->Hq * s->rows * 4 : 0);
+  q.most = take(backward && s->type == ABS_TYPE_F16 ? 2 * MOST_BLOCKS * 4 : 0);
+  q.total = at;
+  return q;
+}
+AttentionP attention_args(const abs_attention_shape *s) {
+  AttentionP p;
+  std::memset(&p, 0, sizeof(p));
+  p.type = s->type; p.Hq = s->Hq; p.Hkv = s->Hkv; p.D = s->D; p.seqs = s->seqs; p.T = s->T; p.rows = s->rows;
+  p.wide = s->offsets_type == ABS_TYPE_I64;
+  p.ldq = s->ldq; p.hq = s->head_q; p.ldk = s->ldk; p.hk = s->head_k; p.ldv = s->ldv; p.hv = s->head_v; p.ldo = s->ldo; p.ho = s->head_o;
+  p.lddo = s->lddo; p.hdo = s->head_do; p.lddq = s->lddq; p.hdq = s->head_dq; p.lddk = s->lddk; p.hdk = s->head_dk; p.lddv = s->lddv; p.hdv = s->head_dv;
+  return p;
+}
+abs_status check_attention(const abs_attention_shape *s, bool backward) {
+  if (!s) return set_error(ABS_EINVAL, "shape is NULL");
+  if (!known_type(s->type)) return set_error(ABS_EINVAL, "unknown type");
+  if (s->offsets_type && s->offsets_type != ABS_TYPE_I32 && s->offsets_type != ABS_TYPE_I64)
+    return set_error(ABS_EINVAL, "offsets_type must be ABS_TYPE_I32, ABS_TYPE_I64, or 0 for sequences of T rows");
+  if (s->seqs < 1 || s->rows < 1 || s->Hq < 1 || s->Hkv < 1 || s->D < 1) return set_error(ABS_EINVAL, "seqs, rows, Hq, Hkv and D must be at least 1");
+  if (s->Hq % s->Hkv) return set_error(ABS_EINVAL, "Hq must be a multiple of Hkv");
+  if (!s->offsets_type && (s->T < 1 || (int64_t)s->seqs * s->T != s->rows)) return set_error(ABS_EINVAL, "without offsets rows must be seqs times T");
+  if (s->D > ATTENTION_MAX_D) return set_error(ABS_EUNSUPPORTED, "heads of more than 128 values");
+  if (s->rows > 0x7fffffff) return set_error(ABS_EUNSUPPORTED, "more than 2^31 - 1 rows");
+  AttentionP p = attention_args(s);
+  p.offsets = s->offsets_type ? s : nullptr;             // (asked whether there are any)
+  if (attention_tiles(p) > 0xff0000 / s->Hq) return set_error(ABS_EUNSUPPORTED, "more heads of 128-row tiles than a grid counts");
+  const int heads[8] = {s->Hq, s->Hkv, s->Hkv, s->Hq, s->Hq, s->Hq, s->Hkv, s->Hkv};
+  const int64_t ld[8] = {s->ldq, s->ldk, s->ldv, s->ldo, s->lddo, s->lddq, s->lddk, s->lddv};
+  const int64_t head[8] = {s->head_q, s->head_k, s->head_v, s->head_o, s->head_do, s->head_dq, s->head_dk, s->head_dv};
+  for (int i = 0; i < (backward ? 8 : 4); ++i)
+    if (!strides_ok(heads[i], head[i], s->rows, ld[i], s->D)) return set_error(ABS_EINVAL, "strides: ld >= D, and rows and heads must not overlap");
+  return ABS_OK;
+}
+abs_status check_attention_call(const abs_attention_shape *s, const void *offsets, float scale, const void *workspace, size_t have, size_t need) {
+  if ((offsets != nullptr) != (s->offsets_type != 0)) return set_error(ABS_EINVAL, "offsets_dev is given where there is an offsets_type, and nowhere else");
+  if (!aligned_to(offsets, s->offsets_type == ABS_TYPE_I64 ? 8 : 4)) return set_error(ABS_EINVAL, "pointers must be aligned to their type");
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return set_error(ABS_EINVAL, "scale must be positive and finite");
+  if (need && (!workspace || !aligned_to(workspace, 256))) return set_error(ABS_EINVAL, "workspace must be a 256-byte aligned device pointer");
+  if (have < need) return set_error(ABS_ENOMEM, "workspace too small (see abs_causal_attention_workspace_bytes)");
+  return ABS_OK;
+}
+Block offsets_of(const abs_attention_shape *s, const void *offsets) { return piece(offsets, (int64_t)s->seqs + 1, s->offsets_type == ABS_TYPE_I64 ? 8 : 4); }
+
 }  // namespace
 
 extern "C" {
@@ -169,6 +226,67 @@ abs_status abs_rms_norm_backward(const abs_rms_norm_shape *shape, const void *dy
   if (outputs_overlap(out, in)) return set_error(ABS_EINVAL, "outputs and the workspace must not overlap an input or each other");
   p.x = h_dev; p.res = dh_dev; p.w = w_dev; p.rstd = const_cast<float *>(rstd_dev); p.dy = dy_dev; p.dx = dx_dev; p.dw = dw_dev; p.n = n_dev; p.q = q_dev;
   return hip_status(launch_rms_norm_backward(p, workspace, static_cast<hipStream_t>(hip_stream)), "abs_rms_norm_backward");
+} catch (...) { return exception_status(); }
+
+abs_status abs_causal_attention_workspace_bytes(const abs_attention_shape *shape, int backward, size_t *bytes) try {
+  if (!bytes) return set_error(ABS_EINVAL, "bytes is NULL");
+  abs_status st = check_attention(shape, backward != 0);
+  if (st != ABS_OK) return st;
+  *bytes = attention_pieces(shape, backward != 0).total;
+  return ABS_OK;
+} catch (...) { return exception_status(); }
+
+abs_status abs_causal_attention(const abs_attention_shape *shape, const void *q_dev, const void *k_dev, const void *v_dev, const void *offsets_dev,
+                                float scale, void *o_dev, float *lse_dev, int zero_rest, void *workspace, size_t workspace_bytes, void *hip_stream) try {
+  abs_status st = check_attention(shape, false);
+  if (st != ABS_OK) return st;
+  if (!q_dev || !k_dev || !v_dev || !o_dev) return set_error(ABS_EINVAL, "NULL argument");
+  const AttentionPieces at = attention_pieces(shape, false);
+  st = check_attention_call(shape, offsets_dev, scale, workspace, workspace_bytes, at.total);
+  if (st != ABS_OK) return st;
+  const int e = type_bytes(shape->type);
+  if (!aligned_to(q_dev, e) || !aligned_to(k_dev, e) || !aligned_to(v_dev, e) || !aligned_to(o_dev, e) || !aligned_to(lse_dev, 4))
+    return set_error(ABS_EINVAL, "pointers must be aligned to their type");
+  const Block in[] = {heads_of(q_dev, shape, shape->Hq, shape->ldq, shape->head_q), heads_of(k_dev, shape, shape->Hkv, shape->ldk, shape->head_k),
+                      heads_of(v_dev, shape, shape->Hkv, shape->ldv, shape->head_v), offsets_of(shape, offsets_dev)};
+  const Block out[] = {heads_of(o_dev, shape, shape->Hq, shape->ldo, shape->head_o), piece(lse_dev, shape->Hq * shape->rows, 4),
+                       piece(at.total ? workspace : nullptr, (int64_t)at.total, 1)};
+  if (outputs_overlap(out, in)) return set_error(ABS_EINVAL, "outputs and the workspace must not overlap an input or each other");
+  AttentionP p = attention_args(shape);
+  unsigned char *ws = static_cast<unsigned char *>(workspace);
+  p.q = q_dev; p.k = k_dev; p.v = v_dev; p.offsets = offsets_dev; p.scale = scale; p.o = o_dev; p.lse = lse_dev; p.zero_rest = zero_rest != 0;
+  p.first = reinterpret_cast<const int *>(ws + at.first);
+  return hip_status(launch_attention(p, static_cast<hipStream_t>(hip_stream)), "abs_causal_attention");
+} catch (...) { return exception_status(); }
+
+abs_status abs_causal_attention_backward(const abs_attention_shape *shape, const void *do_dev, const void *q_dev, const void *k_dev, const void *v_dev,
+                                         const void *o_dev, const float *lse_dev, const void *offsets_dev, float scale, void *dq_dev, void *dk_dev,
+                                         void *dv_dev, int zero_rest, void *workspace, size_t workspace_bytes, void *hip_stream) try {
+  abs_status st = check_attention(shape, true);
+  if (st != ABS_OK) return st;
+  if (!do_dev || !q_dev || !k_dev || !v_dev || !o_dev || !lse_dev || !dq_dev || !dk_dev || !dv_dev) return set_error(ABS_EINVAL, "NULL argument");
+  const AttentionPieces at = attention_pieces(shape, true);
+  st = check_attention_call(shape, offsets_dev, scale, workspace, workspace_bytes, at.total);
+  if (st != ABS_OK) return st;
+  const int e = type_bytes(shape->type);
+  for (const void *t : {do_dev, q_dev, k_dev, v_dev, o_dev, (const void *)dq_dev, (const void *)dk_dev, (const void *)dv_dev})
+    if (!aligned_to(t, e)) return set_error(ABS_EINVAL, "pointers must be aligned to their type");
+  if (!aligned_to(lse_dev, 4)) return set_error(ABS_EINVAL, "pointers must be aligned to their type");
+  const Block in[] = {heads_of(do_dev, shape, shape->Hq, shape->lddo, shape->head_do), heads_of(q_dev, shape, shape->Hq, shape->ldq, shape->head_q),
+                      heads_of(k_dev, shape, shape->Hkv, shape->ldk, shape->head_k), heads_of(v_dev, shape, shape->Hkv, shape->ldv, shape->head_v),
+                      heads_of(o_dev, shape, shape->Hq, shape->ldo, shape->head_o), piece(lse_dev, shape->Hq * shape->rows, 4), offsets_of(shape, offsets_dev)};
+  const Block out[] = {heads_of(dq_dev, shape, shape->Hq, shape->lddq, shape->head_dq), heads_of(dk_dev, shape, shape->Hkv, shape->lddk, shape->head_dk),
+                       heads_of(dv_dev, shape, shape->Hkv, shape->lddv, shape->head_dv), piece(workspace, (int64_t)at.total, 1)};
+  if (outputs_overlap(out, in)) return set_error(ABS_EINVAL, "outputs and the workspace must not overlap an input or each other");
+  AttentionP p = attention_args(shape);
+  unsigned char *ws = static_cast<unsigned char *>(workspace);
+  p.dout = do_dev; p.q = q_dev; p.k = k_dev; p.v = v_dev; p.o = const_cast<void *>(o_dev); p.lse = const_cast<float *>(lse_dev);
+  p.offsets = offsets_dev; p.scale = scale; p.dq = dq_dev; p.dk = dk_dev; p.dv = dv_dev; p.zero_rest = zero_rest != 0;
+  p.first = reinterpret_cast<const int *>(ws + at.first);
+  p.inner = reinterpret_cast<float *>(ws + at.inner);
+  p.most = reinterpret_cast<float *>(ws + at.most);
+  p.nmost = (int)std::max<int64_t>(1, std::min<int64_t>(MOST_BLOCKS, (shape->rows * shape->Hq + 63) / 64));
+  return hip_status(launch_attention_backward(p, static_cast<hipStream_t>(hip_stream)), "abs_causal_attention_backward");
 } catch (...) { return exception_status(); }
 
 }  // extern "C"

@@ -127,4 +127,39 @@ size_t embedding_backward_bytes(const EmbeddingP &p, bool want_n, bool want_q);
 hipError_t launch_embedding(const EmbeddingP &p, hipStream_t s);
 hipError_t launch_embedding_backward(const EmbeddingP &p, void *workspace, hipStream_t s);
 
+// ---- causal attention ------------------------------------------------------------------------------------------------
+
+constexpr int ATTENTION_ROWS = 128;      // queries or keys of a block
+constexpr int ATTENTION_MAX_D = 128;
+
+// `seqs` sequences among `rows` rows: between offsets[s] and offsets[s + 1], or without offsets of T rows each.  Strides: values from row to row
+// (ld) and from head to head (h).
+struct AttentionP {
+  int type, Hq, Hkv, D, seqs, T;
+  int wide;                                // offsets of 64 bits, not 32
+  int zero_rest;                           // zeros in rows of no sequence (else they stay as they are)
+  long long rows;
+  const void *offsets;
+  const int *first;                        // workspace, with more than 64 sequences: tiles before each
+  long long ldq, hq, ldk, hk, ldv, hv, ldo, ho;
+  const void *q, *k, *v;
+  float scale;
+  void *o; float *lse;                     // lse [Hq][rows]: forward an output (may be null), backward an input
+  // backward
+  long long lddo, hdo, lddq, hdq, lddk, hdk, lddv, hdv;
+  const void *dout;
+  void *dq, *dk, *dv;
+  float *inner;                            // workspace [Hq][rows]: do_i . o_i
+  float *most;                             // workspace: largest squared lengths of do_i and of v_j, by block
+  int nmost;
+};
+// Tiles of all sequences: what they are, or with offsets the most that they can be
+inline long long attention_tiles(const AttentionP &p) {
+  if (!p.offsets) return (long long)p.seqs * ((p.T + ATTENTION_ROWS - 1) / ATTENTION_ROWS);
+  return p.rows / ATTENTION_ROWS + p.seqs;
+}
+hipError_t launch_attention_tiles(const AttentionP &p, hipStream_t s);
+hipError_t launch_attention(const AttentionP &p, hipStream_t s);
+hipError_t launch_attention_backward(const AttentionP &p, hipStream_t s);
+
 }  // namespace absk
