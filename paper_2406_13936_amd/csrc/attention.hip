@@ -54,8 +54,6 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
   const bool in = row < w.len;
   const int kvh = head / (p.Hq / p.Hkv);
   const E *q = static_cast<const E *>(p.q) + w.start * p.ldq + head * p.hq;
-  const E *k = static_cast<const E *>(p.k) + w.start * p.ldk + kvh * p.hk;
-  const E *v = static_cast<const E *>(p.v) + w.start * p.ldv + kvh * p.hv;
   Frag8<TYPE> qf[2 * ND];
 #pragma unroll
   for (int i = 0; i < 2 * ND; ++i) qf[i] = row_frag<TYPE, VEC>(q, (long long)row * p.ldq, in, i, p.D);
@@ -65,78 +63,97 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
   float top = -__builtin_inff(), sum = 0.0f;
   const float c = p.scale * LOG2E;
   const int end = min(w.len, q0 + ATTENTION_ROWS), tiles = (end + BK - 1) / BK;
+  Rows<TYPE> rk(p.k, w.start * p.ldk + kvh * p.hk, p.ldk, w.len, p.D), rv(p.v, w.start * p.ldv + kvh * p.hv, p.ldv, w.len, p.D);
   KV tk, tv;
-  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-  tk.template load<VEC>(k, p.ldk, 0, w.len, p.D);
-  tv.template load<VEC>(v, p.ldv, 0, w.len, p.D);
-  __syncthreads();
-  tk.store(lds);
-  tv.store(lds + KV::ELEMS);
-  if (BK > q0 && tv.any()) odd[0] = 1;
-  __syncthreads();
-  for (int j = 0; j < tiles; ++j) {
-    const int k0 = j * BK, cur = j & 1;
+  auto load = [&] {
+    tk.template load<VEC>(rk);
+    tv.template load<VEC>(rv);
+    rk.skip(BK);
+    rv.skip(BK);
+  };
+  auto store = [&](int buf, int k0) {
+    E *to = lds + buf * 2 * KV::ELEMS;
+    tk.store(to);
+    tv.store(to + KV::ELEMS);
+    if (k0 + BK > q0 && tv.any()) odd[buf] = 1;        // (a tile that some wavefront masks; the mark stays: a false one costs time alone)
+  };
+  // MASKED: some wavefront of the block masks the tile
+  auto step = [&](int k0, int cur, auto masked_tile) {
+    constexpr bool MASKED = decltype(masked_tile)::value;
     const E *lk = lds + cur * 2 * KV::ELEMS, *lv = lk + KV::ELEMS;
-    const bool more = j + 1 < tiles;
-    if (more) {
-      tk.template load<VEC>(k, p.ldk, k0 + BK, w.len, p.D);
-      tv.template load<VEC>(v, p.ldv, k0 + BK, w.len, p.D);
+    if (MASKED && (k0 > mine + 31 || mine >= w.len)) return;
+    f32x16 s[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) s[b] = zeros16();
+#pragma unroll
+    for (int i = 0; i < 2 * ND; ++i)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) mma<TYPE>(s[b], KV::rows(lk, 32 * b, i), qf[i]);
+    if (MASKED) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (k0 + 32 * b + 8 * (r >> 2) + 4 * h + (r & 3) > row) s[b][r] = -__builtin_inff();
     }
-    if (k0 <= mine + 31 && mine < w.len) {
-      f32x16 s[NB];
+    float most = s[0][0];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) s[b] = zeros16();
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < 2 * ND; ++i)
+      for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][r]);
+    most = fmaxf(most, __shfl_xor(most, 32, 64)) * c;
+    // A row's reference follows its maximum only when that is 2^8 beyond it (whatever other rows' do): results are the same, what is summed
+    // stays below 2^8 times the number of keys
+    if (__any(most > top + 8.0f)) {
+      const float next = most > top + 8.0f ? most : top, by = __builtin_amdgcn_exp2f(top - (next == -__builtin_inff() ? 0.0f : next));
+      top = next;
+      sum *= by;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) mma<TYPE>(s[b], KV::rows(lk, 32 * b, i), qf[i]);
-      const bool masked = k0 + BK - 1 > mine;
-      if (masked) {
+      for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int r = 0; r < 16; ++r) o[d][r] *= by;
+    }
+    const float ref = top == -__builtin_inff() ? 0.0f : top;
+    Frag8<TYPE> x[NB][2];
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (k0 + 32 * b + 8 * (r >> 2) + 4 * h + (r & 3) > row) s[b][r] = -__builtin_inff();
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -ref));
+        sum += s[b][r];
       }
-      float most = s[0][0];
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][r]);
-      most = fmaxf(most, __shfl_xor(most, 32, 64)) * c;
-      // A row's reference follows its maximum only when that is 2^8 beyond it (whatever other rows' do): results are the same, what is summed
-      // stays below 2^8 times the number of keys
-      if (__any(most > top + 8.0f)) {
-        const float next = most > top + 8.0f ? most : top, by = __builtin_amdgcn_exp2f(top - (next == -__builtin_inff() ? 0.0f : next));
-        top = next;
-        sum *= by;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][r] *= by;
-      }
-      const float ref = top == -__builtin_inff() ? 0.0f : top;
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -ref));
-          sum += s[b][r];
-        }
-      const bool clean = masked && odd[cur];
+      x[b][0] = as_frag<TYPE>(s[b], 0);
+      x[b][1] = as_frag<TYPE>(s[b], 1);
+    }
+    if (MASKED && odd[cur]) {
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const Frag8<TYPE> x[2] = {as_frag<TYPE>(s[b], 0), as_frag<TYPE>(s[b], 1)};
-        add_cols<TYPE, BK, ND>(o, lv, 32 * b, x, clean);
-        if (clean) add_unusual<TYPE, BK, ND>(o, lv, 32 * b, [&](int r) { return k0 + 32 * b + r <= row; });
+        add_cols<true, TYPE, BK, ND>(o, lv, 32 * b, x[b]);
+        add_unusual<TYPE, BK, ND>(o, lv, 32 * b, [&](int r) { return k0 + 32 * b + r <= row; });
       }
+    } else {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) add_cols<false, TYPE, BK, ND>(o, lv, 32 * b, x[b]);
     }
-    if (more) {
-      E *next = lds + (cur ^ 1) * 2 * KV::ELEMS;
-      tk.store(next);
-      tv.store(next + KV::ELEMS);
-      if (k0 + 2 * BK > q0 && tv.any()) odd[cur ^ 1] = 1;      // (a tile that some wavefront masks; the mark stays: a false one costs time alone)
-    }
+  };
+  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+  load();
+  __syncthreads();
+  store(0, 0);
+  __syncthreads();
+  const int whole = q0 / BK;                           // tiles that no wavefront masks
+  int j = 0;
+  for (; j < whole; ++j) {
+    load();                                            // (there is a next tile: the diagonal's)
+    step(j * BK, j & 1, std::false_type{});
+    store(~j & 1, (j + 1) * BK);
+    __syncthreads();
+  }
+  for (; j < tiles; ++j) {
+    const bool more = j + 1 < tiles;
+    if (more) load();
+    step(j * BK, j & 1, std::true_type{});
+    if (more) store(~j & 1, (j + 1) * BK);
     __syncthreads();
   }
   sum += __shfl_xor(sum, 32, 64);
@@ -175,8 +192,8 @@ hipError_t launch_attention_tiles(const AttentionP &p, hipStream_t s) {
 hipError_t launch_attention(const AttentionP &p, hipStream_t s) {
   const hipError_t e = launch_attention_tiles(p, s);
   if (e != hipSuccess) return e;
-  const bool vec = rows_of_vectors(p.q, p.type, p.hq, p.ldq, p.D) && rows_of_vectors(p.k, p.type, p.hk, p.ldk, p.D) &&
-                   rows_of_vectors(p.v, p.type, p.hv, p.ldv, p.D) && rows_of_vectors(p.o, p.type, p.ho, p.ldo, p.D);
+  const bool vec = attention_vectors(p.q, p.type, p.hq, p.ldq, p.D) && attention_vectors(p.k, p.type, p.hk, p.ldk, p.D) &&
+                   attention_vectors(p.v, p.type, p.hv, p.ldv, p.D) && attention_vectors(p.o, p.type, p.ho, p.ldo, p.D);
   switch (p.type) {
     case TYPE_F32: return vec ? forward_width<TYPE_F32, true>(p, s) : forward_width<TYPE_F32, false>(p, s);
     case TYPE_BF16: return vec ? forward_width<TYPE_BF16, true>(p, s) : forward_width<TYPE_BF16, false>(p, s);

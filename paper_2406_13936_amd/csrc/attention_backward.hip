@@ -124,13 +124,22 @@ __global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) atte
 #pragma unroll
   for (int d = 0; d < ND; ++d) dk[d] = dv[d] = zeros16();
   const float c = p.scale * LOG2E;
-  const int first = k0 / BQ, each = (w.len + BQ - 1) / BQ - first, total = each * G;
+  // tiles of queries from the diagonal to the sequence's end, of one head after the other; of each head the first ones are masked
+  const int first = k0 / BQ, each = (w.len + BQ - 1) / BQ - first, total = each * G, diagonal = ATTENTION_ROWS / BQ;
   T tq, td;
   float lse = 0.0f, inner = 0.0f;
-  auto load = [&](int head, int j) {
-    const int r0 = j * BQ;
-    tq.template load<VEC>(static_cast<const E *>(p.q) + w.start * p.ldq + head * p.hq, p.ldq, r0, w.len, p.D);
-    td.template load<VEC>(static_cast<const E *>(p.dout) + w.start * p.lddo + head * p.hdo, p.lddo, r0, w.len, p.D);
+  int head = kvh * G, j = 0;                           // the next tile to load
+  Rows<TYPE> rq(p.q, 0, p.ldq, 0, p.D), rd(p.dout, 0, p.lddo, 0, p.D);
+  auto load = [&] {
+    const int r0 = (first + j) * BQ;
+    if (j == 0) {
+      rq = Rows<TYPE>(p.q, (w.start + r0) * p.ldq + head * p.hq, p.ldq, w.len - r0, p.D);
+      rd = Rows<TYPE>(p.dout, (w.start + r0) * p.lddo + head * p.hdo, p.lddo, w.len - r0, p.D);
+    }
+    tq.template load<VEC>(rq);
+    td.template load<VEC>(rd);
+    rq.skip(BQ);
+    rd.skip(BQ);
     if (threadIdx.x < BQ) {
       const int r = r0 + threadIdx.x;
       const long long at = head * p.rows + w.start + (r < w.len ? r : 0);
@@ -138,35 +147,27 @@ __global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) atte
       inner = r < w.len ? p.inner[at] : 0.0f;
     }
   };
-  auto store = [&](int buf, int j) {
+  auto store = [&](int buf) {
     tq.store(lds + buf * 2 * T::ELEMS);
     td.store(lds + buf * 2 * T::ELEMS + T::ELEMS);
     if (threadIdx.x < BQ) { stat[buf][0][threadIdx.x] = lse; stat[buf][1][threadIdx.x] = inner; }
-    if (j * BQ < k0 + ATTENTION_ROWS && (tq.any() || td.any())) odd[buf] = 1;      // (a tile that some wavefront masks)
+    if (j < diagonal && (tq.any() || td.any())) odd[buf] = 1;
+    if (++j == each) { j = 0; ++head; }
   };
-  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-  int head = kvh * G, j = first;
-  load(head, j);
-  __syncthreads();
-  store(0, j);
-  __syncthreads();
-  for (int it = 0; it < total; ++it) {
-    const int cur = it & 1, r0 = j * BQ;
+  // MASKED: some wavefront of the block masks the tile, or queries end in it
+  auto step = [&](int r0, int cur, auto masked_tile) {
+    constexpr bool MASKED = decltype(masked_tile)::value;
     const E *lq = lds + cur * 2 * T::ELEMS, *ld = lq + T::ELEMS;
-    if (++j == first + each) { j = first; ++head; }
-    const bool more = it + 1 < total;
-    if (more) load(head, j);
 #pragma unroll
     for (int b = 0; b < BQ / 32; ++b) {
       const int q0 = r0 + 32 * b;
-      if (q0 + 31 < mine || q0 >= w.len || mine >= w.len) continue;
+      if (MASKED && (q0 + 31 < mine || q0 >= w.len || mine >= w.len)) continue;
       f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
       for (int i = 0; i < 2 * ND; ++i) {
         mma<TYPE>(s, T::rows(lq, 32 * b, i), kf[i]);
         mma<TYPE>(dp, T::rows(ld, 32 * b, i), vf[i]);
       }
-      const bool masked = q0 < mine + 31;
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const float4 l4 = *reinterpret_cast<const float4 *>(&stat[cur][0][32 * b + 8 * r4 + 4 * h]);
@@ -175,22 +176,36 @@ __global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) atte
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * r4 + e;
-          float x = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[e])), y = x * ((dp[r] - dd[e]) * g);
-          if (masked && q0 + 8 * r4 + 4 * h + e < key) x = y = 0.0f;
+          float x = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[e])), y = TYPE == TYPE_F16 ? x * ((dp[r] - dd[e]) * g) : x * (dp[r] - dd[e]);
+          if (MASKED && q0 + 8 * r4 + 4 * h + e < key) x = y = 0.0f;
           s[r] = x;
           dp[r] = y;
         }
       }
-      const bool clean = masked && odd[cur];
       const Frag8<TYPE> x[2] = {as_frag<TYPE>(s, 0), as_frag<TYPE>(s, 1)}, y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
-      add_cols<TYPE, BQ, ND>(dv, ld, 32 * b, x, clean);
-      add_cols<TYPE, BQ, ND>(dk, lq, 32 * b, y, clean);
-      if (clean) {
+      if (MASKED && odd[cur]) {
+        add_cols<true, TYPE, BQ, ND>(dv, ld, 32 * b, x);
+        add_cols<true, TYPE, BQ, ND>(dk, lq, 32 * b, y);
         add_unusual<TYPE, BQ, ND>(dv, ld, 32 * b, [&](int r) { return q0 + r >= key; });
         add_unusual<TYPE, BQ, ND>(dk, lq, 32 * b, [&](int r) { return q0 + r >= key; });
+      } else {
+        add_cols<false, TYPE, BQ, ND>(dv, ld, 32 * b, x);
+        add_cols<false, TYPE, BQ, ND>(dk, lq, 32 * b, y);
       }
     }
-    if (more) store(cur ^ 1, j);
+  };
+  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+  load();
+  __syncthreads();
+  store(0);
+  __syncthreads();
+  for (int it = 0, at = 0; it < total; ++it) {
+    const bool more = it + 1 < total;
+    if (more) load();
+    if (at < diagonal || k0 + ATTENTION_ROWS > w.len) step((first + at) * BQ, it & 1, std::true_type{});
+    else step((first + at) * BQ, it & 1, std::false_type{});
+    if (++at == each) at = 0;
+    if (more) store(~it & 1);
     __syncthreads();
   }
   if (!in) return;
@@ -217,8 +232,6 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
   const int q0 = w.tile * ATTENTION_ROWS, mine = q0 + wave * 32, row = mine + (lane & 31);
   const bool in = row < w.len;
   const int kvh = head / (p.Hq / p.Hkv);
-  const E *k = static_cast<const E *>(p.k) + w.start * p.ldk + kvh * p.hk;
-  const E *v = static_cast<const E *>(p.v) + w.start * p.ldv + kvh * p.hv;
   const float f = ds_factor<TYPE>(p);
   Frag8<TYPE> qf[2 * ND], of[2 * ND];
 #pragma unroll
@@ -232,51 +245,66 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
 #pragma unroll
   for (int d = 0; d < ND; ++d) dq[d] = zeros16();
   const int end = min(w.len, q0 + ATTENTION_ROWS), tiles = (end + BK - 1) / BK;
+  Rows<TYPE> rk(p.k, w.start * p.ldk + kvh * p.hk, p.ldk, w.len, p.D), rv(p.v, w.start * p.ldv + kvh * p.hv, p.ldv, w.len, p.D);
   T tk, tv;
-  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-  tk.template load<VEC>(k, p.ldk, 0, w.len, p.D);
-  tv.template load<VEC>(v, p.ldv, 0, w.len, p.D);
-  __syncthreads();
-  tk.store(lds);
-  tv.store(lds + T::ELEMS);
-  if (BK > q0 && tk.any()) odd[0] = 1;
-  __syncthreads();
-  for (int j = 0; j < tiles; ++j) {
-    const int k0 = j * BK, cur = j & 1;
+  auto load = [&] {
+    tk.template load<VEC>(rk);
+    tv.template load<VEC>(rv);
+    rk.skip(BK);
+    rv.skip(BK);
+  };
+  auto store = [&](int buf, int k0) {
+    E *to = lds + buf * 2 * T::ELEMS;
+    tk.store(to);
+    tv.store(to + T::ELEMS);
+    if (k0 + BK > q0 && tk.any()) odd[buf] = 1;
+  };
+  auto step = [&](int k0, int cur, auto masked_tile) {
+    constexpr bool MASKED = decltype(masked_tile)::value;
     const E *lk = lds + cur * 2 * T::ELEMS, *lv = lk + T::ELEMS;
-    const bool more = j + 1 < tiles;
-    if (more) {
-      tk.template load<VEC>(k, p.ldk, k0 + BK, w.len, p.D);
-      tv.template load<VEC>(v, p.ldv, k0 + BK, w.len, p.D);
-    }
 #pragma unroll
     for (int b = 0; b < BK / 32; ++b) {
       const int kb = k0 + 32 * b;
-      if (kb > mine + 31 || kb >= w.len || mine >= w.len) continue;
+      if (MASKED && (kb > mine + 31 || mine >= w.len)) continue;
       f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
       for (int i = 0; i < 2 * ND; ++i) {
         mma<TYPE>(s, T::rows(lk, 32 * b, i), qf[i]);
         mma<TYPE>(dp, T::rows(lv, 32 * b, i), of[i]);
       }
-      const bool masked = kb + 31 > mine;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float x = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse));
-        dp[r] = x * ((dp[r] - inner) * f);
-        if (masked && kb + 8 * (r >> 2) + 4 * h + (r & 3) > row) dp[r] = 0.0f;
+        dp[r] = TYPE == TYPE_F16 ? x * ((dp[r] - inner) * f) : x * (dp[r] - inner);
+        if (MASKED && kb + 8 * (r >> 2) + 4 * h + (r & 3) > row) dp[r] = 0.0f;
       }
-      const bool clean = masked && odd[cur];
       const Frag8<TYPE> y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
-      add_cols<TYPE, BK, ND>(dq, lk, 32 * b, y, clean);
-      if (clean) add_unusual<TYPE, BK, ND>(dq, lk, 32 * b, [&](int r) { return kb + r <= row; });
+      if (MASKED && odd[cur]) {
+        add_cols<true, TYPE, BK, ND>(dq, lk, 32 * b, y);
+        add_unusual<TYPE, BK, ND>(dq, lk, 32 * b, [&](int r) { return kb + r <= row; });
+      } else {
+        add_cols<false, TYPE, BK, ND>(dq, lk, 32 * b, y);
+      }
     }
-    if (more) {
-      E *next = lds + (cur ^ 1) * 2 * T::ELEMS;
-      tk.store(next);
-      tv.store(next + T::ELEMS);
-      if (k0 + 2 * BK > q0 && tk.any()) odd[cur ^ 1] = 1;
-    }
+  };
+  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+  load();
+  __syncthreads();
+  store(0, 0);
+  __syncthreads();
+  const int whole = q0 / BK;                           // tiles that no wavefront masks
+  int j = 0;
+  for (; j < whole; ++j) {
+    load();
+    step(j * BK, j & 1, std::false_type{});
+    store(~j & 1, (j + 1) * BK);
+    __syncthreads();
+  }
+  for (; j < tiles; ++j) {
+    const bool more = j + 1 < tiles;
+    if (more) load();
+    step(j * BK, j & 1, std::true_type{});
+    if (more) store(~j & 1, (j + 1) * BK);
     __syncthreads();
   }
   if (!in) return;
@@ -310,7 +338,7 @@ template <int TYPE, bool VEC> hipError_t backward_width(const AttentionP &p, hip
 hipError_t launch_attention_backward(const AttentionP &p, hipStream_t s) {
   const hipError_t e = launch_attention_tiles(p, s);
   if (e != hipSuccess) return e;
-  const auto rows = [&](const void *t, long long h, long long ld) { return rows_of_vectors(t, p.type, h, ld, p.D); };
+  const auto rows = [&](const void *t, long long h, long long ld) { return attention_vectors(t, p.type, h, ld, p.D); };
   const bool vec = rows(p.q, p.hq, p.ldq) && rows(p.k, p.hk, p.ldk) && rows(p.v, p.hv, p.ldv) && rows(p.o, p.ho, p.ldo) && rows(p.dout, p.hdo, p.lddo) &&
                    rows(p.dq, p.hdq, p.lddq) && rows(p.dk, p.hdk, p.lddk) && rows(p.dv, p.hdv, p.lddv);
   switch (p.type) {

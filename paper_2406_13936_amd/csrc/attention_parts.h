@@ -85,6 +85,25 @@ template <int TYPE> __device__ __forceinline__ Frag8<TYPE> usual(Frag8<TYPE> f) 
   return f;
 }
 
+// ---- rows of a sequence ------------------------------------------------------------------------------------------------
+
+// Where the next tile of a head begins: `left` rows of D values, `ld` apart (not above ROWS_LD)
+constexpr long long ROWS_LD = 1 << 22;                 // a tile's offsets are below 2^31 bytes
+template <int TYPE> struct Rows {
+  typedef typename ElemOf<TYPE>::type E;
+  const E *at;
+  long long ld;
+  int left, D;
+  __device__ __forceinline__ Rows(const void *base, long long first, long long ld_, int left_, int D_)
+      : at(static_cast<const E *>(base) + first), ld(ld_), left(left_), D(D_) {}
+  __device__ __forceinline__ void skip(int rows) { at += rows * ld; left -= rows; }
+  // of `rows` rows at most: the machine gives zeros beyond them (ld >= D, so no later row begins before the last one's end)
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(int rows) const {
+    const int n = min(left, rows);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<E *>(at), 0, n > 0 ? (int)(((n - 1) * (int)ld + D) * sizeof(E)) : 0, 0x00020000);
+  }
+};
+
 // ---- operand tiles in LDS ----------------------------------------------------------------------------------------------
 
 // ROWS rows of 32 ND values.  16-bit: rows of 4, 8 or 16 chunks of 16 bytes, whose places are exchanged by an XOR of the row so that neither reads
@@ -105,25 +124,23 @@ template <int TYPE, int ROWS, int ND> struct Tile {
     return TYPE == TYPE_F32 ? row * LD + chunk * 4 : row * LD + (chunk ^ swizzle(row)) * 8;
   }
 
-  // A thread's part of rows row0 .. of a sequence of `len` rows whose first value is at `base`: zeros beyond the sequence and beyond D.
-  // (Every thread loads, from a place of the tensor where it has none.)
+  // A thread's part of the tile's rows, from the next row of a sequence (Rows): zeros beyond the sequence and beyond D
   uint4 q[NV];
-  template <bool VEC> __device__ __forceinline__ void load(const void *base, long long ld, int row0, int len, int D) {
+  template <bool VEC> __device__ __forceinline__ void load(const Rows<TYPE> &m) {
+    const __amdgpu_buffer_rsrc_t rsrc = m.rsrc(ROWS);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = threadIdx.x + i * 256, row = c / (32 * ND / PER), col = c % (32 * ND / PER) * PER;
-      const int r = row0 + row;
+      const bool there = col < m.D && (VECS % 256 == 0 || row < ROWS);
       if constexpr (VEC) {
-        const bool in = r < len && col < D && (VECS % 256 == 0 || row < ROWS);
-        const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const E *>(base) + (in ? r * ld + col : 0));
-        q[i] = make_uint4(in ? w.x : 0u, in ? w.y : 0u, in ? w.z : 0u, in ? w.w : 0u);
+        q[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, there ? (uint32_t)(row * m.ld + col) * sizeof(E) : OOB, 0, 0));
       } else {
         uint32_t w[4] = {0u, 0u, 0u, 0u};
-        if (r < len && (VECS % 256 == 0 || row < ROWS)) {
-          const E *p = static_cast<const E *>(base) + r * ld + col;
+        if (there && row < m.left) {
+          const E *p = m.at + row * m.ld + col;
 #pragma unroll
           for (int e = 0; e < PER; ++e)
-            if (col + e < D) {
+            if (col + e < m.D) {
               if constexpr (TYPE == TYPE_F32) w[e] = __float_as_uint(p[e]);
               else w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
             }
@@ -219,18 +236,18 @@ __device__ __forceinline__ Frag8<TYPE> row_frag(const void *base, long long at, 
 }
 
 // acc[d] += sum over the tile's rows row0 .. of (row, place) X^T Y: the two fragments of x are rows of the reduction
-template <int TYPE, int ROWS, int ND>
-__device__ __forceinline__ void add_cols(f32x16 (&acc)[ND], const typename ElemOf<TYPE>::type *lds, int row0, const Frag8<TYPE> (&x)[2], bool clean) {
+template <bool CLEAN, int TYPE, int ROWS, int ND>
+__device__ __forceinline__ void add_cols(f32x16 (&acc)[ND], const typename ElemOf<TYPE>::type *lds, int row0, const Frag8<TYPE> (&x)[2]) {
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
       Frag8<TYPE> f = Tile<TYPE, ROWS, ND>::cols(lds, row0 + 16 * b, d);
-      if (clean) f = usual<TYPE>(f);
+      if (CLEAN) f = usual<TYPE>(f);
       mma<TYPE>(acc[d], f, x[b]);
     }
 }
-// What add_cols left out with `clean`: infinities and NaN of the tile's rows row0 .. row0 + 31, in the columns of acc (the lane's own) that the mask
+// What add_cols left out with CLEAN: infinities and NaN of the tile's rows row0 .. row0 + 31, in the columns of acc (the lane's own) that the mask
 // leaves to them.  They count as they are: weights are positive or make them NaN.
 template <int TYPE, int ROWS, int ND, class F>
 __device__ __forceinline__ void add_unusual(f32x16 (&acc)[ND], const typename ElemOf<TYPE>::type *lds, int row0, F &&sees) {
@@ -361,6 +378,9 @@ __device__ __forceinline__ void zero_rest(const AttentionP &p, void *out, int ty
 constexpr int REST_BLOCKS = 64;
 
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.69314718055994531f;
+
+// rows that 16-byte loads may take
+inline bool attention_vectors(const void *t, int type, long long head, long long ld, int D) { return ld <= ROWS_LD && rows_of_vectors(t, type, head, ld, D); }
 
 }  // namespace
 }  // namespace absk
