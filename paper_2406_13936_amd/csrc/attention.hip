@@ -40,9 +40,9 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
   constexpr int BK = TYPE == TYPE_F32 ? 32 : 64, NB = BK / 32;
   typedef Tile<TYPE, BK, ND> KV;
   typedef typename KV::E E;
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-  __shared__ int odd[2];                               // values of a masked tile hold infinities or NaN
-  E *const lds = reinterpret_cast<E *>(lds_raw);       // [2][keys, values]
+  constexpr bool DIRECT = VEC && KV::DIRECT;
+  // two buffers, by name, so that the compiler can tell what is read from what is on its way
+  __shared__ __attribute__((aligned(16))) E keys_a[KV::ELEMS], values_a[KV::ELEMS], keys_b[KV::ELEMS], values_b[KV::ELEMS];
   if ((int)blockIdx.x >= blocks) return zero_rest(p, p.o, TYPE, p.Hq, p.ldo, p.ho, p.lse, blockIdx.x - blocks, REST_BLOCKS);
   int head, t;
   head_and_tile(blockIdx.x, p.Hq, head, t);
@@ -65,22 +65,31 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
   const int end = min(w.len, q0 + ATTENTION_ROWS), tiles = (end + BK - 1) / BK;
   Rows<TYPE> rk(p.k, w.start * p.ldk + kvh * p.hk, p.ldk, w.len, p.D), rv(p.v, w.start * p.ldv + kvh * p.hv, p.ldv, w.len, p.D);
   KV tk, tv;
-  auto load = [&] {
-    tk.template load<VEC>(rk);
-    tv.template load<VEC>(rv);
+  if constexpr (DIRECT) {
+    tk.place_loads(rk);
+    tv.place_loads(rv);
+  }
+  auto fetch = [&](auto buffer) {                      // the next tile
+    if constexpr (DIRECT) {
+      tk.fetch(decltype(buffer)::value ? keys_b : keys_a, rk);
+      tv.fetch(decltype(buffer)::value ? values_b : values_a, rv);
+    } else {
+      tk.template load<VEC>(rk);
+      tv.template load<VEC>(rv);
+    }
     rk.skip(BK);
     rv.skip(BK);
   };
-  auto store = [&](int buf, int k0) {
-    E *to = lds + buf * 2 * KV::ELEMS;
-    tk.store(to);
-    tv.store(to + KV::ELEMS);
-    if (k0 + BK > q0 && tv.any()) odd[buf] = 1;        // (a tile that some wavefront masks; the mark stays: a false one costs time alone)
+  auto settle = [&](auto buffer) {
+    if constexpr (!DIRECT) {
+      tk.store(decltype(buffer)::value ? keys_b : keys_a);
+      tv.store(decltype(buffer)::value ? values_b : values_a);
+    }
   };
   // MASKED: some wavefront of the block masks the tile
-  auto step = [&](int k0, int cur, auto masked_tile) {
+  auto step = [&](int k0, auto buffer, auto masked_tile, bool odd) {
     constexpr bool MASKED = decltype(masked_tile)::value;
-    const E *lk = lds + cur * 2 * KV::ELEMS, *lv = lk + KV::ELEMS;
+    const E *lk = decltype(buffer)::value ? keys_b : keys_a, *lv = decltype(buffer)::value ? values_b : values_a;
     if (MASKED && (k0 > mine + 31 || mine >= w.len)) return;
     f32x16 s[NB];
 #pragma unroll
@@ -125,7 +134,7 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
       x[b][0] = as_frag<TYPE>(s[b], 0);
       x[b][1] = as_frag<TYPE>(s[b], 1);
     }
-    if (MASKED && odd[cur]) {
+    if (MASKED && odd) {
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         add_cols<true, TYPE, BK, ND>(o, lv, 32 * b, x[b]);
@@ -136,25 +145,31 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
       for (int b = 0; b < NB; ++b) add_cols<false, TYPE, BK, ND>(o, lv, 32 * b, x[b]);
     }
   };
-  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-  load();
-  __syncthreads();
-  store(0, 0);
-  __syncthreads();
   const int whole = q0 / BK;                           // tiles that no wavefront masks
   int j = 0;
-  for (; j < whole; ++j) {
-    load();                                            // (there is a next tile: the diagonal's)
-    step(j * BK, j & 1, std::false_type{});
-    store(~j & 1, (j + 1) * BK);
-    __syncthreads();
+  auto turn = [&](auto buffer, auto masked_tile) {
+    constexpr bool MASKED = decltype(masked_tile)::value;
+    std::integral_constant<bool, !decltype(buffer)::value> other;
+    const bool more = !MASKED || j + 1 < tiles, odd = MASKED && __syncthreads_or(KV::any(decltype(buffer)::value ? values_b : values_a));
+    if (more) fetch(other);
+    step(j * BK, buffer, masked_tile, odd);
+    if (more) settle(other);
+    arrived<DIRECT>();
+    ++j;
+  };
+  const std::false_type a, below;
+  const std::true_type b, diagonal;
+  fetch(a);
+  settle(a);
+  arrived<DIRECT>();
+  while (j + 2 <= whole) {
+    turn(a, below);
+    turn(b, below);
   }
-  for (; j < tiles; ++j) {
-    const bool more = j + 1 < tiles;
-    if (more) load();
-    step(j * BK, j & 1, std::true_type{});
-    if (more) store(~j & 1, (j + 1) * BK);
-    __syncthreads();
+  if (j < whole) turn(a, below);
+  while (j < tiles) {
+    if (j & 1) turn(b, diagonal);
+    else turn(a, diagonal);
   }
   sum += __shfl_xor(sum, 32, 64);
   if (!in) return;
@@ -163,13 +178,8 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
 }
 
 template <int TYPE, int ND, bool VEC> hipError_t forward_launch(const AttentionP &p, hipStream_t s) {
-  constexpr int BK = TYPE == TYPE_F32 ? 32 : 64;
-  constexpr size_t bytes = 4 * Tile<TYPE, BK, ND>::ELEMS * sizeof(typename ElemOf<TYPE>::type);
-  static std::atomic<uint64_t> done{0};
-  const hipError_t e = allow_lds(reinterpret_cast<const void *>(&attention_kernel<TYPE, ND, VEC>), bytes, done);
-  if (e != hipSuccess) return e;
   const long long blocks = attention_tiles(p) * p.Hq, rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
-  hipLaunchKernelGGL((attention_kernel<TYPE, ND, VEC>), dim3((unsigned)(blocks + rest)), dim3(256), bytes, s, p, (int)blocks);
+  hipLaunchKernelGGL((attention_kernel<TYPE, ND, VEC>), dim3((unsigned)(blocks + rest)), dim3(256), 0, s, p, (int)blocks);
   return hipGetLastError();
 }
 template <int TYPE, bool VEC> hipError_t forward_width(const AttentionP &p, hipStream_t s) {

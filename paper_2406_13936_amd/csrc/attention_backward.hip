@@ -92,16 +92,19 @@ template <int TYPE> __device__ __forceinline__ float ds_factor(const AttentionP 
   return ldexpf(1.0f, max(-100, min(100, 14 - e)));
 }
 
+// Queries of a tile of the pass over keys
+constexpr int keys_tile(int type, int nd) { return type == TYPE_F32 || nd >= 3 ? 32 : 64; }
+
 // dk and dv of 128 keys
 template <int TYPE, int ND, bool VEC>
 __global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) attention_keys_kernel(const AttentionP p, const int blocks) {
-  constexpr int BQ = TYPE == TYPE_F32 || ND >= 3 ? 32 : 64;
+  constexpr int BQ = keys_tile(TYPE, ND);
   typedef Tile<TYPE, BQ, ND> T;
   typedef typename T::E E;
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-  __shared__ __attribute__((aligned(16))) float stat[2][2][BQ];      // lse (to base 2) and D of a tile's queries
-  __shared__ int odd[2];
-  E *const lds = reinterpret_cast<E *>(lds_raw);       // [2][queries, do]
+  constexpr bool DIRECT = VEC && T::DIRECT;
+  // two buffers, by name, so that the compiler can tell what is read from what is on its way
+  __shared__ __attribute__((aligned(16))) E queries_a[T::ELEMS], signals_a[T::ELEMS], queries_b[T::ELEMS], signals_b[T::ELEMS];
+  __shared__ __attribute__((aligned(16))) float stat_a[2][BQ], stat_b[2][BQ];      // lse (to base 2) and D of a tile's queries
   if ((int)blockIdx.x >= blocks) {
     zero_rest(p, p.dk, TYPE, p.Hkv, p.lddk, p.hdk, nullptr, blockIdx.x - blocks, REST_BLOCKS);
     return zero_rest(p, p.dv, TYPE, p.Hkv, p.lddv, p.hdv, nullptr, blockIdx.x - blocks, REST_BLOCKS);
@@ -130,34 +133,42 @@ __global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) atte
   float lse = 0.0f, inner = 0.0f;
   int head = kvh * G, j = 0;                           // the next tile to load
   Rows<TYPE> rq(p.q, 0, p.ldq, 0, p.D), rd(p.dout, 0, p.lddo, 0, p.D);
-  auto load = [&] {
+  auto fetch = [&](auto buffer) {
     const int r0 = (first + j) * BQ;
     if (j == 0) {
       rq = Rows<TYPE>(p.q, (w.start + r0) * p.ldq + head * p.hq, p.ldq, w.len - r0, p.D);
       rd = Rows<TYPE>(p.dout, (w.start + r0) * p.lddo + head * p.hdo, p.lddo, w.len - r0, p.D);
     }
-    tq.template load<VEC>(rq);
-    td.template load<VEC>(rd);
-    rq.skip(BQ);
-    rd.skip(BQ);
     if (threadIdx.x < BQ) {
       const int r = r0 + threadIdx.x;
       const long long at = head * p.rows + w.start + (r < w.len ? r : 0);
       lse = r < w.len ? p.lse[at] * LOG2E - P_SHIFT<TYPE> : __builtin_inff();
       inner = r < w.len ? p.inner[at] : 0.0f;
     }
-  };
-  auto store = [&](int buf) {
-    tq.store(lds + buf * 2 * T::ELEMS);
-    td.store(lds + buf * 2 * T::ELEMS + T::ELEMS);
-    if (threadIdx.x < BQ) { stat[buf][0][threadIdx.x] = lse; stat[buf][1][threadIdx.x] = inner; }
-    if (j < diagonal && (tq.any() || td.any())) odd[buf] = 1;
+    if constexpr (DIRECT) {
+      tq.fetch(decltype(buffer)::value ? queries_b : queries_a, rq);
+      td.fetch(decltype(buffer)::value ? signals_b : signals_a, rd);
+    } else {
+      tq.template load<VEC>(rq);
+      td.template load<VEC>(rd);
+    }
+    rq.skip(BQ);
+    rd.skip(BQ);
     if (++j == each) { j = 0; ++head; }
   };
+  auto settle = [&](auto buffer) {
+    constexpr bool B = decltype(buffer)::value;
+    if constexpr (!DIRECT) {
+      tq.store(B ? queries_b : queries_a);
+      td.store(B ? signals_b : signals_a);
+    }
+    if (threadIdx.x < BQ) { (B ? stat_b : stat_a)[0][threadIdx.x] = lse; (B ? stat_b : stat_a)[1][threadIdx.x] = inner; }
+  };
   // MASKED: some wavefront of the block masks the tile, or queries end in it
-  auto step = [&](int r0, int cur, auto masked_tile) {
-    constexpr bool MASKED = decltype(masked_tile)::value;
-    const E *lq = lds + cur * 2 * T::ELEMS, *ld = lq + T::ELEMS;
+  auto step = [&](int r0, auto buffer, auto masked_tile, bool odd) {
+    constexpr bool MASKED = decltype(masked_tile)::value, B = decltype(buffer)::value;
+    const E *lq = B ? queries_b : queries_a, *ld = B ? signals_b : signals_a;
+    const float(*stat)[BQ] = B ? stat_b : stat_a;
 #pragma unroll
     for (int b = 0; b < BQ / 32; ++b) {
       const int q0 = r0 + 32 * b;
@@ -170,8 +181,8 @@ __global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) atte
       }
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
-        const float4 l4 = *reinterpret_cast<const float4 *>(&stat[cur][0][32 * b + 8 * r4 + 4 * h]);
-        const float4 d4 = *reinterpret_cast<const float4 *>(&stat[cur][1][32 * b + 8 * r4 + 4 * h]);
+        const float4 l4 = *reinterpret_cast<const float4 *>(&stat[0][32 * b + 8 * r4 + 4 * h]);
+        const float4 d4 = *reinterpret_cast<const float4 *>(&stat[1][32 * b + 8 * r4 + 4 * h]);
         const float l[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -183,7 +194,7 @@ __global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) atte
         }
       }
       const Frag8<TYPE> x[2] = {as_frag<TYPE>(s, 0), as_frag<TYPE>(s, 1)}, y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
-      if (MASKED && odd[cur]) {
+      if (MASKED && odd) {
         add_cols<true, TYPE, BQ, ND>(dv, ld, 32 * b, x);
         add_cols<true, TYPE, BQ, ND>(dk, lq, 32 * b, y);
         add_unusual<TYPE, BQ, ND>(dv, ld, 32 * b, [&](int r) { return q0 + r >= key; });
@@ -194,19 +205,37 @@ __global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) atte
       }
     }
   };
-  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-  load();
-  __syncthreads();
-  store(0);
-  __syncthreads();
-  for (int it = 0, at = 0; it < total; ++it) {
-    const bool more = it + 1 < total;
-    if (more) load();
-    if (at < diagonal || k0 + ATTENTION_ROWS > w.len) step((first + at) * BQ, it & 1, std::true_type{});
-    else step((first + at) * BQ, it & 1, std::false_type{});
+  if constexpr (DIRECT) {
+    rq.ld = p.ldq;
+    tq.place_loads(rq);
+    td.place_loads(rd);
+  }
+  const std::false_type a, plain;
+  const std::true_type b, masked;
+  fetch(a);
+  settle(a);
+  arrived<DIRECT>();
+  int it = 0, at = 0;
+  auto turn = [&](auto buffer, auto masked_tile) {
+    constexpr bool MASKED = decltype(masked_tile)::value, B = decltype(buffer)::value;
+    std::integral_constant<bool, !B> other;
+    const bool more = it + 1 < total, odd = MASKED && at < diagonal && __syncthreads_or(T::any(B ? queries_b : queries_a) || T::any(B ? signals_b : signals_a));
+    if (more) fetch(other);
+    step((first + at) * BQ, buffer, masked_tile, odd);
+    if (more) settle(other);
+    arrived<DIRECT>();
     if (++at == each) at = 0;
-    if (more) store(~it & 1);
-    __syncthreads();
+    ++it;
+  };
+  const bool ends = k0 + ATTENTION_ROWS > w.len;       // (some wavefronts may have no keys)
+  while (it < total) {
+    if (at < diagonal || ends) {
+      if (it & 1) turn(b, masked);
+      else turn(a, masked);
+    } else {
+      if (it & 1) turn(b, plain);
+      else turn(a, plain);
+    }
   }
   if (!in) return;
   store_row<TYPE, ND, VEC>(p.dk, (w.start + key) * p.lddk + kvh * p.hdk, dk, p.scale / f, p.D);
@@ -219,9 +248,8 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
   constexpr int BK = TYPE == TYPE_F32 ? 32 : 64;
   typedef Tile<TYPE, BK, ND> T;
   typedef typename T::E E;
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-  __shared__ int odd[2];
-  E *const lds = reinterpret_cast<E *>(lds_raw);       // [2][keys, values]
+  constexpr bool DIRECT = VEC && T::DIRECT;
+  __shared__ __attribute__((aligned(16))) E keys_a[T::ELEMS], values_a[T::ELEMS], keys_b[T::ELEMS], values_b[T::ELEMS];
   if ((int)blockIdx.x >= blocks) return zero_rest(p, p.dq, TYPE, p.Hq, p.lddq, p.hdq, nullptr, blockIdx.x - blocks, REST_BLOCKS);
   int head, t;
   head_and_tile(blockIdx.x, p.Hq, head, t);
@@ -247,21 +275,30 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
   const int end = min(w.len, q0 + ATTENTION_ROWS), tiles = (end + BK - 1) / BK;
   Rows<TYPE> rk(p.k, w.start * p.ldk + kvh * p.hk, p.ldk, w.len, p.D), rv(p.v, w.start * p.ldv + kvh * p.hv, p.ldv, w.len, p.D);
   T tk, tv;
-  auto load = [&] {
-    tk.template load<VEC>(rk);
-    tv.template load<VEC>(rv);
+  if constexpr (DIRECT) {
+    tk.place_loads(rk);
+    tv.place_loads(rv);
+  }
+  auto fetch = [&](auto buffer) {                      // the next tile
+    if constexpr (DIRECT) {
+      tk.fetch(decltype(buffer)::value ? keys_b : keys_a, rk);
+      tv.fetch(decltype(buffer)::value ? values_b : values_a, rv);
+    } else {
+      tk.template load<VEC>(rk);
+      tv.template load<VEC>(rv);
+    }
     rk.skip(BK);
     rv.skip(BK);
   };
-  auto store = [&](int buf, int k0) {
-    E *to = lds + buf * 2 * T::ELEMS;
-    tk.store(to);
-    tv.store(to + T::ELEMS);
-    if (k0 + BK > q0 && tk.any()) odd[buf] = 1;
+  auto settle = [&](auto buffer) {
+    if constexpr (!DIRECT) {
+      tk.store(decltype(buffer)::value ? keys_b : keys_a);
+      tv.store(decltype(buffer)::value ? values_b : values_a);
+    }
   };
-  auto step = [&](int k0, int cur, auto masked_tile) {
+  auto step = [&](int k0, auto buffer, auto masked_tile, bool odd) {
     constexpr bool MASKED = decltype(masked_tile)::value;
-    const E *lk = lds + cur * 2 * T::ELEMS, *lv = lk + T::ELEMS;
+    const E *lk = decltype(buffer)::value ? keys_b : keys_a, *lv = decltype(buffer)::value ? values_b : values_a;
 #pragma unroll
     for (int b = 0; b < BK / 32; ++b) {
       const int kb = k0 + 32 * b;
@@ -279,7 +316,7 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
         if (MASKED && kb + 8 * (r >> 2) + 4 * h + (r & 3) > row) dp[r] = 0.0f;
       }
       const Frag8<TYPE> y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
-      if (MASKED && odd[cur]) {
+      if (MASKED && odd) {
         add_cols<true, TYPE, BK, ND>(dq, lk, 32 * b, y);
         add_unusual<TYPE, BK, ND>(dq, lk, 32 * b, [&](int r) { return kb + r <= row; });
       } else {
@@ -287,41 +324,41 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
       }
     }
   };
-  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-  load();
-  __syncthreads();
-  store(0, 0);
-  __syncthreads();
   const int whole = q0 / BK;                           // tiles that no wavefront masks
   int j = 0;
-  for (; j < whole; ++j) {
-    load();
-    step(j * BK, j & 1, std::false_type{});
-    store(~j & 1, (j + 1) * BK);
-    __syncthreads();
+  auto turn = [&](auto buffer, auto masked_tile) {
+    constexpr bool MASKED = decltype(masked_tile)::value;
+    std::integral_constant<bool, !decltype(buffer)::value> other;
+    const bool more = !MASKED || j + 1 < tiles, odd = MASKED && __syncthreads_or(T::any(decltype(buffer)::value ? keys_b : keys_a));
+    if (more) fetch(other);
+    step(j * BK, buffer, masked_tile, odd);
+    if (more) settle(other);
+    arrived<DIRECT>();
+    ++j;
+  };
+  const std::false_type a, below;
+  const std::true_type b, diagonal;
+  fetch(a);
+  settle(a);
+  arrived<DIRECT>();
+  while (j + 2 <= whole) {
+    turn(a, below);
+    turn(b, below);
   }
-  for (; j < tiles; ++j) {
-    const bool more = j + 1 < tiles;
-    if (more) load();
-    step(j * BK, j & 1, std::true_type{});
-    if (more) store(~j & 1, (j + 1) * BK);
-    __syncthreads();
+  if (j < whole) turn(a, below);
+  while (j < tiles) {
+    if (j & 1) turn(b, diagonal);
+    else turn(a, diagonal);
   }
   if (!in) return;
   store_row<TYPE, ND, VEC>(p.dq, (w.start + row) * p.lddq + head * p.hdq, dq, p.scale / f, p.D);
 }
 
 template <int TYPE, int ND, bool VEC> hipError_t backward_launch(const AttentionP &p, hipStream_t s) {
-  constexpr int BQ = TYPE == TYPE_F32 || ND >= 3 ? 32 : 64, BK = TYPE == TYPE_F32 ? 32 : 64;
-  constexpr size_t e = sizeof(typename ElemOf<TYPE>::type), keys = 4 * Tile<TYPE, BQ, ND>::ELEMS * e, queries = 4 * Tile<TYPE, BK, ND>::ELEMS * e;
-  static std::atomic<uint64_t> done_keys{0}, done_queries{0};
-  hipError_t err = allow_lds(reinterpret_cast<const void *>(&attention_keys_kernel<TYPE, ND, VEC>), keys, done_keys);
-  if (err == hipSuccess) err = allow_lds(reinterpret_cast<const void *>(&attention_queries_kernel<TYPE, ND, VEC>), queries, done_queries);
-  if (err != hipSuccess) return err;
   const long long tiles = attention_tiles(p), rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
   hipLaunchKernelGGL((attention_inner_kernel<TYPE, VEC>), dim3(p.nmost), dim3(256), 0, s, p);
-  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hkv + rest)), dim3(256), keys, s, p, (int)(tiles * p.Hkv));
-  hipLaunchKernelGGL((attention_queries_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hq + rest)), dim3(256), queries, s, p, (int)(tiles * p.Hq));
+  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hkv + rest)), dim3(256), 0, s, p, (int)(tiles * p.Hkv));
+  hipLaunchKernelGGL((attention_queries_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hq + rest)), dim3(256), 0, s, p, (int)(tiles * p.Hq));
   return hipGetLastError();
 }
 template <int TYPE, bool VEC> hipError_t backward_width(const AttentionP &p, hipStream_t s) {

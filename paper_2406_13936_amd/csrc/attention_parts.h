@@ -56,26 +56,22 @@ __device__ __forceinline__ f32x16 zeros16() {
   return z;
 }
 // an infinity or NaN?
-template <int TYPE> __device__ __forceinline__ bool unusual(float v) { return !(fabsf(v) < __builtin_inff()); }
+__device__ __forceinline__ bool unusual(float v) { return !(fabsf(v) < __builtin_inff()); }
 template <int TYPE> __device__ __forceinline__ uint32_t unusual_half(uint32_t w) {      // of a word's low 16 bits
   constexpr uint32_t E = TYPE == TYPE_BF16 ? 0x7f80u : 0x7c00u;
   return (w & E) == E;
 }
-template <int TYPE> __device__ __forceinline__ bool any_unusual(const uint4 q) {
-  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-  bool any = false;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if constexpr (TYPE == TYPE_F32) any |= unusual<TYPE>(__uint_as_float(w[e]));
-    else any |= unusual_half<TYPE>(w[e]) || unusual_half<TYPE>(w[e] >> 16);
-  }
-  return any;
+// the sign bits are set where a value's exponent is all ones (one more carries into the sign's place)
+template <int TYPE> __device__ __forceinline__ uint32_t unusual_signs(const uint4 q) {
+  constexpr uint32_t E = TYPE == TYPE_F32 ? 0x7f800000u : TYPE == TYPE_BF16 ? 0x7f807f80u : 0x7c007c00u;
+  constexpr uint32_t ONE = TYPE == TYPE_F32 ? 0x00800000u : TYPE == TYPE_BF16 ? 0x00800080u : 0x04000400u;
+  return (((q.x & E) + ONE) | ((q.y & E) + ONE)) | (((q.z & E) + ONE) | ((q.w & E) + ONE));
 }
 // zeros in the place of infinities and NaN
 template <int TYPE> __device__ __forceinline__ Frag8<TYPE> usual(Frag8<TYPE> f) {
   if constexpr (TYPE == TYPE_F32) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.v[e] = unusual<TYPE>(f.v[e]) ? 0.0f : f.v[e];
+    for (int e = 0; e < 8; ++e) f.v[e] = unusual(f.v[e]) ? 0.0f : f.v[e];
   } else {
     uint32_t w[4] = {f.q.x, f.q.y, f.q.z, f.q.w};
 #pragma unroll
@@ -97,12 +93,22 @@ template <int TYPE> struct Rows {
   __device__ __forceinline__ Rows(const void *base, long long first, long long ld_, int left_, int D_)
       : at(static_cast<const E *>(base) + first), ld(ld_), left(left_), D(D_) {}
   __device__ __forceinline__ void skip(int rows) { at += rows * ld; left -= rows; }
-  // of `rows` rows at most: the machine gives zeros beyond them (ld >= D, so no later row begins before the last one's end)
-  __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(int rows) const {
+  // Bytes of `rows` rows at most: the machine gives zeros beyond them (ld >= D, so no later row begins before the last one's end)
+  __device__ __forceinline__ int bytes(int rows) const {
     const int n = min(left, rows);
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<E *>(at), 0, n > 0 ? (int)(((n - 1) * (int)ld + D) * sizeof(E)) : 0, 0x00020000);
+    return n > 0 ? (int)(((n - 1) * (int)ld + D) * sizeof(E)) : 0;
   }
 };
+
+// 16 bytes of a run of `bytes` bytes, zeros beyond it: into registers, and (a wavefront's 1 KB) into LDS.  The run is the same for all lanes.
+__device__ __forceinline__ uint4 run_load(const void *run, int bytes, uint32_t offset) {
+  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(run), 0, bytes, 0x00020000);
+  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, 0, 0));
+}
+__device__ __forceinline__ void run_fetch(const void *run, int bytes, uint32_t offset, void *lds) {
+  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(run), 0, bytes, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void *)lds, 16, offset, 0, 0, 0);
+}
 
 // ---- operand tiles in LDS ----------------------------------------------------------------------------------------------
 
@@ -127,13 +133,13 @@ template <int TYPE, int ROWS, int ND> struct Tile {
   // A thread's part of the tile's rows, from the next row of a sequence (Rows): zeros beyond the sequence and beyond D
   uint4 q[NV];
   template <bool VEC> __device__ __forceinline__ void load(const Rows<TYPE> &m) {
-    const __amdgpu_buffer_rsrc_t rsrc = m.rsrc(ROWS);
+    const int bytes = m.bytes(ROWS);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = threadIdx.x + i * 256, row = c / (32 * ND / PER), col = c % (32 * ND / PER) * PER;
       const bool there = col < m.D && (VECS % 256 == 0 || row < ROWS);
       if constexpr (VEC) {
-        q[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, there ? (uint32_t)(row * m.ld + col) * sizeof(E) : OOB, 0, 0));
+        q[i] = run_load(m.at, bytes, there ? (uint32_t)(row * (int)m.ld + col) * sizeof(E) : OOB);
       } else {
         uint32_t w[4] = {0u, 0u, 0u, 0u};
         if (there && row < m.left) {
@@ -156,11 +162,33 @@ template <int TYPE, int ROWS, int ND> struct Tile {
       if (VECS % 256 == 0 || row < ROWS) *reinterpret_cast<uint4 *>(lds + place(row, chunk)) = q[i];
     }
   }
-  __device__ __forceinline__ bool any() const {
-    bool a = false;
+  // The same straight into LDS, 1 KB to a wavefront's load: a lane's place is given, so it fetches the chunk that belongs there
+  static constexpr bool DIRECT = TYPE != TYPE_F32 && ROWS * CH >= 256;
+  static constexpr int ND_LOADS = DIRECT ? ROWS * CH / 256 : 1;
+  uint32_t offset[ND_LOADS];                                         // a lane's chunk of each, in bytes
+  __device__ __forceinline__ void place_loads(const Rows<TYPE> &m) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) a |= any_unusual<TYPE>(q[i]);
-    return a;
+    for (int i = 0; i < ND_LOADS; ++i) {
+      const int c = ((threadIdx.x >> 6) * ND_LOADS + i) * 64 + (threadIdx.x & 63), row = c / CH, col = ((c % CH) ^ swizzle(row)) * 8;
+      offset[i] = col < m.D ? (uint32_t)(row * (int)m.ld + col) * 2u : OOB;
+    }
+  }
+  __device__ __forceinline__ void fetch(E *lds, const Rows<TYPE> &m) const {
+    const int bytes = m.bytes(ROWS);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < ND_LOADS; ++i)
+      run_fetch(m.at, bytes, offset[i], lds + (wave * ND_LOADS + i) * 512);
+  }
+  // Are there infinities or NaN in the tile?  This thread's part of it (what lies between rows' values and their places does not count)
+  static __device__ __forceinline__ bool any(const E *lds) {
+    uint32_t signs = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = threadIdx.x + i * 256, row = c / (32 * ND / PER), chunk = c % (32 * ND / PER);
+      if (VECS % 256 == 0 || row < ROWS) signs |= unusual_signs<TYPE>(*reinterpret_cast<const uint4 *>(lds + place(row, chunk)));
+    }
+    return signs & (TYPE == TYPE_F32 ? 0x80000000u : 0x80008000u);
   }
 
   // Fragment of rows row0 .. row0 + 31 for step k of the values (16 k ..)
@@ -198,6 +226,12 @@ template <int TYPE, int ROWS, int ND> struct Tile {
     else return TYPE == TYPE_BF16 ? bf2f(v) : f16_val(v);
   }
 };
+
+// Every thread's part of the next tile is in LDS, and nobody reads the present one any more
+template <bool DIRECT> __device__ __forceinline__ void arrived() {
+  if (DIRECT) wait_vmcnt<0>();
+  __syncthreads();
+}
 
 // The fragment of one row of memory for step k: the row's values 16 k + 8 (lane >> 5) + e; zeros where there is no row, and beyond D
 template <int TYPE, bool VEC>
@@ -259,7 +293,7 @@ __device__ __forceinline__ void add_unusual(f32x16 (&acc)[ND], const typename El
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
         const float v = Tile<TYPE, ROWS, ND>::value(lds, row0 + r, 32 * d + 8 * (k >> 2) + 4 * h + (k & 3));
-        if (unusual<TYPE>(v)) acc[d][k] += v;
+        if (unusual(v)) acc[d][k] += v;
       }
   }
 }
