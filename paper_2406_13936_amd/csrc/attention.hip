@@ -11,28 +11,53 @@
 namespace absk {
 namespace {
 
-// Tiles before each sequence, for more than 64 of them: first[s], s = 0 .. seqs
-__global__ void __launch_bounds__(256) attention_tiles_kernel(const AttentionP p, int *first, const int size) {
-  __shared__ int sums[4];
-  int before = 0;
-  for (int s0 = 0; s0 < p.seqs; s0 += 256) {
-    const int s = s0 + threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n = s < p.seqs ? (span_of(p, s).len + size - 1) / size : 0;
-    int upto = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += v;
-    }
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    int at = before;
-    for (int w = 0; w < wave; ++w) at += sums[w];
-    if (s < p.seqs) first[s] = at + upto - n;
-    before += sums[0] + sums[1] + sums[2] + sums[3];
-    __syncthreads();
+// Sequence and level of every tile, those of the longest sequences first, for more than 64 sequences: list[0].x of them from list[1] on.  Sequences of about
+// the same number of tiles share one of 1024 places, in an order that may differ from run to run (nothing that is computed depends on it).
+__global__ void __launch_bounds__(1024) attention_tiles_kernel(const AttentionP p, int2 *list, const int size) {
+  constexpr int PLACES = 1024, ALONE = 32;
+  __shared__ int place[PLACES];
+  __shared__ int most, sums[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  place[threadIdx.x] = 0;
+  if (threadIdx.x == 0) most = 0;
+  __syncthreads();
+  auto tiles_of = [&](int s) { return s < p.seqs ? (span_of(p, s).len + size - 1) / size : 0; };
+  int n = 0;
+  for (int s = threadIdx.x; s < p.seqs; s += 1024) n = max(n, tiles_of(s));
+  atomicMax(&most, n);
+  __syncthreads();
+  const int unit = max(1, (most + PLACES - 1) / PLACES);
+  for (int s = threadIdx.x; s < p.seqs; s += 1024) {
+    const int mine = tiles_of(s);
+    if (mine) atomicAdd(&place[PLACES - 1 - (mine - 1) / unit], mine);
   }
-  if (threadIdx.x == 0) first[p.seqs] = before;
+  __syncthreads();
+  const int count = place[threadIdx.x];
+  int upto = count;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) upto += sums[w];
+  place[threadIdx.x] = upto - count;
+  // (offsets that are no list may ask for more tiles than there are places)
+  const int room = (int)min(attention_tiles(p), (long long)0x7fffffff);
+  if (threadIdx.x == PLACES - 1) list[0] = make_int2(min(upto, room), 0);
+  __syncthreads();
+  // a lane writes the first tiles of its sequence, a wavefront the others of each that has more
+  for (int s0 = wave * 64; s0 < p.seqs; s0 += 1024) {
+    const int mine = tiles_of(s0 + lane), at = mine ? atomicAdd(&place[PLACES - 1 - (mine - 1) / unit], mine) : 0;
+    for (int i = 0; i < min(mine, ALONE); ++i)
+      if (at + i < room) list[1 + at + i] = make_int2(s0 + lane, mine - i);
+    for (uint64_t m = __ballot(mine > ALONE); m; m &= m - 1) {
+      const int from = __ffsll((unsigned long long)m) - 1, all = __shfl(mine, from, 64), first = __shfl(at, from, 64);
+      for (int i = ALONE + lane; i < all; i += 64)
+        if (first + i < room) list[1 + first + i] = make_int2(s0 + from, all - i);
+    }
+  }
 }
 
 template <int TYPE, int ND, bool VEC>
@@ -46,11 +71,10 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
   if ((int)blockIdx.x >= blocks) return zero_rest(p, p.o, TYPE, p.Hq, p.ldo, p.ho, p.lse, blockIdx.x - blocks, REST_BLOCKS);
   int head, t;
   head_and_tile(blockIdx.x, p.Hq, head, t);
-  Work w = find_tile(p, t, ATTENTION_ROWS);
-  if (w.tile < 0) return;
-  w.tile = (w.len + ATTENTION_ROWS - 1) / ATTENTION_ROWS - 1 - w.tile;      // the longest first
+  const Work w = find_tile(p, t, ATTENTION_ROWS);
+  if (!w.level) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const int q0 = w.tile * ATTENTION_ROWS, mine = q0 + wave * 32, row = mine + (lane & 31);
+  const int q0 = (w.level - 1) * ATTENTION_ROWS, mine = q0 + wave * 32, row = mine + (lane & 31);
   const bool in = row < w.len;
   const int kvh = head / (p.Hq / p.Hkv);
   const E *q = static_cast<const E *>(p.q) + w.start * p.ldq + head * p.hq;
@@ -66,10 +90,10 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
   Rows<TYPE> rk(p.k, w.start * p.ldk + kvh * p.hk, p.ldk, w.len, p.D), rv(p.v, w.start * p.ldv + kvh * p.hv, p.ldv, w.len, p.D);
   KV tk, tv;
   if constexpr (DIRECT) {
-    tk.place_loads(rk);
-    tv.place_loads(rv);
+    tk.place_loads(p.ldk, p.D);
+    tv.place_loads(p.ldv, p.D);
   }
-  auto fetch = [&](auto buffer) {                      // the next tile
+  auto fetch = [&](auto buffer) INLINE {                      // the next tile
     if constexpr (DIRECT) {
       tk.fetch(decltype(buffer)::value ? keys_b : keys_a, rk);
       tv.fetch(decltype(buffer)::value ? values_b : values_a, rv);
@@ -80,17 +104,16 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
     rk.skip(BK);
     rv.skip(BK);
   };
-  auto settle = [&](auto buffer) {
+  auto settle = [&](auto buffer) INLINE {
     if constexpr (!DIRECT) {
       tk.store(decltype(buffer)::value ? keys_b : keys_a);
       tv.store(decltype(buffer)::value ? values_b : values_a);
     }
   };
-  // MASKED: some wavefront of the block masks the tile
-  auto step = [&](int k0, auto buffer, auto masked_tile, bool odd) {
+  // MASKED: the diagonal may run through the tile
+  auto step = [&](int k0, auto buffer, auto masked_tile) INLINE {
     constexpr bool MASKED = decltype(masked_tile)::value;
     const E *lk = decltype(buffer)::value ? keys_b : keys_a, *lv = decltype(buffer)::value ? values_b : values_a;
-    if (MASKED && (k0 > mine + 31 || mine >= w.len)) return;
     f32x16 s[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) s[b] = zeros16();
@@ -134,31 +157,27 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
       x[b][0] = as_frag<TYPE>(s[b], 0);
       x[b][1] = as_frag<TYPE>(s[b], 1);
     }
-    if (MASKED && odd) {
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        add_cols<true, TYPE, BK, ND>(o, lv, 32 * b, x[b]);
-        add_unusual<TYPE, BK, ND>(o, lv, 32 * b, [&](int r) { return k0 + 32 * b + r <= row; });
-      }
-    } else {
-#pragma unroll
-      for (int b = 0; b < NB; ++b) add_cols<false, TYPE, BK, ND>(o, lv, 32 * b, x[b]);
+    for (int b = 0; b < NB; ++b) {
+      add_cols<MASKED, TYPE, BK, ND>(o, lv, 32 * b, x[b]);
+      if (MASKED && KV::any(lv, 32 * b)) add_unusual<TYPE, BK, ND>(o, lv, 32 * b, [&](int r) { return k0 + 32 * b + r <= row; });
     }
   };
-  const int whole = q0 / BK;                           // tiles that no wavefront masks
   int j = 0;
-  auto turn = [&](auto buffer, auto masked_tile) {
-    constexpr bool MASKED = decltype(masked_tile)::value;
+  const int whole = q0 / BK;                           // tiles below every wavefront's diagonal
+  auto turn = [&](auto buffer, auto last_tiles) INLINE {
+    constexpr bool LAST = decltype(last_tiles)::value;
     std::integral_constant<bool, !decltype(buffer)::value> other;
-    const bool more = !MASKED || j + 1 < tiles, odd = MASKED && __syncthreads_or(KV::any(decltype(buffer)::value ? values_b : values_a));
+    const int k0 = j * BK;
+    const bool more = !LAST || j + 1 < tiles;
     if (more) fetch(other);
-    step(j * BK, buffer, masked_tile, odd);
+    if (!LAST || (k0 <= mine + 31 && mine < w.len)) step(k0, buffer, last_tiles);
     if (more) settle(other);
     arrived<DIRECT>();
     ++j;
   };
   const std::false_type a, below;
-  const std::true_type b, diagonal;
+  const std::true_type b, last;
   fetch(a);
   settle(a);
   arrived<DIRECT>();
@@ -168,8 +187,8 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
   }
   if (j < whole) turn(a, below);
   while (j < tiles) {
-    if (j & 1) turn(b, diagonal);
-    else turn(a, diagonal);
+    if (j & 1) turn(b, last);
+    else turn(a, last);
   }
   sum += __shfl_xor(sum, 32, 64);
   if (!in) return;
@@ -195,7 +214,7 @@ template <int TYPE, bool VEC> hipError_t forward_width(const AttentionP &p, hipS
 
 hipError_t launch_attention_tiles(const AttentionP &p, hipStream_t s) {
   if (!p.offsets || p.seqs <= 64) return hipSuccess;
-  hipLaunchKernelGGL(attention_tiles_kernel, dim3(1), dim3(256), 0, s, p, const_cast<int *>(p.first), ATTENTION_ROWS);
+  hipLaunchKernelGGL(attention_tiles_kernel, dim3(1), dim3(1024), 0, s, p, const_cast<int2 *>(p.list), ATTENTION_ROWS);
   return hipGetLastError();
 }
 

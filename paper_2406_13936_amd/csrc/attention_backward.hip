@@ -95,26 +95,30 @@ template <int TYPE> __device__ __forceinline__ float ds_factor(const AttentionP 
 // Queries of a tile of the pass over keys
 constexpr int keys_tile(int type, int nd) { return type == TYPE_F32 || nd >= 3 ? 32 : 64; }
 
+// Groups of four wavefronts that go through the same keys' queries in turn and add up what they have at the end: a block with the longest work takes half as
+// long, with the same wavefronts to a CU.  (Wider heads take the registers of two; narrower ones' tiles have no room for the exchange.)
+constexpr int keys_groups(int nd) { return nd == 2 ? 2 : 1; }
+
 // dk and dv of 128 keys
 template <int TYPE, int ND, bool VEC>
-__global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) attention_keys_kernel(const AttentionP p, const int blocks) {
-  constexpr int BQ = keys_tile(TYPE, ND);
+__global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attention_keys_kernel(const AttentionP p, const int blocks) {
+  constexpr int BQ = keys_tile(TYPE, ND), GROUPS = keys_groups(ND);
   typedef Tile<TYPE, BQ, ND> T;
   typedef typename T::E E;
   constexpr bool DIRECT = VEC && T::DIRECT;
   // two buffers, by name, so that the compiler can tell what is read from what is on its way
-  __shared__ __attribute__((aligned(16))) E queries_a[T::ELEMS], signals_a[T::ELEMS], queries_b[T::ELEMS], signals_b[T::ELEMS];
-  __shared__ __attribute__((aligned(16))) float stat_a[2][BQ], stat_b[2][BQ];      // lse (to base 2) and D of a tile's queries
+  __shared__ __attribute__((aligned(16))) E queries_a[GROUPS * T::ELEMS], signals_a[GROUPS * T::ELEMS], queries_b[GROUPS * T::ELEMS], signals_b[GROUPS * T::ELEMS];
+  __shared__ __attribute__((aligned(16))) float stat_a[GROUPS][2][BQ], stat_b[GROUPS][2][BQ];      // lse (to base 2) and D of a tile's queries
   if ((int)blockIdx.x >= blocks) {
     zero_rest(p, p.dk, TYPE, p.Hkv, p.lddk, p.hdk, nullptr, blockIdx.x - blocks, REST_BLOCKS);
     return zero_rest(p, p.dv, TYPE, p.Hkv, p.lddv, p.hdv, nullptr, blockIdx.x - blocks, REST_BLOCKS);
   }
   int kvh, t;
   head_and_tile(blockIdx.x, p.Hkv, kvh, t);
-  const Work w = find_tile(p, t, ATTENTION_ROWS);      // (the first keys of a sequence, seen by most queries, come first)
-  if (w.tile < 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const int k0 = w.tile * ATTENTION_ROWS, mine = k0 + wave * 32, key = mine + (lane & 31), G = p.Hq / p.Hkv;
+  const Work w = find_tile(p, t, ATTENTION_ROWS);
+  if (!w.level) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6 & 3, group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0, h = lane >> 5;
+  const int k0 = (w.tiles - w.level) * ATTENTION_ROWS, mine = k0 + wave * 32, key = mine + (lane & 31), G = p.Hq / p.Hkv;
   const bool in = key < w.len;
   const float f = ds_factor<TYPE>(p), g = f * __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>);
   Frag8<TYPE> kf[2 * ND], vf[2 * ND];
@@ -127,58 +131,48 @@ __global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) atte
 #pragma unroll
   for (int d = 0; d < ND; ++d) dk[d] = dv[d] = zeros16();
   const float c = p.scale * LOG2E;
-  // tiles of queries from the diagonal to the sequence's end, of one head after the other; of each head the first ones are masked
-  const int first = k0 / BQ, each = (w.len + BQ - 1) / BQ - first, total = each * G, diagonal = ATTENTION_ROWS / BQ;
+  // tiles of queries from the diagonal to the sequence's end, of one head after the other
+  const int first = k0 / BQ, each = (w.len + BQ - 1) / BQ - first, total = each * G;
   T tq, td;
   float lse = 0.0f, inner = 0.0f;
-  int head = kvh * G, j = 0;                           // the next tile to load
-  Rows<TYPE> rq(p.q, 0, p.ldq, 0, p.D), rd(p.dout, 0, p.lddo, 0, p.D);
-  auto fetch = [&](auto buffer) {
-    const int r0 = (first + j) * BQ;
-    if (j == 0) {
-      rq = Rows<TYPE>(p.q, (w.start + r0) * p.ldq + head * p.hq, p.ldq, w.len - r0, p.D);
-      rd = Rows<TYPE>(p.dout, (w.start + r0) * p.lddo + head * p.hdo, p.lddo, w.len - r0, p.D);
-    }
-    if (threadIdx.x < BQ) {
-      const int r = r0 + threadIdx.x;
+  const int thread = threadIdx.x & 255;
+  auto fetch = [&](auto buffer, int tile, int of) INLINE {    // of the of-th head
+    const int r0 = (first + tile) * BQ, head = kvh * G + of;
+    const Rows<TYPE> rq(p.q, (w.start + r0) * p.ldq + head * p.hq, p.ldq, w.len - r0, p.D);
+    const Rows<TYPE> rd(p.dout, (w.start + r0) * p.lddo + head * p.hdo, p.lddo, w.len - r0, p.D);
+    if (thread < BQ) {
+      const int r = r0 + thread;
       const long long at = head * p.rows + w.start + (r < w.len ? r : 0);
       lse = r < w.len ? p.lse[at] * LOG2E - P_SHIFT<TYPE> : __builtin_inff();
       inner = r < w.len ? p.inner[at] : 0.0f;
     }
     if constexpr (DIRECT) {
-      tq.fetch(decltype(buffer)::value ? queries_b : queries_a, rq);
-      td.fetch(decltype(buffer)::value ? signals_b : signals_a, rd);
+      tq.fetch((decltype(buffer)::value ? queries_b : queries_a) + group * T::ELEMS, rq);
+      td.fetch((decltype(buffer)::value ? signals_b : signals_a) + group * T::ELEMS, rd);
     } else {
       tq.template load<VEC>(rq);
       td.template load<VEC>(rd);
     }
-    rq.skip(BQ);
-    rd.skip(BQ);
-    if (++j == each) { j = 0; ++head; }
   };
-  auto settle = [&](auto buffer) {
+  auto settle = [&](auto buffer) INLINE {
     constexpr bool B = decltype(buffer)::value;
     if constexpr (!DIRECT) {
-      tq.store(B ? queries_b : queries_a);
-      td.store(B ? signals_b : signals_a);
+      tq.store((B ? queries_b : queries_a) + group * T::ELEMS);
+      td.store((B ? signals_b : signals_a) + group * T::ELEMS);
     }
-    if (threadIdx.x < BQ) { (B ? stat_b : stat_a)[0][threadIdx.x] = lse; (B ? stat_b : stat_a)[1][threadIdx.x] = inner; }
+    if (thread < BQ) { (B ? stat_b : stat_a)[group][0][thread] = lse; (B ? stat_b : stat_a)[group][1][thread] = inner; }
   };
-  // MASKED: some wavefront of the block masks the tile, or queries end in it
-  auto step = [&](int r0, auto buffer, auto masked_tile, bool odd) {
-    constexpr bool MASKED = decltype(masked_tile)::value, B = decltype(buffer)::value;
-    const E *lq = B ? queries_b : queries_a, *ld = B ? signals_b : signals_a;
-    const float(*stat)[BQ] = B ? stat_b : stat_a;
+  // Queries q0 .. q0 + 31, block b of a tile; MASKED: perhaps the diagonal's
+  auto step = [&](int q0, int b, auto buffer, auto masked_block) INLINE {
+    constexpr bool MASKED = decltype(masked_block)::value, B = decltype(buffer)::value;
+    const E *lq = (B ? queries_b : queries_a) + group * T::ELEMS, *ld = (B ? signals_b : signals_a) + group * T::ELEMS;
+    const float(*stat)[BQ] = (B ? stat_b : stat_a)[group];
+    f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
-    for (int b = 0; b < BQ / 32; ++b) {
-      const int q0 = r0 + 32 * b;
-      if (MASKED && (q0 + 31 < mine || q0 >= w.len || mine >= w.len)) continue;
-      f32x16 s = zeros16(), dp = zeros16();
-#pragma unroll
-      for (int i = 0; i < 2 * ND; ++i) {
-        mma<TYPE>(s, T::rows(lq, 32 * b, i), kf[i]);
-        mma<TYPE>(dp, T::rows(ld, 32 * b, i), vf[i]);
-      }
+    for (int i = 0; i < 2 * ND; ++i) {
+      mma<TYPE>(s, T::rows(lq, 32 * b, i), kf[i]);
+      mma<TYPE>(dp, T::rows(ld, 32 * b, i), vf[i]);
+    }
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const float4 l4 = *reinterpret_cast<const float4 *>(&stat[0][32 * b + 8 * r4 + 4 * h]);
@@ -193,53 +187,79 @@ __global__ void __launch_bounds__(256, ND >= 3 || TYPE == TYPE_F32 ? 1 : 2) atte
           dp[r] = y;
         }
       }
-      const Frag8<TYPE> x[2] = {as_frag<TYPE>(s, 0), as_frag<TYPE>(s, 1)}, y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
-      if (MASKED && odd) {
-        add_cols<true, TYPE, BQ, ND>(dv, ld, 32 * b, x);
-        add_cols<true, TYPE, BQ, ND>(dk, lq, 32 * b, y);
-        add_unusual<TYPE, BQ, ND>(dv, ld, 32 * b, [&](int r) { return q0 + r >= key; });
-        add_unusual<TYPE, BQ, ND>(dk, lq, 32 * b, [&](int r) { return q0 + r >= key; });
-      } else {
-        add_cols<false, TYPE, BQ, ND>(dv, ld, 32 * b, x);
-        add_cols<false, TYPE, BQ, ND>(dk, lq, 32 * b, y);
-      }
-    }
+    const Frag8<TYPE> x[2] = {as_frag<TYPE>(s, 0), as_frag<TYPE>(s, 1)}, y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
+    add_cols<MASKED, TYPE, BQ, ND>(dv, ld, 32 * b, x);
+    add_cols<MASKED, TYPE, BQ, ND>(dk, lq, 32 * b, y);
+    if (MASKED && T::any(ld, 32 * b)) add_unusual<TYPE, BQ, ND>(dv, ld, 32 * b, [&](int r) { return q0 + r >= key; });
+    if (MASKED && T::any(lq, 32 * b)) add_unusual<TYPE, BQ, ND>(dk, lq, 32 * b, [&](int r) { return q0 + r >= key; });
   };
   if constexpr (DIRECT) {
-    rq.ld = p.ldq;
-    tq.place_loads(rq);
-    td.place_loads(rd);
+    tq.place_loads(p.ldq, p.D);
+    td.place_loads(p.lddo, p.D);
   }
-  const std::false_type a, plain;
-  const std::true_type b, masked;
-  fetch(a);
-  settle(a);
+  const std::false_type a;
+  const std::true_type b;
+  const int rounds = (total + GROUPS - 1) / GROUPS;
+  int it = 0, now = group % each, now_head = group / each;      // this group's tile: the now-th of a head, if that is one of the G
+  int next = now, next_head = now_head;
+  auto advance = [&](int &tile, int &of) INLINE {
+    tile += GROUPS;
+    while (tile >= each) { tile -= each; ++of; }
+  };
+  if (next_head < G) {
+    fetch(a, next, next_head);
+    settle(a);
+  }
   arrived<DIRECT>();
-  int it = 0, at = 0;
-  auto turn = [&](auto buffer, auto masked_tile) {
-    constexpr bool MASKED = decltype(masked_tile)::value, B = decltype(buffer)::value;
-    std::integral_constant<bool, !B> other;
-    const bool more = it + 1 < total, odd = MASKED && at < diagonal && __syncthreads_or(T::any(B ? queries_b : queries_a) || T::any(B ? signals_b : signals_a));
-    if (more) fetch(other);
-    step((first + at) * BQ, buffer, masked_tile, odd);
+  auto turn = [&](auto buffer) INLINE {
+    std::integral_constant<bool, !decltype(buffer)::value> other;
+    advance(next, next_head);
+    const bool more = next_head < G;
+    if (more) fetch(other, next, next_head);
+    if (now_head < G && mine < w.len) {
+      const int q0 = (first + now) * BQ;
+      if (q0 > mine && q0 + BQ <= w.len) {
+#pragma unroll
+        for (int i = 0; i < BQ / 32; ++i) step(q0 + 32 * i, i, buffer, std::false_type{});
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < BQ / 32; ++i)
+          if (q0 + 32 * i >= mine && q0 + 32 * i < w.len) step(q0 + 32 * i, i, buffer, std::true_type{});
+      }
+    }
     if (more) settle(other);
     arrived<DIRECT>();
-    if (++at == each) at = 0;
+    now = next;
+    now_head = next_head;
     ++it;
   };
-  const bool ends = k0 + ATTENTION_ROWS > w.len;       // (some wavefronts may have no keys)
-  while (it < total) {
-    if (at < diagonal || ends) {
-      if (it & 1) turn(b, masked);
-      else turn(a, masked);
-    } else {
-      if (it & 1) turn(b, plain);
-      else turn(a, plain);
+  while (it < rounds) {
+    turn(a);
+    if (it < rounds) turn(b);
+  }
+  if constexpr (GROUPS == 2) {                         // one group ends with dk, the other with dv
+    static_assert(GROUPS * T::ELEMS * sizeof(E) >= 4 * 64 * 16 * 4, "four wavefronts' registers of 32 values");
+    const int at = wave * 64 * 16 + lane;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      float *const to = reinterpret_cast<float *>(group ? (d ? queries_b : queries_a) : (d ? signals_b : signals_a));
+#pragma unroll
+      for (int r = 0; r < 16; ++r) to[at + r * 64] = group ? dk[d][r] : dv[d][r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      const float *const from = reinterpret_cast<const float *>(group ? (d ? signals_b : signals_a) : (d ? queries_b : queries_a));
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (group) dv[d][r] += from[at + r * 64];
+        else dk[d][r] += from[at + r * 64];
+      }
     }
   }
   if (!in) return;
-  store_row<TYPE, ND, VEC>(p.dk, (w.start + key) * p.lddk + kvh * p.hdk, dk, p.scale / f, p.D);
-  store_row<TYPE, ND, VEC>(p.dv, (w.start + key) * p.lddv + kvh * p.hdv, dv, __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>), p.D);
+  if (GROUPS == 1 || !group) store_row<TYPE, ND, VEC>(p.dk, (w.start + key) * p.lddk + kvh * p.hdk, dk, p.scale / f, p.D);
+  if (GROUPS == 1 || group) store_row<TYPE, ND, VEC>(p.dv, (w.start + key) * p.lddv + kvh * p.hdv, dv, __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>), p.D);
 }
 
 // dq of 128 queries of a head
@@ -253,11 +273,10 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
   if ((int)blockIdx.x >= blocks) return zero_rest(p, p.dq, TYPE, p.Hq, p.lddq, p.hdq, nullptr, blockIdx.x - blocks, REST_BLOCKS);
   int head, t;
   head_and_tile(blockIdx.x, p.Hq, head, t);
-  Work w = find_tile(p, t, ATTENTION_ROWS);
-  if (w.tile < 0) return;
-  w.tile = (w.len + ATTENTION_ROWS - 1) / ATTENTION_ROWS - 1 - w.tile;      // the longest first
+  const Work w = find_tile(p, t, ATTENTION_ROWS);
+  if (!w.level) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const int q0 = w.tile * ATTENTION_ROWS, mine = q0 + wave * 32, row = mine + (lane & 31);
+  const int q0 = (w.level - 1) * ATTENTION_ROWS, mine = q0 + wave * 32, row = mine + (lane & 31);
   const bool in = row < w.len;
   const int kvh = head / (p.Hq / p.Hkv);
   const float f = ds_factor<TYPE>(p);
@@ -276,10 +295,10 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
   Rows<TYPE> rk(p.k, w.start * p.ldk + kvh * p.hk, p.ldk, w.len, p.D), rv(p.v, w.start * p.ldv + kvh * p.hv, p.ldv, w.len, p.D);
   T tk, tv;
   if constexpr (DIRECT) {
-    tk.place_loads(rk);
-    tv.place_loads(rv);
+    tk.place_loads(p.ldk, p.D);
+    tv.place_loads(p.ldv, p.D);
   }
-  auto fetch = [&](auto buffer) {                      // the next tile
+  auto fetch = [&](auto buffer) INLINE {                      // the next tile
     if constexpr (DIRECT) {
       tk.fetch(decltype(buffer)::value ? keys_b : keys_a, rk);
       tv.fetch(decltype(buffer)::value ? values_b : values_a, rv);
@@ -290,54 +309,53 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
     rk.skip(BK);
     rv.skip(BK);
   };
-  auto settle = [&](auto buffer) {
+  auto settle = [&](auto buffer) INLINE {
     if constexpr (!DIRECT) {
       tk.store(decltype(buffer)::value ? keys_b : keys_a);
       tv.store(decltype(buffer)::value ? values_b : values_a);
     }
   };
-  auto step = [&](int k0, auto buffer, auto masked_tile, bool odd) {
-    constexpr bool MASKED = decltype(masked_tile)::value;
+  // Keys kb .. kb + 31, block b of a tile; MASKED: perhaps the diagonal's
+  auto step = [&](int kb, int b, auto buffer, auto masked_block) INLINE {
+    constexpr bool MASKED = decltype(masked_block)::value;
     const E *lk = decltype(buffer)::value ? keys_b : keys_a, *lv = decltype(buffer)::value ? values_b : values_a;
+    f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
-    for (int b = 0; b < BK / 32; ++b) {
-      const int kb = k0 + 32 * b;
-      if (MASKED && (kb > mine + 31 || mine >= w.len)) continue;
-      f32x16 s = zeros16(), dp = zeros16();
-#pragma unroll
-      for (int i = 0; i < 2 * ND; ++i) {
-        mma<TYPE>(s, T::rows(lk, 32 * b, i), qf[i]);
-        mma<TYPE>(dp, T::rows(lv, 32 * b, i), of[i]);
-      }
+    for (int i = 0; i < 2 * ND; ++i) {
+      mma<TYPE>(s, T::rows(lk, 32 * b, i), qf[i]);
+      mma<TYPE>(dp, T::rows(lv, 32 * b, i), of[i]);
+    }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float x = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse));
         dp[r] = TYPE == TYPE_F16 ? x * ((dp[r] - inner) * f) : x * (dp[r] - inner);
         if (MASKED && kb + 8 * (r >> 2) + 4 * h + (r & 3) > row) dp[r] = 0.0f;
       }
-      const Frag8<TYPE> y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
-      if (MASKED && odd) {
-        add_cols<true, TYPE, BK, ND>(dq, lk, 32 * b, y);
-        add_unusual<TYPE, BK, ND>(dq, lk, 32 * b, [&](int r) { return kb + r <= row; });
-      } else {
-        add_cols<false, TYPE, BK, ND>(dq, lk, 32 * b, y);
-      }
-    }
+    const Frag8<TYPE> y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
+    add_cols<MASKED, TYPE, BK, ND>(dq, lk, 32 * b, y);
+    if (MASKED && T::any(lk, 32 * b)) add_unusual<TYPE, BK, ND>(dq, lk, 32 * b, [&](int r) { return kb + r <= row; });
   };
-  const int whole = q0 / BK;                           // tiles that no wavefront masks
   int j = 0;
-  auto turn = [&](auto buffer, auto masked_tile) {
-    constexpr bool MASKED = decltype(masked_tile)::value;
+  const int whole = q0 / BK;                           // tiles below every wavefront's diagonal
+  auto turn = [&](auto buffer, auto last_tiles) INLINE {
+    constexpr bool LAST = decltype(last_tiles)::value;
     std::integral_constant<bool, !decltype(buffer)::value> other;
-    const bool more = !MASKED || j + 1 < tiles, odd = MASKED && __syncthreads_or(T::any(decltype(buffer)::value ? keys_b : keys_a));
+    const bool more = !LAST || j + 1 < tiles;
     if (more) fetch(other);
-    step(j * BK, buffer, masked_tile, odd);
+    if constexpr (!LAST) {
+#pragma unroll
+      for (int i = 0; i < BK / 32; ++i) step(j * BK + 32 * i, i, buffer, std::false_type{});
+    } else if (mine < w.len) {
+#pragma unroll 1
+      for (int i = 0; i < BK / 32; ++i)
+        if (j * BK + 32 * i <= mine) step(j * BK + 32 * i, i, buffer, std::true_type{});
+    }
     if (more) settle(other);
     arrived<DIRECT>();
     ++j;
   };
   const std::false_type a, below;
-  const std::true_type b, diagonal;
+  const std::true_type b, last;
   fetch(a);
   settle(a);
   arrived<DIRECT>();
@@ -347,8 +365,8 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
   }
   if (j < whole) turn(a, below);
   while (j < tiles) {
-    if (j & 1) turn(b, diagonal);
-    else turn(a, diagonal);
+    if (j & 1) turn(b, last);
+    else turn(a, last);
   }
   if (!in) return;
   store_row<TYPE, ND, VEC>(p.dq, (w.start + row) * p.lddq + head * p.hdq, dq, p.scale / f, p.D);
@@ -357,7 +375,7 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
 template <int TYPE, int ND, bool VEC> hipError_t backward_launch(const AttentionP &p, hipStream_t s) {
   const long long tiles = attention_tiles(p), rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
   hipLaunchKernelGGL((attention_inner_kernel<TYPE, VEC>), dim3(p.nmost), dim3(256), 0, s, p);
-  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hkv + rest)), dim3(256), 0, s, p, (int)(tiles * p.Hkv));
+  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hkv + rest)), dim3(256 * keys_groups(ND)), 0, s, p, (int)(tiles * p.Hkv));
   hipLaunchKernelGGL((attention_queries_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hq + rest)), dim3(256), 0, s, p, (int)(tiles * p.Hq));
   return hipGetLastError();
 }

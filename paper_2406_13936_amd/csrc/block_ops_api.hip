@@ -64,13 +64,13 @@ RmsNormP rms_args(const abs_rms_norm_shape *s) {
 Block heads_of(const void *t, const abs_attention_shape *s, int heads, int64_t ld, int64_t head) {
   return {t, heads, head, s->rows, ld, s->D, type_bytes(s->type)};
 }
-struct AttentionPieces { size_t first, inner, most, total; };
+struct AttentionPieces { size_t list, inner, most, total; };
 constexpr int MOST_BLOCKS = 1024;
 AttentionPieces attention_pieces(const abs_attention_shape *s, bool backward) {
   AttentionPieces q;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t r = at; at = (at + bytes + 255) / 256 * 256; return r; };
-  q.first = take(s->offsets_type && s->seqs > 64 ? ((size_t)s->seqs + 1) * 4 : 0);
+  q.list = take(s->offsets_type && s->seqs > 64 ? ((size_t)(s->rows / ATTENTION_ROWS) + s->seqs + 1) * 8 : 0);
   q.inner = take(backward ? (size_t)s->Hq * s->rows * 4 : 0);
   q.most = take(backward && s->type == ABS_TYPE_F16 ? 2 * MOST_BLOCKS * 4 : 0);
   q.total = at;
@@ -255,7 +255,7 @@ abs_status abs_causal_attention(const abs_attention_shape *shape, const void *q_
   AttentionP p = attention_args(shape);
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   p.q = q_dev; p.k = k_dev; p.v = v_dev; p.offsets = offsets_dev; p.scale = scale; p.o = o_dev; p.lse = lse_dev; p.zero_rest = zero_rest != 0;
-  p.first = reinterpret_cast<const int *>(ws + at.first);
+  p.list = reinterpret_cast<const int2 *>(ws + at.list);
   return hip_status(launch_attention(p, static_cast<hipStream_t>(hip_stream)), "abs_causal_attention");
 } catch (...) { return exception_status(); }
 
@@ -282,7 +282,7 @@ abs_status abs_causal_attention_backward(const abs_attention_shape *shape, const
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   p.dout = do_dev; p.q = q_dev; p.k = k_dev; p.v = v_dev; p.o = const_cast<void *>(o_dev); p.lse = const_cast<float *>(lse_dev);
   p.offsets = offsets_dev; p.scale = scale; p.dq = dq_dev; p.dk = dk_dev; p.dv = dv_dev; p.zero_rest = zero_rest != 0;
-  p.first = reinterpret_cast<const int *>(ws + at.first);
+  p.list = reinterpret_cast<const int2 *>(ws + at.list);
   p.inner = reinterpret_cast<float *>(ws + at.inner);
   p.most = reinterpret_cast<float *>(ws + at.most);
   p.nmost = (int)std::max<int64_t>(1, std::min<int64_t>(MOST_BLOCKS, (shape->rows * shape->Hq + 63) / 64));

@@ -140,7 +140,7 @@ struct AttentionP {
   int zero_rest;                           // zeros in rows of no sequence (else they stay as they are)
   long long rows;
   const void *offsets;
-  const int *first;                        // workspace, with more than 64 sequences: tiles before each
+  const int2 *list;                        // workspace, with more than 64 sequences: number of tiles; sequence and level of each
   long long ldq, hq, ldk, hk, ldv, hv, ldo, ho;
   const void *q, *k, *v;
   float scale;
@@ -154,7 +154,7 @@ struct AttentionP {
   int nmost;
 };
 // Tiles of all sequences: what they are, or with offsets the most that they can be
-inline long long attention_tiles(const AttentionP &p) {
+__host__ __device__ inline long long attention_tiles(const AttentionP &p) {
   if (!p.offsets) return (long long)p.seqs * ((p.T + ATTENTION_ROWS - 1) / ATTENTION_ROWS);
   return p.rows / ATTENTION_ROWS + p.seqs;
 }
