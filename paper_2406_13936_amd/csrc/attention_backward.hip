@@ -18,8 +18,8 @@ namespace {
 
 template <int TYPE> constexpr float P_SHIFT = TYPE == TYPE_F16 ? 12.0f : 0.0f;
 
-// D_i of every row and query head, 16 lanes each; WIDE 0: any alignment.  fp16: the largest squared lengths of do_i and v_j that each block meets
-template <int TYPE, bool VEC>
+// fp16: D_i of every row and query head, 16 lanes each, and the largest squared lengths of do_i and v_j that each block meets
+template <bool VEC>
 __global__ void __launch_bounds__(256) attention_inner_kernel(const AttentionP p) {
   const int g = threadIdx.x / 16, l = threadIdx.x % 16, D = p.D;
   const long long start = span_of(p, 0).start;
@@ -27,14 +27,13 @@ __global__ void __launch_bounds__(256) attention_inner_kernel(const AttentionP p
   const long long n = max(0LL, last.start + last.len - start);
   const long long step = (long long)gridDim.x * 16;
   float longest = 0.0f, longest_v = 0.0f;
-  typedef typename ElemOf<TYPE>::type E;
   auto values = [&](const void *base, long long at, float (&v)[8]) {
-    const E *src = static_cast<const E *>(base) + at + l * 8;
+    const uint16_t *src = static_cast<const uint16_t *>(base) + at + l * 8;
     if (VEC && l * 8 < D) {
-      load8(src, TYPE, 0, v);
+      load8(src, TYPE_F16, 0, v);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = l * 8 + e < D ? load_as_f32(src, TYPE, e) : 0.0f;
+      for (int e = 0; e < 8; ++e) v[e] = l * 8 + e < D ? load_as_f32(src, TYPE_F16, e) : 0.0f;
     }
   };
   for (long long i = (long long)blockIdx.x * 16 + g; i < n * p.Hq; i += step) {
@@ -44,37 +43,29 @@ __global__ void __launch_bounds__(256) attention_inner_kernel(const AttentionP p
     values(p.dout, row * p.lddo + h * p.hdo, a);
     values(p.o, row * p.ldo + h * p.ho, b);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      s = fmaf(a[e], b[e], s);
-      if (TYPE == TYPE_F16) t = fmaf(a[e], a[e], t);
-    }
+    for (int e = 0; e < 8; ++e) { s = fmaf(a[e], b[e], s); t = fmaf(a[e], a[e], t); }
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1) {
-      s += __shfl_xor(s, o, 16);
-      if (TYPE == TYPE_F16) t += __shfl_xor(t, o, 16);
-    }
+    for (int o = 1; o < 16; o <<= 1) { s += __shfl_xor(s, o, 16); t += __shfl_xor(t, o, 16); }
     if (l == 0) p.inner[h * p.rows + row] = s;
-    if (TYPE == TYPE_F16 && t < __builtin_inff()) longest = fmaxf(longest, t);
+    if (t < __builtin_inff()) longest = fmaxf(longest, t);
   }
-  if constexpr (TYPE == TYPE_F16) {
-    for (long long i = (long long)blockIdx.x * 16 + g; i < n * p.Hkv; i += step) {
-      const long long r = i / p.Hkv, row = start + r;
-      float a[8], t = 0.0f;
-      values(p.v, row * p.ldv + (i - r * p.Hkv) * p.hv, a);
+  for (long long i = (long long)blockIdx.x * 16 + g; i < n * p.Hkv; i += step) {
+    const long long r = i / p.Hkv, row = start + r;
+    float a[8], t = 0.0f;
+    values(p.v, row * p.ldv + (i - r * p.Hkv) * p.hv, a);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) t = fmaf(a[e], a[e], t);
+    for (int e = 0; e < 8; ++e) t = fmaf(a[e], a[e], t);
 #pragma unroll
-      for (int o = 1; o < 16; o <<= 1) t += __shfl_xor(t, o, 16);
-      if (t < __builtin_inff()) longest_v = fmaxf(longest_v, t);
-    }
-    __shared__ float sm[2][16];
-    if (l == 0) { sm[0][g] = longest; sm[1][g] = longest_v; }
-    __syncthreads();
-    if (threadIdx.x < 2) {
-      float m = 0.0f;
-      for (int k = 0; k < 16; ++k) m = fmaxf(m, sm[threadIdx.x][k]);
-      p.most[threadIdx.x * p.nmost + blockIdx.x] = m;
-    }
+    for (int o = 1; o < 16; o <<= 1) t += __shfl_xor(t, o, 16);
+    if (t < __builtin_inff()) longest_v = fmaxf(longest_v, t);
+  }
+  __shared__ float sm[2][16];
+  if (l == 0) { sm[0][g] = longest; sm[1][g] = longest_v; }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    float m = 0.0f;
+    for (int k = 0; k < 16; ++k) m = fmaxf(m, sm[threadIdx.x][k]);
+    p.most[threadIdx.x * p.nmost + blockIdx.x] = m;
   }
 }
 
@@ -135,17 +126,18 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
   const int first = k0 / BQ, each = (w.len + BQ - 1) / BQ - first, total = each * G;
   T tq, td;
   float lse = 0.0f, inner = 0.0f;
+  bool there = false;
   const int thread = threadIdx.x & 255;
   auto fetch = [&](auto buffer, int tile, int of) INLINE {    // of the of-th head
     const int r0 = (first + tile) * BQ, head = kvh * G + of;
     const Rows<TYPE> rq(p.q, (w.start + r0) * p.ldq + head * p.hq, p.ldq, w.len - r0, p.D);
     const Rows<TYPE> rd(p.dout, (w.start + r0) * p.lddo + head * p.hdo, p.lddo, w.len - r0, p.D);
-    if (thread < BQ) {
-      const int r = r0 + thread;
-      const long long at = head * p.rows + w.start + (r < w.len ? r : 0);
-      lse = r < w.len ? p.lse[at] * LOG2E - P_SHIFT<TYPE> : __builtin_inff();
-      inner = r < w.len ? p.inner[at] : 0.0f;
-    }
+    // (as they come: what is made of them here would be waited for here)
+    const int r = r0 + thread % BQ;
+    const long long at = head * p.rows + w.start + min(r, w.len - 1);
+    there = r < w.len;
+    lse = p.lse[at];
+    inner = p.inner[at];
     if constexpr (DIRECT) {
       tq.fetch((decltype(buffer)::value ? queries_b : queries_a) + group * T::ELEMS, rq);
       td.fetch((decltype(buffer)::value ? signals_b : signals_a) + group * T::ELEMS, rd);
@@ -160,7 +152,10 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
       tq.store((B ? queries_b : queries_a) + group * T::ELEMS);
       td.store((B ? signals_b : signals_a) + group * T::ELEMS);
     }
-    if (thread < BQ) { (B ? stat_b : stat_a)[group][0][thread] = lse; (B ? stat_b : stat_a)[group][1][thread] = inner; }
+    if (thread < BQ) {
+      (B ? stat_b : stat_a)[group][0][thread] = there ? lse * LOG2E - P_SHIFT<TYPE> : __builtin_inff();
+      (B ? stat_b : stat_a)[group][1][thread] = there ? inner : 0.0f;
+    }
   };
   // Queries q0 .. q0 + 31, block b of a tile; MASKED: perhaps the diagonal's
   auto step = [&](int q0, int b, auto buffer, auto masked_block) INLINE {
@@ -219,8 +214,11 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
     if (now_head < G && mine < w.len) {
       const int q0 = (first + now) * BQ;
       if (q0 > mine && q0 + BQ <= w.len) {
+        constexpr int ONCE = BQ < 64 ? 1 : 2;
+#pragma unroll 1
+        for (int i = 0; i < BQ / 32; i += ONCE)
 #pragma unroll
-        for (int i = 0; i < BQ / 32; ++i) step(q0 + 32 * i, i, buffer, std::false_type{});
+          for (int k = 0; k < ONCE; ++k) step(q0 + 32 * (i + k), i + k, buffer, std::false_type{});
       } else {
 #pragma unroll 1
         for (int i = 0; i < BQ / 32; ++i)
@@ -287,7 +285,23 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
     of[i] = row_frag<TYPE, VEC>(p.dout, (w.start + row) * p.lddo + head * p.hdo, in, i, p.D);
   }
   const long long at = head * p.rows + w.start + (in ? row : 0);
-  const float lse = in ? p.lse[at] * LOG2E : __builtin_inff(), inner = in ? p.inner[at] : 0.0f, c = p.scale * LOG2E;
+  const float lse = in ? p.lse[at] * LOG2E : __builtin_inff(), c = p.scale * LOG2E;
+  // D_i, for the pass over keys too, which comes behind (of fp16 operands it is there already, for the power of two)
+  float inner = 0.0f;
+  if constexpr (TYPE == TYPE_F16) {
+    inner = in ? p.inner[at] : 0.0f;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2 * ND; ++i) {
+      float a[8], b[8];
+      frag_values<TYPE>(of[i], a);
+      frag_values<TYPE>(row_frag<TYPE, VEC>(p.o, (w.start + row) * p.ldo + head * p.ho, in, i, p.D), b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) inner = fmaf(a[e], b[e], inner);
+    }
+    inner += __shfl_xor(inner, 32, 64);
+    if (in && h == 0) p.inner[at] = inner;
+  }
   f32x16 dq[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) dq[d] = zeros16();
@@ -374,9 +388,9 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
 
 template <int TYPE, int ND, bool VEC> hipError_t backward_launch(const AttentionP &p, hipStream_t s) {
   const long long tiles = attention_tiles(p), rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
-  hipLaunchKernelGGL((attention_inner_kernel<TYPE, VEC>), dim3(p.nmost), dim3(256), 0, s, p);
-  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hkv + rest)), dim3(256 * keys_groups(ND)), 0, s, p, (int)(tiles * p.Hkv));
+  if (TYPE == TYPE_F16) hipLaunchKernelGGL((attention_inner_kernel<VEC>), dim3(p.nmost), dim3(256), 0, s, p);
   hipLaunchKernelGGL((attention_queries_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hq + rest)), dim3(256), 0, s, p, (int)(tiles * p.Hq));
+  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hkv + rest)), dim3(256 * keys_groups(ND)), 0, s, p, (int)(tiles * p.Hkv));
   return hipGetLastError();
 }
 template <int TYPE, bool VEC> hipError_t backward_width(const AttentionP &p, hipStream_t s) {

@@ -52,6 +52,14 @@ template <int TYPE> __device__ __forceinline__ Frag8<TYPE> as_frag(const f32x16 
   }
   return f;
 }
+template <int TYPE> __device__ __forceinline__ void frag_values(const Frag8<TYPE> &f, float (&v)[8]) {
+  if constexpr (TYPE == TYPE_F32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = f.v[e];
+  } else {
+    unpack8(f.q, TYPE, v);
+  }
+}
 __device__ __forceinline__ f32x16 zeros16() {
   f32x16 z;
 #pragma unroll
