@@ -65,7 +65,8 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
   constexpr int BK = TYPE == TYPE_F32 ? 32 : 64, NB = BK / 32;
   typedef Tile<TYPE, BK, ND> KV;
   typedef typename KV::E E;
-  constexpr bool DIRECT = VEC && KV::DIRECT;
+  constexpr bool DIRECT = VEC && KV::DIRECT, GROUPED = TYPE != TYPE_F32;
+  constexpr int KSTEPS = 2 * ND % 4 == 0 ? 4 : 2;      // of a group of reads
   // two buffers, by name, so that the compiler can tell what is read from what is on its way
   __shared__ __attribute__((aligned(16))) E keys_a[KV::ELEMS], values_a[KV::ELEMS], keys_b[KV::ELEMS], values_b[KV::ELEMS];
   if ((int)blockIdx.x >= blocks) return zero_rest(p, p.o, TYPE, p.Hq, p.ldo, p.ho, p.lse, blockIdx.x - blocks, REST_BLOCKS);
@@ -118,9 +119,19 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
 #pragma unroll
     for (int b = 0; b < NB; ++b) s[b] = zeros16();
 #pragma unroll
-    for (int i = 0; i < 2 * ND; ++i)
+    for (int i0 = 0; i0 < 2 * ND; i0 += KSTEPS) {
+      Frag8<TYPE> f[NB][KSTEPS];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) mma<TYPE>(s[b], KV::rows(lk, 32 * b, i), qf[i]);
+      for (int i = 0; i < KSTEPS; ++i)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) f[b][i] = KV::rows(lk, 32 * b, i0 + i);
+      if (GROUPED) group_ends();
+#pragma unroll
+      for (int i = 0; i < KSTEPS; ++i)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) mma<TYPE>(s[b], f[b][i], qf[i0 + i]);
+      if (GROUPED) group_ends();
+    }
     if (MASKED) {
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -159,7 +170,10 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      add_cols<MASKED, TYPE, BK, ND>(o, lv, 32 * b, x[b]);
+      Frag8<TYPE> vf[2][ND];
+      read_cols<TYPE, BK, ND>(vf, lv, 32 * b);
+      if (GROUPED) group_ends();
+      add_cols<MASKED, TYPE, ND>(o, vf, x[b]);
       if (MASKED && KV::any(lv, 32 * b)) add_unusual<TYPE, BK, ND>(o, lv, 32 * b, [&](int r) { return k0 + 32 * b + r <= row; });
     }
   };

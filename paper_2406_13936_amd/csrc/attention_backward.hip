@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
   constexpr int BQ = keys_tile(TYPE, ND), GROUPS = keys_groups(ND);
   typedef Tile<TYPE, BQ, ND> T;
   typedef typename T::E E;
-  constexpr bool DIRECT = VEC && T::DIRECT;
+  constexpr bool DIRECT = VEC && T::DIRECT, GROUPED = TYPE != TYPE_F32;
   // two buffers, by name, so that the compiler can tell what is read from what is on its way
   __shared__ __attribute__((aligned(16))) E queries_a[GROUPS * T::ELEMS], signals_a[GROUPS * T::ELEMS], queries_b[GROUPS * T::ELEMS], signals_b[GROUPS * T::ELEMS];
   __shared__ __attribute__((aligned(16))) float stat_a[GROUPS][2][BQ], stat_b[GROUPS][2][BQ];      // lse (to base 2) and D of a tile's queries
@@ -163,28 +163,40 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
     const E *lq = (B ? queries_b : queries_a) + group * T::ELEMS, *ld = (B ? signals_b : signals_a) + group * T::ELEMS;
     const float(*stat)[BQ] = (B ? stat_b : stat_a)[group];
     f32x16 s = zeros16(), dp = zeros16();
+    {
+      Frag8<TYPE> fq[2 * ND], fd[2 * ND];
+      read_rows<TYPE, BQ, ND>(fq, lq, 32 * b);
+      read_rows<TYPE, BQ, ND>(fd, ld, 32 * b);
+      if (GROUPED) group_ends();
 #pragma unroll
-    for (int i = 0; i < 2 * ND; ++i) {
-      mma<TYPE>(s, T::rows(lq, 32 * b, i), kf[i]);
-      mma<TYPE>(dp, T::rows(ld, 32 * b, i), vf[i]);
-    }
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const float4 l4 = *reinterpret_cast<const float4 *>(&stat[0][32 * b + 8 * r4 + 4 * h]);
-        const float4 d4 = *reinterpret_cast<const float4 *>(&stat[1][32 * b + 8 * r4 + 4 * h]);
-        const float l[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 4 * r4 + e;
-          float x = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[e])), y = TYPE == TYPE_F16 ? x * ((dp[r] - dd[e]) * g) : x * (dp[r] - dd[e]);
-          if (MASKED && q0 + 8 * r4 + 4 * h + e < key) x = y = 0.0f;
-          s[r] = x;
-          dp[r] = y;
-        }
+      for (int i = 0; i < 2 * ND; ++i) {
+        mma<TYPE>(s, fq[i], kf[i]);
+        mma<TYPE>(dp, fd[i], vf[i]);
       }
+    }
+    if (GROUPED) group_ends();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 l4 = *reinterpret_cast<const float4 *>(&stat[0][32 * b + 8 * k + 4 * h]);
+      const float4 d4 = *reinterpret_cast<const float4 *>(&stat[1][32 * b + 8 * k + 4 * h]);
+      const float l[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 4 * k + e;
+        float x = __builtin_amdgcn_exp2f(fmaf(s[r], c, -l[e])), y = TYPE == TYPE_F16 ? x * ((dp[r] - dd[e]) * g) : x * (dp[r] - dd[e]);
+        if (MASKED && q0 + 8 * k + 4 * h + e < key) x = y = 0.0f;
+        s[r] = x;
+        dp[r] = y;
+      }
+    }
     const Frag8<TYPE> x[2] = {as_frag<TYPE>(s, 0), as_frag<TYPE>(s, 1)}, y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
-    add_cols<MASKED, TYPE, BQ, ND>(dv, ld, 32 * b, x);
-    add_cols<MASKED, TYPE, BQ, ND>(dk, lq, 32 * b, y);
+    Frag8<TYPE> cq[2][ND], cd[2][ND];
+    if (GROUPED) group_ends();
+    read_cols<TYPE, BQ, ND>(cd, ld, 32 * b);
+    read_cols<TYPE, BQ, ND>(cq, lq, 32 * b);
+    if (GROUPED) group_ends();
+    add_cols<MASKED, TYPE, ND>(dv, cd, x);
+    add_cols<MASKED, TYPE, ND>(dk, cq, y);
     if (MASKED && T::any(ld, 32 * b)) add_unusual<TYPE, BQ, ND>(dv, ld, 32 * b, [&](int r) { return q0 + r >= key; });
     if (MASKED && T::any(lq, 32 * b)) add_unusual<TYPE, BQ, ND>(dk, lq, 32 * b, [&](int r) { return q0 + r >= key; });
   };
@@ -266,7 +278,7 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
   constexpr int BK = TYPE == TYPE_F32 ? 32 : 64;
   typedef Tile<TYPE, BK, ND> T;
   typedef typename T::E E;
-  constexpr bool DIRECT = VEC && T::DIRECT;
+  constexpr bool DIRECT = VEC && T::DIRECT, GROUPED = TYPE != TYPE_F32;
   __shared__ __attribute__((aligned(16))) E keys_a[T::ELEMS], values_a[T::ELEMS], keys_b[T::ELEMS], values_b[T::ELEMS];
   if ((int)blockIdx.x >= blocks) return zero_rest(p, p.dq, TYPE, p.Hq, p.lddq, p.hdq, nullptr, blockIdx.x - blocks, REST_BLOCKS);
   int head, t;
@@ -334,10 +346,22 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
     constexpr bool MASKED = decltype(masked_block)::value;
     const E *lk = decltype(buffer)::value ? keys_b : keys_a, *lv = decltype(buffer)::value ? values_b : values_a;
     f32x16 s = zeros16(), dp = zeros16();
+    {
+      Frag8<TYPE> fk[2 * ND], fv[2 * ND];
+      read_rows<TYPE, BK, ND>(fk, lk, 32 * b);
+      if (GROUPED && ND > 2) group_ends();             // (all at once take the registers that there are)
+      read_rows<TYPE, BK, ND>(fv, lv, 32 * b);
+      if (GROUPED && ND <= 2) group_ends();
 #pragma unroll
-    for (int i = 0; i < 2 * ND; ++i) {
-      mma<TYPE>(s, T::rows(lk, 32 * b, i), qf[i]);
-      mma<TYPE>(dp, T::rows(lv, 32 * b, i), of[i]);
+      for (int i = 0; i < 2 * ND; ++i) mma<TYPE>(s, fk[i], qf[i]);
+#pragma unroll
+      for (int i = 0; i < 2 * ND; ++i) mma<TYPE>(dp, fv[i], of[i]);
+    }
+    Frag8<TYPE> ck[2][ND];
+    if (GROUPED) {
+      group_ends();
+      read_cols<TYPE, BK, ND>(ck, lk, 32 * b);
+      group_ends();
     }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -346,7 +370,8 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
         if (MASKED && kb + 8 * (r >> 2) + 4 * h + (r & 3) > row) dp[r] = 0.0f;
       }
     const Frag8<TYPE> y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
-    add_cols<MASKED, TYPE, BK, ND>(dq, lk, 32 * b, y);
+    if (!GROUPED) read_cols<TYPE, BK, ND>(ck, lk, 32 * b);
+    add_cols<MASKED, TYPE, ND>(dq, ck, y);
     if (MASKED && T::any(lk, 32 * b)) add_unusual<TYPE, BK, ND>(dq, lk, 32 * b, [&](int r) { return kb + r <= row; });
   };
   int j = 0;

@@ -280,17 +280,29 @@ __device__ __forceinline__ Frag8<TYPE> row_frag(const void *base, long long at, 
   return f;
 }
 
-// acc[d] += sum over the tile's rows row0 .. of (row, place) X^T Y: the two fragments of x are rows of the reduction
-template <bool CLEAN, int TYPE, int ROWS, int ND>
-__device__ __forceinline__ void add_cols(f32x16 (&acc)[ND], const typename ElemOf<TYPE>::type *lds, int row0, const Frag8<TYPE> (&x)[2]) {
+// Reads and products in groups: left to itself the compiler puts each read in front of the product that takes it and waits for it there (gradients of
+// 32768 packed rows, 16 heads of 64: TIMES us).  Nothing crosses the line.
+__device__ __forceinline__ void group_ends() { __builtin_amdgcn_sched_barrier(0); }
+
+template <int TYPE, int ROWS, int ND>
+__device__ __forceinline__ void read_rows(Frag8<TYPE> (&f)[2 * ND], const typename ElemOf<TYPE>::type *lds, int row0) {
+#pragma unroll
+  for (int i = 0; i < 2 * ND; ++i) f[i] = Tile<TYPE, ROWS, ND>::rows(lds, row0, i);
+}
+template <int TYPE, int ROWS, int ND>
+__device__ __forceinline__ void read_cols(Frag8<TYPE> (&f)[2][ND], const typename ElemOf<TYPE>::type *lds, int row0) {
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int d = 0; d < ND; ++d) {
-      Frag8<TYPE> f = Tile<TYPE, ROWS, ND>::cols(lds, row0 + 16 * b, d);
-      if (CLEAN) f = usual<TYPE>(f);
-      mma<TYPE>(acc[d], f, x[b]);
-    }
+    for (int d = 0; d < ND; ++d) f[b][d] = Tile<TYPE, ROWS, ND>::cols(lds, row0 + 16 * b, d);
+}
+// acc[d] += sum over 32 rows of (row, place) X^T Y: the two fragments of x have the rows as the reduction's places
+template <bool CLEAN, int TYPE, int ND>
+__device__ __forceinline__ void add_cols(f32x16 (&acc)[ND], const Frag8<TYPE> (&f)[2][ND], const Frag8<TYPE> (&x)[2]) {
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int d = 0; d < ND; ++d) mma<TYPE>(acc[d], CLEAN ? usual<TYPE>(f[b][d]) : f[b][d], x[b]);
 }
 // What add_cols left out with CLEAN: infinities and NaN of the tile's rows row0 .. row0 + 31, in the columns of acc (the lane's own) that the mask
 // leaves to them.  They count as they are: weights are positive or make them NaN.
