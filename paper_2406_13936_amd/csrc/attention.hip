@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
   constexpr int BK = TYPE == TYPE_F32 ? 32 : 64, NB = BK / 32;
   typedef Tile<TYPE, BK, ND> KV;
   typedef typename KV::E E;
-  constexpr bool DIRECT = VEC && KV::DIRECT, GROUPED = TYPE != TYPE_F32;
+  constexpr bool DIRECT = VEC && KV::DIRECT, GROUPED = TYPE != TYPE_F32 && ND <= 2;      // (wider heads have no registers for it)
   constexpr int KSTEPS = 2 * ND % 4 == 0 ? 4 : 2;      // of a group of reads
   // two buffers, by name, so that the compiler can tell what is read from what is on its way
   __shared__ __attribute__((aligned(16))) E keys_a[KV::ELEMS], values_a[KV::ELEMS], keys_b[KV::ELEMS], values_b[KV::ELEMS];

@@ -274,11 +274,11 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
 
 // dq of 128 queries of a head
 template <int TYPE, int ND, bool VEC>
-__global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) attention_queries_kernel(const AttentionP p, const int blocks) {
+__global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : ND <= 2 && TYPE != TYPE_F32 ? 3 : 2) attention_queries_kernel(const AttentionP p, const int blocks) {
   constexpr int BK = TYPE == TYPE_F32 ? 32 : 64;
   typedef Tile<TYPE, BK, ND> T;
   typedef typename T::E E;
-  constexpr bool DIRECT = VEC && T::DIRECT, GROUPED = TYPE != TYPE_F32;
+  constexpr bool DIRECT = VEC && T::DIRECT, GROUPED = TYPE != TYPE_F32 && ND <= 2;      // (wider heads have no registers for it)
   __shared__ __attribute__((aligned(16))) E keys_a[T::ELEMS], values_a[T::ELEMS], keys_b[T::ELEMS], values_b[T::ELEMS];
   if ((int)blockIdx.x >= blocks) return zero_rest(p, p.dq, TYPE, p.Hq, p.lddq, p.hdq, nullptr, blockIdx.x - blocks, REST_BLOCKS);
   int head, t;
@@ -347,22 +347,18 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
     const E *lk = decltype(buffer)::value ? keys_b : keys_a, *lv = decltype(buffer)::value ? values_b : values_a;
     f32x16 s = zeros16(), dp = zeros16();
     {
-      Frag8<TYPE> fk[2 * ND], fv[2 * ND];
-      read_rows<TYPE, BK, ND>(fk, lk, 32 * b);
-      if (GROUPED && ND > 2) group_ends();             // (all at once take the registers that there are)
-      read_rows<TYPE, BK, ND>(fv, lv, 32 * b);
-      if (GROUPED && ND <= 2) group_ends();
+      Frag8<TYPE> f[2 * ND];
+      read_rows<TYPE, BK, ND>(f, lk, 32 * b);
+      if (GROUPED) group_ends();
 #pragma unroll
-      for (int i = 0; i < 2 * ND; ++i) mma<TYPE>(s, fk[i], qf[i]);
+      for (int i = 0; i < 2 * ND; ++i) mma<TYPE>(s, f[i], qf[i]);
+      if (GROUPED) group_ends();
+      read_rows<TYPE, BK, ND>(f, lv, 32 * b);
+      if (GROUPED) group_ends();
 #pragma unroll
-      for (int i = 0; i < 2 * ND; ++i) mma<TYPE>(dp, fv[i], of[i]);
+      for (int i = 0; i < 2 * ND; ++i) mma<TYPE>(dp, f[i], of[i]);
     }
-    Frag8<TYPE> ck[2][ND];
-    if (GROUPED) {
-      group_ends();
-      read_cols<TYPE, BK, ND>(ck, lk, 32 * b);
-      group_ends();
-    }
+    if (GROUPED) group_ends();
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float x = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse));
@@ -370,7 +366,10 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : 2) atte
         if (MASKED && kb + 8 * (r >> 2) + 4 * h + (r & 3) > row) dp[r] = 0.0f;
       }
     const Frag8<TYPE> y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
-    if (!GROUPED) read_cols<TYPE, BK, ND>(ck, lk, 32 * b);
+    Frag8<TYPE> ck[2][ND];
+    if (GROUPED) group_ends();
+    read_cols<TYPE, BK, ND>(ck, lk, 32 * b);
+    if (GROUPED) group_ends();
     add_cols<MASKED, TYPE, ND>(dq, ck, y);
     if (MASKED && T::any(lk, 32 * b)) add_unusual<TYPE, BK, ND>(dq, lk, 32 * b, [&](int r) { return kb + r <= row; });
   };

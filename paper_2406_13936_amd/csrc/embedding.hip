@@ -120,21 +120,26 @@ __device__ __forceinline__ uint32_t sort_key(const EmbeddingP &p, const SortBuff
   return pass == 0 ? token_at(p.tokens, p.wide, base + i, p.V) : t.key[(pass - 1) & 1][base + i];
 }
 
-// Blocks from `first` on fill the table's gradient with zeros
-__device__ __forceinline__ void fill_zeros(float *out, long long n, int first) {
-  const long long step = (long long)(gridDim.x - first) * blockDim.x, i0 = (long long)(blockIdx.x - first) * blockDim.x + threadIdx.x;
+// Blocks from `first` on fill the part-th of `parts` parts of the table's gradient with zeros: each launch of the sort has some to do
+struct Fill { int part, parts; };
+__device__ __forceinline__ void fill_zeros(float *out, long long n, int first, const Fill f) {
   typedef float f4 __attribute__((ext_vector_type(4)));
   const long long head = min((long long)((16 - (reinterpret_cast<uintptr_t>(out) & 15)) & 15) / 4, n), n4 = (n - head) / 4, tail = head + n4 * 4;
+  const long long each = (n4 + f.parts - 1) / f.parts, i0 = f.part * each, i1 = min(i0 + each, n4);
+  const long long step = (long long)(gridDim.x - first) * 256, at = (long long)(blockIdx.x - first) * 256 + threadIdx.x;
   f4 *v = reinterpret_cast<f4 *>(out + head);
   const f4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (long long i = i0; i < n4; i += step) __builtin_nontemporal_store(zero, v + i);
-  if (i0 < head) out[i0] = 0.0f;
-  if (i0 < n - tail) out[tail + i0] = 0.0f;
+#pragma unroll 4
+  for (long long i = i0 + at; i < i1; i += step) __builtin_nontemporal_store(zero, v + i);
+  if (f.part == 0) {
+    if (at < head) out[at] = 0.0f;
+    if (at < n - tail) out[tail + at] = 0.0f;
+  }
 }
 
-__global__ void __launch_bounds__(256) sort_count_kernel(const EmbeddingP p, const SortPlan w, const SortBuffers t, const int pass) {
+__global__ void __launch_bounds__(256) sort_count_kernel(const EmbeddingP p, const SortPlan w, const SortBuffers t, const int pass, const Fill f) {
   __shared__ uint32_t count[1 << DIGIT_BITS];
-  if ((int)blockIdx.x >= p.M * w.nb) return fill_zeros(p.dtable, (long long)p.M * p.V * p.D, p.M * w.nb);
+  if ((int)blockIdx.x >= p.M * w.nb) return fill_zeros(p.dtable, (long long)p.M * p.V * p.D, p.M * w.nb, f);
   const int m = blockIdx.x / w.nb, j = blockIdx.x - m * w.nb, R = 1 << w.bits;
   const long long n = (long long)p.b * p.T, base = m * n, i0 = (long long)j * w.items, i1 = min(i0 + w.items, n);
   for (int d = threadIdx.x; d < R; d += 256) count[d] = 0;
@@ -145,10 +150,10 @@ __global__ void __launch_bounds__(256) sort_count_kernel(const EmbeddingP p, con
 }
 
 // Passes [first, last): of several only where one block has all tokens of its replica (nb == 1).
-__global__ void __launch_bounds__(256) sort_deal_kernel(const EmbeddingP p, const SortPlan w, const SortBuffers t, const int first, const int last) {
+__global__ void __launch_bounds__(256) sort_deal_kernel(const EmbeddingP p, const SortPlan w, const SortBuffers t, const int first, const int last, const Fill f) {
   __shared__ uint32_t at[SORT_WAVES][1 << DIGIT_BITS];      // how many of a digit each wavefront has; then where its next one goes
   __shared__ uint32_t sums[SORT_WAVES];
-  if ((int)blockIdx.x >= p.M * w.nb) return fill_zeros(p.dtable, (long long)p.M * p.V * p.D, p.M * w.nb);
+  if ((int)blockIdx.x >= p.M * w.nb) return fill_zeros(p.dtable, (long long)p.M * p.V * p.D, p.M * w.nb, f);
   const int m = blockIdx.x / w.nb, j = blockIdx.x - m * w.nb, R = 1 << w.bits, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const long long n = (long long)p.b * p.T, base = m * n, i0 = (long long)j * w.items, i1 = min(i0 + w.items, n);
   const int part = w.items / SORT_WAVES;
@@ -244,6 +249,11 @@ SumPlan sum_plan(const EmbeddingP &p) {
   return w;
 }
 
+// lane k's value in a group of G lanes; k is the same for all of them
+template <int G> __device__ __forceinline__ uint32_t of_lane(uint32_t v, int k) {
+  if constexpr (G == 64) return (uint32_t)__builtin_amdgcn_readlane((int)v, k);
+  else return __shfl(v, k, G);
+}
 template <int TYPE, int G, bool VEC>
 __device__ __forceinline__ void add_raw(float (&a)[8], const Raw<TYPE, 1> &r) {
   float f[8];
@@ -269,7 +279,7 @@ template <int TYPE, int G> __device__ __forceinline__ void store_columns(float *
 template <int TYPE, int G, bool VEC, bool NORM>
 __global__ void __launch_bounds__(256) embedding_sums_kernel(const EmbeddingP p, const SumPlan w, const SumBuffers t, const float by) {
   constexpr int GP = 256 / G, U = TYPE == TYPE_F32 ? 4 : 8;
-  const int gid = threadIdx.x / G, l = threadIdx.x % G;
+  const int gid = G == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : threadIdx.x / G, l = threadIdx.x % G;
   const long long item = (long long)blockIdx.x * GP + gid;
   const long long per = (long long)w.chunks * w.tiles;
   if (item >= per * p.M) return;
@@ -288,7 +298,7 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const EmbeddingP p,
     sample_before = i0 > 0 ? t.pos[base + i0 - 1] / (uint32_t)p.T : 0u;
     sample_behind = i0 + count < n ? t.pos[base + i0 + count] / (uint32_t)p.T : 0u;
   }
-  const uint32_t key0 = __shfl(key, 0, G), sample0 = __shfl(sample, 0, G);
+  const uint32_t key0 = of_lane<G>(key, 0), sample0 = of_lane<G>(sample, 0);
   bool word_cut = key0 == key_before, run_cut = word_cut && sample0 == sample_before;      // began before this group's rows
   float word[8], run[8];
 #pragma unroll
@@ -304,15 +314,15 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const EmbeddingP p,
     Raw<TYPE, 1> raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t at = __shfl(pos, min(q0 + u, count - 1), G);
+      const uint32_t at = of_lane<G>(pos, min(q0 + u, count - 1));
       load_raw<TYPE, G, 1, VEC>(raw[u], p.dy, m * p.sy + (long long)at * p.ldy + c0, D, l);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int q = q0 + u;
       if (q >= count) break;
-      const uint32_t k = __shfl(key, q, G), k1 = q + 1 < count ? __shfl(key, q + 1, G) : key_behind;
-      const uint32_t at = __shfl(pos, q, G);
+      const uint32_t k = of_lane<G>(key, q), k1 = q + 1 < count ? of_lane<G>(key, q + 1) : key_behind;
+      const uint32_t at = of_lane<G>(pos, q);
       if (k >= (uint32_t)p.V) {                   // padding, behind all words
         if (NORM && l == 0) share[at] = 0.0f;
         continue;
@@ -320,7 +330,7 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const EmbeddingP p,
       const bool word_ends = k1 != k;
       add_raw<TYPE, G, VEC>(NORM ? run : word, raw[u]);
       if (NORM) {
-        const uint32_t s = __shfl(sample, q, G), s1 = q + 1 < count ? __shfl(sample, q + 1, G) : sample_behind;
+        const uint32_t s = of_lane<G>(sample, q), s1 = q + 1 < count ? of_lane<G>(sample, q + 1) : sample_behind;
         if (word_ends || s1 != s) {
           if (run_cut) {
             store_columns<TYPE, G>(shead, D, l, run, 1.0f);
@@ -348,7 +358,7 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const EmbeddingP p,
     }
   }
   // what goes on behind this group's rows
-  const uint32_t kl = __shfl(key, count - 1, G), sl = __shfl(sample, count - 1, G);
+  const uint32_t kl = of_lane<G>(key, count - 1), sl = of_lane<G>(sample, count - 1);
   if (kl < (uint32_t)p.V && kl == key_behind) {
     if (NORM) {
       if (sl == sample_behind) store_columns<TYPE, G>(run_cut ? shead : stail, D, l, run, 1.0f);
@@ -359,19 +369,29 @@ __global__ void __launch_bounds__(256) embedding_sums_kernel(const EmbeddingP p,
   }
 }
 
-// Words and runs that cross the ends of groups: the group where one begins adds the partial rows of those behind it.  Place of the first sorted
-// row in [from, n) that is of another word (or, by samples, of another sample)
-__device__ __forceinline__ long long run_end(const uint32_t *key, const uint32_t *pos, long long from, long long n, uint32_t k, uint32_t s, uint32_t T, bool by_sample) {
-  long long lo = from, hi = n;                     // rows before lo are of the run, row hi is not
-  while (lo < hi) {
-    const long long mid = (lo + hi) >> 1;
-    const bool in = key[mid] == k && (!by_sample || pos[mid] / T == s);
-    if (in) lo = mid + 1; else hi = mid;
+// Words and runs that cross the ends of groups: the group where one begins adds the partial rows of those behind it.
+// How many of the next groups' first rows (from row i1 on, `rows` apart) are in the run: the lanes look at one each
+template <int G, class F> __device__ __forceinline__ int groups_behind(long long i1, int rows, long long n, F &&in_run) {
+  const int l = threadIdx.x % G, base = threadIdx.x & 63 & ~(G - 1);
+  for (int more = 0;; more += G) {
+    const long long at = i1 + (long long)(more + l) * rows;
+    const uint64_t in = __ballot(at < n && in_run(at)) >> base, all = G == 64 ? ~0ull : (1ull << (G & 63)) - 1;
+    if ((in & all) != all) return more + __ffsll((unsigned long long)(~in & all)) - 1;
   }
-  return lo;
 }
 template <int G>
 __device__ __forceinline__ void add_partials(float (&a)[8], const float *tail, const float *head, int more, int stride, int D, int l) {
+  if (l * 8 + 8 <= D && !((reinterpret_cast<uintptr_t>(tail) | reinterpret_cast<uintptr_t>(head) | (uintptr_t)stride * 4) & 15)) {
+    load8(tail, TYPE_F32, l * 8, a);
+#pragma unroll 4
+    for (int k = 0; k < more; ++k) {
+      float v[8];
+      load8(head, TYPE_F32, (long long)k * stride + l * 8, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) a[e] += v[e];
+    }
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int c = l * 8 + e, at = c < D ? c : 0;
@@ -384,7 +404,7 @@ __device__ __forceinline__ void add_partials(float (&a)[8], const float *tail, c
 template <int G, bool NORM>
 __global__ void __launch_bounds__(256) embedding_join_kernel(const EmbeddingP p, const SumPlan w, const SumBuffers t, const float by) {
   constexpr int GP = 256 / G;
-  const int gid = threadIdx.x / G, l = threadIdx.x % G;
+  const int gid = G == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : threadIdx.x / G, l = threadIdx.x % G;
   const long long item = (long long)blockIdx.x * GP + gid, per = (long long)w.chunks * w.tiles;
   if (item >= per * p.M) return;
   const int m = (int)(item / per), rest = (int)(item - m * per), chunk = rest / w.tiles, tile = rest - chunk * w.tiles;
@@ -392,27 +412,30 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const EmbeddingP p,
   const long long n = (long long)p.b * p.T, base = m * n, i0 = (long long)chunk * w.rows, i1 = i0 + w.rows;
   if (i1 >= n) return;                             // nothing behind the last group
   const uint32_t *key = t.key + base, *pos = t.pos + base;
-  const uint32_t k = key[i1 - 1], T = (uint32_t)p.T;
-  if (k >= (uint32_t)p.V || key[i1] != k) return;
+  const uint32_t k = key[i1 - 1], T = (uint32_t)p.T, next = key[i1], before = i0 > 0 ? key[i0 - 1] : 0xffffffffu;
+  const uint32_t pl = pos[i1 - 1], pn = pos[i1], pb = i0 > 0 ? pos[i0 - 1] : 0u;
+  if (k >= (uint32_t)p.V || next != k) return;
   const long long slot = ((long long)m * w.chunks + chunk) * p.D + c0;
   float a[8];
-  if (i0 == 0 || key[i0 - 1] != k) {               // the word begins here
-    const long long end = run_end(key, pos, i1, n, k, 0u, T, false);
-    const int more = (int)((end - 1) / w.rows - chunk);
+  if (before != k) {                               // the word begins here
+    const int more = groups_behind<G>(i1, w.rows, n, [&](long long i) { return key[i] == k; });
     add_partials<G>(a, t.tail + slot, t.head + slot + p.D, more, p.D, D, l);
     store_columns<TYPE_BF16, G>(p.dtable + ((long long)m * p.V + k) * p.D + c0, D, l, a, by);
   }
   if (NORM) {
-    const uint32_t s = pos[i1 - 1] / T;
-    if (pos[i1] / T == s && (i0 == 0 || key[i0 - 1] != k || pos[i0 - 1] / T != s)) {
-      const long long end = run_end(key, pos, i1, n, k, s, T, true);
-      const int more = (int)((end - 1) / w.rows - chunk);
+    const uint32_t s = pl / T;
+    auto in_run = [&](long long i) { return key[i] == k && pos[i] / T == s; };
+    if (pn / T == s && (before != k || pb / T != s)) {
+      const int more = groups_behind<G>(i1, w.rows, n, in_run);
       add_partials<G>(a, t.stail + slot, t.shead + slot + p.D, more, p.D, D, l);
       float v = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v = fmaf(a[e], a[e], v);
       v = lanes_sum<G>(v);
-      if (l == 0) t.share[((long long)tile * p.M + m) * n + pos[end - 1]] = v;
+      // the run's last row is in the last of them, which has no more rows than the group has lanes
+      const long long last = i1 + (long long)(more - 1) * w.rows;
+      const int in = groups_behind<G>(last, 1, min(n, last + w.rows), in_run);
+      if (l == 0) t.share[((long long)tile * p.M + m) * n + pos[last + in - 1]] = v;
     }
   }
 }
@@ -421,7 +444,7 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const EmbeddingP p,
 template <int TYPE, int G, bool VEC>
 __global__ void __launch_bounds__(256) embedding_inner_kernel(const EmbeddingP p, const SumPlan w, const SumBuffers t) {
   constexpr int GP = 256 / G, U = 4;
-  const int gid = threadIdx.x / G, l = threadIdx.x % G;
+  const int gid = G == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : threadIdx.x / G, l = threadIdx.x % G;
   const long long item = (long long)blockIdx.x * GP + gid;
   if (item >= (long long)p.M * p.b * w.inner_chunks) return;
   const long long i = item / w.inner_chunks, m = i / p.b, n = (long long)p.b * p.T;
@@ -456,24 +479,30 @@ __global__ void __launch_bounds__(256) embedding_inner_kernel(const EmbeddingP p
   if (l == 0) t.inner[item] = a;
 }
 
-// n_i = s^2 sum of the shares of its tokens, q_i = s sum of its parts: a wavefront to a sample
-__global__ void __launch_bounds__(256) embedding_finish_kernel(const EmbeddingP p, const SumPlan w, const SumBuffers t) {
-  const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+// n_i = s^2 sum of the shares of its tokens, q_i = s sum of its parts: W wavefronts to a sample
+template <int W> __global__ void __launch_bounds__(256) embedding_finish_kernel(const EmbeddingP p, const SumPlan w, const SumBuffers t) {
+  __shared__ double sm[W];
+  const long long i = W == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
   if (i >= (long long)p.M * p.b) return;
-  const int l = threadIdx.x & 63;
+  const int l = W == 1 ? threadIdx.x & 63 : threadIdx.x;
   const long long all = (long long)p.M * p.b * p.T, r0 = i * p.T;
-  if (p.n) {
-    double a = 0.0;
+  double a = 0.0, b = 0.0;
+  if (p.n)
     for (int tile = 0; tile < w.tiles; ++tile)
-      for (int k = l; k < p.T; k += 64) a += t.share[tile * all + r0 + k];
+#pragma unroll 4
+      for (int k = l; k < p.T; k += W * 64) a += t.share[tile * all + r0 + k];
+  if (p.q)
+    for (int k = l; k < w.inner_chunks; k += W * 64) b += t.inner[i * w.inner_chunks + k];
+  if constexpr (W == 1) {
     a = wave_sum(a);
-    if (l == 0) p.n[i] = (float)(a * p.scale * p.scale);
+    b = wave_sum(b);
+  } else {
+    a = block_sum<W>(a, sm);
+    b = block_sum<W>(b, sm);
   }
-  if (p.q) {
-    double a = 0.0;
-    for (int k = l; k < w.inner_chunks; k += 64) a += t.inner[i * w.inner_chunks + k];
-    a = wave_sum(a);
-    if (l == 0) p.q[i] = (float)(a * p.scale);
+  if (l == 0) {
+    if (p.n) p.n[i] = (float)(a * p.scale * p.scale);
+    if (p.q) p.q[i] = (float)(b * p.scale);
   }
 }
 
@@ -510,7 +539,10 @@ template <int TYPE, int G, bool VEC> hipError_t backward_launches(const Embeddin
     hipLaunchKernelGGL((embedding_join_kernel<G, false>), dim3((unsigned)blocks), dim3(256), 0, s, p, w, t, by);
   }
   if (p.q) hipLaunchKernelGGL((embedding_inner_kernel<TYPE, G, VEC>), dim3((unsigned)looks), dim3(256), 0, s, p, w, t);
-  if (p.n || p.q) hipLaunchKernelGGL(embedding_finish_kernel, dim3((unsigned)(((long long)p.M * p.b + 3) / 4)), dim3(256), 0, s, p, w, t);
+  const long long samples = (long long)p.M * p.b;
+  if (!p.n && !p.q) return hipGetLastError();
+  if (p.T < 256 || samples > 1 << 20) hipLaunchKernelGGL((embedding_finish_kernel<1>), dim3((unsigned)((samples + 3) / 4)), dim3(256), 0, s, p, w, t);
+  else hipLaunchKernelGGL((embedding_finish_kernel<4>), dim3((unsigned)samples), dim3(256), 0, s, p, w, t);
   return hipGetLastError();
 }
 template <int TYPE, bool VEC> hipError_t backward_group(const EmbeddingP &p, const SumPlan &w, const SumBuffers &t, hipStream_t s) {
@@ -542,12 +574,13 @@ hipError_t launch_embedding_backward(const EmbeddingP &p, void *workspace, hipSt
   const SortBuffers b = {{words(at.key[0]), words(at.key[1])}, {words(at.pos[0]), words(at.pos[1])}, words(at.count)};
   const long long cells = (long long)p.M * p.V * p.D;
   const int sorting = p.M * o.nb, filling = (int)std::max(1LL, std::min(cells / 4096, 2048LL));
+  const dim3 grid(sorting + filling);
   if (o.nb == 1) {
-    hipLaunchKernelGGL(sort_deal_kernel, dim3(sorting + filling), dim3(256), 0, s, p, o, b, 0, o.passes);
+    hipLaunchKernelGGL(sort_deal_kernel, grid, dim3(256), 0, s, p, o, b, 0, o.passes, (Fill{0, 1}));
   } else {
     for (int pass = 0; pass < o.passes; ++pass) {
-      hipLaunchKernelGGL(sort_count_kernel, dim3(sorting + (pass == 0 ? filling : 0)), dim3(256), 0, s, p, o, b, pass);
-      hipLaunchKernelGGL(sort_deal_kernel, dim3(sorting), dim3(256), 0, s, p, o, b, pass, pass + 1);
+      hipLaunchKernelGGL(sort_count_kernel, grid, dim3(256), 0, s, p, o, b, pass, (Fill{2 * pass, 2 * o.passes}));
+      hipLaunchKernelGGL(sort_deal_kernel, grid, dim3(256), 0, s, p, o, b, pass, pass + 1, (Fill{2 * pass + 1, 2 * o.passes}));
     }
   }
   hipError_t e = hipGetLastError();
