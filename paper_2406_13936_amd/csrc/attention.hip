@@ -171,10 +171,10 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       Frag8<TYPE> vf[2][ND];
-      read_cols<TYPE, BK, ND>(vf, lv, 32 * b);
+      read_cols<KV>(vf, lv, 32 * b);
       if (GROUPED) group_ends();
       add_cols<MASKED, TYPE, ND>(o, vf, x[b]);
-      if (MASKED && KV::any(lv, 32 * b)) add_unusual<TYPE, BK, ND>(o, lv, 32 * b, [&](int r) { return k0 + 32 * b + r <= row; });
+      if (MASKED && KV::any(lv, 32 * b)) add_unusual<KV>(o, lv, 32 * b, [&](int r) { return k0 + 32 * b + r <= row; });
     }
   };
   int j = 0;

@@ -86,15 +86,17 @@ template <int TYPE> __device__ __forceinline__ float ds_factor(const AttentionP 
 // Queries of a tile of the pass over keys
 constexpr int keys_tile(int type, int nd) { return type == TYPE_F32 || nd >= 3 ? 32 : 64; }
 
-// Groups of four wavefronts that go through the same keys' queries in turn and add up what they have at the end: a block with the longest work takes half as
-// long, with the same wavefronts to a CU.  (Wider heads take the registers of two; narrower ones' tiles have no room for the exchange.)
-constexpr int keys_groups(int nd) { return nd == 2 ? 2 : 1; }
+// Wavefronts side by side, of 32 keys each, and groups of them that go through the same keys' queries in turn and add up what they have at the end: a block
+// with the longest work takes half as long, with the same wavefronts to a CU.  (Heads of more than 64 values take the registers of two wavefronts; tiles of
+// heads of up to 32 have no room for the exchange.)
+constexpr int keys_waves(int nd) { return nd >= 3 ? 2 : 4; }
+constexpr int keys_groups(int nd) { return nd >= 2 ? 2 : 1; }
 
-// dk and dv of 128 keys
+// dk and dv of 32 keys to a wavefront of a group
 template <int TYPE, int ND, bool VEC>
-__global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attention_keys_kernel(const AttentionP p, const int blocks) {
-  constexpr int BQ = keys_tile(TYPE, ND), GROUPS = keys_groups(ND);
-  typedef Tile<TYPE, BQ, ND> T;
+__global__ void __launch_bounds__(64 * keys_waves(ND) * keys_groups(ND), ND >= 3 ? 1 : 2) attention_keys_kernel(const AttentionP p, const int blocks) {
+  constexpr int BQ = keys_tile(TYPE, ND), GROUPS = keys_groups(ND), WAVES = keys_waves(ND), THREADS = 64 * WAVES, PARTS = ATTENTION_ROWS / (32 * WAVES);
+  typedef Tile<TYPE, BQ, ND, THREADS> T;
   typedef typename T::E E;
   constexpr bool DIRECT = VEC && T::DIRECT, GROUPED = TYPE != TYPE_F32;
   // two buffers, by name, so that the compiler can tell what is read from what is on its way
@@ -106,11 +108,12 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
   }
   int kvh, t;
   head_and_tile(blockIdx.x, p.Hkv, kvh, t);
-  const Work w = find_tile(p, t, ATTENTION_ROWS);
+  const Work w = find_tile(p, t / PARTS, ATTENTION_ROWS);
   if (!w.level) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6 & 3, group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0, h = lane >> 5;
-  const int k0 = (w.tiles - w.level) * ATTENTION_ROWS, mine = k0 + wave * 32, key = mine + (lane & 31), G = p.Hq / p.Hkv;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x % THREADS / 64, group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0, h = lane >> 5;
+  const int k0 = (w.tiles - w.level) * ATTENTION_ROWS + t % PARTS * (32 * WAVES), mine = k0 + wave * 32, key = mine + (lane & 31), G = p.Hq / p.Hkv;
   const bool in = key < w.len;
+  if (k0 >= w.len) return;
   const float f = ds_factor<TYPE>(p), g = f * __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>);
   Frag8<TYPE> kf[2 * ND], vf[2 * ND];
 #pragma unroll
@@ -127,7 +130,7 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
   T tq, td;
   float lse = 0.0f, inner = 0.0f;
   bool there = false;
-  const int thread = threadIdx.x & 255;
+  const int thread = threadIdx.x % THREADS;
   auto fetch = [&](auto buffer, int tile, int of) INLINE {    // of the of-th head
     const int r0 = (first + tile) * BQ, head = kvh * G + of;
     const Rows<TYPE> rq(p.q, (w.start + r0) * p.ldq + head * p.hq, p.ldq, w.len - r0, p.D);
@@ -165,8 +168,8 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
     f32x16 s = zeros16(), dp = zeros16();
     {
       Frag8<TYPE> fq[2 * ND], fd[2 * ND];
-      read_rows<TYPE, BQ, ND>(fq, lq, 32 * b);
-      read_rows<TYPE, BQ, ND>(fd, ld, 32 * b);
+      read_rows<T>(fq, lq, 32 * b);
+      read_rows<T>(fd, ld, 32 * b);
       if (GROUPED) group_ends();
 #pragma unroll
       for (int i = 0; i < 2 * ND; ++i) {
@@ -192,13 +195,13 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
     const Frag8<TYPE> x[2] = {as_frag<TYPE>(s, 0), as_frag<TYPE>(s, 1)}, y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
     Frag8<TYPE> cq[2][ND], cd[2][ND];
     if (GROUPED) group_ends();
-    read_cols<TYPE, BQ, ND>(cd, ld, 32 * b);
-    read_cols<TYPE, BQ, ND>(cq, lq, 32 * b);
+    read_cols<T>(cd, ld, 32 * b);
+    read_cols<T>(cq, lq, 32 * b);
     if (GROUPED) group_ends();
     add_cols<MASKED, TYPE, ND>(dv, cd, x);
     add_cols<MASKED, TYPE, ND>(dk, cq, y);
-    if (MASKED && T::any(ld, 32 * b)) add_unusual<TYPE, BQ, ND>(dv, ld, 32 * b, [&](int r) { return q0 + r >= key; });
-    if (MASKED && T::any(lq, 32 * b)) add_unusual<TYPE, BQ, ND>(dk, lq, 32 * b, [&](int r) { return q0 + r >= key; });
+    if (MASKED && T::any(ld, 32 * b)) add_unusual<T>(dv, ld, 32 * b, [&](int r) { return q0 + r >= key; });
+    if (MASKED && T::any(lq, 32 * b)) add_unusual<T>(dk, lq, 32 * b, [&](int r) { return q0 + r >= key; });
   };
   if constexpr (DIRECT) {
     tq.place_loads(p.ldq, p.D);
@@ -248,18 +251,19 @@ __global__ void __launch_bounds__(256 * keys_groups(ND), ND >= 3 ? 1 : 2) attent
     if (it < rounds) turn(b);
   }
   if constexpr (GROUPS == 2) {                         // one group ends with dk, the other with dv
-    static_assert(GROUPS * T::ELEMS * sizeof(E) >= 4 * 64 * 16 * 4, "four wavefronts' registers of 32 values");
+    constexpr int SIZE = WAVES * 64 * 16, HELD = (int)(GROUPS * T::ELEMS * sizeof(E) / (SIZE * 4));      // values of 32 columns, how many of these a tile's place holds
+    static_assert(2 * HELD >= ND, "room for the exchange");
     const int at = wave * 64 * 16 + lane;
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
-      float *const to = reinterpret_cast<float *>(group ? (d ? queries_b : queries_a) : (d ? signals_b : signals_a));
+      float *const to = reinterpret_cast<float *>(group ? (d / HELD ? queries_b : queries_a) : (d / HELD ? signals_b : signals_a)) + d % HELD * SIZE;
 #pragma unroll
       for (int r = 0; r < 16; ++r) to[at + r * 64] = group ? dk[d][r] : dv[d][r];
     }
     __syncthreads();
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
-      const float *const from = reinterpret_cast<const float *>(group ? (d ? signals_b : signals_a) : (d ? queries_b : queries_a));
+      const float *const from = reinterpret_cast<const float *>(group ? (d / HELD ? signals_b : signals_a) : (d / HELD ? queries_b : queries_a)) + d % HELD * SIZE;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         if (group) dv[d][r] += from[at + r * 64];
@@ -348,12 +352,12 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : ND <= 2
     f32x16 s = zeros16(), dp = zeros16();
     {
       Frag8<TYPE> f[2 * ND];
-      read_rows<TYPE, BK, ND>(f, lk, 32 * b);
+      read_rows<T>(f, lk, 32 * b);
       if (GROUPED) group_ends();
 #pragma unroll
       for (int i = 0; i < 2 * ND; ++i) mma<TYPE>(s, f[i], qf[i]);
       if (GROUPED) group_ends();
-      read_rows<TYPE, BK, ND>(f, lv, 32 * b);
+      read_rows<T>(f, lv, 32 * b);
       if (GROUPED) group_ends();
 #pragma unroll
       for (int i = 0; i < 2 * ND; ++i) mma<TYPE>(dp, f[i], of[i]);
@@ -368,10 +372,10 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : ND <= 2
     const Frag8<TYPE> y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
     Frag8<TYPE> ck[2][ND];
     if (GROUPED) group_ends();
-    read_cols<TYPE, BK, ND>(ck, lk, 32 * b);
+    read_cols<T>(ck, lk, 32 * b);
     if (GROUPED) group_ends();
     add_cols<MASKED, TYPE, ND>(dq, ck, y);
-    if (MASKED && T::any(lk, 32 * b)) add_unusual<TYPE, BK, ND>(dq, lk, 32 * b, [&](int r) { return kb + r <= row; });
+    if (MASKED && T::any(lk, 32 * b)) add_unusual<T>(dq, lk, 32 * b, [&](int r) { return kb + r <= row; });
   };
   int j = 0;
   const int whole = q0 / BK;                           // tiles below every wavefront's diagonal
@@ -411,10 +415,10 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : ND <= 2
 }
 
 template <int TYPE, int ND, bool VEC> hipError_t backward_launch(const AttentionP &p, hipStream_t s) {
-  const long long tiles = attention_tiles(p), rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
+  const long long tiles = attention_tiles(p), key_tiles = tiles * (ATTENTION_ROWS / (32 * keys_waves(ND))), rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
   if (TYPE == TYPE_F16) hipLaunchKernelGGL((attention_inner_kernel<VEC>), dim3(p.nmost), dim3(256), 0, s, p);
   hipLaunchKernelGGL((attention_queries_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hq + rest)), dim3(256), 0, s, p, (int)(tiles * p.Hq));
-  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hkv + rest)), dim3(256 * keys_groups(ND)), 0, s, p, (int)(tiles * p.Hkv));
+  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(key_tiles * p.Hkv + rest)), dim3(64 * keys_waves(ND) * keys_groups(ND)), 0, s, p, (int)(key_tiles * p.Hkv));
   return hipGetLastError();
 }
 template <int TYPE, bool VEC> hipError_t backward_width(const AttentionP &p, hipStream_t s) {

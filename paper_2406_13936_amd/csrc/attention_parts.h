@@ -125,14 +125,16 @@ __device__ __forceinline__ void run_fetch(const void *run, int bytes, uint32_t o
 
 // ROWS rows of 32 ND values.  16-bit: rows of 4, 8 or 16 chunks of 16 bytes, whose places are exchanged by an XOR of the row so that neither reads
 // of 16 rows' same chunk nor transposing reads of four rows' four chunks meet in a bank.  fp32: rows four words apart from a multiple of 64.
-template <int TYPE, int ROWS, int ND> struct Tile {
+template <int TYPE, int ROWS, int ND, int THREADS = 256> struct Tile {
   typedef typename ElemOf<TYPE>::type E;
+  typedef Frag8<TYPE> Frag;
+  static constexpr int WIDTH = ND;
   static constexpr int CH = ND == 1 ? 4 : ND == 2 ? 8 : 16;          // chunks of a row, of which 4 ND hold values
   static constexpr int PER = TYPE == TYPE_F32 ? 4 : 8;               // values of a 16-byte vector
   static constexpr int LD = TYPE == TYPE_F32 ? ((32 * ND + 63) / 64 * 64 + 4) : CH * 8;
   static constexpr int ELEMS = ROWS * LD;
   static constexpr int VECS = ROWS * 32 * ND / PER;                  // vectors of the tile
-  static constexpr int NV = (VECS + 255) / 256;                      // of a thread (256 share a tile)
+  static constexpr int NV = (VECS + THREADS - 1) / THREADS;          // of a thread (THREADS share a tile)
 
   static __device__ __forceinline__ int swizzle(int row) {
     return CH == 16 ? 4 * (row & 3) | (row >> 2 & 3) : CH == 8 ? 4 * (row >> 1 & 1) | (row >> 2 & 3) : row >> 2 & 3;
@@ -147,8 +149,8 @@ template <int TYPE, int ROWS, int ND> struct Tile {
     const int bytes = m.bytes(ROWS);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (threadIdx.x & 255) + i * 256, row = c / (32 * ND / PER), col = c % (32 * ND / PER) * PER;
-      const bool there = col < m.D && (VECS % 256 == 0 || row < ROWS);
+      const int c = threadIdx.x % THREADS + i * THREADS, row = c / (32 * ND / PER), col = c % (32 * ND / PER) * PER;
+      const bool there = col < m.D && (VECS % THREADS == 0 || row < ROWS);
       if constexpr (VEC) {
         q[i] = run_load(m.at, bytes, there ? (uint32_t)(row * (int)m.ld + col) * sizeof(E) : OOB);
       } else {
@@ -169,24 +171,24 @@ template <int TYPE, int ROWS, int ND> struct Tile {
   __device__ __forceinline__ void store(E *lds) const {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (threadIdx.x & 255) + i * 256, row = c / (32 * ND / PER), chunk = c % (32 * ND / PER);
-      if (VECS % 256 == 0 || row < ROWS) *reinterpret_cast<uint4 *>(lds + place(row, chunk)) = q[i];
+      const int c = threadIdx.x % THREADS + i * THREADS, row = c / (32 * ND / PER), chunk = c % (32 * ND / PER);
+      if (VECS % THREADS == 0 || row < ROWS) *reinterpret_cast<uint4 *>(lds + place(row, chunk)) = q[i];
     }
   }
   // The same straight into LDS, 1 KB to a wavefront's load: a lane's place is given, so it fetches the chunk that belongs there
-  static constexpr bool DIRECT = TYPE != TYPE_F32 && ROWS * CH >= 256;
-  static constexpr int ND_LOADS = DIRECT ? ROWS * CH / 256 : 1;
+  static constexpr bool DIRECT = TYPE != TYPE_F32 && ROWS * CH >= THREADS;
+  static constexpr int ND_LOADS = DIRECT ? ROWS * CH / THREADS : 1;
   uint32_t offset[ND_LOADS];                                         // a lane's chunk of each, in bytes
   __device__ __forceinline__ void place_loads(long long ld, int D) {
 #pragma unroll
     for (int i = 0; i < ND_LOADS; ++i) {
-      const int c = ((threadIdx.x >> 6 & 3) * ND_LOADS + i) * 64 + (threadIdx.x & 63), row = c / CH, col = ((c % CH) ^ swizzle(row)) * 8;
+      const int c = (threadIdx.x % THREADS / 64 * ND_LOADS + i) * 64 + (threadIdx.x & 63), row = c / CH, col = ((c % CH) ^ swizzle(row)) * 8;
       offset[i] = col < D ? (uint32_t)(row * (int)ld + col) * 2u : OOB;
     }
   }
   __device__ __forceinline__ void fetch(E *lds, const Rows<TYPE> &m) const {
     const int bytes = m.bytes(ROWS);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x % THREADS / 64);
 #pragma unroll
     for (int i = 0; i < ND_LOADS; ++i)
       run_fetch(m.at, bytes, offset[i], lds + (wave * ND_LOADS + i) * 512);
@@ -284,17 +286,15 @@ __device__ __forceinline__ Frag8<TYPE> row_frag(const void *base, long long at, 
 // 32768 packed rows, 16 heads of 64: TIMES us).  Nothing crosses the line.
 __device__ __forceinline__ void group_ends() { __builtin_amdgcn_sched_barrier(0); }
 
-template <int TYPE, int ROWS, int ND>
-__device__ __forceinline__ void read_rows(Frag8<TYPE> (&f)[2 * ND], const typename ElemOf<TYPE>::type *lds, int row0) {
+template <class T> __device__ __forceinline__ void read_rows(typename T::Frag (&f)[2 * T::WIDTH], const typename T::E *lds, int row0) {
 #pragma unroll
-  for (int i = 0; i < 2 * ND; ++i) f[i] = Tile<TYPE, ROWS, ND>::rows(lds, row0, i);
+  for (int i = 0; i < 2 * T::WIDTH; ++i) f[i] = T::rows(lds, row0, i);
 }
-template <int TYPE, int ROWS, int ND>
-__device__ __forceinline__ void read_cols(Frag8<TYPE> (&f)[2][ND], const typename ElemOf<TYPE>::type *lds, int row0) {
+template <class T> __device__ __forceinline__ void read_cols(typename T::Frag (&f)[2][T::WIDTH], const typename T::E *lds, int row0) {
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int d = 0; d < ND; ++d) f[b][d] = Tile<TYPE, ROWS, ND>::cols(lds, row0 + 16 * b, d);
+    for (int d = 0; d < T::WIDTH; ++d) f[b][d] = T::cols(lds, row0 + 16 * b, d);
 }
 // acc[d] += sum over 32 rows of (row, place) X^T Y: the two fragments of x have the rows as the reduction's places
 template <bool CLEAN, int TYPE, int ND>
@@ -306,16 +306,16 @@ __device__ __forceinline__ void add_cols(f32x16 (&acc)[ND], const Frag8<TYPE> (&
 }
 // What add_cols left out with CLEAN: infinities and NaN of the tile's rows row0 .. row0 + 31, in the columns of acc (the lane's own) that the mask
 // leaves to them.  They count as they are: weights are positive or make them NaN.
-template <int TYPE, int ROWS, int ND, class F>
-__device__ __forceinline__ void add_unusual(f32x16 (&acc)[ND], const typename ElemOf<TYPE>::type *lds, int row0, F &&sees) {
+template <class T, class F>
+__device__ __forceinline__ void add_unusual(f32x16 (&acc)[T::WIDTH], const typename T::E *lds, int row0, F &&sees) {
   const int h = threadIdx.x >> 5 & 1;
   for (int r = 0; r < 32; ++r) {
     if (!sees(r)) continue;
 #pragma unroll
-    for (int d = 0; d < ND; ++d) {
+    for (int d = 0; d < T::WIDTH; ++d) {
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
-        const float v = Tile<TYPE, ROWS, ND>::value(lds, row0 + r, 32 * d + 8 * (k >> 2) + 4 * h + (k & 3));
+        const float v = T::value(lds, row0 + r, 32 * d + 8 * (k >> 2) + 4 * h + (k & 3));
         if (unusual(v)) acc[d][k] += v;
       }
       __builtin_amdgcn_sched_barrier(0);               // (no more than these in registers)

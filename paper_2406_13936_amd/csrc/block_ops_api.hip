@@ -97,7 +97,7 @@ abs_status check_attention(const abs_attention_shape *s, bool backward) {
   if (s->rows > 0x7fffffff) return set_error(ABS_EUNSUPPORTED, "more than 2^31 - 1 rows");
   AttentionP p = attention_args(s);
   p.offsets = s->offsets_type ? s : nullptr;             // (asked whether there are any)
-  if (attention_tiles(p) > 0xff0000 / s->Hq) return set_error(ABS_EUNSUPPORTED, "more heads of 128-row tiles than a grid counts");
+  if (attention_tiles(p) > 0x7f0000 / s->Hq) return set_error(ABS_EUNSUPPORTED, "more heads of 128-row tiles than a grid counts");
   const int heads[8] = {s->Hq, s->Hkv, s->Hkv, s->Hq, s->Hq, s->Hq, s->Hkv, s->Hkv};
   const int64_t ld[8] = {s->ldq, s->ldk, s->ldv, s->ldo, s->lddo, s->lddq, s->lddk, s->lddv};
   const int64_t head[8] = {s->head_q, s->head_k, s->head_v, s->head_o, s->head_do, s->head_dq, s->head_dk, s->head_dv};
