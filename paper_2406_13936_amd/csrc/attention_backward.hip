@@ -4,9 +4,13 @@
 //   dv_j = sum_i p_ij do_i,  dk_j = sum_i ds_ij q_i  (query heads that share the key head add up),  dq_i = sum_j ds_ij k_j
 //
 // Scores are formed again from q and k.  Two kernels, so that every sum has one owner and an order of its own (the same bits every time): one takes 128
-// keys, 32 to a wavefront, and goes through the queries of all heads that share them; the other takes 128 queries and goes through their keys.
-// Together seven products where one kernel would need five, but no sums of dq in memory by atomics.  Scores stay in registers: what is a result of the
-// first products is, rounded, an operand of the second ones, whose other operand is read transposed from the tile that is in LDS anyway.
+// queries, 32 to a wavefront, and goes through their keys (and leaves D_i for the other); the other takes 64 keys and goes through the queries of all
+// heads that share them.  Together seven products where one kernel would need five, but no sums of dq in memory by atomics.  Scores stay in registers: what
+// is a result of the first products is, rounded, an operand of the second ones, whose other operand is read transposed from the tile that is in LDS anyway.
+//
+// Bound by the exponentials and what surrounds them beside the products, which the few wavefronts that fit overlap only in part: of five products 0.50
+// PFLOP/s for 16 heads of 64 over 32768 rows in 40 sequences of 15 to 4211 (588 us: keys 400, queries 260 by profile), 0.55 for one sequence of 8192,
+// 0.57 for heads of 128.
 //
 // fp16 operands hold p and ds in 16 bits with powers of two: p by 2^12 (else values below 2^-14, those of a row of many keys, lose bits), ds by the power that
 // takes twice the largest |do_i| |v_j|, a bound on |ds / a|, to 2^14 at most.
@@ -86,16 +90,16 @@ template <int TYPE> __device__ __forceinline__ float ds_factor(const AttentionP 
 // Queries of a tile of the pass over keys
 constexpr int keys_tile(int type, int nd) { return type == TYPE_F32 || nd >= 3 ? 32 : 64; }
 
-// Wavefronts side by side, of 32 keys each, and groups of them that go through the same keys' queries in turn and add up what they have at the end: a block
-// with the longest work takes half as long, with the same wavefronts to a CU.  (Heads of more than 64 values take the registers of two wavefronts; tiles of
-// heads of up to 32 have no room for the exchange.)
-constexpr int keys_waves(int nd) { return nd >= 3 ? 2 : 4; }
-constexpr int keys_groups(int nd) { return nd >= 2 ? 2 : 1; }
+// A block's wavefronts: two side by side, of 32 keys each, in two groups that go through the same keys' queries in turn and add up what they have at the end.
+// Four side by side in one group made the longest block's work four times as long (16 heads over 4 of 64 values, 32768 rows in 40 sequences: 264 tiles of
+// queries where the average of what a CU's wavefronts take is 115; one sequence of 8192, 16 heads of 128: 1752 us, so 1210), four in two groups left a CU one
+// block, whose wavefronts wait for each other (the first of these 610 us, so 588).
+constexpr int KEYS_WAVES = 2, KEYS_GROUPS = 2, KEYS_PARTS = ATTENTION_ROWS / (32 * KEYS_WAVES);
 
 // dk and dv of 32 keys to a wavefront of a group
 template <int TYPE, int ND, bool VEC>
-__global__ void __launch_bounds__(64 * keys_waves(ND) * keys_groups(ND), ND >= 3 ? 1 : 2) attention_keys_kernel(const AttentionP p, const int blocks) {
-  constexpr int BQ = keys_tile(TYPE, ND), GROUPS = keys_groups(ND), WAVES = keys_waves(ND), THREADS = 64 * WAVES, PARTS = ATTENTION_ROWS / (32 * WAVES);
+__global__ void __launch_bounds__(64 * KEYS_WAVES * KEYS_GROUPS, ND >= 3 ? 1 : 2) attention_keys_kernel(const AttentionP p, const int blocks) {
+  constexpr int BQ = keys_tile(TYPE, ND), GROUPS = KEYS_GROUPS, WAVES = KEYS_WAVES, THREADS = 64 * WAVES;
   typedef Tile<TYPE, BQ, ND, THREADS> T;
   typedef typename T::E E;
   constexpr bool DIRECT = VEC && T::DIRECT, GROUPED = TYPE != TYPE_F32;
@@ -108,10 +112,10 @@ __global__ void __launch_bounds__(64 * keys_waves(ND) * keys_groups(ND), ND >= 3
   }
   int kvh, t;
   head_and_tile(blockIdx.x, p.Hkv, kvh, t);
-  const Work w = find_tile(p, t / PARTS, ATTENTION_ROWS);
+  const Work w = find_tile(p, t / KEYS_PARTS, ATTENTION_ROWS);
   if (!w.level) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x % THREADS / 64, group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0, h = lane >> 5;
-  const int k0 = (w.tiles - w.level) * ATTENTION_ROWS + t % PARTS * (32 * WAVES), mine = k0 + wave * 32, key = mine + (lane & 31), G = p.Hq / p.Hkv;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x % THREADS / 64, group = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS), h = lane >> 5;
+  const int k0 = (w.tiles - w.level) * ATTENTION_ROWS + t % KEYS_PARTS * (32 * WAVES), mine = k0 + wave * 32, key = mine + (lane & 31), G = p.Hq / p.Hkv;
   const bool in = key < w.len;
   if (k0 >= w.len) return;
   const float f = ds_factor<TYPE>(p), g = f * __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>);
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(64 * keys_waves(ND) * keys_groups(ND), ND >= 3
     turn(a);
     if (it < rounds) turn(b);
   }
-  if constexpr (GROUPS == 2) {                         // one group ends with dk, the other with dv
+  {                                                    // one group ends with dk, the other with dv
     constexpr int SIZE = WAVES * 64 * 16, HELD = (int)(GROUPS * T::ELEMS * sizeof(E) / (SIZE * 4));      // values of 32 columns, how many of these a tile's place holds
     static_assert(2 * HELD >= ND, "room for the exchange");
     const int at = wave * 64 * 16 + lane;
@@ -272,8 +276,8 @@ __global__ void __launch_bounds__(64 * keys_waves(ND) * keys_groups(ND), ND >= 3
     }
   }
   if (!in) return;
-  if (GROUPS == 1 || !group) store_row<TYPE, ND, VEC>(p.dk, (w.start + key) * p.lddk + kvh * p.hdk, dk, p.scale / f, p.D);
-  if (GROUPS == 1 || group) store_row<TYPE, ND, VEC>(p.dv, (w.start + key) * p.lddv + kvh * p.hdv, dv, __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>), p.D);
+  if (!group) store_row<TYPE, ND, VEC>(p.dk, (w.start + key) * p.lddk + kvh * p.hdk, dk, p.scale / f, p.D);
+  else store_row<TYPE, ND, VEC>(p.dv, (w.start + key) * p.lddv + kvh * p.hdv, dv, __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>), p.D);
 }
 
 // dq of 128 queries of a head
@@ -415,10 +419,10 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : ND <= 2
 }
 
 template <int TYPE, int ND, bool VEC> hipError_t backward_launch(const AttentionP &p, hipStream_t s) {
-  const long long tiles = attention_tiles(p), key_tiles = tiles * (ATTENTION_ROWS / (32 * keys_waves(ND))), rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
+  const long long tiles = attention_tiles(p), key_tiles = tiles * KEYS_PARTS, rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
   if (TYPE == TYPE_F16) hipLaunchKernelGGL((attention_inner_kernel<VEC>), dim3(p.nmost), dim3(256), 0, s, p);
   hipLaunchKernelGGL((attention_queries_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hq + rest)), dim3(256), 0, s, p, (int)(tiles * p.Hq));
-  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(key_tiles * p.Hkv + rest)), dim3(64 * keys_waves(ND) * keys_groups(ND)), 0, s, p, (int)(key_tiles * p.Hkv));
+  hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(key_tiles * p.Hkv + rest)), dim3(64 * KEYS_WAVES * KEYS_GROUPS), 0, s, p, (int)(key_tiles * p.Hkv));
   return hipGetLastError();
 }
 template <int TYPE, bool VEC> hipError_t backward_width(const AttentionP &p, hipStream_t s) {

@@ -433,3 +433,57 @@ def test_gradients_against_differences():
         # 3840 results of about 1, off by some 40 U32 each, over e; e^2 / 6 of a third derivative: of 240 rows' weights along scores that d changes by
         # about 3, cubed
         assert abs(slope - want) <= math.sqrt(3840) * 40 * U32 / e * 4 + e * e / 6 * 240 * 27
+
+
+# ---- many and long sequences --------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("long,D", [(5000, 24), (140000, 8)])
+def test_many_sequences_beside_a_long_one(long, D):
+    """More than 64 sequences take a list of tiles, in which one of more than 32 tiles is written by a wavefront, and more than 1024 share places.  A sequence's
+    results are the same bits alone."""
+    import torch
+    A = _A()
+    lens = [3, 0, 130, 1] * 20 + [long] + [64, 2] * 5
+    ends = _ends(lens)
+    q, k, v, do = _tensors(ends[-1], 2, 1, D, "bf16", 3)
+    off = torch.tensor(ends, device="cuda")
+    o, lse = A.causal_attention(q, k, v, offsets=off)
+    grads = A.causal_attention_backward(do, q, k, v, o, lse, offsets=off)
+    for a, e in zip(ends, ends[1:]):
+        if e - a not in (long, 130):
+            continue
+        one = [t[a:e] for t in (q, k, v, do)]
+        o1, lse1 = A.causal_attention(*one[:3])
+        assert torch.equal(o[a:e], o1) and torch.equal(lse[:, a:e], lse1)
+        for g, g1 in zip(grads, A.causal_attention_backward(one[3], *one[:3], o1, lse1)):
+            assert torch.equal(g[a:e], g1)
+    a = ends[80]
+    for i in (0, 1, long // 2, long - 1):            # some rows of the long one by the definition
+        s = (q[a + i].double() @ k[a:a + i + 1, 0].double().T) / math.sqrt(D)
+        want = torch.softmax(s, 1) @ v[a:a + i + 1, 0].double()
+        # half a step for each weight and the result; scores of these inputs are off by less than 2^-18, sums by i U32
+        bound = (torch.softmax(s, 1) @ v[a:a + i + 1, 0].double().abs()) * (2 * U["bf16"] + 2.0 ** -17 + (i + 8) * U32)
+        assert ((o[a + i].double() - want).abs() <= bound).all()
+
+
+@gpu
+def test_rows_beyond_32_bits():
+    """Heads whose rows end beyond 2^31 values and 2^32 bytes."""
+    import torch
+    A = _A()
+    R, Hq, D, n = 280_000, 64, 128, 100
+    q = torch.zeros((R, Hq, D), device="cuda", dtype=torch.bfloat16)
+    k, v = torch.zeros((2, R, 1, D), device="cuda", dtype=torch.bfloat16)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    for t in (q, k, v):
+        t[-n:] = torch.randn(t[-n:].shape, device="cuda", generator=gen).to(torch.bfloat16)
+    do = q.flip(1)
+    off = torch.arange(0, R + 1, n, dtype=torch.int64, device="cuda")
+    o, lse = A.causal_attention(q, k, v, offsets=off)
+    grads = A.causal_attention_backward(do, q, k, v, o, lse, offsets=off)
+    one = [t[-n:].contiguous() for t in (q, k, v, do)]
+    o1, lse1 = A.causal_attention(*one[:3])
+    assert torch.equal(o[-n:], o1) and torch.equal(lse[:, -n:], lse1)
+    for g, g1 in zip(grads, A.causal_attention_backward(one[3], *one[:3], o1, lse1)):
+        assert torch.equal(g[-n:], g1) and (g[:-n] == 0).all()

@@ -1,0 +1,128 @@
+"""The operators of a language model's blocks together, as a training step uses them: embedding, norms behind residuals, attention with grouped heads over
+packed documents, their gradients and statistics, between linear layers that torch computes.  Against autograd of the definition in 64 bits."""
+import pytest
+
+U32 = 2.0 ** -24
+pytestmark = pytest.mark.gpu
+
+
+def _setup(M, b, T, V, D, Hq, Hkv, hd, seed):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    w = dict(table=r(M, V, D) / D ** 0.5, n1=1 + 0.1 * r(M, D), n2=1 + 0.1 * r(M, D), qkv=r(M, D, (Hq + 2 * Hkv) * hd) / D ** 0.5, out=r(M, Hq * hd, D) / (Hq * hd) ** 0.5)
+    tok = torch.randint(0, V, (M, b, T), device="cuda", generator=gen)
+    tok[:, 0, T - 3:] = -1                           # padding
+    signal = r(M, b, T, D)
+    return w, tok, signal
+
+
+def _step(A, w, tok, signal, off, Hq, Hkv, hd, scale):
+    """One pass forward and back; linear layers' gradients are means over the samples too."""
+    import torch
+    M, b, T = tok.shape
+    D = signal.shape[-1]
+    x = A.embedding(tok, w["table"], scale=scale)
+    y1, h1, r1 = A.rms_norm(x, w["n1"])
+    qkv = torch.matmul(y1.view(M, b * T, D), w["qkv"]).view(M * b * T, Hq + 2 * Hkv, hd)
+    q, k, v = torch.split(qkv, [Hq, Hkv, Hkv], 1)
+    o, lse = A.causal_attention(q, k, v, offsets=off)
+    branch = torch.matmul(o.view(M, b * T, Hq * hd), w["out"]).view(M, b, T, D)
+    y2, h2, r2 = A.rms_norm(branch, w["n2"], residual=x)
+    dh2, dn2, n2, q2 = A.rms_norm_backward(signal, h2, w["n2"], r2, want_norms=True, want_inner=True)
+    db = dh2.view(M, b * T, D)
+    dout = torch.matmul(o.view(M, b * T, -1).transpose(1, 2).contiguous(), db) / b
+    do = torch.matmul(db, w["out"].transpose(1, 2).contiguous()).view(M * b * T, Hq, hd)
+    grads = torch.empty_like(qkv)                    # side by side, as the projection's backward pass wants them
+    A.causal_attention_backward(do, q, k, v, o, lse, offsets=off, out=tuple(torch.split(grads, [Hq, Hkv, Hkv], 1)))
+    flat = grads.view(M, b * T, -1)
+    dqkv = torch.matmul(y1.view(M, b * T, D).transpose(1, 2).contiguous(), flat) / b
+    dy1 = torch.matmul(flat, w["qkv"].transpose(1, 2).contiguous()).view(M, b, T, D)
+    dx, dn1, n1, q1 = A.rms_norm_backward(dy1, h1, w["n1"], r1, dh=dh2, want_norms=True, want_inner=True)
+    dtable, nt, qt = A.embedding_backward(dx, tok, w["table"].shape[1], scale=scale, want_norms=True, want_inner=True)
+    return y2, dict(table=dtable, n1=dn1, n2=dn2, qkv=dqkv, out=dout), dict(table=(nt, qt), n1=(n1, q1), n2=(n2, q2))
+
+
+def _definition(w, tok, ends, Hq, Hkv, hd, scale):
+    import torch
+    M, b, T = tok.shape
+    V, D = w["table"].shape[1:]
+    ok = ((tok >= 0) & (tok < V)).double()[..., None]
+    x = torch.stack([w["table"][m][tok[m].clamp(0, V - 1)] for m in range(M)]) * scale * ok
+    norm = lambda h, g: h / torch.sqrt((h * h).mean(-1, keepdim=True) + 1e-6) * g[:, None, None]  # noqa: E731
+    y = norm(x, w["n1"])
+    qkv = torch.einsum("mbtd,mde->mbte", y, w["qkv"]).reshape(M * b * T, Hq + 2 * Hkv, hd)
+    q, k, v = torch.split(qkv, [Hq, Hkv, Hkv], 1)
+    pieces = [torch.zeros((ends[0], Hq, hd), dtype=torch.float64)]
+    for a, e in zip(ends, ends[1:]):
+        kk, vv = (t[a:e].repeat_interleave(Hq // Hkv, 1) for t in (k, v))
+        s = torch.einsum("ihd,jhd->hij", q[a:e], kk) / hd ** 0.5
+        s = s.masked_fill(~torch.ones(e - a, e - a).tril().bool(), float("-inf"))
+        pieces.append(torch.einsum("hij,jhd->ihd", torch.softmax(s, -1), vv))
+    o = torch.cat(pieces).reshape(M, b, T, Hq * hd)
+    return norm(torch.einsum("mbte,med->mbtd", o, w["out"]) + x, w["n2"])
+
+
+def test_a_block_forward_and_back_with_statistics():
+    import torch
+    import paper_2406_13936_amd as A
+    M, b, T, V, D, Hq, Hkv, hd, scale = 2, 3, 40, 50, 48, 4, 2, 16, 3.0
+    w, tok, signal = _setup(M, b, T, V, D, Hq, Hkv, hd, 0)
+    # documents within samples: some end where samples do
+    ends = sorted(set(range(0, M * b * T + 1, T)) | {7, 25, 61, 100, 130, 131, 201})
+    off = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    y, grads, stats = _step(A, w, tok, signal, off, Hq, Hkv, hd, scale)
+    w64 = {n: t.double().cpu().requires_grad_(True) for n, t in w.items()}
+    want = _definition(w64, tok.cpu(), ends, Hq, Hkv, hd, scale)
+    # each of the ten operators and products on the way sums at most b T = 120 terms in fp32, off by 128 U32 of the terms' sizes; norms and softmaxes of these inputs
+    # pass relative errors on at most fivefold, terms are at most five times what they add up to
+    tol = 10 * 128 * U32 * 25
+    assert float(((y.double().cpu() - want).norm() / want.norm()).detach()) < tol
+    c = signal.double().cpu()
+    each = {n: torch.zeros((M, b) + tuple(t.shape[1:]), dtype=torch.float64) for n, t in w.items()}
+    for i in range(b):                               # per-sample gradients, one backward pass to a sample (replicas are independent)
+        g = torch.autograd.grad((want[:, i] * c[:, i]).sum(), list(w64.values()), retain_graph=True)
+        for n, v in zip(w64, g):
+            each[n][:, i] = v
+    for n in w:
+        bar = each[n].mean(1)
+        assert float((grads[n].double().cpu() - bar).norm() / bar.norm()) < tol, n
+        if n in stats:
+            flat, fbar = each[n].flatten(2), bar.flatten(1)
+            ni, qi = flat.square().sum(-1), (flat * fbar[:, None]).sum(-1)
+            assert ((stats[n][0].double().cpu() - ni).abs() <= 2 * tol * ni).all(), n
+            assert ((stats[n][1].double().cpu() - qi).abs() <= 2 * tol * ni.sqrt() * fbar.norm(dim=-1)[:, None]).all(), n
+
+
+def test_steps_of_a_block_in_a_graph():
+    """Forward, back, update and the replicas' average captured once and replayed: the same bits as the calls themselves."""
+    import torch
+    import paper_2406_13936_amd as A
+    M, b, T, V, D, Hq, Hkv, hd = 2, 2, 30, 40, 32, 2, 1, 16
+    w, tok, signal = _setup(M, b, T, V, D, Hq, Hkv, hd, 1)
+    off = torch.arange(0, M * b * T + 1, T, dtype=torch.int32, device="cuda")
+    mom = {n: torch.zeros_like(w[n]) for n in ("qkv", "out")}
+
+    def step(w, mom):
+        y, grads, _ = _step(A, w, tok, signal, off, Hq, Hkv, hd, 2.0)
+        for n in ("table", "n1", "n2"):
+            w[n].sub_(grads[n], alpha=0.01)
+        for n in ("qkv", "out"):
+            A.muon_step(w[n], grads[n], mom[n], 0.02)
+        return y
+    eager = ({n: t.clone() for n, t in w.items()}, {n: t.clone() for n, t in mom.items()})
+    step({n: t.clone() for n, t in w.items()}, {n: t.clone() for n, t in mom.items()})       # (workspaces and libraries before the capture)
+    graph = torch.cuda.CUDAGraph()
+    kept = ({n: t.clone() for n, t in w.items()}, {n: t.clone() for n, t in mom.items()})
+    with torch.cuda.graph(graph):
+        y = step(w, mom)
+    for n in w:
+        w[n].copy_(kept[0][n])
+    for n in mom:
+        mom[n].copy_(kept[1][n])
+    for _ in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step(*eager)
+        assert torch.equal(y, want)
+        assert all(torch.equal(w[n], eager[0][n]) for n in w) and all(torch.equal(mom[n], eager[1][n]) for n in mom)
