@@ -3,11 +3,11 @@
 //   y_t = s table[token_t];   g_i = s sum_t dy_t e(token_t)^T of sample i (T tokens),  gbar = mean_i g_i,  n_i = ||g_i||^2,  q_i = <g_i, gbar>
 //   A token outside the table is padding: zeros, no gradient.
 //
-// Forward is bound by memory (4 x 8192 rows of 1024 from fp32 tables of 32000 words into bf16: FWD us, of 20 that the bytes take).  The gradient sorts the tokens of a replica (stable, so that equal ones stay in the order of the samples) and
+// Forward is bound by memory (4 x 8192 rows of 1024 from fp32 tables of 32000 words into bf16: 27.6 us, of 20 that the bytes take).  The gradient sorts the tokens of a replica (stable, so that equal ones stay in the order of the samples) and
 // sums runs of rows of dy in that order: no atomics on values, the same bits every time.  What it moves: dy once (twice with q_i, whose
 // second look reads the finished gbar), the table's gradient once; zeros for words that no token names are written while the sort, which is
 // all latency, is under way (the same sizes with n_i and q_i: 194 us, of them 118 the fill and the sort, 28 sums, 12 join, 24 the second look; the fill alone
-would be 105).
+// would be 85).
 //   sort      stable passes of up to 11 bits of the key: counts per block, then every block adds up the counts before its own and
 //             deals out its part, wavefront after wavefront; one launch for all passes where one block takes a replica's tokens
 //   sums      a group of lanes takes up to 64 sorted rows: runs of one (word, sample) give n_i's shares, runs of a word gbar's row; what

@@ -19,29 +19,33 @@ namespace {
 constexpr float E4M3_MAX = 448.0f;
 constexpr float SMALLEST_SCALE = 0x1p-100f;      // (its inverse is finite)
 
-__device__ __forceinline__ float scale_of(float rstd, float most) {
-  const float c = rstd * most / E4M3_MAX;        // NaN of a row with NaN or infinities stays
+__device__ __forceinline__ float scale_of(float rstd, double most) {
+  const float c = rstd * (float)most / E4M3_MAX; // NaN of a row with NaN or infinities stays
   return c < SMALLEST_SCALE ? SMALLEST_SCALE : c;
 }
+// y / c = 448 h w / max |h w|, in which r has cancelled, is rounded to e4m3 as if it were exact, ties to even: products of two 16-bit values are often just
+// between two of e4m3's, and in fp32 one value in a million came out on the other side of a border.
+struct Quotient {
+  double by, most;                               // 448 / max |h w|, or r / c where c is the smallest scale; then there is no `most`
+  __device__ __forceinline__ Quotient(float rstd, float c, double most_) : by(c > SMALLEST_SCALE ? (double)E4M3_MAX / most_ : (double)rstd / (double)c), most(c > SMALLEST_SCALE ? most_ : 0.0) {}
+  // in fp32, cut off, the last bit set if anything was: as good as the value itself to a rounding to fewer bits
+  __device__ __forceinline__ float of(double hw) const {
+    const float f = (float)(hw * by);            // at most half a step of fp32 away
+    // |f| most - 448 |h w|: both products are exact (51 bits of the second, and one rounding of the difference keeps its sign)
+    const double over = fma(fabs((double)f), most, -(double)E4M3_MAX * fabs(hw));
+    if (most == 0.0 || over == 0.0 || !(fabsf(f) < __builtin_inff())) return f;
+    const uint32_t u = __float_as_uint(f);
+    return __uint_as_float((over > 0.0 ? u - 1 : u) | 1u);
+  }
+};
 // four values in e4m3, to the nearest, ties to even (the machine's conversion)
 __device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float d) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
-template <int G> __device__ __forceinline__ float lanes_max(float v) {
-  v = fmaxf(v, dpp<0xB1>(v));
-  v = fmaxf(v, dpp<0x4E>(v));
-  v = fmaxf(v, dpp<0x141>(v));
-  v = fmaxf(v, dpp<0x140>(v));
-  if (G == 64) {
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    v = fmaxf(v, __shfl_xor(v, 32, 64));
-  }
-  return v;
-}
-// Sum and, if MAX, maximum over the group; sm: 4 floats to a wavefront, `turn` as in group_sums
-template <int G, bool MAX> __device__ __forceinline__ void group_sum_max(float &s, float &m, float *sm, int turn) {
+// Sum and, if MAX, maximum over the group; sm: 6 floats to a wavefront, `turn` as in group_sums
+template <int G, bool MAX> __device__ __forceinline__ void group_sum_max(float &s, double &m, float *sm, int turn) {
   if (!MAX) {
     float v[1] = {s};
     group_sums<G, 1>(v, sm, turn);
@@ -50,17 +54,19 @@ template <int G, bool MAX> __device__ __forceinline__ void group_sum_max(float &
   }
   constexpr int W = G > 64 ? G / 64 : 4;
   s = lanes_sum<(G < 64 ? G : 64)>(s);
-  m = lanes_max<(G < 64 ? G : 64)>(m);
-  if (G <= 64) return;
-  float *at = sm + (turn & 1) * 2 * W;
-  if ((threadIdx.x & 63) == 0) { at[threadIdx.x >> 6] = s; at[W + (threadIdx.x >> 6)] = m; }
-  __syncthreads();
-  s = m = 0.0f;
 #pragma unroll
-  for (int h = 0; h < W; h += 4) {
-    const float4 f = *reinterpret_cast<const float4 *>(at + h), g = *reinterpret_cast<const float4 *>(at + W + h);
-    s += (f.x + f.y) + (f.z + f.w);
-    m = fmaxf(m, fmaxf(fmaxf(g.x, g.y), fmaxf(g.z, g.w)));
+  for (int o = 1; o < (G < 64 ? G : 64); o <<= 1) m = fmax(m, __shfl_xor(m, o, 64));
+  if (G <= 64) return;
+  double *most = reinterpret_cast<double *>(sm) + (turn & 1) * W;
+  float *at = sm + 4 * W + (turn & 1) * W;
+  if ((threadIdx.x & 63) == 0) { at[threadIdx.x >> 6] = s; most[threadIdx.x >> 6] = m; }
+  __syncthreads();
+  s = 0.0f;
+  m = 0.0;
+#pragma unroll
+  for (int h = 0; h < W; h += 4) {               // (in the order of group_sums: the same bits)
+    s += (at[h] + at[h + 1]) + (at[h + 2] + at[h + 3]);
+    m = fmax(m, fmax(fmax(most[h], most[h + 1]), fmax(most[h + 2], most[h + 3])));
   }
 }
 
@@ -90,7 +96,7 @@ __device__ __forceinline__ void store_e4m3(void *p, long long at, int D, int l, 
 template <int TYPE, int G, int V, bool VEC, bool ADD, bool EIGHT>
 __global__ void __launch_bounds__(ln_threads(G)) rms_forward_kernel(const RmsNormP p, const int nb) {
   constexpr int GP = ln_threads(G) / G;
-  __shared__ __attribute__((aligned(16))) float sm[ln_threads(G) / 16];
+  __shared__ __attribute__((aligned(16))) float sm[ln_threads(G) / 64 * 6];
   const int m = blockIdx.x / nb, j = blockIdx.x - m * nb, gid = threadIdx.x / G, l = threadIdx.x % G;
   const long long rows = (long long)p.b * p.T, step = (long long)nb * GP;
   const int D = p.D;
@@ -112,7 +118,8 @@ __global__ void __launch_bounds__(ln_threads(G)) rms_forward_kernel(const RmsNor
       load_raw<TYPE, G, V, VEC>(nx, p.x, m * p.sx + (r + step) * p.ldx, D, l);
       if (ADD) load_raw<TYPE, G, V, VEC>(nr, p.res, m * p.sr + (r + step) * p.ldr, D, l);
     }
-    float h[V][8], s = 0.0f, most = 0.0f;
+    float h[V][8], s = 0.0f;
+    double most = 0.0;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       raw_vals<TYPE, V>(rx, v, h[v]);
@@ -127,13 +134,13 @@ __global__ void __launch_bounds__(ln_threads(G)) rms_forward_kernel(const RmsNor
 #pragma unroll
       for (int e = 0; e < 8; ++e) {               // (zeros beyond the row)
         s = fmaf(h[v][e], h[v][e], s);
-        if (EIGHT) most = fmaxf(most, fabsf(h[v][e] * w[v][e]));
+        if (EIGHT) most = fmax(most, fabs((double)h[v][e] * w[v][e]));
       }
     }
     group_sum_max<G, EIGHT>(s, most, sm, turn++);
     const float rstd = 1.0f / sqrtf(s / n + p.eps);
-    float c = 0.0f, by = rstd;
-    if (EIGHT) { c = scale_of(rstd, most); by = rstd * (1.0f / c); }
+    const float c = EIGHT ? scale_of(rstd, most) : 0.0f;
+    const Quotient quotient(rstd, c, EIGHT ? most : 1.0);
     if (l == 0) {
       if (p.rstd) p.rstd[m * rows + r] = rstd;
       if (EIGHT) p.scale[m * rows + r] = c;
@@ -141,7 +148,7 @@ __global__ void __launch_bounds__(ln_threads(G)) rms_forward_kernel(const RmsNor
 #pragma unroll
     for (int v = 0; v < V; ++v) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[v][e] = EIGHT ? (h[v][e] * w[v][e]) * by : (h[v][e] * rstd) * w[v][e];
+      for (int e = 0; e < 8; ++e) h[v][e] = EIGHT ? quotient.of((double)h[v][e] * w[v][e]) : (h[v][e] * rstd) * w[v][e];
       if (EIGHT) store_e4m3<TYPE, G>(p.y, m * p.sy + r * p.ldy, D, l, v, h[v], whole);
       else store_vals<TYPE, G, VEC>(p.y, m * p.sy + r * p.ldy, D, l, v, h[v]);
     }
@@ -152,10 +159,11 @@ __global__ void __launch_bounds__(ln_threads(G)) rms_forward_kernel(const RmsNor
 // A launch takes RMS_LONG_ROWS rows: a grid counts its threads in 32 bits.
 constexpr int RMS_LONG_ROWS = 1 << 18;
 __global__ void __launch_bounds__(256) rms_forward_long_kernel(const RmsNormP p, const int eight, const long long first) {
-  __shared__ __attribute__((aligned(16))) float sm[16];
+  __shared__ __attribute__((aligned(16))) float sm[24];
   const long long rows = (long long)p.b * p.T, i = first + blockIdx.x, m = i / rows, r = i - m * rows;
   const long long xa = m * p.sx + r * p.ldx, ra = m * p.sr + r * p.ldr, ha = m * p.sh + r * p.ldh, ya = m * p.sy + r * p.ldy, pa = m * p.D;
-  float s = 0.0f, most = 0.0f;
+  float s = 0.0f;
+  double most = 0.0;
   for (int c = threadIdx.x; c < p.D; c += 256) {
     float h = load_as_f32(p.x, p.type, xa + c);
     if (p.res) {
@@ -164,17 +172,18 @@ __global__ void __launch_bounds__(256) rms_forward_long_kernel(const RmsNormP p,
       h = load_as_f32(p.h, p.type, ha + c);
     }
     s = fmaf(h, h, s);
-    if (eight) most = fmaxf(most, fabsf(h * load_as_f32(p.w, p.ptype, pa + c)));
+    if (eight) most = fmax(most, fabs((double)h * load_as_f32(p.w, p.ptype, pa + c)));
   }
   group_sum_max<256, true>(s, most, sm, 0);
-  const float rstd = 1.0f / sqrtf(s / (float)p.D + p.eps), scale = scale_of(rstd, most), by = rstd * (1.0f / scale);
+  const float rstd = 1.0f / sqrtf(s / (float)p.D + p.eps), scale = scale_of(rstd, most);
+  const Quotient quotient(rstd, scale, most);
   if (threadIdx.x == 0) {
     if (p.rstd) p.rstd[m * rows + r] = rstd;
     if (eight) p.scale[m * rows + r] = scale;
   }
   for (int c = threadIdx.x; c < p.D; c += 256) {
     const float h = p.res ? load_as_f32(p.h, p.type, ha + c) : load_as_f32(p.x, p.type, xa + c), w = load_as_f32(p.w, p.ptype, pa + c);
-    if (eight) static_cast<uint8_t *>(p.y)[ya + c] = (uint8_t)pack4_e4m3((h * w) * by, 0.0f, 0.0f, 0.0f);
+    if (eight) static_cast<uint8_t *>(p.y)[ya + c] = (uint8_t)pack4_e4m3(quotient.of((double)h * w), 0.0f, 0.0f, 0.0f);
     else store_from_f32(p.y, p.type, ya + c, (h * rstd) * w);
   }
 }

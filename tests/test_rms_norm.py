@@ -140,6 +140,28 @@ def test_forward(size, dtype, param, add):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,param", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("size", [(2, 7, 3, 129), (1, 40, 64, 2048), (2, 9, 5, 8200), (8, 300, 4, 64)], ids=str)
+def test_8_bits_are_the_nearest_values(size, dtype, param):
+    """Every value is the nearest of e4m3's to 448 h w / max |h w|, ties to even, next to the borders between two and on them.  h w has at most 48 bits
+    and a border 5, so products with 448 = 7 2^6 and of a border with the maximum are exact in 64 bits, and so are comparisons of the two."""
+    import torch
+    A = _A()
+    M, b, T, D = size
+    x, _, w, _, _ = _inputs(M, b, T, D, dtype, param, False, D)
+    y8 = A.rms_norm_8bit(x, w, eps=EPS)[0].double().cpu()
+    p = x.double().cpu() * w.double().cpu()[:, None, None]
+    most = p.abs().amax(-1, keepdim=True)
+    v = p.abs() * (448 / most)
+    units = torch.tensor([2.0 ** e for e in range(-9, 6)], dtype=torch.float64)
+    unit = units[torch.clamp(torch.frexp(v).exponent - 4, min=-9).long() + 9]
+    low = torch.floor(v / unit)
+    side = p.abs() * 448 - (low + 0.5) * unit * most
+    n = torch.where(side > 0, low + 1, torch.where(side < 0, low, low + low % 2))
+    assert torch.equal(y8, torch.sign(p) * n * unit)
+
+
+@gpu
 @pytest.mark.parametrize("add", [False, True])
 @pytest.mark.parametrize("dtype,param", [("f32", "f32"), ("bf16", "f32"), ("f16", "f16")])
 @pytest.mark.parametrize("size", SIZES + [(2, 40, 1, 64), (1, 2, 600, 96), (2, 130, 16, 40), (3, 2, 300, 777), (1, 600, 7, 2056)], ids=str)
