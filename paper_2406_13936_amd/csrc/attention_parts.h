@@ -11,6 +11,7 @@
 #include "device_utils.h"
 #include "mfma_tile.h"
 #include "ops.h"
+#include "row_groups.h"
 #include "typed_mem.h"
 
 namespace absk {
@@ -154,17 +155,9 @@ template <int TYPE, int ROWS, int ND, int THREADS = 256> struct Tile {
       if constexpr (VEC) {
         q[i] = run_load(m.at, bytes, there ? (uint32_t)(row * (int)m.ld + col) * sizeof(E) : OOB);
       } else {
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
-        if (there && row < m.left) {
-          const E *p = m.at + row * m.ld + col;
-#pragma unroll
-          for (int e = 0; e < PER; ++e)
-            if (col + e < m.D) {
-              if constexpr (TYPE == TYPE_F32) w[e] = __float_as_uint(p[e]);
-              else w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
-            }
-        }
-        q[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        const bool in = there && row < m.left;
+        const uint4 w = load16<sizeof(E), false>(m.at, in ? row * m.ld : 0, in ? col : 0, m.D);
+        q[i] = make_uint4(in ? w.x : 0u, in ? w.y : 0u, in ? w.z : 0u, in ? w.w : 0u);
       }
     }
   }
@@ -252,32 +245,18 @@ __device__ __forceinline__ Frag8<TYPE> row_frag(const void *base, long long at, 
   typedef typename ElemOf<TYPE>::type E;
   const int col = 16 * k + 8 * (threadIdx.x >> 5 & 1);
   Frag8<TYPE> f;
-  float v[8];
-  const E *p = static_cast<const E *>(base) + (in && col < D ? at + col : 0);
-  const bool ok = in && col < D;
   if constexpr (TYPE == TYPE_F32) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (VEC) {
-        const bool o = ok && col + 4 * h < D;
-        const float4 a = *reinterpret_cast<const float4 *>(o ? p + 4 * h : p);
-        v[4 * h] = o ? a.x : 0.0f; v[4 * h + 1] = o ? a.y : 0.0f; v[4 * h + 2] = o ? a.z : 0.0f; v[4 * h + 3] = o ? a.w : 0.0f;
-      } else {
-#pragma unroll
-        for (int e = 4 * h; e < 4 * h + 4; ++e) v[e] = ok && col + e < D ? p[e] : 0.0f;
-      }
+      const bool ok = in && col + 4 * h < D;
+      const uint4 w = load16<4, VEC>(base, ok ? at : 0, ok ? col + 4 * h : 0, D);
+      f.v[4 * h] = ok ? __uint_as_float(w.x) : 0.0f; f.v[4 * h + 1] = ok ? __uint_as_float(w.y) : 0.0f;
+      f.v[4 * h + 2] = ok ? __uint_as_float(w.z) : 0.0f; f.v[4 * h + 3] = ok ? __uint_as_float(w.w) : 0.0f;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f.v[e] = v[e];
-  } else if constexpr (VEC) {
-    const uint4 w = *reinterpret_cast<const uint4 *>(p);
-    f.q = make_uint4(ok ? w.x : 0u, ok ? w.y : 0u, ok ? w.z : 0u, ok ? w.w : 0u);
   } else {
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (ok && col + e < D) w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
-    f.q = make_uint4(w[0], w[1], w[2], w[3]);
+    const bool ok = in && col < D;
+    const uint4 w = load16<2, VEC>(base, ok ? at : 0, ok ? col : 0, D);
+    f.q = make_uint4(ok ? w.x : 0u, ok ? w.y : 0u, ok ? w.z : 0u, ok ? w.w : 0u);
   }
   return f;
 }

@@ -126,3 +126,49 @@ def test_steps_of_a_block_in_a_graph():
         want = step(*eager)
         assert torch.equal(y, want)
         assert all(torch.equal(w[n], eager[0][n]) for n in w) and all(torch.equal(mom[n], eager[1][n]) for n in mom)
+
+
+def test_calls_on_two_streams_at_once():
+    import torch
+    import paper_2406_13936_amd as A
+    sets = []
+    for seed in (2, 3):
+        w, tok, signal = _setup(2, 4, 90, 300, 64, 4, 2, 16, seed)
+        ends = list(range(0, 2 * 4 * 90 + 1, 9))     # 80 sequences: a list of tiles in the workspace
+        sets.append((w, tok, signal, torch.tensor(ends, device="cuda"), torch.cuda.Stream()))
+    want = [_step(A, *s[:4], 4, 2, 16, 1.5) for s in sets]
+    for _ in range(3):
+        torch.cuda.synchronize()
+        got = []
+        for s in sets:
+            with torch.cuda.stream(s[4]):
+                got.append(_step(A, *s[:4], 4, 2, 16, 1.5))
+        torch.cuda.synchronize()
+        for (y, g, st), (y2, g2, st2) in zip(want, got):
+            assert torch.equal(y, y2) and all(torch.equal(g[n], g2[n]) for n in g)
+            assert all(torch.equal(a, b) for n in st for a, b in zip(st[n], st2[n]))
+
+
+def test_broadcast_operands_are_refused():
+    """Rows that lie on each other (stride 0) are refused, as inputs too: make them contiguous first."""
+    import torch
+    import paper_2406_13936_amd as A
+    one = torch.ones((1, 1, 1, 32), device="cuda")
+    x, w = one.expand(2, 3, 4, 32), torch.ones((2, 32), device="cuda")
+    with pytest.raises(A.AbsError):
+        A.rms_norm(x, w)
+    full = x.contiguous()
+    y, h, r = A.rms_norm(full, w)
+    with pytest.raises(A.AbsError):
+        A.rms_norm_backward(x, h, w, r)
+    tok = torch.zeros((2, 3, 4), dtype=torch.int32, device="cuda")
+    with pytest.raises(A.AbsError):
+        A.embedding_backward(x, tok, 5)
+    with pytest.raises(A.AbsError, match="contiguous"):
+        A.embedding(tok[:, :1, :1].expand(2, 3, 4), torch.ones((2, 5, 32), device="cuda"))
+    q = torch.ones((6, 4, 16), device="cuda")
+    k = torch.ones((6, 1, 16), device="cuda")
+    with pytest.raises(A.AbsError):
+        A.causal_attention(q, k.expand(6, 4, 16), k.expand(6, 4, 16))
+    with pytest.raises(A.AbsError):
+        A.causal_attention(q[:1].expand(6, 4, 16), k, k)
