@@ -17,10 +17,11 @@ namespace {
 
 // Sequence and level of every tile, those of the longest sequences first, for more than 64 sequences: list[0].x of them from list[1] on.  Sequences of about
 // the same number of tiles share one of 1024 places, in an order that may differ from run to run (nothing that is computed depends on it).
+// Offsets that are no list may ask for far more tiles than there is room for, up to rows / 128 in every sequence: places are counted in 64 bits.
 __global__ void __launch_bounds__(1024) attention_tiles_kernel(const AttentionP p, int2 *list, const int size) {
   constexpr int PLACES = 1024, ALONE = 32;
-  __shared__ int place[PLACES];
-  __shared__ int most, sums[16];
+  __shared__ unsigned long long place[PLACES], sums[16];
+  __shared__ int most;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   place[threadIdx.x] = 0;
   if (threadIdx.x == 0) most = 0;
@@ -33,33 +34,33 @@ __global__ void __launch_bounds__(1024) attention_tiles_kernel(const AttentionP 
   const int unit = max(1, (most + PLACES - 1) / PLACES);
   for (int s = threadIdx.x; s < p.seqs; s += 1024) {
     const int mine = tiles_of(s);
-    if (mine) atomicAdd(&place[PLACES - 1 - (mine - 1) / unit], mine);
+    if (mine) atomicAdd(&place[PLACES - 1 - (mine - 1) / unit], (unsigned long long)mine);
   }
   __syncthreads();
-  const int count = place[threadIdx.x];
-  int upto = count;
+  const unsigned long long count = place[threadIdx.x];
+  unsigned long long upto = count;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(upto, o, 64);
+    const unsigned long long v = __shfl_up(upto, o, 64);
     if (lane >= o) upto += v;
   }
   if (lane == 63) sums[wave] = upto;
   __syncthreads();
   for (int w = 0; w < wave; ++w) upto += sums[w];
   place[threadIdx.x] = upto - count;
-  // (offsets that are no list may ask for more tiles than there are places)
-  const int room = (int)min(attention_tiles(p), (long long)0x7fffffff);
-  if (threadIdx.x == PLACES - 1) list[0] = make_int2(min(upto, room), 0);
+  const long long room = attention_tiles(p);           // (fits an int: a grid counts as many blocks)
+  if (threadIdx.x == PLACES - 1) list[0] = make_int2((int)min((long long)upto, room), 0);
   __syncthreads();
   // a lane writes the first tiles of its sequence, a wavefront the others of each that has more
   for (int s0 = wave * 64; s0 < p.seqs; s0 += 1024) {
-    const int mine = tiles_of(s0 + lane), at = mine ? atomicAdd(&place[PLACES - 1 - (mine - 1) / unit], mine) : 0;
-    for (int i = 0; i < min(mine, ALONE); ++i)
-      if (at + i < room) list[1 + at + i] = make_int2(s0 + lane, mine - i);
-    for (uint64_t m = __ballot(mine > ALONE); m; m &= m - 1) {
-      const int from = __ffsll((unsigned long long)m) - 1, all = __shfl(mine, from, 64), first = __shfl(at, from, 64);
-      for (int i = ALONE + lane; i < all; i += 64)
-        if (first + i < room) list[1 + first + i] = make_int2(s0 + from, all - i);
+    const int mine = tiles_of(s0 + lane);
+    const long long at = mine ? (long long)atomicAdd(&place[PLACES - 1 - (mine - 1) / unit], (unsigned long long)mine) : 0;
+    const int here = (int)max(0LL, min((long long)mine, room - at));
+    for (int i = 0; i < min(here, ALONE); ++i) list[1 + at + i] = make_int2(s0 + lane, mine - i);
+    for (uint64_t m = __ballot(here > ALONE); m; m &= m - 1) {
+      const int from = __ffsll((unsigned long long)m) - 1, all = __shfl(mine, from, 64), upto_room = __shfl(here, from, 64);
+      const long long first = __shfl(at, from, 64);
+      for (int i = ALONE + lane; i < upto_room; i += 64) list[1 + first + i] = make_int2(s0 + from, all - i);
     }
   }
 }

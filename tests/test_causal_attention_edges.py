@@ -1,0 +1,81 @@
+"""Causal attention at the edges of what its entry points take: offsets that are no list, sizes next to the limits, infinite keys."""
+import ctypes as C
+import math
+import struct
+
+import pytest
+
+from test_causal_attention import _lib, _shape, _tensors
+
+gpu = pytest.mark.gpu
+
+
+# ---- offsets that are no list -------------------------------------------------------------------------------------------
+
+def _list_kernel_arguments(seqs, rows, offsets, out):
+    """The kernels' parameters with what the list of tiles is made from: offsets of 32 bits, no sums of more than the list."""
+    p = bytearray(512)
+    struct.pack_into("<8i", p, 0, 0, 1, 1, 8, seqs, 0, 0, 0)           # type, Hq, Hkv, D, seqs, T, wide, zero_rest
+    struct.pack_into("<qQQ", p, 32, rows, offsets, out)
+    return (C.c_char * len(p)).from_buffer(p)
+
+
+@gpu
+@pytest.mark.parametrize("rows,full", [(1 << 20, (1 << 18) + 2), (1 << 22, 1 << 17), (1000, 300), (128, 40)])
+def test_the_list_of_tiles_ends_where_its_room_does(rows, full):
+    """Sequences that all have all rows, an empty one behind each: up to 2^32 tiles of which the list holds rows / 128 + sequences."""
+    import torch
+    lib, seqs = _lib(), 2 * full
+    off = torch.tensor([0, rows] * full + [0], dtype=torch.int32, device="cuda")
+    room, guard = rows // 128 + seqs, 4096
+    buf = torch.full((room + 1 + 2 * guard, 2), -7, dtype=torch.int32, device="cuda")
+    call = lib["_ZN4absk22launch_attention_tilesERKNS_10AttentionPEP12ihipStream_t"]
+    p = _list_kernel_arguments(seqs, rows, off.data_ptr(), buf[guard].data_ptr())
+    assert call(C.byref(p), C.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+    torch.cuda.synchronize()
+    assert (buf[:guard] == -7).all() and (buf[-guard:] == -7).all()
+    used, each = min(room, full * (-(-rows // 128))), -(-rows // 128)
+    entries = buf[guard + 1:-guard].long()
+    assert buf[guard].tolist() == [used, 0] and (entries[used:] == -7).all()
+    entries = entries[:used]
+    assert (entries[:, 0] % 2 == 0).all() and (entries[:, 0] >= 0).all() and (entries[:, 0] < seqs).all()
+    # every sequence's tiles side by side, from its last to its first
+    place = torch.arange(used, device="cuda")
+    assert torch.equal(entries[:, 1], each - place % each)
+    assert torch.equal(entries[:, 0], entries[place - place % each, 0])
+
+
+@gpu
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("f16", 24), ("f32", 40)])
+def test_many_offsets_that_are_no_list_stay_inside(dtype, D):
+    """More than 64 sequences, through the C entry points, with all that is written between guards."""
+    import torch
+    from paper_2406_13936_amd import binding as B
+    lib, R, H = _lib(), 300, 2
+    q, k, v, do = _tensors(R, H, H, D, dtype)
+    e, ld = q.element_size(), H * D
+    for bad in ([0, R] * 60, [-9, 5000] * 40, [R, 0] * 50, list(range(R, R - 100, -1)), [0] * 70 + [R], [(i * 7919) % 400 - 50 for i in range(129)]):
+        off = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        s = _shape(type={"f32": 0, "bf16": 1, "f16": 2}[dtype], seqs=len(bad) - 1, Hq=H, Hkv=H, D=D, rows=R,
+                   **{n: ld if n[0] == "l" else D for n in [f for f, _ in B.AttentionShape._fields_ if f[:2] == "ld" or f[:5] == "head_"]})
+        guarded = []
+
+        def room(nbytes):
+            nbytes = (nbytes + 255) // 256 * 256
+            t = torch.full((nbytes + 2048,), 0x5a, dtype=torch.uint8, device="cuda")
+            guarded.append(t)
+            return t[1024:].data_ptr()
+        n = C.c_size_t(0)
+        stream = torch.cuda.current_stream().cuda_stream
+        o, lse = room(R * ld * e), room(H * R * 4)
+        for zero_rest in (0, 1):
+            assert lib.abs_causal_attention_workspace_bytes(C.byref(s), 0, C.byref(n)) == 0
+            assert lib.abs_causal_attention(C.byref(s), q.data_ptr(), k.data_ptr(), v.data_ptr(), off.data_ptr(), 0.2, o, lse, zero_rest,
+                                            room(n.value), n.value, stream) == 0
+            assert lib.abs_causal_attention_workspace_bytes(C.byref(s), 1, C.byref(n)) == 0
+            grads = [room(R * ld * e) for _ in range(3)]
+            assert lib.abs_causal_attention_backward(C.byref(s), do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o, lse, off.data_ptr(), 0.2,
+                                                     *grads, zero_rest, room(n.value), n.value, stream) == 0
+        torch.cuda.synchronize()
+        for t in guarded:
+            assert (t[:1024] == 0x5a).all() and (t[-1024:] == 0x5a).all()
