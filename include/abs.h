@@ -484,7 +484,8 @@ abs_status abs_rms_norm_backward(const abs_rms_norm_shape *shape /*host*/, const
  * other.  Rows of no sequence (before the first, behind the last) are not read, and are left as they are in the outputs or set to zeros.
  * What a row's mask leaves out has no part in it, infinities and NaN included.
  * Sums, maxima and the softmax are fp32; with 16-bit types softmax weights are rounded to that type for the product with v (and their
- * gradients for the products with q and k).  Heads of up to 128 values, at most 2^31 - 1 rows; beyond: ABS_EUNSUPPORTED.
+ * gradients for the products with q and k).  Heads of up to 128 values, at most 2^31 - 1 rows and 8323072 tiles, which are Hq times the sum over
+ * sequences of their rows / 128, rounded up (with offsets: Hq (rows / 128 + seqs), rounded down); beyond: ABS_EUNSUPPORTED.
  */
 typedef struct {
   int type;                   /* ABS_TYPE_* of q, k, v, o, do, dq, dk and dv */

@@ -155,7 +155,7 @@ struct AttentionP {
 };
 // Tiles of all sequences: what they are, or with offsets the most that they can be
 __host__ __device__ inline long long attention_tiles(const AttentionP &p) {
-  if (!p.offsets) return (long long)p.seqs * ((p.T + ATTENTION_ROWS - 1) / ATTENTION_ROWS);
+  if (!p.offsets) return p.seqs * ((p.T + (ATTENTION_ROWS - 1LL)) / ATTENTION_ROWS);
   return p.rows / ATTENTION_ROWS + p.seqs;
 }
 hipError_t launch_attention_tiles(const AttentionP &p, hipStream_t s);

@@ -5,9 +5,33 @@ import struct
 
 import pytest
 
-from test_causal_attention import _lib, _shape, _tensors
+from test_causal_attention import EUNSUPPORTED, _lib, _shape, _tensors
 
 gpu = pytest.mark.gpu
+
+
+# ---- sizes (no GPU call is made) ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("seqs,T,Hq,status", [
+    (1, (1 << 31) - 1, 1, EUNSUPPORTED), (1, (1 << 31) - 127, 1, EUNSUPPORTED), (1, (1 << 31) - 128, 1, EUNSUPPORTED), (1, 1 << 30, 2, EUNSUPPORTED),
+    (1, 8323072 * 128 + 1, 1, EUNSUPPORTED), (1, 8323072 * 128, 1, 0), (8323072, 1, 1, 0), (8323073, 1, 1, EUNSUPPORTED), (8323072 // 4, 1, 4, 0)])
+def test_sequences_of_one_length_at_the_limit(seqs, T, Hq, status):
+    """8323072 tiles of 128 rows are what a launch takes; T + 127 may pass 31 bits."""
+    lib, n = _lib(), C.c_size_t(0)
+    D = 1
+    s = _shape(seqs=seqs, T=T, rows=seqs * T, Hq=Hq, Hkv=1, D=D, offsets_type=0, ldq=Hq, ldk=1, ldv=1, ldo=Hq, head_q=1, head_k=1, head_v=1, head_o=1,
+               lddo=Hq, lddq=Hq, lddk=1, lddv=1, head_do=1, head_dq=1, head_dk=1, head_dv=1)
+    for backward in (0, 1):
+        assert lib.abs_causal_attention_workspace_bytes(C.byref(s), backward, C.byref(n)) == status
+
+
+@pytest.mark.parametrize("rows,seqs,Hq,status", [
+    (8323071 * 128, 1, 1, 0), (8323072 * 128, 1, 1, EUNSUPPORTED), ((1 << 31) - 1, 1, 1, EUNSUPPORTED), (100, 8323072, 1, 0), (128, 8323072, 1, EUNSUPPORTED)])
+def test_packed_sequences_at_the_limit(rows, seqs, Hq, status):
+    lib, n = _lib(), C.c_size_t(0)
+    s = _shape(seqs=seqs, rows=rows, Hq=Hq, Hkv=1, D=1, **{k + n: 1 for k in ("ld", "head_") for n in ("q", "k", "v", "o", "do", "dq", "dk", "dv")})
+    for backward in (0, 1):
+        assert lib.abs_causal_attention_workspace_bytes(C.byref(s), backward, C.byref(n)) == status
 
 
 # ---- offsets that are no list -------------------------------------------------------------------------------------------
