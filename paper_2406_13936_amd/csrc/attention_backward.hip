@@ -164,7 +164,8 @@ __global__ void __launch_bounds__(64 * KEYS_WAVES * KEYS_GROUPS, ND >= 3 ? 1 : 2
       (B ? stat_b : stat_a)[group][1][thread] = there ? inner : 0.0f;
     }
   };
-  // Queries q0 .. q0 + 31, block b of a tile; MASKED: perhaps the diagonal's
+  bool odd = false;                                    // are there infinities or NaN in the wavefront's keys and values?
+  // Queries q0 .. q0 + 31, block b of a tile; MASKED: perhaps the diagonal's, or the sequence's last
   auto step = [&](int q0, int b, auto buffer, auto masked_block) INLINE {
     constexpr bool MASKED = decltype(masked_block)::value, B = decltype(buffer)::value;
     const E *lq = (B ? queries_b : queries_a) + group * T::ELEMS, *ld = (B ? signals_b : signals_a) + group * T::ELEMS;
@@ -196,6 +197,11 @@ __global__ void __launch_bounds__(64 * KEYS_WAVES * KEYS_GROUPS, ND >= 3 ? 1 : 2
         dp[r] = y;
       }
     }
+    if (MASKED && odd && q0 + 32 > w.len) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (q0 + 8 * (r >> 2) + 4 * h + (r & 3) >= w.len) s[r] = dp[r] = 0.0f;
+    }
     const Frag8<TYPE> x[2] = {as_frag<TYPE>(s, 0), as_frag<TYPE>(s, 1)}, y[2] = {as_frag<TYPE>(dp, 0), as_frag<TYPE>(dp, 1)};
     Frag8<TYPE> cq[2][ND], cd[2][ND];
     if (GROUPED) group_ends();
@@ -224,6 +230,11 @@ __global__ void __launch_bounds__(64 * KEYS_WAVES * KEYS_GROUPS, ND >= 3 ? 1 : 2
     fetch(a, next, next_head);
     settle(a);
   }
+  // Rows beyond a sequence's end have weight 0, as their lse is infinite, but 0 times an infinite key makes NaN of it: where a wavefront has such keys or
+  // values those rows are masked (in every block that ends a sequence: 300 sequences of 32768 rows 318 us, so 353)
+#pragma unroll
+  for (int i = 0; i < 2 * ND; ++i) odd |= any_unusual<TYPE>(kf[i]) || any_unusual<TYPE>(vf[i]);
+  odd = __any(odd);
   arrived<DIRECT>();
   auto turn = [&](auto buffer) INLINE {
     std::integral_constant<bool, !decltype(buffer)::value> other;

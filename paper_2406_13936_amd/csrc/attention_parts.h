@@ -79,6 +79,16 @@ template <int TYPE> __device__ __forceinline__ uint32_t unusual_signs(const uint
   constexpr uint32_t ONE = TYPE == TYPE_F32 ? 0x00800000u : TYPE == TYPE_BF16 ? 0x00800080u : 0x04000400u;
   return (((q.x & E) + ONE) | ((q.y & E) + ONE)) | (((q.z & E) + ONE) | ((q.w & E) + ONE));
 }
+template <int TYPE> __device__ __forceinline__ bool any_unusual(const Frag8<TYPE> &f) {
+  if constexpr (TYPE == TYPE_F32) {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) odd |= unusual(f.v[e]);
+    return odd;
+  } else {
+    return (unusual_signs<TYPE>(f.q) & 0x80008000u) != 0;
+  }
+}
 // zeros in the place of infinities and NaN
 template <int TYPE> __device__ __forceinline__ Frag8<TYPE> usual(Frag8<TYPE> f) {
   if constexpr (TYPE == TYPE_F32) {

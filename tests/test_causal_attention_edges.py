@@ -5,7 +5,7 @@ import struct
 
 import pytest
 
-from test_causal_attention import EUNSUPPORTED, _lib, _shape, _tensors
+from test_causal_attention import EUNSUPPORTED, _A, _lib, _shape, _tensors
 
 gpu = pytest.mark.gpu
 
@@ -103,3 +103,35 @@ def test_many_offsets_that_are_no_list_stay_inside(dtype, D):
         torch.cuda.synchronize()
         for t in guarded:
             assert (t[:1024] == 0x5a).all() and (t[-1024:] == 0x5a).all()
+
+
+# ---- infinite keys ------------------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 100), ("f16", 80), ("f32", 48)])
+@pytest.mark.parametrize("T", [2, 31, 32, 33, 63, 64, 65, 97, 130])
+def test_infinite_keys_whose_scores_are_minus_infinity(T, dtype, D):
+    """A key that every query that sees it scores with minus infinity has no weight in any row: its gradients are zeros whether or not its block of
+    queries ends behind the sequence's last, as are others' with their key in its place."""
+    import torch
+    A = _A()
+    q, k, v, do = _tensors(T + 40, 2, 1, D, dtype, T)
+    off = torch.tensor([0, T, T + 40], dtype=torch.int32, device="cuda")
+    c = D // 3
+    q[..., c] = -q[..., c].abs() - 0.25
+    for at in {T - 1, T // 2, max(1, T - 33)}:
+        k2 = k.clone()
+        k2[at, 0, c] = float("inf")
+        o, lse = A.causal_attention(q, k2, v, offsets=off)
+        assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+        dq, dk, dv = A.causal_attention_backward(do, q, k2, v, o, lse, offsets=off)
+        assert (dk[at] == 0).all() and (dv[at] == 0).all()
+        assert torch.isfinite(dk).all() and torch.isfinite(dv).all()
+        # a query that sees it has 0 times infinity in one place
+        others = [i for i in range(D) if i != c]
+        assert torch.isfinite(dq[:, :, others]).all() and torch.isfinite(dq[:at]).all() and torch.isfinite(dq[T:]).all()
+        # the same with the key far away instead: a score that leaves it no weight either
+        k2[at, 0, c] = 30000.0
+        o1, lse1 = A.causal_attention(q, k2, v, offsets=off)
+        _, dk1, dv1 = A.causal_attention_backward(do, q, k2, v, o1, lse1, offsets=off)
+        assert torch.equal(o1, o) and torch.equal(lse1, lse) and torch.equal(dk1, dk) and torch.equal(dv1, dv)
