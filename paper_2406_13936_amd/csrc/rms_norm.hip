@@ -19,8 +19,9 @@ namespace {
 constexpr float E4M3_MAX = 448.0f;
 constexpr float SMALLEST_SCALE = 0x1p-100f;      // (its inverse is finite)
 
-__device__ __forceinline__ float scale_of(float rstd, double most) {
-  const float c = rstd * (float)most / E4M3_MAX; // NaN of a row with NaN or infinities stays
+// odd: infinities or NaN in the row's gains, so its results have them.  (Its own are in rstd: NaN, or 0, which times an infinite maximum is NaN.)
+__device__ __forceinline__ float scale_of(float rstd, double most, bool odd) {
+  const float c = odd ? __builtin_nanf("") : rstd * (float)most / E4M3_MAX;
   return c < SMALLEST_SCALE ? SMALLEST_SCALE : c;
 }
 // y / c = 448 h w / max |h w|, in which r has cancelled, is rounded to e4m3 as if it were exact, ties to even: products of two 16-bit values are often just
@@ -42,6 +43,21 @@ struct Quotient {
 __device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float d) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// Are there infinities or NaN among a replica's gains, of which each group of the block has all?  (The maximum of |h w| would pass over NaN.)
+// Gains of zero become the smallest normal value: an infinity times it is infinite, not a NaN that the maximum passes over, and of anything else the
+// quotient is below sqrt(D) 2^-126 / 2^-100 and rounds to zero as before.
+template <int V> __device__ __forceinline__ bool look_at_gains(float (&w)[V][8]) {
+  bool odd = false;
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      odd |= !(fabsf(w[v][e]) < __builtin_inff());
+      w[v][e] = w[v][e] == 0.0f ? copysignf(0x1p-126f, w[v][e]) : w[v][e];
+    }
+  return __builtin_amdgcn_readfirstlane(__syncthreads_or(odd));
 }
 
 // Sum and, if MAX, maximum over the group; sm: 6 floats to a wavefront, `turn` as in group_sums
@@ -111,6 +127,7 @@ __global__ void __launch_bounds__(ln_threads(G)) rms_forward_kernel(const RmsNor
   }
   float w[V][8];
   load_param<TYPE, G, V, VEC>(w, p.w, p.ptype, (long long)m * D, D, l);
+  const bool odd = EIGHT && look_at_gains<V>(w);
   // G >= 256: every thread of the block goes through every exchange (one group to a block: they agree on r)
   for (; r < rows; r += step) {
     const Raw<TYPE, V> rx = nx, rr = nr;
@@ -139,7 +156,7 @@ __global__ void __launch_bounds__(ln_threads(G)) rms_forward_kernel(const RmsNor
     }
     group_sum_max<G, EIGHT>(s, most, sm, turn++);
     const float rstd = 1.0f / sqrtf(s / n + p.eps);
-    const float c = EIGHT ? scale_of(rstd, most) : 0.0f;
+    const float c = EIGHT ? scale_of(rstd, most, odd) : 0.0f;
     const Quotient quotient(rstd, c, EIGHT ? most : 1.0);
     if (l == 0) {
       if (p.rstd) p.rstd[m * rows + r] = rstd;
@@ -164,6 +181,7 @@ __global__ void __launch_bounds__(256) rms_forward_long_kernel(const RmsNormP p,
   const long long xa = m * p.sx + r * p.ldx, ra = m * p.sr + r * p.ldr, ha = m * p.sh + r * p.ldh, ya = m * p.sy + r * p.ldy, pa = m * p.D;
   float s = 0.0f;
   double most = 0.0;
+  bool odd = false;
   for (int c = threadIdx.x; c < p.D; c += 256) {
     float h = load_as_f32(p.x, p.type, xa + c);
     if (p.res) {
@@ -172,10 +190,15 @@ __global__ void __launch_bounds__(256) rms_forward_long_kernel(const RmsNormP p,
       h = load_as_f32(p.h, p.type, ha + c);
     }
     s = fmaf(h, h, s);
-    if (eight) most = fmax(most, fabs((double)h * load_as_f32(p.w, p.ptype, pa + c)));
+    if (eight) {
+      const float w = load_as_f32(p.w, p.ptype, pa + c);
+      odd |= !(fabsf(w) < __builtin_inff()) || !(fabsf(h) < __builtin_inff());
+      most = fmax(most, fabs((double)h * w));
+    }
   }
+  odd = __syncthreads_or(odd);
   group_sum_max<256, true>(s, most, sm, 0);
-  const float rstd = 1.0f / sqrtf(s / (float)p.D + p.eps), scale = scale_of(rstd, most);
+  const float rstd = 1.0f / sqrtf(s / (float)p.D + p.eps), scale = scale_of(rstd, most, odd);
   const Quotient quotient(rstd, scale, most);
   if (threadIdx.x == 0) {
     if (p.rstd) p.rstd[m * rows + r] = rstd;

@@ -1,0 +1,49 @@
+"""The 8-bit result of the root-mean-square norm at gains that are infinite or NaN."""
+import pytest
+
+from test_rms_norm import EPS, _A, _inputs
+
+gpu = pytest.mark.gpu
+
+
+@gpu
+@pytest.mark.parametrize("dtype,param", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("f32", "f32")])
+@pytest.mark.parametrize("D", [1, 100, 129, 1000, 2048, 4100, 8192, 8200])
+def test_gains_that_are_infinite_or_nan(D, dtype, param):
+    """Such a gain leaves every row of its replica an infinity or NaN: the scale is NaN, and what is held in 8 bits with it."""
+    import torch
+    A = _A()
+    x, res, w, _, _ = _inputs(3, 4, 5, D, dtype, param, True, D)
+    x[1, 2, 3] = 0
+    res[1, 2, 3] = 0                                  # (a row of zeros: 0 times infinity)
+    want8, want_c, h, rstd = A.rms_norm_8bit(x, w, residual=res, eps=EPS)
+    assert torch.isfinite(want_c).all()
+    for at in {0, D // 2, D - 1}:
+        for value in (float("nan"), float("inf"), float("-inf")):
+            w2 = w.clone()
+            w2[1, at] = value
+            y8, c, h2, r2 = A.rms_norm_8bit(x, w2, residual=res, eps=EPS)
+            assert torch.equal(h2, h) and torch.equal(r2, rstd)
+            assert torch.isnan(c[1]).all() and torch.isnan(y8[1].float()).all()
+            for m in (0, 2):
+                assert torch.equal(c[m], want_c[m]) and torch.equal(y8[m].float(), want8[m].float())
+
+
+@gpu
+@pytest.mark.parametrize("D", [16, 100, 129, 1000, 2048, 4100, 8192, 8200])
+def test_infinities_in_a_row_where_its_gain_is_zero(D):
+    """Infinity times 0 is NaN in that place, and so is the scale; other rows, and those whose squares pass fp32's range, keep theirs."""
+    import torch
+    A = _A()
+    x, _, w, _, _ = _inputs(2, 5, 7, D, "bf16", "f32", False, D)
+    w[:, D // 2] = 0
+    x[0, 0, 0] = 2.0 ** 100                           # (1 / sqrt(infinity) = 0: zeros)
+    want8, want_c, _, _ = A.rms_norm_8bit(x, w, eps=EPS)
+    assert want_c[0, 0, 0] == 2.0 ** -100 and (want8[0, 0, 0].float() == 0).all()
+    rows = torch.zeros(x.shape[:-1], dtype=torch.bool, device="cuda")
+    for m, i, t, value in ((0, 0, 1, float("inf")), (0, 3, 6, float("-inf")), (1, 4, 0, float("inf")), (1, 4, 1, float("nan"))):
+        x[m, i, t, D // 2] = value
+        rows[m, i, t] = True
+    y8, c, _, _ = A.rms_norm_8bit(x, w, eps=EPS)
+    assert torch.isnan(c[rows]).all() and torch.isnan(y8.float()[rows]).all()
+    assert torch.equal(c[~rows], want_c[~rows]) and torch.equal(y8.float()[~rows], want8.float()[~rows])
