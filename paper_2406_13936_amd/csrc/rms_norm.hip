@@ -21,7 +21,8 @@ constexpr float SMALLEST_SCALE = 0x1p-100f;      // (its inverse is finite)
 
 // odd: infinities or NaN in the row's gains, so its results have them.  (Its own are in rstd: NaN, or 0, which times an infinite maximum is NaN.)
 __device__ __forceinline__ float scale_of(float rstd, double most, bool odd) {
-  const float c = odd ? __builtin_nanf("") : rstd * (float)most / E4M3_MAX;
+  // (in fp64: the maximum may be beyond fp32's range, or among its last bits, where r times it is not)
+  const float c = odd ? __builtin_nanf("") : (float)((double)rstd * most * (1.0 / E4M3_MAX));
   return c < SMALLEST_SCALE ? SMALLEST_SCALE : c;
 }
 // y / c = 448 h w / max |h w|, in which r has cancelled, is rounded to e4m3 as if it were exact, ties to even: products of two 16-bit values are often just

@@ -1,7 +1,7 @@
-"""The 8-bit result of the root-mean-square norm at gains that are infinite or NaN."""
+"""The 8-bit result of the root-mean-square norm at gains that are infinite or NaN, or whose products with the rows pass fp32's range."""
 import pytest
 
-from test_rms_norm import EPS, _A, _inputs
+from test_rms_norm import EPS, U32, _A, _inputs
 
 gpu = pytest.mark.gpu
 
@@ -47,3 +47,26 @@ def test_infinities_in_a_row_where_its_gain_is_zero(D):
     y8, c, _, _ = A.rms_norm_8bit(x, w, eps=EPS)
     assert torch.isnan(c[rows]).all() and torch.isnan(y8.float()[rows]).all()
     assert torch.equal(c[~rows], want_c[~rows]) and torch.equal(y8.float()[~rows], want8.float()[~rows])
+
+
+@gpu
+@pytest.mark.parametrize("D", [16, 200, 2048, 8200])
+@pytest.mark.parametrize("row,gain,eps", [(1e10, 1e30, 1e-6), (3e-5, 1e-41, 0.0), (1e-18, 1e-27, 0.0), (1e-17, 3e-28, 0.0), (1e15, 1e25, 0.0)])
+def test_products_of_rows_and_gains_beyond_fp32(row, gain, eps, D):
+    """max |h w| may be above fp32's range, or among its last bits, where max |h r w| / 448 is not: the scale is right in both, and so are the values."""
+    import torch
+    A = _A()
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    x = row * (0.5 + torch.rand((2, 3, 4, D), device="cuda", generator=gen)) * (2.0 * (torch.rand((2, 3, 4, D), device="cuda", generator=gen) < 0.5) - 1.0)
+    w = gain * (0.5 + torch.rand((2, D), device="cuda", generator=gen))
+    y8, c, _, rstd = A.rms_norm_8bit(x, w, eps=eps)
+    p = x.double() * w.double()[:, None, None]
+    r = 1 / torch.sqrt(x.double().square().mean(-1) + eps)
+    # squares of 1e-18 are held to half of 2^-149 of 1e-36 and more: 2^-30; the root halves it
+    rel = (D / 2 + 8) * U32 + 2.0 ** -30
+    assert ((rstd.double() - r).abs() <= rel * r).all()
+    want_c = (p.abs().amax(-1) * r / 448).clamp(min=2.0 ** -100)
+    assert ((c.double() - want_c).abs() <= 2 * rel * want_c).all()
+    v = p * r[..., None] / want_c[..., None]
+    got = y8.double()
+    assert torch.isfinite(got).all() and ((got - v).abs() <= torch.maximum(v.abs() * (2.0 ** -4 + 4 * rel), torch.full_like(v, 2.0 ** -10 * (1 + rel)))).all()
