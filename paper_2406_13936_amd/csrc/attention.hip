@@ -65,6 +65,10 @@ __global__ void __launch_bounds__(1024) attention_tiles_kernel(const AttentionP 
   }
 }
 
+// fp16 weights are held times 2^7: at most 2^8 of the reference, they stay below 65504, and those below 2^-14 of it, of which a long row has most, keep
+// seven more bits.  Sums are of the same weights; lse is corrected, o divided by the sum.
+template <int TYPE> constexpr float WEIGHT_SHIFT = TYPE == TYPE_F16 ? 7.0f : 0.0f;
+
 template <int TYPE, int ND, bool VEC>
 __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, const int blocks) {
   constexpr int BK = TYPE == TYPE_F32 ? 32 : 64, NB = BK / 32;
@@ -161,7 +165,7 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= by;
     }
-    const float ref = top == -__builtin_inff() ? 0.0f : top;
+    const float ref = (top == -__builtin_inff() ? 0.0f : top) - WEIGHT_SHIFT<TYPE>;
     Frag8<TYPE> x[NB][2];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -212,7 +216,7 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttentionP p, c
   sum += __shfl_xor(sum, 32, 64);
   if (!in) return;
   store_row<TYPE, ND, VEC>(static_cast<E *>(p.o) + w.start * p.ldo + head * p.ho, (long long)row * p.ldo, o, 1.0f / sum, p.D);
-  if (p.lse && h == 0) p.lse[head * p.rows + w.start + row] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+  if (p.lse && h == 0) p.lse[head * p.rows + w.start + row] = (top - WEIGHT_SHIFT<TYPE> + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
 template <int TYPE, int ND, bool VEC> hipError_t forward_launch(const AttentionP &p, hipStream_t s) {

@@ -1,11 +1,11 @@
-"""Causal attention at the edges of what its entry points take: offsets that are no list, sizes next to the limits, infinite keys."""
+"""Causal attention at the edges of what its entry points take: offsets that are no list, sizes next to the limits, infinite keys, rows of many small weights."""
 import ctypes as C
 import math
 import struct
 
 import pytest
 
-from test_causal_attention import EUNSUPPORTED, _A, _lib, _shape, _tensors
+from test_causal_attention import EUNSUPPORTED, U, U32, _A, _check, _dt, _lib, _shape, _tensors
 
 gpu = pytest.mark.gpu
 
@@ -135,3 +135,35 @@ def test_infinite_keys_whose_scores_are_minus_infinity(T, dtype, D):
         o1, lse1 = A.causal_attention(q, k2, v, offsets=off)
         _, dk1, dv1 = A.causal_attention_backward(do, q, k2, v, o1, lse1, offsets=off)
         assert torch.equal(o1, o) and torch.equal(lse1, lse) and torch.equal(dk1, dk) and torch.equal(dv1, dv)
+
+
+# ---- weights in 16 bits -------------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("score,place", [(18.0, 0), (18.0, 77), (11.0, 0), (5.5, 200), (5.5, 4000), (20.0, 9000)])
+def test_long_rows_that_one_key_dominates(score, place, dtype):
+    """Weights e^-18 = 2^-26 of the largest add up to 2^-11 of o over tens of thousands of keys.  In fp16 they are held times 2^7, so that one is off by half
+    a step, 2^-25, of that: by 2^-32 of the largest weight, and a key that comes 2^7.9 above the reference is at most 2^15."""
+    import torch
+    A = _A()
+    T, D, dt = 32768, 16, _dt(dtype)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k = (torch.randn((T, h, D), device="cuda", generator=gen).to(dt) for h in (2, 1))
+    v = (1 + 0.1 * torch.randn((T, 1, D), device="cuda", generator=gen)).to(dt)
+    q[..., 0], q[..., 1:], k[..., 0] = 1, 0, 0       # scores are 0, exactly, but of one key
+    k[place, 0, 0], v[place] = score, 0
+    o, lse = A.causal_attention(q, k, v, scale=1.0)
+    u = 0.0 if dtype == "f32" else U[dtype]
+    for i in (0, 63, 64, 300, 4001, 9010, 20001, T - 1):
+        s = torch.zeros(i + 1, dtype=torch.float64, device="cuda")
+        if place <= i:
+            s[place] = score
+        p, top, vv = torch.softmax(s, 0), torch.logsumexp(s, 0), v[:i + 1, 0].double()
+        rel = (D + 4) * U32 * score + 8 * U32 * (1 + score + float(top))
+        err = (u + 4 * rel + (i + 9) * U32) * (p @ vv.abs()) + (2.0 ** -32 * vv.abs().sum(0) if dtype == "f16" else 0)
+        want = p @ vv
+        off = err + U[dtype] * (want.abs() + err) + (2.0 ** -25 if dtype == "f16" else 0)
+        for h in range(2):
+            _check(o[i, h], want.cpu(), off.cpu(), (i, h))
+            assert abs(float(lse[h, i]) - float(top)) <= 2 * rel + (i + 9) * U32 + 4 * U32 * float(top)
