@@ -515,8 +515,8 @@ abs_status abs_causal_attention(const abs_attention_shape *shape /*host*/, const
  * Its gradients, from the signals do at its result, and o and lse of the forward pass:
  *   p_ij = exp(s_ij - lse_i),  ds_ij = scale p_ij (do_i . v_j - do_i . o_i)
  *   dv_j = sum_i p_ij do_i,  dk_j = sum_i ds_ij q_i  over the rows and query heads that see key j,   dq_i = sum_j ds_ij k_j
- * Arguments as above (zero_rest: of dq, dk and dv).  With ABS_TYPE_F16 p is held in 16 bits times 2^12, ds times a power of two that goes by the largest
- * |do_i| and |v_j| of the call (finite ones).
+ * Arguments as above (zero_rest: of dq, dk and dv).  With ABS_TYPE_F16 p is held in 16 bits times 2^12 (and in the forward pass times 2^7), ds times a power
+ * of two that goes by the largest finite |do_i| and |v_j| of the sequence and of the head (dq) or of the heads that share keys (dk).
  */
 abs_status abs_causal_attention_backward(const abs_attention_shape *shape /*host*/, const void *do_dev, const void *q_dev, const void *k_dev,
                                          const void *v_dev, const void *o_dev, const float *lse_dev, const void *offsets_dev, float scale,

@@ -13,7 +13,7 @@
 // 0.57 for heads of 128.
 //
 // fp16 operands hold p and ds in 16 bits with powers of two: p by 2^12 (else values below 2^-14, those of a row of many keys, lose bits), ds by the power that
-// takes twice the largest |do_i| |v_j|, a bound on |ds / a|, to 2^14 at most.
+// takes twice the largest |do_i| |v_j| of the sequence and heads in question, a bound on |ds / a|, to 2^14 at most.
 #include <algorithm>
 #include "attention_parts.h"
 
@@ -22,16 +22,16 @@ namespace {
 
 template <int TYPE> constexpr float P_SHIFT = TYPE == TYPE_F16 ? 12.0f : 0.0f;
 
-// fp16: D_i of every row and query head, 16 lanes each, and the largest squared lengths of do_i and v_j that each block meets
+// fp16: of every tile of 128 rows D_i of each query head, 16 lanes to a row, and the largest squared lengths of do_i and, further heads, of v_j
+constexpr int INNER_ROWS = 4;                          // of a group under way
 template <bool VEC>
 __global__ void __launch_bounds__(256) attention_inner_kernel(const AttentionP p) {
-  const int g = threadIdx.x / 16, l = threadIdx.x % 16, D = p.D;
-  const long long start = span_of(p, 0).start;
-  const Span last = span_of(p, p.seqs - 1);
-  const long long n = max(0LL, last.start + last.len - start);
-  const long long step = (long long)gridDim.x * 16;
-  float longest = 0.0f, longest_v = 0.0f;
-  auto values = [&](const void *base, long long at, float (&v)[8]) {
+  const int g = threadIdx.x / 16, l = threadIdx.x % 16, D = p.D, heads = p.Hq + p.Hkv, t = blockIdx.x / heads, head = blockIdx.x - t * heads;
+  const Work w = find_tile(p, t, ATTENTION_ROWS);
+  if (!w.level) return;
+  const int r0 = (w.level - 1) * ATTENTION_ROWS, r1 = min(r0 + ATTENTION_ROWS, w.len);
+  const bool of_v = head >= p.Hq;
+  auto values = [&](const void *base, long long at, float (&v)[8]) INLINE {
     const uint16_t *src = static_cast<const uint16_t *>(base) + at + l * 8;
     if (VEC && l * 8 < D) {
       load8(src, TYPE_F16, 0, v);
@@ -40,44 +40,53 @@ __global__ void __launch_bounds__(256) attention_inner_kernel(const AttentionP p
       for (int e = 0; e < 8; ++e) v[e] = l * 8 + e < D ? load_as_f32(src, TYPE_F16, e) : 0.0f;
     }
   };
-  for (long long i = (long long)blockIdx.x * 16 + g; i < n * p.Hq; i += step) {
-    const long long r = i / p.Hq, row = start + r;
-    const int h = (int)(i - r * p.Hq);
-    float a[8], b[8], s = 0.0f, t = 0.0f;
-    values(p.dout, row * p.lddo + h * p.hdo, a);
-    values(p.o, row * p.ldo + h * p.ho, b);
+  float longest = 0.0f;
+  for (int r = r0 + g; r < r1; r += 16 * INNER_ROWS) {
+    float a[INNER_ROWS][8], b[INNER_ROWS][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { s = fmaf(a[e], b[e], s); t = fmaf(a[e], a[e], t); }
+    for (int k = 0; k < INNER_ROWS; ++k) {             // (of the group's first row again where there are fewer)
+      const long long row = w.start + (r + 16 * k < r1 ? r + 16 * k : r);
+      if (of_v) {
+        values(p.v, row * p.ldv + (head - p.Hq) * p.hv, a[k]);
+      } else {
+        values(p.dout, row * p.lddo + head * p.hdo, a[k]);
+        values(p.o, row * p.ldo + head * p.ho, b[k]);
+      }
+    }
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1) { s += __shfl_xor(s, o, 16); t += __shfl_xor(t, o, 16); }
-    if (l == 0) p.inner[h * p.rows + row] = s;
-    if (t < __builtin_inff()) longest = fmaxf(longest, t);
+    for (int k = 0; k < INNER_ROWS; ++k) {
+      float s = 0.0f, n = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (!of_v) s = fmaf(a[k][e], b[k][e], s);
+        n = fmaf(a[k][e], a[k][e], n);
+      }
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) { s += __shfl_xor(s, o, 16); n += __shfl_xor(n, o, 16); }
+      if (!of_v && l == 0 && r + 16 * k < r1) p.inner[head * p.rows + w.start + r + 16 * k] = s;
+      if (n < __builtin_inff()) longest = fmaxf(longest, n);
+    }
   }
-  for (long long i = (long long)blockIdx.x * 16 + g; i < n * p.Hkv; i += step) {
-    const long long r = i / p.Hkv, row = start + r;
-    float a[8], t = 0.0f;
-    values(p.v, row * p.ldv + (i - r * p.Hkv) * p.hv, a);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) t = fmaf(a[e], a[e], t);
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) t += __shfl_xor(t, o, 16);
-    if (t < __builtin_inff()) longest_v = fmaxf(longest_v, t);
-  }
-  __shared__ float sm[2][16];
-  if (l == 0) { sm[0][g] = longest; sm[1][g] = longest_v; }
+  __shared__ float sm[16];
+  if (l == 0) sm[g] = longest;
   __syncthreads();
-  if (threadIdx.x < 2) {
-    float m = 0.0f;
-    for (int k = 0; k < 16; ++k) m = fmaxf(m, sm[threadIdx.x][k]);
-    p.most[threadIdx.x * p.nmost + blockIdx.x] = m;
+  if (threadIdx.x == 0) {
+    for (int k = 1; k < 16; ++k) longest = fmaxf(longest, sm[k]);
+    p.most[head * attention_tiles(p) + t] = longest;
   }
 }
 
-// The power of two that ds is held with
-template <int TYPE> __device__ __forceinline__ float ds_factor(const AttentionP &p) {
+// The power of two that ds is held with, by the signals of `heads` heads from `head` on and the values of their keys' head in the sequence that has the t-th
+// tile w: what other sequences and heads hold has no part in it
+template <int TYPE> __device__ __forceinline__ float ds_factor(const AttentionP &p, const Work &w, int t, int head, int heads, int kvh) {
   if constexpr (TYPE != TYPE_F16) return 1.0f;
+  const long long all = attention_tiles(p), first = t - (w.tiles - w.level);
+  const int n = (int)min((long long)w.tiles, all - first);      // (offsets that are no list may name tiles that have no place)
   float a = 0.0f, b = 0.0f;
-  for (int i = threadIdx.x & 63; i < p.nmost; i += 64) { a = fmaxf(a, p.most[i]); b = fmaxf(b, p.most[p.nmost + i]); }
+  for (int i = threadIdx.x & 63; i < n; i += 64) {
+    for (int h = 0; h < heads; ++h) a = fmaxf(a, p.most[(head + h) * all + first + i]);
+    b = fmaxf(b, p.most[(p.Hq + kvh) * all + first + i]);
+  }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) { a = fmaxf(a, __shfl_xor(a, o, 64)); b = fmaxf(b, __shfl_xor(b, o, 64)); }
   const float bound = 2.0f * sqrtf(a) * sqrtf(b);
@@ -118,7 +127,7 @@ __global__ void __launch_bounds__(64 * KEYS_WAVES * KEYS_GROUPS, ND >= 3 ? 1 : 2
   const int k0 = (w.tiles - w.level) * ATTENTION_ROWS + t % KEYS_PARTS * (32 * WAVES), mine = k0 + wave * 32, key = mine + (lane & 31), G = p.Hq / p.Hkv;
   const bool in = key < w.len;
   if (k0 >= w.len) return;
-  const float f = ds_factor<TYPE>(p), g = f * __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>);
+  const float f = ds_factor<TYPE>(p, w, t / KEYS_PARTS, kvh * G, G, kvh), g = f * __builtin_amdgcn_exp2f(-P_SHIFT<TYPE>);
   Frag8<TYPE> kf[2 * ND], vf[2 * ND];
 #pragma unroll
   for (int i = 0; i < 2 * ND; ++i) {
@@ -308,7 +317,7 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : ND <= 2
   const int q0 = (w.level - 1) * ATTENTION_ROWS, mine = q0 + wave * 32, row = mine + (lane & 31);
   const bool in = row < w.len;
   const int kvh = head / (p.Hq / p.Hkv);
-  const float f = ds_factor<TYPE>(p);
+  const float f = ds_factor<TYPE>(p, w, t, head, 1, kvh);
   Frag8<TYPE> qf[2 * ND], of[2 * ND];
 #pragma unroll
   for (int i = 0; i < 2 * ND; ++i) {
@@ -431,7 +440,7 @@ __global__ void __launch_bounds__(256, TYPE == TYPE_F32 && ND >= 3 ? 1 : ND <= 2
 
 template <int TYPE, int ND, bool VEC> hipError_t backward_launch(const AttentionP &p, hipStream_t s) {
   const long long tiles = attention_tiles(p), key_tiles = tiles * KEYS_PARTS, rest = p.offsets && p.zero_rest ? REST_BLOCKS : 0;
-  if (TYPE == TYPE_F16) hipLaunchKernelGGL((attention_inner_kernel<VEC>), dim3(p.nmost), dim3(256), 0, s, p);
+  if (TYPE == TYPE_F16) hipLaunchKernelGGL((attention_inner_kernel<VEC>), dim3((unsigned)(tiles * (p.Hq + p.Hkv))), dim3(256), 0, s, p);
   hipLaunchKernelGGL((attention_queries_kernel<TYPE, ND, VEC>), dim3((unsigned)(tiles * p.Hq + rest)), dim3(256), 0, s, p, (int)(tiles * p.Hq));
   hipLaunchKernelGGL((attention_keys_kernel<TYPE, ND, VEC>), dim3((unsigned)(key_tiles * p.Hkv + rest)), dim3(64 * KEYS_WAVES * KEYS_GROUPS), 0, s, p, (int)(key_tiles * p.Hkv));
   return hipGetLastError();

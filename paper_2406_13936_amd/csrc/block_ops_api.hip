@@ -64,18 +64,6 @@ RmsNormP rms_args(const abs_rms_norm_shape *s) {
 Block heads_of(const void *t, const abs_attention_shape *s, int heads, int64_t ld, int64_t head) {
   return {t, heads, head, s->rows, ld, s->D, type_bytes(s->type)};
 }
-struct AttentionPieces { size_t list, inner, most, total; };
-constexpr int MOST_BLOCKS = 1024;
-AttentionPieces attention_pieces(const abs_attention_shape *s, bool backward) {
-  AttentionPieces q;
-  size_t at = 0;
-  auto take = [&](size_t bytes) { const size_t r = at; at = (at + bytes + 255) / 256 * 256; return r; };
-  q.list = take(s->offsets_type && s->seqs > 64 ? ((size_t)(s->rows / ATTENTION_ROWS) + s->seqs + 1) * 8 : 0);
-  q.inner = take(backward ? (size_t)s->Hq * s->rows * 4 : 0);
-  q.most = take(backward && s->type == ABS_TYPE_F16 ? 2 * MOST_BLOCKS * 4 : 0);
-  q.total = at;
-  return q;
-}
 AttentionP attention_args(const abs_attention_shape *s) {
   AttentionP p;
   std::memset(&p, 0, sizeof(p));
@@ -84,6 +72,22 @@ AttentionP attention_args(const abs_attention_shape *s) {
   p.ldq = s->ldq; p.hq = s->head_q; p.ldk = s->ldk; p.hk = s->head_k; p.ldv = s->ldv; p.hv = s->head_v; p.ldo = s->ldo; p.ho = s->head_o;
   p.lddo = s->lddo; p.hdo = s->head_do; p.lddq = s->lddq; p.hdq = s->head_dq; p.lddk = s->lddk; p.hdk = s->head_dk; p.lddv = s->lddv; p.hdv = s->head_dv;
   return p;
+}
+int64_t shape_tiles(const abs_attention_shape *s) {
+  AttentionP p = attention_args(s);
+  p.offsets = s->offsets_type ? s : nullptr;             // (asked whether there are any)
+  return attention_tiles(p);
+}
+struct AttentionPieces { size_t list, inner, most, total; };
+AttentionPieces attention_pieces(const abs_attention_shape *s, bool backward) {
+  AttentionPieces q;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t r = at; at = (at + bytes + 255) / 256 * 256; return r; };
+  q.list = take(s->offsets_type && s->seqs > 64 ? ((size_t)shape_tiles(s) + 1) * 8 : 0);
+  q.inner = take(backward ? (size_t)s->Hq * s->rows * 4 : 0);
+  q.most = take(backward && s->type == ABS_TYPE_F16 ? (size_t)shape_tiles(s) * (s->Hq + s->Hkv) * 4 : 0);
+  q.total = at;
+  return q;
 }
 abs_status check_attention(const abs_attention_shape *s, bool backward) {
   if (!s) return set_error(ABS_EINVAL, "shape is NULL");
@@ -95,9 +99,7 @@ abs_status check_attention(const abs_attention_shape *s, bool backward) {
   if (!s->offsets_type && (s->T < 1 || (int64_t)s->seqs * s->T != s->rows)) return set_error(ABS_EINVAL, "without offsets rows must be seqs times T");
   if (s->D > ATTENTION_MAX_D) return set_error(ABS_EUNSUPPORTED, "heads of more than 128 values");
   if (s->rows > 0x7fffffff) return set_error(ABS_EUNSUPPORTED, "more than 2^31 - 1 rows");
-  AttentionP p = attention_args(s);
-  p.offsets = s->offsets_type ? s : nullptr;             // (asked whether there are any)
-  if (attention_tiles(p) > 0x7f0000 / s->Hq) return set_error(ABS_EUNSUPPORTED, "more heads of 128-row tiles than a grid counts");
+  if (shape_tiles(s) > 0x7f0000 / s->Hq) return set_error(ABS_EUNSUPPORTED, "more heads of 128-row tiles than a grid counts");
   const int heads[8] = {s->Hq, s->Hkv, s->Hkv, s->Hq, s->Hq, s->Hq, s->Hkv, s->Hkv};
   const int64_t ld[8] = {s->ldq, s->ldk, s->ldv, s->ldo, s->lddo, s->lddq, s->lddk, s->lddv};
   const int64_t head[8] = {s->head_q, s->head_k, s->head_v, s->head_o, s->head_do, s->head_dq, s->head_dk, s->head_dv};
@@ -285,7 +287,6 @@ abs_status abs_causal_attention_backward(const abs_attention_shape *shape, const
   p.list = reinterpret_cast<const int2 *>(ws + at.list);
   p.inner = reinterpret_cast<float *>(ws + at.inner);
   p.most = reinterpret_cast<float *>(ws + at.most);
-  p.nmost = (int)std::max<int64_t>(1, std::min<int64_t>(MOST_BLOCKS, (shape->rows * shape->Hq + 63) / 64));
   return hip_status(launch_attention_backward(p, static_cast<hipStream_t>(hip_stream)), "abs_causal_attention_backward");
 } catch (...) { return exception_status(); }
 

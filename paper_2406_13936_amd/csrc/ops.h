@@ -150,8 +150,7 @@ struct AttentionP {
   const void *dout;
   void *dq, *dk, *dv;
   float *inner;                            // workspace [Hq][rows]: do_i . o_i
-  float *most;                             // workspace: largest squared lengths of do_i and of v_j, by block
-  int nmost;
+  float *most;                             // workspace (fp16) [Hq + Hkv][tiles]: largest squared lengths of do_i, and of v_j, of each tile's rows
 };
 // Tiles of all sequences: what they are, or with offsets the most that they can be
 __host__ __device__ inline long long attention_tiles(const AttentionP &p) {

@@ -1,11 +1,12 @@
-"""Causal attention at the edges of what its entry points take: offsets that are no list, sizes next to the limits, infinite keys, rows of many small weights."""
+"""Causal attention at the edges of what its entry points take: offsets that are no list, sizes next to the limits, infinite keys, rows of many small weights, fp16
+signals of very different sizes."""
 import ctypes as C
 import math
 import struct
 
 import pytest
 
-from test_causal_attention import EUNSUPPORTED, U, U32, _A, _check, _dt, _lib, _shape, _tensors
+from test_causal_attention import EUNSUPPORTED, U, U32, _A, _check, _dt, _ends, _lib, _reference, _shape, _tensors
 
 gpu = pytest.mark.gpu
 
@@ -167,3 +168,40 @@ def test_long_rows_that_one_key_dominates(score, place, dtype):
         for h in range(2):
             _check(o[i, h], want.cpu(), off.cpu(), (i, h))
             assert abs(float(lse[h, i]) - float(top)) <= 2 * rel + (i + 9) * U32 + 4 * U32 * float(top)
+
+
+@gpu
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("D", [40, 64, 75, 128])
+def test_fp16_gradients_of_a_sequence_and_head_do_not_depend_on_others(D, many):
+    """Signals and values 2^25 apart: what one sequence, or one group of heads, has in a call is what it has alone, to the bit."""
+    import torch
+    A = _A()
+    lens = [70, 1, 0, 200, 129, 64] + ([3, 0] * 40 if many else [])
+    ends, Hq, Hkv = _ends(lens), 4, 2
+    q, k, v, do = _tensors(ends[-1], Hq, Hkv, D, "f16", D)
+    factor = [2.0 ** 9, 1.0, 1.0, 2.0 ** -12, 2.0 ** -3, 2.0 ** 3]
+    for i, f in enumerate(factor):
+        do[ends[i]:ends[i + 1]] *= f
+        v[ends[i]:ends[i + 1]] *= f ** 0.25
+    do[:, 2:] *= 2.0 ** 4
+    v[:, 1] *= 2.0 ** 2
+    off = torch.tensor(ends, device="cuda")
+    o, lse = A.causal_attention(q, k, v, offsets=off)
+    grads = A.causal_attention_backward(do, q, k, v, o, lse, offsets=off)
+    for i in range(6):
+        a, e = ends[i], ends[i + 1]
+        if a == e:
+            continue
+        alone = A.causal_attention_backward(do[a:e], q[a:e], k[a:e], v[a:e], o[a:e], lse[:, a:e].contiguous())
+        assert all(torch.equal(g[a:e], t) for g, t in zip(grads, alone)), i
+        for g in range(Hkv):
+            hq, hk = slice(2 * g, 2 * g + 2), slice(g, g + 1)
+            alone = A.causal_attention_backward(do[a:e, hq], q[a:e, hq], k[a:e, hk], v[a:e, hk], o[a:e, hq], lse[hq, a:e].contiguous())
+            assert all(torch.equal(t[a:e, h], x) for t, h, x in zip(grads, (hq, hk, hk), alone)), (i, g)
+        assert all((g[a:e] != 0).any() for g in grads) or e - a == 1
+    # and they are right: small signals keep their bits beside large ones
+    a, e = ends[3], ends[4]
+    want, err = _reference(q[a:e], k[a:e], v[a:e], [0, e - a], 1 / math.sqrt(D), "f16", do[a:e], o[a:e], lse[:, a:e])
+    for g, n in zip(grads, ("dq", "dk", "dv")):
+        _check(g[a:e], want[n], err[n], n)
