@@ -19,10 +19,10 @@ namespace {
 constexpr float E4M3_MAX = 448.0f;
 constexpr float SMALLEST_SCALE = 0x1p-100f;      // (its inverse is finite)
 
-// odd: infinities or NaN in the row's gains, so its results have them.  (Its own are in rstd: NaN, or 0, which times an infinite maximum is NaN.)
-__device__ __forceinline__ float scale_of(float rstd, double most, bool odd) {
+// An infinite maximum stands for infinities or NaN in the row or its gains (a row's NaN are in rstd, too)
+__device__ __forceinline__ float scale_of(float rstd, double most) {
   // (in fp64: the maximum may be beyond fp32's range, or among its last bits, where r times it is not)
-  const float c = odd ? __builtin_nanf("") : (float)((double)rstd * most * (1.0 / E4M3_MAX));
+  const float c = most < (double)__builtin_inff() ? (float)((double)rstd * most * (1.0 / E4M3_MAX)) : __builtin_nanf("");
   return c < SMALLEST_SCALE ? SMALLEST_SCALE : c;
 }
 // y / c = 448 h w / max |h w|, in which r has cancelled, is rounded to e4m3 as if it were exact, ties to even: products of two 16-bit values are often just
@@ -46,7 +46,7 @@ __device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float 
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
-// Are there infinities or NaN among a replica's gains, of which each group of the block has all?  (The maximum of |h w| would pass over NaN.)
+// Are there infinities or NaN among a lane's gains?  (The maximum of |h w| would pass over NaN; the lane's is infinite then.)
 // Gains of zero become the smallest normal value: an infinity times it is infinite, not a NaN that the maximum passes over, and of anything else the
 // quotient is below sqrt(D) 2^-126 / 2^-100 and rounds to zero as before.
 template <int V> __device__ __forceinline__ bool look_at_gains(float (&w)[V][8]) {
@@ -58,7 +58,7 @@ template <int V> __device__ __forceinline__ bool look_at_gains(float (&w)[V][8])
       odd |= !(fabsf(w[v][e]) < __builtin_inff());
       w[v][e] = w[v][e] == 0.0f ? copysignf(0x1p-126f, w[v][e]) : w[v][e];
     }
-  return __builtin_amdgcn_readfirstlane(__syncthreads_or(odd));
+  return odd;
 }
 
 // Sum and, if MAX, maximum over the group; sm: 6 floats to a wavefront, `turn` as in group_sums
@@ -155,9 +155,10 @@ __global__ void __launch_bounds__(ln_threads(G)) rms_forward_kernel(const RmsNor
         if (EIGHT) most = fmax(most, fabs((double)h[v][e] * w[v][e]));
       }
     }
+    if (odd) most = __builtin_inff();
     group_sum_max<G, EIGHT>(s, most, sm, turn++);
     const float rstd = 1.0f / sqrtf(s / n + p.eps);
-    const float c = EIGHT ? scale_of(rstd, most, odd) : 0.0f;
+    const float c = EIGHT ? scale_of(rstd, most) : 0.0f;
     const Quotient quotient(rstd, c, EIGHT ? most : 1.0);
     if (l == 0) {
       if (p.rstd) p.rstd[m * rows + r] = rstd;
@@ -197,9 +198,9 @@ __global__ void __launch_bounds__(256) rms_forward_long_kernel(const RmsNormP p,
       most = fmax(most, fabs((double)h * w));
     }
   }
-  odd = __syncthreads_or(odd);
+  if (odd) most = __builtin_inff();
   group_sum_max<256, true>(s, most, sm, 0);
-  const float rstd = 1.0f / sqrtf(s / (float)p.D + p.eps), scale = scale_of(rstd, most, odd);
+  const float rstd = 1.0f / sqrtf(s / (float)p.D + p.eps), scale = scale_of(rstd, most);
   const Quotient quotient(rstd, scale, most);
   if (threadIdx.x == 0) {
     if (p.rstd) p.rstd[m * rows + r] = rstd;
