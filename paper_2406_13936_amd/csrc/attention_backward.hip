@@ -32,13 +32,8 @@ __global__ void __launch_bounds__(256) attention_inner_kernel(const AttentionP p
   const int r0 = (w.level - 1) * ATTENTION_ROWS, r1 = min(r0 + ATTENTION_ROWS, w.len);
   const bool of_v = head >= p.Hq;
   auto values = [&](const void *base, long long at, float (&v)[8]) INLINE {
-    const uint16_t *src = static_cast<const uint16_t *>(base) + at + l * 8;
-    if (VEC && l * 8 < D) {
-      load8(src, TYPE_F16, 0, v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = l * 8 + e < D ? load_as_f32(src, TYPE_F16, e) : 0.0f;
-    }
+    const uint4 q = load16<2, VEC>(base, at, l * 8, D);
+    unpack8(q, TYPE_F16, v);
   };
   float longest = 0.0f;
   for (int r = r0 + g; r < r1; r += 16 * INNER_ROWS) {
