@@ -864,13 +864,15 @@ def _rms_norm(x, weight, residual, eps, out, residual_out, eight):
         _written(out)
     if residual_out is not None:
         _written(residual_out)
-    return y, scales, (x if h is None else h), rstd
+    if h is None and (eight or y.data_ptr() != x.data_ptr()):
+        h = x
+    return y, scales, h, rstd
 
 
 def rms_norm(x, weight, residual=None, eps: float = 1e-6, out=None, residual_out=None):
     """Root-mean-square norm of h = x + residual, rounded to its type, for [M, b, ..., D] over the last dimension with gains [M, D] (fp32 or
-    x's type), one set per replica.  Returns (y, h, rstd): h is x where there is no residual, rstd fp32 [M, b, ...]; `out` and
-    `residual_out` may be x or residual.  No autograd graph is kept: gradients are rms_norm_backward's."""
+    x's type), one set per replica.  Returns (y, h, rstd): h is x where there is no residual (None where `out` takes x's place), rstd fp32
+    [M, b, ...]; `out` and `residual_out` may be x or residual.  No autograd graph is kept: gradients are rms_norm_backward's."""
     y, _, h, rstd = _rms_norm(x, weight, residual, eps, out, residual_out, False)
     return y, h, rstd
 
@@ -887,6 +889,8 @@ def rms_norm_backward(dy, h, weight, rstd, dh=None, want_norms: bool = False, wa
     residual alike, dweight the batch gradient fp32 [M, D] (mean over the b samples), n_i = ||g_i||^2 and q_i = <g_i, gbar> fp32 [M, b],
     None unless asked for."""
     lib, torch = _lib_and_torch()
+    if h is None:
+        raise AbsError("h must be rms_norm's (it has none where its result took x's place)")
     kind = _type_of(h, "h")
     pt = _norm_params(h, weight, "weight")
     if rstd.dtype != torch.float32 or rstd.shape != h.shape[:-1] or not rstd.is_contiguous():
