@@ -27,3 +27,27 @@ def test_h_that_the_result_took_the_place_of_is_not_returned(D):
     x2 = x.clone()
     y2, h2, _ = A.rms_norm(x2, w, residual=res, out=x2)
     assert torch.equal(h2, h) and torch.equal(y2, y)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [(2, 3, 5, 72), (3, 4, 33, 77), (2, 5, 6, 1024), (2, 40, 1, 264), (1, 2, 3, 9000)], ids=str)
+def test_gradients_and_statistics_are_the_same_bits_in_other_layouts(size, dtype):
+    """Rows among wider ones, and replicas interleaved by rows: the same reads and sums where rows begin on the same kind of places."""
+    import torch
+    A = _A()
+    M, b, T, D = size
+    h, _, w, dy, dh = _inputs(M, b, T, D, dtype, "f32", True, D)
+    rstd = (h.float().square().mean(-1) + 1e-6).rsqrt()
+
+    def laid(t, interleaved):
+        buf = torch.full((b * T, M, D + 16) if interleaved else (M, b * T, D + 16), 99.0, device="cuda").to(t.dtype)
+        v = (buf.transpose(0, 1) if interleaved else buf)[..., 8:8 + D].unflatten(1, (b, T))
+        v.copy_(t)
+        return v
+    for norms, inner in ((True, True), (True, False), (False, True), (False, False)):
+        want = A.rms_norm_backward(dy, h, w, rstd, dh=dh, want_norms=norms, want_inner=inner)
+        for how in ((False, False, False), (True, True, True), (True, False, True), (False, True, False)):
+            got = A.rms_norm_backward(laid(dy, how[0]), laid(h, how[1]), w, rstd, dh=laid(dh, how[2]), want_norms=norms, want_inner=inner)
+            for a, g in zip(want, got):
+                assert (a is None and g is None) or torch.equal(a, g)
