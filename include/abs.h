@@ -441,7 +441,7 @@ abs_status abs_embedding_backward(const abs_embedding_shape *shape /*host*/, con
  * Root-mean-square norm over the last dimension behind the addition of a residual, M replicas with gains of their own (fp32 arithmetic):
  *   h = x + residual, rounded to its type;   r = 1 / sqrt(mean_d h^2 + eps),   y = h r w      (of h as it is stored)
  * or, with scale_dev, in 8 bits:   c = max(max_d |y| / 448, 2^-100) of each row,   y / c rounded to e4m3 (four exponent and three
- * mantissa bits, no infinities) as if it were exact, ties to even; a row with an infinity or NaN has c = NaN.
+ * mantissa bits, no infinities) as if it were exact, ties to even; a row whose y has an infinity or NaN has c = NaN.
  * At most 2^20 replicas, 2^27 gains (M D) and 2^31 - 1 rows (M b T); beyond: ABS_EUNSUPPORTED.
  */
 typedef struct {

@@ -926,7 +926,7 @@ def _heads(shape, stride, what: str):
         if ld is None:
             ld = step
         elif step != ld * n:
-            raise AbsError(f"{what}: rows must be equally spaced")
+            raise AbsError(f"{what}: rows must be equally spaced (those of a contiguous copy are)")
         n *= size
     heads, D = shape[-2], shape[-1]
     head = stride[-2] if heads > 1 else D
@@ -976,7 +976,8 @@ def causal_attention(q, k, v, offsets=None, scale: Optional[float] = None, out=N
     """Causal attention of q [..., T, Hq, D] over k and v [..., T, Hkv, D], each index before T a sequence of its own, or with `offsets` (int32 or
     int64, [sequences + 1]) of [rows, heads, D] over packed sequences: rows offsets[s] .. offsets[s + 1] - 1.  Hq is a multiple of Hkv, D at most
     128, scale 1 / sqrt(D) by default.  Returns (o, lse), lse fp32 [Hq, ..., T] (or [Hq, rows]); rows of no sequence are zeros, in a given
-    `out` they stay as they are.  q, k and v may be columns of one buffer.  No autograd graph is kept: gradients are causal_attention_backward's."""
+    `out` they stay as they are.  q, k and v may be columns of one buffer; their rows, over all dimensions before the heads, are equally spaced and
+    do not overlap (several [heads, T, D] one behind the other, transposed, and broadcast operands need a copy).  No autograd graph is kept: gradients are causal_attention_backward's."""
     lib, torch = _lib_and_torch()
     kind, packed, seqs, lead = _attention_operands(q, k, v, offsets)
     o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
@@ -997,7 +998,8 @@ def causal_attention(q, k, v, offsets=None, scale: Optional[float] = None, out=N
 
 def causal_attention_backward(do, q, k, v, o, lse, offsets=None, scale: Optional[float] = None, out=None):
     """Gradients (dq, dk, dv) of causal_attention from the signals `do` at its result, and its operands and results.  Of rows of no sequence they
-    are zeros; with out = (dq, dk, dv), for instance columns of one buffer, they are written there and such rows stay as they are."""
+    are zeros; with out = (dq, dk, dv), for instance columns of one buffer, they are written there and such rows stay as they are.  Layouts as there,
+    broadcast signals need a copy."""
     lib, torch = _lib_and_torch()
     kind, packed, seqs, lead = _attention_operands(q, k, v, offsets)
     for t, what in ((do, "do"), (o, "o")):

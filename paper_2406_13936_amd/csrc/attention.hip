@@ -5,10 +5,14 @@
 // One pass over the keys with the running maximum and sum of the softmax.  A block takes 128 queries of a head, 32 to a wavefront, and goes through
 // the keys in tiles of 64 (fp32 32) that it shares, two in LDS, the next one on its way.  S^T = K Q^T, so that a query is a lane's column: its maximum needs
 // one exchange between the two halves of a wavefront, its sum none until the end, and exp(S^T) is, rounded, the operand of O^T += V^T P^T without leaving
-// the registers.  Tiles below the diagonal run in a loop without masks; a wavefront masks the one that its diagonal runs through.
+// the registers.  Tiles below the diagonal run in a loop without masks; a wavefront masks the one that its diagonal runs through.  The weights are rounded
+// to the operands' type since the matrix cores take two operands of one type: with bf16 o is off by 2.0e-3 of its norm, where a result of fp32 weights,
+// rounded once, is by 1.5e-3.
 //
-// Bound by the matrix cores together with the exponentials: one sequence of 16384, 16 heads of 128 over 4 994 us, 1.11 PFLOP/s, where the matrix cores
-// are busy 60 % of the time and a large product of a library reaches 1.49; 16 heads of 64, one sequence of 8192: 184 us, 0.75.
+// Bound by the matrix cores together with the exponentials: one sequence of 16384, 16 heads of 128 over 4 973 to 1020 us by the box, 1.13 to 1.08 PFLOP/s,
+// where the matrix cores are busy 61 % of the time and a library's product of 16384^3 reaches 1.35, with its second operand transposed 1.60; 16 heads of
+// 64, one sequence of 8192: 174 to 179 us, 0.78.  Each 1 KB fragment from LDS feeds one product (1.4 to 2.1 LDS instructions to an MFMA here and in the
+// gradients).
 #include <algorithm>
 #include "attention_parts.h"
 

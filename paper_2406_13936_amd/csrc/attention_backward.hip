@@ -9,8 +9,11 @@
 // is a result of the first products is, rounded, an operand of the second ones, whose other operand is read transposed from the tile that is in LDS anyway.
 //
 // Bound by the exponentials and what surrounds them beside the products, which the few wavefronts that fit overlap only in part: of five products 0.50
-// PFLOP/s for 16 heads of 64 over 32768 rows in 40 sequences of 15 to 4211 (588 us: keys 400, queries 260 by profile), 0.55 for one sequence of 8192,
-// 0.57 for heads of 128.
+// PFLOP/s for 16 heads of 64 over 32768 rows in 40 sequences of 15 to 4211 (581 to 595 us: keys 345, queries 240), 0.56 for one sequence of 8192,
+// 0.60 for heads of 128.  Matrix cores are busy 33 (keys) and 38 % of the time.
+//
+// p and ds are rounded to the operands' type since the matrix cores take two operands of one type: bf16 gradients are off by 2.4e-3 of their norm, where
+// results of fp32 ones, rounded once, are by 1.7e-3; fp16 ones by 3.0e-4, where those are by 2.1e-4.
 //
 // fp16 operands hold p and ds in 16 bits with powers of two: p by 2^12 (else values below 2^-14, those of a row of many keys, lose bits), ds by the power that
 // takes twice the largest |do_i| |v_j| of the sequence and heads in question, a bound on |ds / a|, to 2^14 at most.

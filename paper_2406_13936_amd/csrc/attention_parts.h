@@ -272,7 +272,8 @@ __device__ __forceinline__ Frag8<TYPE> row_frag(const void *base, long long at, 
 }
 
 // Reads and products in groups: left to itself the compiler puts each read in front of the product that takes it and waits for it there (gradients of
-// 32768 packed rows, 16 heads of 64: 651 us, so 621; heads of more than 64 values have no registers for it).  Nothing crosses the line.
+// 32768 packed rows, 16 heads of 64: 651 us, so 621; with heads of more than 64 values the forward and the pass over queries have no registers for it, the
+// pass over keys, one wavefront to a SIMD there, has).  Nothing crosses the line.
 __device__ __forceinline__ void group_ends() { __builtin_amdgcn_sched_barrier(0); }
 
 template <class T> __device__ __forceinline__ void read_rows(typename T::Frag (&f)[2 * T::WIDTH], const typename T::E *lds, int row0) {

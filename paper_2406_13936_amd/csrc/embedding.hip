@@ -13,6 +13,8 @@
 //   sums      a group of lanes takes up to 64 sorted rows: runs of one (word, sample) give n_i's shares, runs of a word gbar's row; what
 //             crosses the group's ends is left as partial rows, which a second launch adds in order
 //   inner     sum_t dy_t . gbar[token_t], and the shares of n_i and q_i added up in fp64
+// A word's partial rows are added by one group of lanes, one after the other: of 2^18 tokens of 512 values half of which are one word it takes 478 us in all,
+// where evenly spread words take 294, of 2^20 of 128 values 5.0 ms.
 #include <algorithm>
 #include <cstring>
 #include "device_utils.h"
