@@ -9,7 +9,7 @@
 // to the operands' type since the matrix cores take two operands of one type: with bf16 o is off by 2.0e-3 of its norm, where a result of fp32 weights,
 // rounded once, is by 1.5e-3.
 //
-// Bound by the matrix cores together with the exponentials: one sequence of 16384, 16 heads of 128 over 4 973 to 1020 us by the box, 1.13 to 1.08 PFLOP/s,
+// Bound by the matrix cores together with the exponentials: one sequence of 16384, 16 heads of 128 over 4 973 to 1020 us on different cards, 1.13 to 1.08 PFLOP/s,
 // where the matrix cores are busy 61 % of the time and a library's product of 16384^3 reaches 1.35, with its second operand transposed 1.60; 16 heads of
 // 64, one sequence of 8192: 174 to 179 us, 0.78.  Each 1 KB fragment from LDS feeds one product (1.4 to 2.1 LDS instructions to an MFMA here and in the
 // gradients).

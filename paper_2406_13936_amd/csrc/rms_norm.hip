@@ -19,11 +19,12 @@ namespace {
 constexpr float E4M3_MAX = 448.0f;
 constexpr float SMALLEST_SCALE = 0x1p-100f;      // (its inverse is finite)
 
-// An infinite maximum stands for infinities or NaN in the row or its gains (a row's NaN are in rstd, too)
+// NaN where results are infinite or NaN: an infinite maximum stands for infinities or NaN in the row or its gains (a row's NaN are in rstd, too), and r is
+// infinite where a row's squares are all below fp32's range and eps is 0
 __device__ __forceinline__ float scale_of(float rstd, double most) {
   // (in fp64: the maximum may be beyond fp32's range, or among its last bits, where r times it is not)
-  const float c = most < (double)__builtin_inff() ? (float)((double)rstd * most * (1.0 / E4M3_MAX)) : __builtin_nanf("");
-  return c < SMALLEST_SCALE ? SMALLEST_SCALE : c;
+  const float c = (float)((double)rstd * most * (1.0 / E4M3_MAX));
+  return c < SMALLEST_SCALE ? SMALLEST_SCALE : c < __builtin_inff() ? c : __builtin_nanf("");
 }
 // y / c = 448 h w / max |h w|, in which r has cancelled, is rounded to e4m3 as if it were exact, ties to even: products of two 16-bit values are often just
 // between two of e4m3's, and in fp32 one value in a million came out on the other side of a border.

@@ -70,3 +70,22 @@ def test_products_of_rows_and_gains_beyond_fp32(row, gain, eps, D):
     v = p * r[..., None] / want_c[..., None]
     got = y8.double()
     assert torch.isfinite(got).all() and ((got - v).abs() <= torch.maximum(v.abs() * (2.0 ** -4 + 4 * rel), torch.full_like(v, 2.0 ** -10 * (1 + rel)))).all()
+
+
+@gpu
+@pytest.mark.parametrize("D", [16, 129, 1000, 2048, 8192, 8200])
+def test_rows_whose_squares_are_below_fp32(D):
+    """Without eps r is infinite and y infinite or NaN: the scale is NaN, also where all gains are zero; with eps such rows are as small as they are."""
+    import torch
+    A = _A()
+    x = torch.full((3, 2, 3, D), 1e-30, device="cuda")
+    w = torch.ones((3, D), device="cuda")
+    w[1] = 0
+    w[2, ::2] = 0
+    y8, c, _, rstd = A.rms_norm_8bit(x, w, eps=0.0)
+    assert torch.isinf(rstd).all() and torch.isnan(c).all() and torch.isnan(y8.float()).all()
+    y8, c, _, rstd = A.rms_norm_8bit(x, w, eps=EPS)
+    # y = 1e-27, c = 1e-27 / 448 = 2.2e-30 above 2^-100, and the quotients 448 and 0
+    r = 1e-30 / EPS ** 0.5 / 448
+    assert ((c[[0, 2]].double() - r).abs() <= 16 * U32 * r).all() and (c[1] == 2.0 ** -100).all()
+    assert (y8[0].float() == 448).all() and (y8[1].float() == 0).all() and torch.equal(y8[2].float(), 448 * w[2].expand(2, 3, D))
